@@ -50,12 +50,14 @@ extern "C" {
 
 #define CMPQ_F16 0 /* IEEE binary16 */
 #define CMPQ_F32 1 /* IEEE binary32 */
+#define CMPQ_BF16 2 /* bfloat16: the calls of 8-bit serving alone (cmpq_int8_*, cmpq_kv_*) */
 
 #define CMPQ_KMAX 16      /* levels per channel at the widest setting (4 bits)   */
 #define CMPQ_PROTECTED 16 /* bits[i] of a channel of O_act: kept whole in FP16   */
 
 #define CMPQ_STATUS_NONFINITE 1
 #define CMPQ_STATUS_ARRANGEMENT 2 /* cmpq_kmeans_quantize_job was handed something that is no kept arrangement */
+#define CMPQ_STATUS_RANGE 4 /* a cmpq_kv_* call was handed a page, position, row or length outside its tables */
 
 /* `op` of cmpq_workspace_bytes */
 #define CMPQ_OP_ACT_STATS 0        /* n = tokens in the call                     */
@@ -70,6 +72,7 @@ extern "C" {
 #define CMPQ_OP_PACK_WITH_ERROR 9  /* n ignored                                  */
 #define CMPQ_OP_LUT4 10            /* sizes ignored                              */
 #define CMPQ_OP_KMEANS_ARRANGEMENT 11 /* bytes of cmpq_kmeans_job.arrangement; n ignored; 0: not available */
+#define CMPQ_OP_INT8_PRODUCT 12    /* n = tokens in the call                     */
 
 /* `mode` / `score` of cmpq_extract_outliers */
 #define CMPQ_OUTLIER_CHANNELS 0
@@ -619,6 +622,144 @@ int cmpq_lut_matvec_group_fp16acc(const cmpq_deployed_layer *layers, int n_layer
  */
 int cmpq_lut_matvec_shape(const cmpq_deployed_layer *layer, int64_t m, int64_t *shape, int64_t *parts,
                           int64_t room);
+
+/*
+ * ---- Serving in 8 bits --------------------------------------------------------------------
+ *
+ * What a decoder's attention needs beside the products of Fig. 4: a product in 8-bit integers (for
+ * layers that are not to go below 8 bits, and for prompts, where multiplications bound the product), a
+ * cache of keys and values held in 8 bits, and attention over it.  These calls take CMPQ_F16, CMPQ_BF16
+ * and CMPQ_F32 where they name a dtype.  One rule makes all the codes, decided in IEEE fp32:
+ *   scale = max(max |x| / 127, 2^-126),  code = rint(x * (1 / scale)), ties to even, within -127..127
+ * over the finite values that share the scale; NaN has code 0, an infinity +-127, and either raises
+ * CMPQ_STATUS_NONFINITE.  A code stands for code * scale.
+ */
+
+/*
+ * A weight W [d_out, d_in] (ldw >= d_in; the framework layout, not the transposed one) in 8 bits, a scale per
+ * output channel (row).
+ *   codes  cmpq_int8_weight_bytes(d_out, d_in) bytes out, 16-byte aligned.  Pieces of 16 rows by 64 inputs, 1 KB
+ *          each, in the order in which the matrix instruction takes them, [ceil(d_out / 16)][2 ceil(d_in / 128)]:
+ *          byte [g][r][j] (g < 4, r < 16, j < 16) of a piece is row r, input 16 g + j; zero beyond the matrix.
+ *   scale  [d_out] fp32 out.
+ * No workspace.  Limits: d_in <= 131072 (sums of products stay below 2^31), d_out < 2^24.
+ */
+size_t cmpq_int8_weight_bytes(int64_t d_out, int64_t d_in);
+int cmpq_int8_prepare(const void *W, int dtype, int64_t d_out, int64_t d_in, int64_t ldw, int8_t *codes,
+                      float *scale, int32_t *status, void *stream);
+
+/*
+ * Y[t,o] = (sum_i cx[t,i] * cw[o,i]) * sx[t] * sw[o]: X [m, d_in] (ldx) is coded with a scale per token on the
+ * way, the sum is exact, its fp32 value is multiplied by the two scales in this order and rounded once more to
+ * y_dtype.  Y [m, d_out] (ldy).  codes, scale: from cmpq_int8_prepare.
+ * Workspace: CMPQ_OP_INT8_PRODUCT with n = m.  Limits: m < 2^24 and those of cmpq_int8_prepare.
+ */
+int cmpq_int8_product(const void *X, int dtype, int64_t m, int64_t d_in, int64_t ldx, const int8_t *codes,
+                      const float *scale, int64_t d_out, void *Y, int y_dtype, int64_t ldy, void *ws,
+                      size_t ws_bytes, int32_t *status, void *stream);
+
+/*
+ * A cache of keys and values in pages of `page` tokens, 8 bits a value, one scale per page and head for the keys
+ * and one for the values.  A byte is code + 128.  Codes of a page and head lie together, in pieces of 32 tokens by
+ * 32 dims (1 KB, in the order in which the matrix instruction takes them), [page / 32][ceil(head_dim / 32)];
+ * byte [g][t][h][j] (g < 4, t < 16, h < 2, j < 8) of a piece is
+ *   keys:    token 16 h + t,                  dim 8 g + j;
+ *   values:  token 16 (j / 4) + 4 g + j % 4,  dim 16 h + t.
+ * Dims from head_dim on hold code 0; bytes of tokens that were never written may be anything.
+ * Nothing has to be cleared before its first use: the first token of a page starts its scale anew.
+ */
+typedef struct cmpq_kv_cache {
+    uint8_t *k_codes, *v_codes; /* device, [n_pages, kv_heads, cmpq_kv_page_bytes], 16-byte aligned */
+    float *k_scale, *v_scale;   /* device, [n_pages, kv_heads] */
+    int64_t n_pages;            /* below 2^31 */
+    int kv_heads, head_dim, page; /* head_dim <= 256; page a multiple of 32, at most 1024 */
+} cmpq_kv_cache;
+size_t cmpq_kv_page_bytes(int head_dim, int page); /* of one page and head: page * 32 * ceil(head_dim / 32); 0: not supported */
+
+/*
+ * Rows of several sequences one after the other: rows cu_rows[i] .. cu_rows[i+1]-1 are the tokens first[i],
+ * first[i]+1, ... of sequence i, whose token p lies in page page_table[i * ld_table + p / page], place p % page.
+ * All arrays are device data, so the host cannot check them: a sequence with first[i] < 0, a row beyond n_rows,
+ * a token beyond ld_table pages or in a page outside 0..n_pages-1 is left out and raises CMPQ_STATUS_RANGE.
+ */
+typedef struct cmpq_kv_rows {
+    const int32_t *page_table; /* device, [n_seq, ld_table] */
+    int64_t ld_table;
+    const int32_t *first;   /* device, [n_seq] */
+    const int32_t *cu_rows; /* device, [n_seq + 1] */
+    int64_t n_seq, n_rows;  /* below 2^31 */
+} cmpq_kv_rows;
+
+/*
+ * Turning by position: of the first `dims` (even) dims of a head, pair j of them, (j, j + dims / 2) or, interleaved,
+ * (2 j, 2 j + 1), becomes (a cos - b sin, b cos + a sin) with cos[p, j], sin[p, j] of the token's position p; in
+ * fp32, each product and sum rounded.  A position beyond the tables takes their last row and raises
+ * CMPQ_STATUS_RANGE.
+ */
+typedef struct cmpq_rotation {
+    const float *cos, *sin; /* device, [positions, dims / 2] */
+    int64_t positions;
+    int dims, interleaved;
+} cmpq_rotation;
+
+/* Strided rows of heads: element (row, head, d) lies at ptr + (row * row_stride + head * head_stride + d) elements. */
+typedef struct cmpq_heads {
+    void *ptr; /* device */
+    int64_t row_stride, head_stride;
+} cmpq_heads;
+
+/*
+ * New tokens into the cache: keys K and values V, [n_rows, kv_heads, head_dim] of `dtype`, keys turned by `rotation`
+ * (nullable) at their token's position.  `rows->first` is the number of tokens a sequence has before.  Every page that gets
+ * tokens, per head and for keys and values apart:
+ *   scale' = max(scale, new max |x| / 127, 2^-126), where scale counts as 0 if the page's first token is among the new;
+ *   codes of the tokens before these in the page become rint(code * (scale * (1 / scale')));
+ *   the new ones are coded with scale'.
+ * A page is given to one sequence alone while tokens are appended to it.  K and V may be views of one tensor.
+ * No workspace.  Status: CMPQ_STATUS_NONFINITE, CMPQ_STATUS_RANGE.
+ */
+int cmpq_kv_append(const cmpq_kv_cache *cache, const cmpq_kv_rows *rows, const cmpq_heads *K, const cmpq_heads *V,
+                   int dtype, const cmpq_rotation *rotation, int32_t *status, void *stream);
+
+/*
+ * The values that tokens of the cache stand for, code * scale rounded once to `dtype`, into K and V
+ * [n_rows, kv_heads, head_dim].  Rows that are left out (see cmpq_kv_rows) are not written.  No workspace.
+ */
+int cmpq_kv_read(const cmpq_kv_cache *cache, const cmpq_kv_rows *rows, const cmpq_heads *K, const cmpq_heads *V,
+                 int dtype, int32_t *status, void *stream);
+
+/*
+ * Attention over the cache.  Sequence i has lengths[i] tokens and the query rows cu_rows[i] .. cu_rows[i+1]-1, which
+ * are its last tokens: row j of q stands at position p = lengths[i] - q + j.  For each row and query head h, which
+ * reads key / value head h / (q_heads / kv_heads),
+ *   O = sum_t w_t v_t / sum_t w_t,  w_t = exp(softmax_scale * q . k_t),  q turned by `rotation` (nullable) at p,
+ * over the tokens t with 0 <= t < lengths[i], and t <= p if `causal`, and t > p - window if window > 0.  A row that
+ * has no such token (a sequence without tokens, or more rows than tokens) gives zeros.
+ *   Q  [n_rows, q_heads, head_dim] of q_dtype;  O  [n_rows, q_heads, head_dim] of o_dtype, CMPQ_F16 or CMPQ_BF16.
+ *   max_rows, max_length  host bounds of the rows and the length of any sequence: rows beyond are not
+ *       written, tokens beyond are left out, and either raises CMPQ_STATUS_RANGE.
+ * Logits, their maximum, the weights' sum and the output are held in fp32; queries (scaled by a power of two per
+ * row) and weights are rounded to FP16 for the matrix instruction, codes are exact in it.  The order of all
+ * additions depends on sizes and lengths alone: results are reproducible bit for bit.
+ * Workspace: cmpq_kv_attention_workspace(job) (a function of the sizes, not of the pointers).
+ */
+typedef struct cmpq_kv_attention_job {
+    cmpq_kv_cache cache;
+    const int32_t *page_table; /* device, [n_seq, ld_table] */
+    int64_t ld_table;
+    const int32_t *lengths;    /* device, [n_seq] */
+    const int32_t *cu_rows;    /* device, [n_seq + 1] */
+    int64_t n_seq, n_rows, max_rows, max_length;
+    cmpq_heads Q, O;
+    int q_dtype, o_dtype, q_heads;
+    float softmax_scale;
+    int causal;
+    int64_t window;
+    cmpq_rotation rotation;    /* cos null: none */
+    int32_t *status;           /* device, nullable */
+} cmpq_kv_attention_job;
+size_t cmpq_kv_attention_workspace(const cmpq_kv_attention_job *job);
+int cmpq_kv_attention(const cmpq_kv_attention_job *job, void *ws, size_t ws_bytes, void *stream);
 
 /*
  * Measurement hook (for a benchmark that wants the duration of one kernel rather than of an

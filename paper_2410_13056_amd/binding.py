@@ -16,13 +16,15 @@ _HERE = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.path.join(_HERE, "libcmpq.so")
 
 OK = 0
-F16, F32 = 0, 1
+F16, F32, BF16 = 0, 1, 2
 KMAX = 16
 PROTECTED = 16
 STATUS_NONFINITE = 1
 OP_OUTLIERS_BY_COLUMN, OP_LUT_MATVEC, OP_PACK_WITH_ERROR, OP_LUT4, OP_KMEANS_ARRANGEMENT = 7, 8, 9, 10, 11
+OP_INT8_PRODUCT = 12
 ARRANGEMENT_NONE, ARRANGEMENT_KEEP, ARRANGEMENT_REUSE = 0, 1, 2
 STATUS_ARRANGEMENT = 2
+STATUS_RANGE = 4
 OP_ACT_STATS, OP_ALLOCATE_BITS, OP_OUTLIER_CHANNELS, OP_OUTLIER_WEIGHTS, OP_KMEANS, OP_PACK, \
     OP_DEQUANT_ERROR = range(7)
 OUTLIER_CHANNELS, OUTLIER_WEIGHTS = 0, 1
@@ -42,7 +44,8 @@ EXPORTS = ("cmpq_workspace_bytes", "cmpq_strerror", "cmpq_count_ppm", "cmpq_act_
            "cmpq_rtn_quantize", "cmpq_select_by_width", "cmpq_lut_matvec_group", "cmpq_lut4_quantize",
            "cmpq_pack_with_error", "cmpq_time_kernel", "cmpq_act_stats_static", "cmpq_kmeans_launch_shape",
            "cmpq_shader_clock_probe", "cmpq_lut_matvec_group_fp16acc", "cmpq_kmeans_build_shape", "cmpq_rank_channels",
-           "cmpq_lut_matvec_shape")
+           "cmpq_lut_matvec_shape", "cmpq_int8_weight_bytes", "cmpq_kv_page_bytes", "cmpq_kv_attention_workspace",
+           "cmpq_int8_prepare", "cmpq_int8_product", "cmpq_kv_append", "cmpq_kv_read", "cmpq_kv_attention")
 
 _i64, _i32, _int, _vp, _dbl, _sz = (ctypes.c_int64, ctypes.c_int32, ctypes.c_int, ctypes.c_void_p,
                                     ctypes.c_double, ctypes.c_size_t)
@@ -68,6 +71,36 @@ class KmeansJob(ctypes.Structure):
                 ("bit_set", _vp), ("n_set", _int), ("counts_host", _vp), ("packed", _vp), ("chan_idx", _vp),
                 ("lut", _vp), ("sumsq", _vp), ("err_ch", _vp), ("err_total", _vp),
                 ("arrangement", _vp), ("arrangement_use", _int)]
+
+
+class KvCacheView(ctypes.Structure):
+    """`cmpq_kv_cache` of the header, field for field."""
+    _fields_ = [("k_codes", _vp), ("v_codes", _vp), ("k_scale", _vp), ("v_scale", _vp), ("n_pages", _i64),
+                ("kv_heads", _int), ("head_dim", _int), ("page", _int)]
+
+
+class KvRows(ctypes.Structure):
+    """`cmpq_kv_rows` of the header, field for field."""
+    _fields_ = [("page_table", _vp), ("ld_table", _i64), ("first", _vp), ("cu_rows", _vp), ("n_seq", _i64),
+                ("n_rows", _i64)]
+
+
+class RotationView(ctypes.Structure):
+    """`cmpq_rotation` of the header, field for field."""
+    _fields_ = [("cos", _vp), ("sin", _vp), ("positions", _i64), ("dims", _int), ("interleaved", _int)]
+
+
+class Heads(ctypes.Structure):
+    """`cmpq_heads` of the header, field for field."""
+    _fields_ = [("ptr", _vp), ("row_stride", _i64), ("head_stride", _i64)]
+
+
+class KvAttentionJob(ctypes.Structure):
+    """`cmpq_kv_attention_job` of the header, field for field."""
+    _fields_ = [("cache", KvCacheView), ("page_table", _vp), ("ld_table", _i64), ("lengths", _vp), ("cu_rows", _vp),
+                ("n_seq", _i64), ("n_rows", _i64), ("max_rows", _i64), ("max_length", _i64), ("Q", Heads), ("O", Heads),
+                ("q_dtype", _int), ("o_dtype", _int), ("q_heads", _int), ("softmax_scale", ctypes.c_float),
+                ("causal", _int), ("window", _i64), ("rotation", RotationView), ("status", _vp)]
 
 
 class CmpqError(RuntimeError):
@@ -120,8 +153,19 @@ def lib() -> ctypes.CDLL:
         L.cmpq_lut_matvec_group.argtypes = [_vp, _int, _i64, _vp, _sz, _vp]
         L.cmpq_lut_matvec_group_fp16acc.argtypes = [_vp, _int, _i64, _vp, _sz, _vp]
         L.cmpq_select_by_width.argtypes = [_vp, _i64, _i64, _vp, _int, _vp, _vp, _vp, _vp, _vp]
+        L.cmpq_int8_weight_bytes.argtypes = [_i64, _i64]
+        L.cmpq_kv_page_bytes.argtypes = [_int, _int]
+        L.cmpq_kv_attention_workspace.argtypes = [ctypes.POINTER(KvAttentionJob)]
+        L.cmpq_int8_prepare.argtypes = [_vp, _int, _i64, _i64, _i64, _vp, _vp, _vp, _vp]
+        L.cmpq_int8_product.argtypes = [_vp, _int, _i64, _i64, _i64, _vp, _vp, _i64, _vp, _int, _i64, _vp, _sz, _vp, _vp]
+        rows = [ctypes.POINTER(KvCacheView), ctypes.POINTER(KvRows), ctypes.POINTER(Heads), ctypes.POINTER(Heads), _int]
+        L.cmpq_kv_append.argtypes = rows + [ctypes.POINTER(RotationView), _vp, _vp]
+        L.cmpq_kv_read.argtypes = rows + [_vp, _vp]
+        L.cmpq_kv_attention.argtypes = [ctypes.POINTER(KvAttentionJob), _vp, _sz, _vp]
         for name in EXPORTS[3:]:
             getattr(L, name).restype = _int
+        for name in ("cmpq_int8_weight_bytes", "cmpq_kv_page_bytes", "cmpq_kv_attention_workspace"):
+            getattr(L, name).restype = _sz
         _lib = L
     return _lib
 
@@ -619,3 +663,143 @@ def lut4_quantize(centroids: torch.Tensor, bits: torch.Tensor, codes4: torch.Ten
     _check(lib().cmpq_lut4_quantize(int(mode), _ptr(centroids), _ptr(bits), d_in, int(iters), _ptr(codes4),
                                     _ptr(table), _ptr(centroids_q), _ptr(buf), buf.numel(), _stream()),
            "cmpq_lut4_quantize")
+
+
+# ---- serving in 8 bits -----------------------------------------------------------------------
+
+_SERVING = {torch.float16: F16, torch.float32: F32, torch.bfloat16: BF16}
+
+
+def serving_dtype(dtype: torch.dtype) -> int:
+    try:
+        return _SERVING[dtype]
+    except KeyError:
+        raise TypeError(f"8-bit serving takes float16, bfloat16 or float32, got {dtype}") from None
+
+
+def int8_weight_bytes(d_out: int, d_in: int) -> int:
+    return int(lib().cmpq_int8_weight_bytes(int(d_out), int(d_in)))
+
+
+def kv_page_bytes(head_dim: int, page: int) -> int:
+    """Bytes of the codes of one page and head (keys or values); 0: not supported."""
+    return int(lib().cmpq_kv_page_bytes(int(head_dim), int(page)))
+
+
+def int8_prepare(W: torch.Tensor, codes: torch.Tensor, scale: torch.Tensor,
+                 status: Optional[torch.Tensor] = None) -> None:
+    """A weight [d_out, d_in] in 8 bits, a scale per output channel (`cmpq_int8_prepare`)."""
+    d_out, d_in, ldw = _rows(W)
+    if codes.dtype != torch.int8 or not codes.is_contiguous() or codes.numel() != int8_weight_bytes(d_out, d_in):
+        raise ValueError("codes must be contiguous int8 of int8_weight_bytes(d_out, d_in)")
+    if scale.dtype != torch.float32 or not scale.is_contiguous() or scale.numel() != d_out:
+        raise ValueError("scale must be contiguous float32 [d_out]")
+    _check(lib().cmpq_int8_prepare(_ptr(W), serving_dtype(W.dtype), d_out, d_in, ldw, _ptr(codes), _ptr(scale),
+                                   _ptr(status), _stream()), "cmpq_int8_prepare")
+
+
+def int8_product(X: torch.Tensor, codes: torch.Tensor, scale: torch.Tensor, Y: torch.Tensor, ws: Workspace,
+                 status: Optional[torch.Tensor] = None) -> None:
+    """Y [m, d_out] = X [m, d_in] times a weight of `int8_prepare`, X in 8 bits with a scale per token on the way."""
+    m, d_in, ldx = _rows(X)
+    my, d_out, ldy = _rows(Y)
+    if my != m or scale.numel() != d_out or codes.numel() != int8_weight_bytes(d_out, d_in):
+        raise ValueError("X must be [m, d_in] and Y [m, d_out] of the prepared weight")
+    buf = ws.get(workspace_bytes(OP_INT8_PRODUCT, d_in, d_out, m))
+    rc = lib().cmpq_int8_product(_ptr(X), serving_dtype(X.dtype), m, d_in, ldx, _ptr(codes), _ptr(scale), d_out, _ptr(Y),
+                                 serving_dtype(Y.dtype), ldy, _ptr(buf), buf.numel(), _ptr(status), _stream())
+    if rc:
+        _check(rc, "cmpq_int8_product")
+
+
+def kv_cache_view(k: torch.Tensor, v: torch.Tensor, k_scale: torch.Tensor, v_scale: torch.Tensor, page: int,
+                  head_dim: int) -> KvCacheView:
+    """The cache's tensors as the library takes them: codes uint8 [n_pages, kv_heads, kv_page_bytes(head_dim, page)],
+    scales float32 [n_pages, kv_heads]."""
+    if k_scale.dim() != 2 or tuple(v_scale.shape) != tuple(k_scale.shape):
+        raise ValueError("scales must be [n_pages, kv_heads]")
+    n_pages, heads = k_scale.shape
+    nbytes = kv_page_bytes(head_dim, page)
+    if nbytes == 0:
+        raise ValueError("head_dim is 1..256, a page 32..1024 tokens and a multiple of 32")
+    for t, dt, shape in ((k, torch.uint8, (n_pages, heads, nbytes)), (v, torch.uint8, (n_pages, heads, nbytes)),
+                         (k_scale, torch.float32, (n_pages, heads)), (v_scale, torch.float32, (n_pages, heads))):
+        if t.dtype != dt or tuple(t.shape) != shape or not t.is_contiguous():
+            raise ValueError("codes are contiguous uint8 [n_pages, kv_heads, kv_page_bytes], scales float32")
+    return KvCacheView(_ptr(k), _ptr(v), _ptr(k_scale), _ptr(v_scale), n_pages, heads, int(head_dim), int(page))
+
+
+def rotation_view(cos: torch.Tensor, sin: torch.Tensor, interleaved: bool) -> RotationView:
+    for t in (cos, sin):
+        if t.dtype != torch.float32 or t.dim() != 2 or not t.is_contiguous() or t.shape != cos.shape:
+            raise ValueError("cos and sin must be contiguous float32 [positions, dims / 2]")
+    return RotationView(_ptr(cos), _ptr(sin), cos.shape[0], 2 * cos.shape[1], int(bool(interleaved)))
+
+
+def heads_view(t: torch.Tensor, n_heads: int, head_dim: int) -> Heads:
+    """A tensor [rows, heads, dims] of any row and head stride."""
+    if t.dim() != 3 or t.shape[1] != n_heads or t.shape[2] != head_dim or (head_dim > 1 and t.stride(2) != 1):
+        raise ValueError(f"expected [rows, {n_heads}, {head_dim}] with unit stride along the dims")
+    return Heads(_ptr(t), t.stride(0), t.stride(1))
+
+
+def _i32_table(t: torch.Tensor, shape, what: str) -> int:
+    if t.dtype != torch.int32 or tuple(t.shape) != tuple(shape) or not t.is_contiguous():
+        raise ValueError(f"{what} must be contiguous int32 {list(shape)}")
+    return _ptr(t)
+
+
+def _kv_rows(page_table: torch.Tensor, first: torch.Tensor, cu_rows: torch.Tensor, n_rows: int) -> KvRows:
+    if page_table.dim() != 2:
+        raise ValueError("page_table must be [n_seq, pages]")
+    n_seq, ld = page_table.shape
+    return KvRows(_i32_table(page_table, (n_seq, ld), "page_table"), ld, _i32_table(first, (n_seq,), "first"),
+                  _i32_table(cu_rows, (n_seq + 1,), "cu_rows"), n_seq, n_rows)
+
+
+def kv_append(cache: KvCacheView, page_table: torch.Tensor, first: torch.Tensor, cu_rows: torch.Tensor, K: torch.Tensor,
+              V: torch.Tensor, rotation: Optional[RotationView] = None, status: Optional[torch.Tensor] = None) -> None:
+    """`cmpq_kv_append`: K and V [rows, kv_heads, head_dim] behind the first[i] tokens of each sequence."""
+    k, v = heads_view(K, cache.kv_heads, cache.head_dim), heads_view(V, cache.kv_heads, cache.head_dim)
+    if K.shape[0] != V.shape[0] or K.dtype != V.dtype:
+        raise ValueError("K and V must have the same rows and dtype")
+    rows = _kv_rows(page_table, first, cu_rows, K.shape[0])
+    rc = lib().cmpq_kv_append(ctypes.byref(cache), ctypes.byref(rows), ctypes.byref(k), ctypes.byref(v),
+                              serving_dtype(K.dtype), ctypes.byref(rotation) if rotation is not None else None,
+                              _ptr(status), _stream())
+    if rc:
+        _check(rc, "cmpq_kv_append")
+
+
+def kv_read(cache: KvCacheView, page_table: torch.Tensor, first: torch.Tensor, cu_rows: torch.Tensor, K: torch.Tensor,
+            V: torch.Tensor, status: Optional[torch.Tensor] = None) -> None:
+    """`cmpq_kv_read`: the values that tokens first[i], first[i]+1, ... of each sequence stand for, into K and V."""
+    k, v = heads_view(K, cache.kv_heads, cache.head_dim), heads_view(V, cache.kv_heads, cache.head_dim)
+    if K.shape[0] != V.shape[0] or K.dtype != V.dtype:
+        raise ValueError("K and V must have the same rows and dtype")
+    rows = _kv_rows(page_table, first, cu_rows, K.shape[0])
+    rc = lib().cmpq_kv_read(ctypes.byref(cache), ctypes.byref(rows), ctypes.byref(k), ctypes.byref(v),
+                            serving_dtype(K.dtype), _ptr(status), _stream())
+    if rc:
+        _check(rc, "cmpq_kv_read")
+
+
+def kv_attention(cache: KvCacheView, page_table: torch.Tensor, lengths: torch.Tensor, cu_rows: torch.Tensor,
+                 Q: torch.Tensor, O: torch.Tensor, max_rows: int, max_length: int, softmax_scale: float,
+                 ws: Workspace, causal: bool = True, window: int = 0, rotation: Optional[RotationView] = None,
+                 status: Optional[torch.Tensor] = None) -> None:
+    """`cmpq_kv_attention`: Q [rows, q_heads, head_dim] over the cache, into O of the same shape."""
+    if O.shape != Q.shape or page_table.dim() != 2 or Q.dim() != 3:
+        raise ValueError("Q and O must be [rows, q_heads, head_dim], page_table [n_seq, pages]")
+    n_seq, ld = page_table.shape
+    job = KvAttentionJob(cache, _i32_table(page_table, (n_seq, ld), "page_table"), ld,
+                         _i32_table(lengths, (n_seq,), "lengths"), _i32_table(cu_rows, (n_seq + 1,), "cu_rows"),
+                         n_seq, Q.shape[0], int(max_rows), int(max_length), heads_view(Q, Q.shape[1], cache.head_dim),
+                         heads_view(O, Q.shape[1], cache.head_dim), serving_dtype(Q.dtype), serving_dtype(O.dtype),
+                         Q.shape[1], float(softmax_scale), int(bool(causal)), int(window),
+                         rotation if rotation is not None else RotationView(), _ptr(status))
+    ref = ctypes.byref(job)
+    buf = ws.get(lib().cmpq_kv_attention_workspace(ref))
+    rc = lib().cmpq_kv_attention(ref, _ptr(buf), buf.numel(), _stream())
+    if rc:
+        _check(rc, "cmpq_kv_attention")

@@ -15,6 +15,7 @@ size_t cmpq_ws_lut_matvec(int64_t d_in, int64_t d_out, int64_t m);
 size_t cmpq_ws_pack_with_error(int64_t d_in);
 size_t cmpq_ws_lut4();
 size_t cmpq_ws_kmeans_arrangement(int64_t d_in, int64_t d_out);
+size_t cmpq_ws_int8_product(int64_t d_in, int64_t m);
 
 extern "C" size_t cmpq_workspace_bytes(int op, int64_t d_in, int64_t d_out, int64_t n) {
     if (d_in < 0 || d_out < 0 || n < 0) return 0;
@@ -31,6 +32,7 @@ extern "C" size_t cmpq_workspace_bytes(int op, int64_t d_in, int64_t d_out, int6
         case CMPQ_OP_PACK_WITH_ERROR: return cmpq_ws_pack_with_error(d_in);
         case CMPQ_OP_LUT4: return cmpq_ws_lut4();
         case CMPQ_OP_KMEANS_ARRANGEMENT: return cmpq_ws_kmeans_arrangement(d_in, d_out);
+        case CMPQ_OP_INT8_PRODUCT: return cmpq_ws_int8_product(d_in, n);
         default: return 0;
     }
 }

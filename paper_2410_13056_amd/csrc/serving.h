@@ -1,0 +1,104 @@
+// What the calls of 8-bit serving share: element types, the one rule of all 8-bit codes, the position rotation and
+// the checks of their arguments.
+#pragma once
+
+#include "common.h"
+
+constexpr float kSmallestScale = 0x1p-126f;  // keeps 1 / scale finite; also the scale of zeros
+
+template <typename T>
+__device__ __forceinline__ float as_f32(T v) {
+    return (float)v;
+}
+
+// fn(T()) for the element type that `dtype` names; the host has checked that it names one.
+template <typename F>
+__device__ __forceinline__ void with_dtype(int dtype, F fn) {
+    if (dtype == CMPQ_F16) fn(_Float16());
+    else if (dtype == CMPQ_BF16) fn(__bf16());
+    else fn(float());
+}
+
+static inline bool serving_dtype(int dtype) { return dtype == CMPQ_F16 || dtype == CMPQ_BF16 || dtype == CMPQ_F32; }
+static inline size_t dtype_bytes(int dtype) { return dtype == CMPQ_F32 ? 4 : 2; }
+
+// N consecutive elements in 32 bits, `valid` of them there (the others read 0).
+template <typename T, int N>
+__device__ __forceinline__ void load_f32(const T *p, int valid, float (&x)[N]) {
+    if (valid >= N) {
+        typedef T V __attribute__((ext_vector_type(N)));
+        typedef V Any __attribute__((aligned(sizeof(T))));
+        const V v = *reinterpret_cast<const Any *>(p);
+#pragma unroll
+        for (int i = 0; i < N; ++i) x[i] = (float)v[i];
+    } else {
+#pragma unroll
+        for (int i = 0; i < N; ++i) x[i] = i < valid ? (float)p[i] : 0.f;
+    }
+}
+
+// |x| where it is finite, else 0; `bad` remembers that one was not.
+__device__ __forceinline__ float finite_abs(float x, bool &bad) {
+    const float a = fabsf(x);
+    const bool fine = a < INFINITY;
+    bad |= !fine;
+    return fine ? a : 0.f;
+}
+
+__device__ __forceinline__ float code_scale(float most) { return fmaxf(most / 127.f, kSmallestScale); }
+
+// rint(x * inv) within -127..127, NaN to 0.
+__device__ __forceinline__ int code_of(float x, float inv) {
+    const float t = rintf(__builtin_amdgcn_fmed3f(x * inv, -127.f, 127.f));
+    return x == x ? (int)t : 0;
+}
+
+// Largest of non-negative values over the workgroup, in every lane.  `scratch`: one float a wavefront.  Has barriers.
+__device__ __forceinline__ float block_max(float v, float *scratch) {
+#pragma unroll
+    for (int s = 32; s > 0; s >>= 1) v = fmaxf(v, __shfl_xor(v, s, CMPQ_WAVE));
+    if ((threadIdx.x & 63) == 0) scratch[threadIdx.x >> 6] = v;
+    __syncthreads();
+    const int waves = (int)(blockDim.x >> 6);
+    float m = scratch[0];
+    for (int w = 1; w < waves; ++w) m = fmaxf(m, scratch[w]);
+    return m;
+}
+
+// The two results of the turn by position.  Products and sums are rounded one by one, as the header says.
+__device__ __forceinline__ float turned_first(float a, float b, float c, float s) {
+#pragma clang fp contract(off)
+    const float ac = a * c, bs = b * s;
+    return ac - bs;
+}
+__device__ __forceinline__ float turned_second(float a, float b, float c, float s) {
+#pragma clang fp contract(off)
+    const float bc = b * c, as = a * s;
+    return bc + as;
+}
+
+// Dim `d` of a head at `p` turned for the row `at` of the tables (null: not turned).
+template <typename T>
+__device__ __forceinline__ float turned(const T *p, int d, const cmpq_rotation &rot, int64_t at) {
+    const float x = (float)p[d];
+    if (!rot.cos || d >= rot.dims) return x;
+    const int half = rot.dims >> 1;
+    const int j = rot.interleaved ? d >> 1 : (d < half ? d : d - half);
+    const bool second = rot.interleaved ? d & 1 : d >= half;
+    const int other = rot.interleaved ? d ^ 1 : (second ? d - half : d + half);
+    const float y = (float)p[other], c = rot.cos[at * half + j], s = rot.sin[at * half + j];
+    return second ? turned_second(y, x, c, s) : turned_first(x, y, c, s);
+}
+
+static inline int check_rotation(const cmpq_rotation *rot, int head_dim) {
+    if (!rot || !rot->cos) return CMPQ_OK;
+    if (!rot->sin || rot->positions < 1 || rot->dims < 2 || (rot->dims & 1)) return CMPQ_EINVAL;
+    return rot->dims <= head_dim ? CMPQ_OK : CMPQ_ESHAPE;
+}
+
+static inline int check_cache(const cmpq_kv_cache &c) {
+    if (!c.k_codes || !c.v_codes || !c.k_scale || !c.v_scale || c.n_pages < 0 || c.kv_heads < 1) return CMPQ_EINVAL;
+    if (!cmpq_kv_page_bytes(c.head_dim, c.page) || c.kv_heads > 65535 || c.n_pages > INT32_MAX) return CMPQ_ESHAPE;
+    if (reinterpret_cast<uintptr_t>(c.k_codes) % 16 || reinterpret_cast<uintptr_t>(c.v_codes) % 16) return CMPQ_EINVAL;
+    return CMPQ_OK;
+}
