@@ -75,6 +75,12 @@ struct Scaled {
     int dtype;
 };
 
+// The smaller scale first: a sum that is not 0 times a scale of at least 2^-126 neither vanishes nor, where the
+// result is in range, overflows on the way.
+__device__ __forceinline__ float scaled(int sum, float sx, float sw) {
+    return (float)sum * fminf(sx, sw) * fmaxf(sx, sw);
+}
+
 // Four outputs next to each other of token t.
 __device__ __forceinline__ void put4(const Scaled &y, int64_t t, int64_t o, const Int4 &acc) {
     if (t >= y.m) return;
@@ -84,7 +90,7 @@ __device__ __forceinline__ void put4(const Scaled &y, int64_t t, int64_t o, cons
         T *p = static_cast<T *>(y.Y) + t * y.ldy + o;
 #pragma unroll
         for (int r = 0; r < 4; ++r)
-            if (o + r < y.d_out) p[r] = (T)((float)acc[r] * sx * y.sw[o + r]);
+            if (o + r < y.d_out) p[r] = (T)scaled(acc[r], sx, y.sw[o + r]);
     });
 }
 

@@ -285,7 +285,8 @@ __global__ __launch_bounds__(kWaves * 64) void attend_kernel(Job j) {
 #pragma unroll
             for (int r = 1; r < 8; ++r) top = fmaxf(top, l[r]);
             if (__ballot(top > m + kSlack) || vscale > unit_scale) {
-                const float next = fmaxf(m, rows_max(top)), keep = __builtin_amdgcn_exp2f(m - next);
+                top = rows_max(top);  // a row's reference moves by its own logits alone
+                const float next = top > m + kSlack ? top : m, keep = __builtin_amdgcn_exp2f(m - next);
                 const float u = fmaxf(unit_scale, vscale), turn = keep * (unit_scale / u);
                 sum *= keep;
 #pragma unroll
