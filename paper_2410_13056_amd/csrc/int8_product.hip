@@ -33,6 +33,16 @@ struct Sixteen {
             for (int i = 0; i < 16; ++i) v[i] = i < valid ? p[i] : (T)0.f;
         }
     }
+    __device__ __forceinline__ uint4 codes(float inv) const {
+        uint32_t w[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            w[i] = 0;
+#pragma unroll
+            for (int j = 0; j < 4; ++j) w[i] |= (uint32_t)(code_of((float)v[4 * i + j], inv) & 255) << (8 * j);
+        }
+        return make_uint4(w[0], w[1], w[2], w[3]);
+    }
 };
 
 // One workgroup a row: its largest magnitude, then its codes, 16 inputs a lane and step.  Rows of up to KEPT * 4096
@@ -60,14 +70,7 @@ __global__ __launch_bounds__(256) void code_rows_kernel(const T *__restrict__ X,
         for (int i = 0; i < 16; ++i) most = fmaxf(most, finite_abs((float)s.v[i], bad));
     };
     auto code = [&](const Sixteen<T> &s, int c, float inv) {
-        uint32_t w[4];
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            w[i] = 0;
-#pragma unroll
-            for (int j = 0; j < 4; ++j) w[i] |= (uint32_t)(code_of((float)s.v[4 * i + j], inv) & 255) << (8 * j);
-        }
-        *reinterpret_cast<uint4 *>(out + c / 4 * kPiece + c % 4 * 256) = make_uint4(w[0], w[1], w[2], w[3]);
+        *reinterpret_cast<uint4 *>(out + c / 4 * kPiece + c % 4 * 256) = s.codes(inv);
     };
     if (KEPT > 0) {
 #pragma unroll
@@ -159,11 +162,14 @@ __device__ __forceinline__ Int4 multiply(const Int4 &w, const Int4 &x, const Int
 // add up through LDS.  Operands come straight from memory, kAhead steps of 64 inputs at once.
 template <typename T, int OP, int TP, int WAVES>
 __global__ __launch_bounds__(WAVES * 64) void shared_depth_kernel(const uint8_t *__restrict__ W,
-                                                                  const uint8_t *__restrict__ X, int deep, Scaled y) {
+                                                                  const uint8_t *__restrict__ X, int deep, int t_tiles,
+                                                                  Scaled y) {
     constexpr int kAhead = OP + TP <= 3 ? 4 : 2;
+    constexpr bool kOverlap = OP * TP >= 8;
     __shared__ Int4 red[WAVES][OP * TP][64];
     const int lane = threadIdx.x & 63, wave = wave_index();
-    const int64_t o0 = (int64_t)blockIdx.x * OP, t0 = (int64_t)blockIdx.y * TP;
+    const int n = (int)die_order(blockIdx.x, gridDim.x);  // the token tiles of an output tile on one die
+    const int64_t o0 = (int64_t)(n / t_tiles) * OP, t0 = (int64_t)(n % t_tiles) * TP;
     const int64_t last_o = (y.d_out - 1) / kRows, last_t = (y.m - 1) / kRows;
     const uint8_t *w[OP], *x[TP];
 #pragma unroll
@@ -172,23 +178,39 @@ __global__ __launch_bounds__(WAVES * 64) void shared_depth_kernel(const uint8_t 
     for (int i = 0; i < TP; ++i) x[i] = X + min(t0 + i, last_t) * deep * kPiece + lane * 16;
     Int4 acc[OP][TP] = {};
     const int k0 = (int)((int64_t)deep * wave / WAVES), k1 = (int)((int64_t)deep * (wave + 1) / WAVES);
-    for (int k = k0; k < k1; k += kAhead) {
-        Int4 a[kAhead][OP], b[kAhead][TP];
+    Int4 a[2][kAhead][OP], b[2][kAhead][TP];
+    auto load = [&](int k, int buf) {  // past the last step: that one again, which nothing multiplies
 #pragma unroll
         for (int u = 0; u < kAhead; ++u) {
             const int at = min(k + u, k1 - 1) * kPiece;
 #pragma unroll
-            for (int i = 0; i < OP; ++i) a[u][i] = *reinterpret_cast<const Int4 *>(w[i] + at);
+            for (int i = 0; i < OP; ++i) a[buf][u][i] = *reinterpret_cast<const Int4 *>(w[i] + at);
 #pragma unroll
-            for (int i = 0; i < TP; ++i) b[u][i] = *reinterpret_cast<const Int4 *>(x[i] + at);
+            for (int i = 0; i < TP; ++i) b[buf][u][i] = *reinterpret_cast<const Int4 *>(x[i] + at);
         }
+    };
+    auto compute = [&](int k, int buf) {
 #pragma unroll
         for (int u = 0; u < kAhead; ++u) {
             if (k + u >= k1) break;
 #pragma unroll
             for (int i = 0; i < OP; ++i)
 #pragma unroll
-                for (int j = 0; j < TP; ++j) acc[i][j] = multiply(a[u][i], b[u][j], acc[i][j]);
+                for (int j = 0; j < TP; ++j) acc[i][j] = multiply(a[buf][u][i], b[buf][u][j], acc[i][j]);
+        }
+    };
+    if (!kOverlap) {
+        for (int k = k0; k < k1; k += kAhead) {
+            load(k, 0);
+            compute(k, 0);
+        }
+    } else if (k0 < k1) {
+        load(k0, 0);
+        for (int k = k0; k < k1; k += 2 * kAhead) {
+            load(k + kAhead, 1);
+            compute(k, 0);
+            load(k + 2 * kAhead, 0);
+            compute(k + kAhead, 1);
         }
     }
 #pragma unroll
@@ -204,94 +226,211 @@ __global__ __launch_bounds__(WAVES * 64) void shared_depth_kernel(const uint8_t 
     }
 }
 
+// One or two tokens in one launch: every workgroup codes the tokens for itself, 16 inputs a lane, while the first pieces
+// of its 16 outputs' weights are on their way; the wavefronts share the depth.  Against coding them in a launch of
+// its own, us: 1 token 8192 -> 1024 5.7 and 9.1, -> 28672 34.3 and 39.2; 2 tokens 8192 -> 8192 17.0 and 19.2; 4
+// tokens 25.8 and 19.3, which is why it ends there.
+constexpr int kFewWaves = 16, kFewDepth = kFewWaves * 64 * 16;
+
+template <typename TX, int M>
+__global__ __launch_bounds__(kFewWaves * 64) void few_tokens_kernel(const uint8_t *__restrict__ W, const TX *__restrict__ X,
+                                                                    int64_t d, int64_t ldx, int deep, Scaled y, int dtype,
+                                                                    int32_t *__restrict__ status) {
+    constexpr int kAhead = 4;
+    __shared__ __align__(16) uint8_t codes[M * kFewDepth];
+    __shared__ Int4 red[kFewWaves][64];
+    __shared__ float most[M][kFewWaves], scales[M];
+    const int lane = threadIdx.x & 63, wave = wave_index(), m = (int)y.m;
+    const uint8_t *w = W + (int64_t)blockIdx.x * deep * kPiece + lane * 16;
+    const int k0 = deep * wave / kFewWaves, k1 = deep * (wave + 1) / kFewWaves;
+    Int4 a[kAhead];
+    auto load = [&](int k) {
+#pragma unroll
+        for (int u = 0; u < kAhead; ++u) a[u] = *reinterpret_cast<const Int4 *>(w + (int64_t)min(k + u, deep - 1) * kPiece);
+    };
+    const int c = threadIdx.x, chunks = deep * 4;
+    Sixteen<TX> x[M];
+#pragma unroll
+    for (int t = 0; t < M; ++t) x[t].load(X + min(t, m - 1) * ldx + c * 16, c < chunks ? d - c * 16 : 0);
+    load(k0);
+    bool bad = false;
+#pragma unroll
+    for (int t = 0; t < M; ++t) {
+        float v = 0.f;
+#pragma unroll
+        for (int i = 0; i < 16; ++i) v = fmaxf(v, finite_abs((float)x[t].v[i], bad));
+#pragma unroll
+        for (int s = 32; s > 0; s >>= 1) v = fmaxf(v, __shfl_xor(v, s, CMPQ_WAVE));
+        if (lane == 0) most[t][wave] = v;
+    }
+    if (bad && status && blockIdx.x == 0) atomicOr(status, CMPQ_STATUS_NONFINITE);
+    __syncthreads();
+#pragma unroll
+    for (int t = 0; t < M; ++t) {
+        float v = most[t][0];
+#pragma unroll
+        for (int q = 1; q < kFewWaves; ++q) v = fmaxf(v, most[t][q]);
+        const float s = code_scale(v), inv = 1.f / s;
+        if (threadIdx.x == 0) scales[t] = s;
+        if (c < chunks) *reinterpret_cast<uint4 *>(codes + t * kFewDepth + c * 16) = x[t].codes(inv);
+    }
+    __syncthreads();
+    Int4 acc = {};
+    const uint8_t *mine = codes + min(lane & 15, m - 1) * kFewDepth + (lane >> 4) * 16;
+    for (int k = k0; k < k1; k += kAhead) {
+#pragma unroll
+        for (int u = 0; u < kAhead; ++u) {
+            if (k + u >= k1) break;
+            acc = multiply(a[u], *reinterpret_cast<const Int4 *>(mine + (k + u) * kDepth), acc);
+        }
+        if (k + kAhead < k1) load(k + kAhead);
+    }
+    red[wave][lane] = acc;
+    __syncthreads();
+    if (wave != 0) return;
+#pragma unroll
+    for (int v = 1; v < kFewWaves; ++v) acc += red[v][lane];
+    y.sx = scales;
+    with_dtype(dtype, [&](auto like) { put4<decltype(like)>(y, lane & 15, (int64_t)blockIdx.x * kRows + (lane >> 4) * 4, acc); });
+}
+
 __device__ __forceinline__ void load_lds16(const uint8_t *src, uint8_t *dst) {
     __builtin_amdgcn_global_load_lds(reinterpret_cast<const __attribute__((address_space(1))) uint32_t *>(reinterpret_cast<uintptr_t>(src)),
                                      reinterpret_cast<__attribute__((address_space(3))) uint32_t *>((uint32_t)reinterpret_cast<uintptr_t>(dst)), 16, 0, 0);
 }
 
-// Many tokens: 256 outputs by 256 tokens a workgroup of 8 wavefronts, 128 by 64 a wavefront.  Pieces reach LDS by direct
-// loads in the order in which they are read (no conflicts); a step of 64 inputs is one buffer of 32 KB, and
-// kBuffers - 1 steps are on their way while one is multiplied.
-constexpr int kTile = 16, kStepBytes = 2 * kTile * kPiece, kBuffers = 4, kBand = 4;
+// Tiles of OT x TT pieces a workgroup, WO x WT wavefronts.  Pieces reach LDS by direct loads in the order in which they
+// are read (no conflicts), BUFS steps of 64 inputs in a ring; while a step is multiplied its operands are in
+// registers, those of the next are on their way from LDS and the steps after it from memory.
+constexpr int kBand = 4;
 
-template <typename T>
-__global__ __launch_bounds__(512, 2) void tile_kernel(const uint8_t *__restrict__ W, const uint8_t *__restrict__ X,
-                                                      int deep, int o_tiles, int t_tiles, Scaled y) {
-    __shared__ __align__(16) uint8_t smem[kBuffers * kStepBytes];
+template <typename T, int OT, int TT, int WO, int WT, int BUFS>
+__global__ __launch_bounds__(WO * WT * 64, 2) void tile_kernel(const uint8_t *__restrict__ W, const uint8_t *__restrict__ X,
+                                                               int deep, int o_tiles, int t_tiles, Scaled y) {
+    constexpr int kWaves = WO * WT, kLoads = (OT + TT) / kWaves, kStepBytes = (OT + TT) * kPiece, A = OT / WO, B = TT / WT;
+    static_assert(kLoads * kWaves == OT + TT && A * WO == OT && B * WT == TT, "shares of the wavefronts");
+    __shared__ __align__(16) uint8_t smem[BUFS * kStepBytes];
     const int lane = threadIdx.x & 63, wave = wave_index();
     // bands of kBand token tiles, all output tiles of a band one after the other
     const int64_t n = die_order(blockIdx.x, (int64_t)o_tiles * t_tiles);
     const int band = (int)(n / ((int64_t)kBand * o_tiles)), in_band = (int)(n - (int64_t)band * kBand * o_tiles);
     const int wide = min(kBand, t_tiles - band * kBand);
-    const int64_t o0 = (int64_t)(in_band / wide) * kTile, t0 = (int64_t)(band * kBand + in_band % wide) * kTile;
+    const int64_t o0 = (int64_t)(in_band / wide) * OT, t0 = (int64_t)(band * kBand + in_band % wide) * TT;
     const int64_t last_o = (y.d_out - 1) / kRows, last_t = (y.m - 1) / kRows;
-    // wavefronts 0..3 bring 4 pieces of W each, the others of X
-    const uint8_t *src[4];
+    const uint8_t *src[kLoads];
 #pragma unroll
-    for (int q = 0; q < 4; ++q) {
-        const int k = 4 * (wave & 3) + q;
-        src[q] = (wave < 4 ? W + min(o0 + k, last_o) * deep * kPiece : X + min(t0 + k, last_t) * deep * kPiece) + lane * 16;
+    for (int q = 0; q < kLoads; ++q) {
+        const int k = wave * kLoads + q;
+        src[q] = (k < OT ? W + min(o0 + k, last_o) * deep * kPiece : X + min(t0 + k - OT, last_t) * deep * kPiece) + lane * 16;
     }
-    uint8_t *dst = smem + wave * 4 * kPiece;
-    auto load = [&](int step) {  // past the last step: that one again, which nothing reads
-        const int64_t at = (int64_t)min(step, deep - 1) * kPiece;
-        uint8_t *to = dst + (step % kBuffers) * kStepBytes;
-#pragma unroll
-        for (int q = 0; q < 4; ++q) load_lds16(src[q] + at, to + q * kPiece);
+    uint8_t *dst = smem + wave * kLoads * kPiece;
+    auto load = [&](int step, int q) {  // past the last step: that one again, which nothing reads
+        load_lds16(src[q] + min(step, deep - 1) * kPiece, dst + (step % BUFS) * kStepBytes + q * kPiece);
     };
-    const int wo = (wave & 1) * 8, wt = (wave >> 1) * 4;
-    Int4 acc[8][4] = {};
-#pragma unroll
-    for (int u = 0; u < kBuffers - 1; ++u) load(u);
-    for (int step = 0; step < deep; ++step) {
-        // This wavefront's 4 loads of the oldest step have landed (two later steps, 8 loads, are under way) and its LDS
-        // reads of the step before have returned.  After the barrier both hold for every wavefront.
-        static_assert(kBuffers == 4, "the count of loads still under way");
-        asm volatile("s_waitcnt vmcnt(8) lgkmcnt(0)" ::: "memory");
+    const int wo = wave % WO * A, wt = wave / WO * B;
+    Int4 acc[A][B] = {}, a[2][A], b[2][B];
+    auto fetch = [&](int step, int buf, int q) {  // operand q of those of W, then of X
+        const uint8_t *from = smem + (step % BUFS) * kStepBytes + lane * 16;
+        if (q < A) a[buf][q] = *reinterpret_cast<const Int4 *>(from + (wo + q) * kPiece);
+        else b[buf][q - A] = *reinterpret_cast<const Int4 *>(from + (OT + wt + q - A) * kPiece);
+    };
+    // This wavefront's loads of `step` have landed (those of BUFS - 2 later steps are under way) and its LDS reads have
+    // returned.  After the barrier both hold for every wavefront: the step may be read, and the buffer of the one
+    // before it loaded again.
+    auto arrive = [&]() {
+        constexpr int kUnder = (BUFS - 2) * kLoads;
+        static_assert(kUnder < 64, "the count of loads still under way");
+        __builtin_amdgcn_sched_barrier(0);
+        __builtin_amdgcn_s_waitcnt((kUnder & 15) | (kUnder >> 4) << 14 | 7 << 4);  // vmcnt(kUnder) lgkmcnt(0)
         __builtin_amdgcn_s_barrier();
         asm volatile("" ::: "memory");
-        load(step + kBuffers - 1);
-        const uint8_t *buf = smem + (step % kBuffers) * kStepBytes + lane * 16;
-        Int4 a[8], b[4];
+    };
+    // Multiplies a step while the next one's operands come from LDS and a later one's pieces from memory, a share of
+    // each at a time: issued together, the loads fill the memory pipeline's queue and hold up all behind them.
+    auto turn = [&](int step, int buf) {
+        arrive();
 #pragma unroll
-        for (int q = 0; q < 4; ++q) b[q] = *reinterpret_cast<const Int4 *>(buf + (kTile + wt + q) * kPiece);
+        for (int s = 0; s < kLoads; ++s) {
 #pragma unroll
-        for (int q = 0; q < 8; ++q) a[q] = *reinterpret_cast<const Int4 *>(buf + (wo + q) * kPiece);
+            for (int q = (A + B) * s / kLoads; q < (A + B) * (s + 1) / kLoads; ++q) fetch(step + 1, buf ^ 1, q);
 #pragma unroll
-        for (int p = 0; p < 8; ++p)
+            for (int i = A * B * s / kLoads; i < A * B * (s + 1) / kLoads; ++i) {
+                acc[i / B][i % B] = multiply(a[buf][i / B], b[buf][i % B], acc[i / B][i % B]);
+                if (i == A * B * (2 * s + 1) / (2 * kLoads)) load(step + BUFS, s);
+            }
+            __builtin_amdgcn_sched_barrier(0);
+        }
+    };
 #pragma unroll
-            for (int q = 0; q < 4; ++q) acc[p][q] = multiply(a[p], b[q], acc[p][q]);
+    for (int u = 0; u < BUFS - 1; ++u)
+#pragma unroll
+        for (int q = 0; q < kLoads; ++q) load(u, q);
+    arrive();
+#pragma unroll
+    for (int q = 0; q < A + B; ++q) fetch(0, 0, q);
+#pragma unroll
+    for (int q = 0; q < kLoads; ++q) load(BUFS - 1, q);
+    for (int step = 0; step < deep; step += 2) {  // the depth is a multiple of two steps
+        turn(step, 0);
+        turn(step + 1, 1);
     }
-    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");  // the loads that nothing reads end before the LDS does
+    asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");  // what nothing reads ends before the LDS does
 #pragma unroll
-    for (int q = 0; q < 4; ++q)
+    for (int q = 0; q < B; ++q)
 #pragma unroll
-        for (int p = 0; p < 8; ++p)
+        for (int p = 0; p < A; ++p)
             put4<T>(y, (t0 + wt + q) * kRows + (lane & 15), (o0 + wo + p) * kRows + (lane >> 4) * 4, acc[p][q]);
+}
+
+template <typename T, int OT, int TT, int WO, int WT, int BUFS>
+void launch_tiles(const uint8_t *W, const uint8_t *X, int deep, const Scaled &y, hipStream_t st) {
+    const int o_tiles = (int)cdiv(y.d_out, OT * kRows), t_tiles = (int)cdiv(y.m, TT * kRows);
+    tile_kernel<T, OT, TT, WO, WT, BUFS><<<dim3((unsigned)(o_tiles * t_tiles)), WO * WT * 64, 0, st>>>(W, X, deep, o_tiles, t_tiles, y);
 }
 
 template <typename T, int OP, int TP, int WAVES>
 void launch_shared(const uint8_t *W, const uint8_t *X, int deep, const Scaled &y, hipStream_t st) {
-    const dim3 grid((unsigned)cdiv(y.d_out, OP * kRows), (unsigned)cdiv(y.m, TP * kRows));
-    shared_depth_kernel<T, OP, TP, WAVES><<<grid, WAVES * 64, 0, st>>>(W, X, deep, y);
+    const int64_t t_tiles = cdiv(y.m, TP * kRows), tiles = cdiv(y.d_out, OP * kRows) * t_tiles;
+    shared_depth_kernel<T, OP, TP, WAVES><<<dim3((unsigned)tiles), WAVES * 64, 0, st>>>(W, X, deep, (int)t_tiles, y);
 }
 
+int64_t tiles_of(const Scaled &y, int ot, int tt) { return cdiv(y.d_out, ot * kRows) * cdiv(y.m, tt * kRows); }
+
+// Which kernel: the largest tile that fills the chip.  A tile of 256 x 256 or 256 x 128 takes a compute unit for itself, so
+// its last round has to be two thirds full, or one of many.  us (4096 tokens 8192 -> 28672; 2048 tokens 4096 ->
+// 4096; 1024 tokens 4096 -> 4096; 512 tokens 4096 -> 11008): 256 x 256 759, 61, 59, 64; 256 x 128 877, 44, 37, 42; 128 x
+// 128 916, 45, 29, 48; 64 x 64 (333 tokens 4099 -> 3001 22.4, 128 x 128 32.5; 48 tokens 4096 -> 11008 17.1, 25.4).  Fewer than
+// 150 tiles of 64 x 64, and up to 32 tokens: wavefronts share the depth (512 tokens 8192 -> 1024 18.8, 64 x 64
+// 22.9; 64 tokens 4096 -> 4096 10.7, 13.4).  Up to 16 tokens: two pieces of outputs a workgroup where there are many
+// (16 tokens 5120 -> 13824 19.8, one piece 22.5), 8 wavefronts for some (8192 -> 8192 19.0, 16 wavefronts 20.4), 16
+// for few (1 token 8192 -> 1024 9.1, 8 wavefronts 10.8).
 template <typename T>
 int launch_product(const uint8_t *W, const uint8_t *X, int deep, const Scaled &y, hipStream_t st) {
-    const int o_tiles = (int)cdiv(y.d_out, kTile * kRows), t_tiles = (int)cdiv(y.m, kTile * kRows);
-    if (y.m <= 16) {
-        if (cdiv(y.d_out, 32) >= 512) launch_shared<T, 2, 1, 8>(W, X, deep, y, st);
-        else launch_shared<T, 1, 1, 16>(W, X, deep, y, st);
-    } else if (y.m <= 32) {
-        launch_shared<T, 2, 2, 8>(W, X, deep, y, st);
-    } else if ((int64_t)o_tiles * t_tiles < 200 && cdiv(y.m, 64) < 65536) {
-        launch_shared<T, 4, 4, 4>(W, X, deep, y, st);
-    } else {
-        if ((int64_t)o_tiles * t_tiles > INT32_MAX) return CMPQ_ESHAPE;
-        tile_kernel<T><<<dim3((unsigned)(o_tiles * t_tiles)), 512, 0, st>>>(W, X, deep, o_tiles, t_tiles, y);
-    }
+    constexpr int64_t kUnits = 256;  // compute units
+    auto fills = [](int64_t n) { return n >= 4 * kUnits || (n >= kUnits * 5 / 8 && (n + kUnits / 3) / kUnits * kUnits >= n); };
+    const int64_t pieces = cdiv(y.d_out, kRows);
+    if (tiles_of(y, 1, 1) > INT32_MAX) return CMPQ_ESHAPE;
+    if (y.m <= 16 && pieces >= 768) launch_shared<T, 2, 1, 8>(W, X, deep, y, st);
+    else if (y.m <= 16 && pieces >= 320) launch_shared<T, 1, 1, 8>(W, X, deep, y, st);
+    else if (y.m <= 16) launch_shared<T, 1, 1, 16>(W, X, deep, y, st);
+    else if (y.m <= 32) launch_shared<T, 4, 2, 4>(W, X, deep, y, st);
+    else if (fills(tiles_of(y, 16, 16))) launch_tiles<T, 16, 16, 4, 2, 4>(W, X, deep, y, st);
+    else if (fills(tiles_of(y, 16, 8))) launch_tiles<T, 16, 8, 4, 2, 4>(W, X, deep, y, st);
+    else if (tiles_of(y, 8, 8) >= 192) launch_tiles<T, 8, 8, 2, 2, 4>(W, X, deep, y, st);
+    else if (tiles_of(y, 4, 4) >= 150) launch_tiles<T, 4, 4, 2, 2, 8>(W, X, deep, y, st);
+    else launch_shared<T, 4, 2, 4>(W, X, deep, y, st);
     CMPQ_LAUNCH_CHECK();
     return CMPQ_OK;
+}
+
+template <typename TX>
+void launch_few(const uint8_t *W, const void *X, int64_t d, int64_t ldx, const Scaled &y, int y_dtype, int32_t *status,
+                hipStream_t st) {
+    const dim3 grid((unsigned)cdiv(y.d_out, kRows));
+    const TX *x = static_cast<const TX *>(X);
+    const int deep = (int)pieces_deep(d);
+    if (y.m == 1) few_tokens_kernel<TX, 1><<<grid, kFewWaves * 64, 0, st>>>(W, x, d, ldx, deep, y, y_dtype, status);
+    else few_tokens_kernel<TX, 2><<<grid, kFewWaves * 64, 0, st>>>(W, x, d, ldx, deep, y, y_dtype, status);
 }
 
 struct Work {
@@ -339,11 +478,18 @@ extern "C" int cmpq_int8_product(const void *X, int dtype, int64_t m, int64_t d_
     const Work w = carve(ws, m, d_in);
     if (!ws || reinterpret_cast<uintptr_t>(ws) % 256 || ws_bytes < w.bytes) return CMPQ_EWORKSPACE;
     hipStream_t st = static_cast<hipStream_t>(stream);
-    if (int rc = launch_code_rows_of(X, dtype, m, d_in, ldx, m, w.codes, w.scale, status, st)) return rc;
     const size_t four = 4 * dtype_bytes(y_dtype);
     const Scaled y = {w.scale, scale, Y, m, d_out, ldy,
                       ldy % 4 == 0 && reinterpret_cast<uintptr_t>(Y) % four == 0 && reinterpret_cast<uintptr_t>(scale) % 16 == 0};
     const uint8_t *cw = reinterpret_cast<const uint8_t *>(codes), *cx = reinterpret_cast<const uint8_t *>(w.codes);
+    if (m <= 2 && d_in <= kFewDepth) {
+        if (dtype == CMPQ_F16) launch_few<_Float16>(cw, X, d_in, ldx, y, y_dtype, status, st);
+        else if (dtype == CMPQ_BF16) launch_few<__bf16>(cw, X, d_in, ldx, y, y_dtype, status, st);
+        else launch_few<float>(cw, X, d_in, ldx, y, y_dtype, status, st);
+        CMPQ_LAUNCH_CHECK();
+        return CMPQ_OK;
+    }
+    if (int rc = launch_code_rows_of(X, dtype, m, d_in, ldx, m, w.codes, w.scale, status, st)) return rc;
     const int deep = (int)pieces_deep(d_in);
     if (y_dtype == CMPQ_F16) return launch_product<_Float16>(cw, cx, deep, y, st);
     if (y_dtype == CMPQ_BF16) return launch_product<__bf16>(cw, cx, deep, y, st);
