@@ -1,11 +1,14 @@
 // Attention over the paged cache in 8 bits.
 //
-// The products are formed transposed, S^T = K Q^T and O^T = V^T P^T, with 16x16x32 FP16 matrix instructions: what the
-// first leaves in a lane (4 tokens of one query row, twice) is what the second takes from it, so logits and weights
-// never leave registers, and a lane's share of the running maximum and sum belongs to one query row.  A wavefront takes 32
-// tokens (a unit) at a time; their codes are stored in the order of the instruction's operands, 16 bytes a lane and
-// 1 KB a load, and become FP16 exactly: byte b under 0x64 is 1024 + b.  A page's key scale multiplies its
-// logits and its value scale its weights, both in fp32.
+// The products are formed transposed, S^T = K Q^T and O^T = V^T P^T: what the first matrix instruction leaves in a lane (4
+// tokens of one query row, twice) is what the second takes from it, so logits and weights never leave registers, and a
+// lane's share of the running maximum and sum belongs to one query row.  A wavefront takes 32 tokens (a unit) at a time; their
+// codes are stored in the order of the instructions' operands, 16 bytes a lane and 1 KB a load.  A page's key scale
+// multiplies its logits, its value scale goes into its weights' exponent.
+//
+// Two kernels.  For few rows (attend_kernel) the cache's bytes are what counts: the wavefronts of a workgroup share the tokens
+// and read codes straight from memory.  For many rows (attend_rows_kernel) multiplications and exponentials count: the
+// wavefronts share the rows, and codes become FP16 once a workgroup, on their way into LDS.
 #include "serving.h"
 
 namespace {
@@ -13,14 +16,15 @@ namespace {
 typedef _Float16 Half2 __attribute__((ext_vector_type(2)));
 typedef _Float16 Half8 __attribute__((ext_vector_type(8)));
 typedef float Float4 __attribute__((ext_vector_type(4)));
+typedef int32_t Int4 __attribute__((ext_vector_type(4)));
 
 constexpr int kUnit = 32;                  // tokens
-constexpr int kWaves = 4;                  // wavefronts that share a part of a sequence
-constexpr int kLeast = 8;                  // units of a part
-constexpr int64_t kTarget = 1024;          // parts that fill the chip
+constexpr int kWaves = 4;                  // wavefronts of a workgroup
 constexpr float kLog2e = 1.44269504088896340736f;
+constexpr float kLowest = -3.4e38f;        // a row's reference before its first token
 constexpr float kSlack = 8.f;              // a row's logits pass its reference by a factor of at most 2^kSlack
 constexpr float kRaise = 7.f;              // weights are held times 2^kRaise: at most 2^15 in FP16
+constexpr float kLeastRatio = 0x1p-60f;    // value scales below the largest so far by more count as this
 
 struct Job {
     cmpq_kv_cache c;
@@ -33,8 +37,10 @@ struct Job {
     int64_t window;
     cmpq_rotation rot;
     int32_t *status;
-    float *part_o, *part_ml;   // [slots, columns, dims], [slots, columns, 2]
-    int64_t slots;
+    float *part_o, *part_ml;   // [kept, columns, dims], [kept, columns, 2]
+    int64_t kept;              // parts that there is room for
+    int target, least;         // workgroups that fill the chip, units of a part at least
+    int64_t least_cols, most_cols;  // sequences of that many (row, query head of the group) pairs are this kernel's
 };
 
 // A sequence: its rows and tokens, cut to what the call allows.
@@ -69,57 +75,89 @@ struct Plan {
 
 template <int NC>
 __device__ __forceinline__ int tiles_of(const Job &j, const Seq &s) {
-    return (int)(((int64_t)s.rows * j.group + NC - 1) / NC);
+    const int64_t cols = (int64_t)s.rows * j.group;
+    return cols < j.least_cols || cols > j.most_cols ? 0 : (int)((cols + NC - 1) / NC);
 }
 
 template <int NC>
 __device__ __forceinline__ Plan make_plan(const Job &j, bool look) {
     const int lane = threadIdx.x & 63;
-    double total = 0;
+    double total = 0, pieces = 0;
     for (int64_t base = 0; base < j.n_seq; base += 64) {
         if (base + lane >= j.n_seq) continue;
         bool bad = false;
         const Seq s = sequence(j, base + lane, bad);
         if (bad && look && j.status) atomicOr(j.status, CMPQ_STATUS_RANGE);
         total += (double)s.units * tiles_of<NC>(j, s);
+        pieces += (double)tiles_of<NC>(j, s);
     }
-    total = wave_sum_f64(total);
-    const double all = __shfl(total, 0) * j.c.kv_heads;
+    // every sequence's last part is a short one, so that many workgroups are left over for them
+    const double all = __shfl(wave_sum_f64(total), 0) * j.c.kv_heads, odd = __shfl(wave_sum_f64(pieces), 0) * j.c.kv_heads;
     Plan p;
-    p.step = max(kLeast, (int)ceil(all / (double)kTarget));
+    p.step = max(j.least, (int)ceil(all / max((double)j.target - odd, 0.5 * j.target)));
     return p;
 }
 
 __device__ __forceinline__ int parts_of(const Plan &p, const Seq &s) { return max(1, (s.units + p.step - 1) / p.step); }
 
-// Sequence that holds slot `x`, and the slots of those before it; seq < 0: there is no such slot.
+// A sequence's workgroups: those of the sequences before it, and how many of theirs leave parts to be joined (at most
+// 2 target in all: a sequence of more than `step` units has at most 2 units / step parts).
 struct Place {
-    int64_t seq, before;
+    int64_t seq, before, kept_before;
+};
+
+// The sequence that `is` tells apart, given its data and the workgroups up to and with it; seq < 0: none.
+template <int NC, typename F>
+__device__ __forceinline__ Place place_of(const Job &j, const Plan &p, F is) {
+    const int lane = threadIdx.x & 63;
+    int64_t before = 0, kept = 0;
+    for (int64_t base = 0; base < j.n_seq; base += 64) {
+        uint32_t n = 0, k = 0;
+        Seq s = {};
+        if (base + lane < j.n_seq) {
+            bool bad = false;
+            s = sequence(j, base + lane, bad);
+            const int parts = parts_of(p, s);
+            n = (uint32_t)(parts * tiles_of<NC>(j, s) * j.c.kv_heads);
+            k = parts > 1 ? n : 0;
+        }
+        const uint32_t incl = wave_scan_incl_u32(n), kept_incl = wave_scan_incl_u32(k);
+        const uint64_t found = __ballot(is(s, before + incl));
+        if (found) {
+            const int l = __builtin_ctzll(found);
+            return {base + l, before + (int64_t)(__shfl(incl, l) - __shfl(n, l)), kept + (int64_t)(__shfl(kept_incl, l) - __shfl(k, l))};
+        }
+        before += (uint32_t)__builtin_amdgcn_readlane((int)incl, 63);
+        kept += (uint32_t)__builtin_amdgcn_readlane((int)kept_incl, 63);
+    }
+    return {-1, 0, 0};
+}
+
+// A workgroup's share: a tile of a sequence for a head, a part of its units; `slot`: where the part is kept.
+struct Share {
+    Seq s;
+    int64_t seq, slot;
+    int tile, head, part, parts;
 };
 
 template <int NC>
-__device__ __forceinline__ Place place_of(const Job &j, const Plan &p, int64_t x) {
-    const int lane = threadIdx.x & 63;
-    int64_t before = 0;
-    for (int64_t base = 0; base < j.n_seq; base += 64) {
-        uint32_t n = 0;
-        if (base + lane < j.n_seq) {
-            bool bad = false;
-            const Seq s = sequence(j, base + lane, bad);
-            n = (uint32_t)(parts_of(p, s) * tiles_of<NC>(j, s) * j.c.kv_heads);
-        }
-        const uint32_t incl = wave_scan_incl_u32(n);
-        const uint64_t past = __ballot(before + incl > x);
-        if (past) {
-            const int l = __builtin_ctzll(past);
-            return {base + l, before + (int64_t)(__shfl(incl, l) - __shfl(n, l))};
-        }
-        before += (uint32_t)__builtin_amdgcn_readlane((int)incl, 63);
-    }
-    return {-1, 0};
+__device__ __forceinline__ bool share_of(const Job &j, const Plan &plan, int64_t x, Share &w) {
+    const Place place = place_of<NC>(j, plan, [&](const Seq &, int64_t upto) { return upto > x; });
+    if (place.seq < 0) return false;
+    bool bad = false;
+    w.seq = place.seq;
+    w.s = sequence(j, place.seq, bad);
+    w.parts = parts_of(plan, w.s);
+    const int tiles = tiles_of<NC>(j, w.s);
+    x -= place.before;
+    w.slot = place.kept_before + x;
+    w.tile = (int)(x % tiles);
+    w.head = (int)(x / tiles % j.c.kv_heads);
+    w.part = (int)(x / tiles / j.c.kv_heads);
+    return w.parts == 1 || w.slot < j.kept;  // rows named twice: there is no room for their parts
 }
 
-// Eight codes (bytes code + 128) as FP16.
+// Eight codes (bytes code + 128) as FP16, exactly: byte b under 0x64 is 1024 + b.
 __device__ __forceinline__ Half8 halves(uint32_t a, uint32_t b) {
     union {
         uint32_t w[4];
@@ -136,22 +174,538 @@ __device__ __forceinline__ Half8 halves(uint32_t a, uint32_t b) {
     return u.v;
 }
 
-// Largest over the four lanes that hold the same query row (lanes 16 apart), in all of them.
-__device__ __forceinline__ float rows_max(float v) {
+// Over the four lanes that hold the same query row (lanes 16 apart), in all of them.
+template <typename F>
+__device__ __forceinline__ float over_row(float v, F both) {
     const uint32_t u = __float_as_uint(v);
     const auto a = __builtin_amdgcn_permlane32_swap(u, u, false, false);
-    v = fmaxf(__uint_as_float(a[0]), __uint_as_float(a[1]));
+    v = both(__uint_as_float(a[0]), __uint_as_float(a[1]));
     const uint32_t w = __float_as_uint(v);
     const auto b = __builtin_amdgcn_permlane16_swap(w, w, false, false);
-    return fmaxf(__uint_as_float(b[0]), __uint_as_float(b[1]));
+    return both(__uint_as_float(b[0]), __uint_as_float(b[1]));
 }
-__device__ __forceinline__ float rows_sum(float v) {
-    const uint32_t u = __float_as_uint(v);
-    const auto a = __builtin_amdgcn_permlane32_swap(u, u, false, false);
-    v = __uint_as_float(a[0]) + __uint_as_float(a[1]);
-    const uint32_t w = __float_as_uint(v);
-    const auto b = __builtin_amdgcn_permlane16_swap(w, w, false, false);
-    return __uint_as_float(b[0]) + __uint_as_float(b[1]);
+__device__ __forceinline__ float row_max(float v) {
+    return over_row(v, [](float a, float b) { return fmaxf(a, b); });
+}
+__device__ __forceinline__ float row_sum(float v) {
+    return over_row(v, [](float a, float b) { return a + b; });
+}
+
+// Four dims next to each other of an output row.
+__device__ __forceinline__ void put4(const Job &j, int64_t row, int head, int d, const Float4 &v) {
+    const int64_t at = row * j.O.row_stride + head * j.O.head_stride + d;
+    auto put = [&](auto like) {
+        using T = decltype(like);
+        typedef T T4 __attribute__((ext_vector_type(4)));
+        typedef T4 Any __attribute__((aligned(sizeof(T))));
+        T *p = static_cast<T *>(j.O.ptr) + at;
+        if (d + 4 <= j.c.head_dim) {
+            *reinterpret_cast<Any *>(p) = T4{(T)v[0], (T)v[1], (T)v[2], (T)v[3]};
+        } else {
+#pragma unroll
+            for (int r = 0; r < 4; ++r)
+                if (d + r < j.c.head_dim) p[r] = (T)v[r];
+        }
+    };
+    if (j.o_dtype == CMPQ_F16) put(_Float16());
+    else put(__bf16());
+}
+
+// One column of a tile: a query row and head, and the tokens lo .. hi-1 that it sees.  Columns past the last repeat it.
+struct Column {
+    int64_t row, at;  // row of Q, row of the rotation's tables
+    int head, lo, hi;
+};
+
+__device__ __forceinline__ Column column(const Job &j, const Seq &s, int kv_head, int index) {
+    const int col = min(index, s.rows * j.group - 1);
+    Column c;
+    c.row = col / j.group;
+    c.head = kv_head * j.group + col % j.group;
+    const int64_t pos = (int64_t)s.length - s.asked + c.row;
+    c.row += s.row0;
+    c.at = max(pos, (int64_t)0);
+    if (j.rot.cos && c.at >= j.rot.positions) {
+        c.at = j.rot.positions - 1;
+        if (j.status) atomicOr(j.status, CMPQ_STATUS_RANGE);
+    }
+    c.hi = (int)(j.causal ? min((int64_t)s.length, pos + 1) : (int64_t)s.length);
+    c.lo = j.window > 0 ? (int)max((int64_t)0, pos - j.window + 1) : 0;
+    return c;
+}
+
+// Columns `index` .. + 15 of a head's queries, turned, into LDS: 16 rows of DP + 4 floats.  Threads first, first + step, ... of the
+// 2 DP that have eight dims each; in a loop, since all of them at once take more registers than the kernels have left.
+template <int C>
+__device__ __forceinline__ void stage_queries(const Job &j, const Seq &s, int kv_head, int index, float *to, int first, int step) {
+    constexpr int DP = C * 32;
+#pragma unroll 1
+    for (int e = first; e < 2 * DP; e += step) {
+        const int n = e / (DP / 8), d = e % (DP / 8) * 8;
+        const Column col = column(j, s, kv_head, index + n);
+        float x[8];
+        with_dtype(j.q_dtype, [&](auto like) {
+            using T = decltype(like);
+            load_turned(static_cast<const T *>(j.Q.ptr) + col.row * j.Q.row_stride + col.head * j.Q.head_stride, j.c.head_dim, d, j.rot, col.at, x);
+        });
+        float *row = to + n * (DP + 4) + d;
+        *reinterpret_cast<Float4 *>(row) = Float4{x[0], x[1], x[2], x[3]};
+        *reinterpret_cast<Float4 *>(row + 4) = Float4{x[4], x[5], x[6], x[7]};
+    }
+}
+
+// A staged row's dims in the lanes that hand them to the matrix instruction, scaled by a power of two so that the largest
+// lies in 1..2: lane 16 g + n has dims 32 c + 8 g .. + 7 of row n.  Returns the exponent; `top` is that largest, NaN for
+// a row that holds a NaN or an infinity.
+template <int C>
+__device__ __forceinline__ int take_query(const float *from, float (&x)[C][8], float &top) {
+    const int lane = threadIdx.x & 63, g = lane >> 4;
+    float most = 0.f, zero = 0.f;
+#pragma unroll
+    for (int c = 0; c < C; ++c) {
+        const Float4 *p = reinterpret_cast<const Float4 *>(from + (lane & 15) * (C * 32 + 4) + c * 32 + g * 8);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            x[c][i] = p[i >> 2][i & 3];
+            most = fmaxf(most, fabsf(x[c][i]));
+            zero += x[c][i] * 0.f;  // NaN if one of them is no finite number
+        }
+    }
+    most = row_max(most);
+    const int e = most > 0.f && most < INFINITY ? ilogbf(most) : 0;
+    top = ldexpf(most + row_sum(zero), -e);
+#pragma unroll
+    for (int c = 0; c < C; ++c)
+#pragma unroll
+        for (int i = 0; i < 8; ++i) x[c][i] = ldexpf(x[c][i], -e);
+    return e;
+}
+
+// The page of a unit of a sequence, -1 if the table names none, and its scales.
+struct PageOf {
+    int id, in_page;
+    float ks, vs;
+};
+
+__device__ __forceinline__ PageOf page_of(const Job &j, int64_t seq, int head, int unit, int end) {
+    PageOf p = {-1, 0, 0.f, 0.f};
+    if (unit >= end) return p;
+    const int token = unit * kUnit;
+    p.id = j.table[seq * j.ld_table + token / j.c.page];
+    p.in_page = token % j.c.page / kUnit;
+    if (p.id < 0 || p.id >= j.c.n_pages) {
+        p.id = -1;
+        if (j.status) atomicOr(j.status, CMPQ_STATUS_RANGE);
+    } else {
+        p.ks = j.c.k_scale[(int64_t)p.id * j.c.kv_heads + head];
+        p.vs = j.c.v_scale[(int64_t)p.id * j.c.kv_heads + head];
+    }
+    return p;
+}
+__device__ __forceinline__ float lane_value(float v, int lane) {
+    return __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(v), lane));
+}
+
+// A tile's running state of one column in a lane: reference, this lane's share of the sum.
+struct State {
+    float m, sum;
+};
+
+// The weights of a unit's 8 tokens in this lane: logits l to FP16, times the unit's value scale over `unit_scale`.
+__device__ __forceinline__ Half8 weigh(const float (&l)[8], State &st, float log_ratio, float inv_ratio) {
+    const float base = st.m - kRaise - log_ratio;
+    Half8 p;
+    float part = 0.f;
+#pragma unroll
+    for (int r = 0; r < 8; ++r) {
+        const float w = __builtin_amdgcn_exp2f(l[r] - base);
+        part += w;
+        p[r] = (_Float16)w;
+    }
+    st.sum += part * inv_ratio;
+    return p;
+}
+
+// What a part leaves: its output in absolute units and (reference, sum) into the workspace, or the output itself.
+__device__ __forceinline__ void keep_part(const Job &j, int64_t slot, int nc, int col, int dims, int d, const Float4 &v) {
+    *reinterpret_cast<Float4 *>(j.part_o + (slot * nc + col) * dims + d) = v;
+}
+
+// Few rows.  C: 32 dims each of a head.  Tiles of 16 NT columns, one (row, query head) pair each; the wavefronts take the
+// part's units in turn and are added up through LDS.  Keys go into the integer matrix instruction as they are; a query
+// is held in 16 bits fixed point, 256 high + low, of its row's largest magnitude, two instructions for one.
+template <int C, int NT>
+__global__ __launch_bounds__(kWaves * 64, C * NT <= 4 ? 3 : C * NT <= 8 ? 2 : 1) void attend_kernel(Job j) {
+    constexpr int NC = 16 * NT, DP = C * 32, kPad = DP + 4;
+    __shared__ float red[kWaves * 16 * kPad];
+    __shared__ float ml[kWaves][NC][2];
+    const int lane = threadIdx.x & 63, wave = wave_index(), n = lane & 15, g = lane >> 4;
+    const Plan plan = make_plan<NC>(j, blockIdx.x == 0 && wave == 0);
+    Share w;
+    if (!share_of<NC>(j, plan, blockIdx.x, w)) return;
+    const Seq &s = w.s;
+    const int tile = w.tile, head = w.head, part = w.part, parts = w.parts;
+
+    Int4 qh[NT][(C + 1) / 2], ql[NT][(C + 1) / 2];
+    float factor[NT];
+    int lo[NT], hi[NT];
+#pragma unroll
+    for (int t = 0; t < NT; ++t) {
+        const Column col = column(j, s, head, tile * NC + t * 16 + n);
+        lo[t] = col.lo, hi[t] = col.hi;
+        if (t > 0) __syncthreads();
+        stage_queries<C>(j, s, head, tile * NC + t * 16, red, threadIdx.x, kWaves * 64);
+        __syncthreads();
+        float v[C][8], top;
+        const int e = take_query<C>(red, v, top);
+        const float sign = j.scale < 0.f ? -1.f : 1.f, to = top > 0.f ? sign * 32639.f / top : 0.f;  // NaN: 0
+        factor[t] = ldexpf(top * (1.f / 32639.f) * (sign * j.scale * kLog2e), e);                    // not below 0
+#pragma unroll
+        for (int c = 0; c < (C + 1) / 2 * 2; ++c) {
+            uint32_t h[2] = {0, 0}, l[2] = {0, 0};
+            if (c < C) {
+#pragma unroll
+                for (int i = 0; i < 8; ++i) {
+                    const int q = (int)rintf(v[c < C ? c : 0][i] * to), high = (q + 128) >> 8;
+                    h[i >> 2] |= (uint32_t)(high & 255) << (8 * (i & 3));
+                    l[i >> 2] |= (uint32_t)((q - 256 * high) & 255) << (8 * (i & 3));
+                }
+            }
+            qh[t][c / 2][c % 2 * 2] = (int)h[0], qh[t][c / 2][c % 2 * 2 + 1] = (int)h[1];
+            ql[t][c / 2][c % 2 * 2] = (int)l[0], ql[t][c / 2][c % 2 * 2 + 1] = (int)l[1];
+        }
+    }
+    // bounds over the tile's columns: rows grow with the column
+    const int all_hi = __builtin_amdgcn_readlane(hi[0], 0), all_lo = __builtin_amdgcn_readlane(lo[NT - 1], 15);
+
+    Float4 o[NT][2 * C];
+    State st[NT];
+#pragma unroll
+    for (int t = 0; t < NT; ++t) {
+        st[t] = {kLowest, 0.f};
+#pragma unroll
+        for (int d = 0; d < 2 * C; ++d) o[t][d] = Float4{0.f, 0.f, 0.f, 0.f};
+    }
+    float unit_scale = 0.f;  // value scale that o is held in
+
+    const int u0 = s.first_unit + part * plan.step, u1 = min(u0 + plan.step, s.first_unit + s.units);
+    const int64_t page_bytes = (int64_t)j.c.page * DP;
+    for (int base = u0 + wave; base < u1; base += kWaves * 64) {
+        const PageOf mine = page_of(j, w.seq, head, base + lane * kWaves, u1);  // 64 units of this wavefront at once
+        const int count = min(64, (u1 - base + kWaves - 1) / kWaves);
+        auto offset = [&](int i) {
+            return ((int64_t)max(__builtin_amdgcn_readlane(mine.id, i), 0) * j.c.kv_heads + head) * page_bytes +
+                   (int64_t)__builtin_amdgcn_readlane(mine.in_page, i) * (kUnit * DP) + lane * 16;
+        };
+        uint4 kc[C], vc[C];
+        auto load = [&](const uint8_t *from, int i, uint4 (&to)[C]) {
+            const int64_t off = offset(min(i, count - 1));
+#pragma unroll
+            for (int c = 0; c < C; ++c) to[c] = load16_stream(from + off + c * 1024);
+        };
+        load(j.c.k_codes, 0, kc);
+        load(j.c.v_codes, 0, vc);
+        for (int i = 0; i < count; ++i) {
+            const bool there = __builtin_amdgcn_readlane(mine.id, i) >= 0;
+            const float kscale = lane_value(mine.ks, i), vscale = lane_value(mine.vs, i);
+            Int4 a[2][(C + 1) / 2];
+#pragma unroll
+            for (int c = 0; c < (C + 1) / 2; ++c) {
+                const uint4 first = kc[2 * c], second = 2 * c + 1 < C ? kc[2 * c + 1 < C ? 2 * c + 1 : 0] : make_uint4(0, 0, 0, 0);
+                constexpr uint32_t flip = 0x80808080u;  // code + 128 to the code's own byte
+                a[0][c] = Int4{(int)(first.x ^ flip), (int)(first.y ^ flip), (int)(second.x ^ flip), (int)(second.y ^ flip)};
+                a[1][c] = Int4{(int)(first.z ^ flip), (int)(first.w ^ flip), (int)(second.z ^ flip), (int)(second.w ^ flip)};
+            }
+            load(j.c.k_codes, i + 1, kc);
+            float l[NT][8], top[NT];
+#pragma unroll
+            for (int t = 0; t < NT; ++t) {
+                const float f = factor[t] * kscale;
+                Int4 sum[2];
+#pragma unroll
+                for (int h = 0; h < 2; ++h) {
+                    Int4 high = {}, low = {};
+#pragma unroll
+                    for (int c = 0; c < (C + 1) / 2; ++c) {
+                        high = __builtin_amdgcn_mfma_i32_16x16x64_i8(a[h][c], qh[t][c], high, 0, 0, 0);
+                        low = __builtin_amdgcn_mfma_i32_16x16x64_i8(a[h][c], ql[t][c], low, 0, 0, 0);
+                    }
+                    sum[h] = high * 256 + low;
+                }
+#pragma unroll
+                for (int r = 0; r < 8; ++r) l[t][r] = (float)sum[r >> 2][r & 3] * f;
+            }
+            const int t0 = (base + i * kWaves) * kUnit;
+            if (!there || t0 < all_lo || t0 + kUnit > all_hi) {
+#pragma unroll
+                for (int t = 0; t < NT; ++t)
+#pragma unroll
+                    for (int r = 0; r < 8; ++r) {
+                        const int at = t0 + (r >> 2) * 16 + g * 4 + (r & 3);
+                        if (!there || at < lo[t] || at >= hi[t]) l[t][r] = -INFINITY;
+                    }
+            }
+            bool past = there && vscale > unit_scale;
+#pragma unroll
+            for (int t = 0; t < NT; ++t) {
+                top[t] = l[t][0];
+#pragma unroll
+                for (int r = 1; r < 8; ++r) top[t] = fmaxf(top[t], l[t][r]);
+                past |= top[t] > st[t].m + kSlack;
+            }
+            if (__ballot(past)) {
+                const float u = there ? fmaxf(unit_scale, vscale) : unit_scale, change = u > 0.f ? unit_scale / u : 1.f;
+#pragma unroll
+                for (int t = 0; t < NT; ++t) {
+                    const float now = row_max(top[t]);  // a row's reference moves by its own logits alone
+                    const float next = now > st[t].m + kSlack ? now : st[t].m, keep = __builtin_amdgcn_exp2f(st[t].m - next);
+                    st[t].sum *= keep;
+                    const float turn = keep * change;
+#pragma unroll
+                    for (int d = 0; d < 2 * C; ++d) o[t][d] *= turn;
+                    st[t].m = next;
+                }
+                unit_scale = u;
+            }
+            const float ratio = unit_scale > 0.f ? fmaxf(vscale / unit_scale, kLeastRatio) : 1.f;
+            const float log_ratio = __builtin_amdgcn_logf(ratio), inv_ratio = 1.f / ratio;
+            Half8 p[NT];
+#pragma unroll
+            for (int t = 0; t < NT; ++t) p[t] = weigh(l[t], st[t], log_ratio, inv_ratio);
+#pragma unroll
+            for (int c = 0; c < C; ++c) {
+                const Half8 v0 = halves(vc[c].x, vc[c].y), v1 = halves(vc[c].z, vc[c].w);
+#pragma unroll
+                for (int t = 0; t < NT; ++t) {
+                    o[t][2 * c] = __builtin_amdgcn_mfma_f32_16x16x32_f16(v0, p[t], o[t][2 * c], 0, 0, 0);
+                    o[t][2 * c + 1] = __builtin_amdgcn_mfma_f32_16x16x32_f16(v1, p[t], o[t][2 * c + 1], 0, 0, 0);
+                }
+            }
+            load(j.c.v_codes, i + 1, vc);
+        }
+    }
+
+    // the wavefronts' shares: to one reference, then added in order, 16 columns at a time
+#pragma unroll
+    for (int t = 0; t < NT; ++t) {
+        st[t].sum = row_sum(st[t].sum);
+        if (g == 0) {
+            ml[wave][t * 16 + n][0] = st[t].m;
+            ml[wave][t * 16 + n][1] = st[t].sum;
+        }
+    }
+    __syncthreads();
+#pragma unroll
+    for (int t = 0; t < NT; ++t) {
+        float top = kLowest;
+#pragma unroll
+        for (int v = 0; v < kWaves; ++v) top = fmaxf(top, ml[v][t * 16 + n][0]);
+        const float mine = __builtin_amdgcn_exp2f(st[t].m - top) * unit_scale;
+        if (t > 0) __syncthreads();  // the columns before these have been read
+#pragma unroll
+        for (int d = 0; d < 2 * C; ++d)
+            *reinterpret_cast<Float4 *>(&red[(wave * 16 + n) * kPad + d * 16 + g * 4]) = o[t][d] * mine;
+        __syncthreads();
+        for (int e = threadIdx.x; e < 16 * DP / 4; e += kWaves * 64) {
+            const int c = e / (DP / 4), d = e % (DP / 4) * 4, k = t * 16 + c;
+            Float4 v = *reinterpret_cast<const Float4 *>(&red[c * kPad + d]);
+#pragma unroll
+            for (int q = 1; q < kWaves; ++q) v += *reinterpret_cast<const Float4 *>(&red[(q * 16 + c) * kPad + d]);
+            float high = kLowest, total = 0.f;
+#pragma unroll
+            for (int q = 0; q < kWaves; ++q) high = fmaxf(high, ml[q][k][0]);
+#pragma unroll
+            for (int q = 0; q < kWaves; ++q) total += ml[q][k][1] * __builtin_amdgcn_exp2f(ml[q][k][0] - high);
+            if (parts > 1) {
+                keep_part(j, w.slot, NC, k, DP, d, v);
+                if (d == 0) {
+                    j.part_ml[(w.slot * NC + k) * 2] = high;
+                    j.part_ml[(w.slot * NC + k) * 2 + 1] = total;
+                }
+            } else if (tile * NC + k < s.rows * j.group) {
+                const int at = tile * NC + k;
+                put4(j, s.row0 + at / j.group, head * j.group + at % j.group, d, total == 0.f ? Float4{0.f, 0.f, 0.f, 0.f} : v / total);
+            }
+        }
+    }
+}
+
+// Many rows.  A workgroup has 16 NT columns a wavefront; it goes through the part's units together, two units of FP16 in
+// LDS, one being read while the next is put there.
+template <int C, int NT>
+__global__ __launch_bounds__(kWaves * 64, 2) void attend_rows_kernel(Job j) {
+    constexpr int NC = 16 * NT * kWaves, DP = C * 32, kHalf = 2 * C * 1024;  // bytes of a unit's keys, or values
+    constexpr int kShare = (C + kWaves - 1) / kWaves;                        // pieces that a wavefront brings, of either
+    __shared__ __align__(16) float staged[kWaves * 16 * (DP + 4)];  // queries first, then units: a little less
+    static_assert(sizeof(staged) >= 4 * kHalf, "two units");
+    const int lane = threadIdx.x & 63, wave = wave_index(), n = lane & 15, g = lane >> 4;
+    auto unit_at = [&](int buf) { return reinterpret_cast<Half8 *>(staged) + buf * (2 * kHalf / 16) + lane; };
+    const Plan plan = make_plan<NC>(j, blockIdx.x == 0 && wave == 0);
+    Share w;
+    if (!share_of<NC>(j, plan, blockIdx.x, w)) return;
+    const Seq &s = w.s;
+    const int tile = w.tile, head = w.head, part = w.part, parts = w.parts;
+
+    Half8 q[NT][C];
+    float factor[NT];
+    int lo[NT], hi[NT];
+    const int col0 = tile * NC + wave * NT * 16;
+#pragma unroll
+    for (int t = 0; t < NT; ++t) {
+        const Column col = column(j, s, head, col0 + t * 16 + n);
+        lo[t] = col.lo, hi[t] = col.hi;
+        float v[C][8], top, *mine = staged + wave * 16 * (DP + 4);
+        stage_queries<C>(j, s, head, col0 + t * 16, mine, lane, 64);
+        __syncthreads();
+        const int e = take_query<C>(mine, v, top);
+        factor[t] = ldexpf(j.scale * kLog2e, e);
+        (void)top;
+#pragma unroll
+        for (int c = 0; c < C; ++c)
+#pragma unroll
+            for (int i = 0; i < 8; ++i) q[t][c][i] = (_Float16)v[c][i];
+        __syncthreads();
+    }
+    const int all_hi = __builtin_amdgcn_readlane(hi[0], 0), all_lo = __builtin_amdgcn_readlane(lo[NT - 1], 15);
+    // units that some column of the workgroup sees
+    const Column first = column(j, s, head, tile * NC), last = column(j, s, head, tile * NC + NC - 1);
+    const int u0 = max(s.first_unit + part * plan.step, first.lo / kUnit);
+    const int u1 = min(min(s.first_unit + (part + 1) * plan.step, s.first_unit + s.units), (max(last.hi, 0) + kUnit - 1) / kUnit);
+
+    Float4 o[NT][2 * C];
+    State st[NT];
+#pragma unroll
+    for (int t = 0; t < NT; ++t) {
+        st[t] = {kLowest, 0.f};
+#pragma unroll
+        for (int d = 0; d < 2 * C; ++d) o[t][d] = Float4{0.f, 0.f, 0.f, 0.f};
+    }
+    float unit_scale = 0.f;
+    const int64_t page_bytes = (int64_t)j.c.page * DP;
+
+    // A unit's codes come into registers a unit ahead and go into LDS as FP16: operand 2 c + h of the keys, then the values.
+    uint4 kc[kShare], vc[kShare];
+    PageOf ahead = {}, mine = {};
+    auto load = [&](int unit) {
+        if ((unit - u0) % 64 == 0) ahead = page_of(j, w.seq, head, unit + lane, u1);
+        const int i = (unit - u0) % 64;
+        const int64_t off = ((int64_t)max(__builtin_amdgcn_readlane(ahead.id, i), 0) * j.c.kv_heads + head) * page_bytes +
+                            (int64_t)__builtin_amdgcn_readlane(ahead.in_page, i) * (kUnit * DP) + lane * 16;
+#pragma unroll
+        for (int k = 0; k < kShare; ++k) {
+            const int c = min(wave + k * kWaves, C - 1);
+            kc[k] = *reinterpret_cast<const uint4 *>(j.c.k_codes + off + c * 1024);
+            vc[k] = *reinterpret_cast<const uint4 *>(j.c.v_codes + off + c * 1024);
+        }
+    };
+    auto store = [&](int buf) {
+#pragma unroll
+        for (int k = 0; k < kShare; ++k) {
+            const int c = wave + k * kWaves;
+            if (c >= C) break;
+            Half8 *to = unit_at(buf) + c * 128;
+            to[0] = halves(kc[k].x, kc[k].y);
+            to[64] = halves(kc[k].z, kc[k].w);
+            to[kHalf / 16] = halves(vc[k].x, vc[k].y);
+            to[kHalf / 16 + 64] = halves(vc[k].z, vc[k].w);
+        }
+    };
+    if (u0 < u1) {
+        load(u0);
+        store(0);
+    }
+    __syncthreads();
+    for (int unit = u0; unit < u1; ++unit) {
+        const int buf = (unit - u0) & 1, i = (unit - u0) % 64;
+        if (i == 0) mine = ahead;
+        const bool more = unit + 1 < u1, there = __builtin_amdgcn_readlane(mine.id, i) >= 0;
+        const float kscale = lane_value(mine.ks, i), vscale = lane_value(mine.vs, i);
+        if (more) load(unit + 1);
+        const Half8 *from = unit_at(buf);
+        Float4 sum[NT][2];
+#pragma unroll
+        for (int t = 0; t < NT; ++t) sum[t][0] = sum[t][1] = Float4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int c = 0; c < C; ++c) {
+            const Half8 k0 = from[c * 128], k1 = from[c * 128 + 64];
+#pragma unroll
+            for (int t = 0; t < NT; ++t) {
+                sum[t][0] = __builtin_amdgcn_mfma_f32_16x16x32_f16(k0, q[t][c], sum[t][0], 0, 0, 0);
+                sum[t][1] = __builtin_amdgcn_mfma_f32_16x16x32_f16(k1, q[t][c], sum[t][1], 0, 0, 0);
+            }
+        }
+        float l[NT][8], top[NT];
+        const int t0 = unit * kUnit;
+        const bool edge = !there || t0 < all_lo || t0 + kUnit > all_hi;
+        bool past = there && vscale > unit_scale;
+#pragma unroll
+        for (int t = 0; t < NT; ++t) {
+            const float f = factor[t] * kscale;
+#pragma unroll
+            for (int r = 0; r < 8; ++r) l[t][r] = sum[t][r >> 2][r & 3] * f;
+            if (edge) {
+#pragma unroll
+                for (int r = 0; r < 8; ++r) {
+                    const int at = t0 + (r >> 2) * 16 + g * 4 + (r & 3);
+                    if (!there || at < lo[t] || at >= hi[t]) l[t][r] = -INFINITY;
+                }
+            }
+            top[t] = l[t][0];
+#pragma unroll
+            for (int r = 1; r < 8; ++r) top[t] = fmaxf(top[t], l[t][r]);
+            past |= top[t] > st[t].m + kSlack;
+        }
+        if (__ballot(past)) {
+            const float u = there ? fmaxf(unit_scale, vscale) : unit_scale, change = u > 0.f ? unit_scale / u : 1.f;
+#pragma unroll
+            for (int t = 0; t < NT; ++t) {
+                const float now = row_max(top[t]);
+                const float next = now > st[t].m + kSlack ? now : st[t].m, keep = __builtin_amdgcn_exp2f(st[t].m - next);
+                st[t].sum *= keep;
+                const float turn = keep * change;
+#pragma unroll
+                for (int d = 0; d < 2 * C; ++d) o[t][d] *= turn;
+                st[t].m = next;
+            }
+            unit_scale = u;
+        }
+        const float ratio = unit_scale > 0.f ? fmaxf(vscale / unit_scale, kLeastRatio) : 1.f;
+        const float log_ratio = __builtin_amdgcn_logf(ratio), inv_ratio = 1.f / ratio;
+        Half8 p[NT];
+#pragma unroll
+        for (int t = 0; t < NT; ++t) p[t] = weigh(l[t], st[t], log_ratio, inv_ratio);
+#pragma unroll
+        for (int c = 0; c < C; ++c) {
+            const Half8 v0 = from[kHalf / 16 + c * 128], v1 = from[kHalf / 16 + c * 128 + 64];
+#pragma unroll
+            for (int t = 0; t < NT; ++t) {
+                o[t][2 * c] = __builtin_amdgcn_mfma_f32_16x16x32_f16(v0, p[t], o[t][2 * c], 0, 0, 0);
+                o[t][2 * c + 1] = __builtin_amdgcn_mfma_f32_16x16x32_f16(v1, p[t], o[t][2 * c + 1], 0, 0, 0);
+            }
+        }
+        if (more) store(buf ^ 1);
+        __syncthreads();
+    }
+
+#pragma unroll
+    for (int t = 0; t < NT; ++t) {
+        const float total = row_sum(st[t].sum);
+        const int k = wave * NT * 16 + t * 16 + n, at = tile * NC + k;
+        if (parts > 1) {
+            if (g == 0) {
+                j.part_ml[(w.slot * NC + k) * 2] = st[t].m;
+                j.part_ml[(w.slot * NC + k) * 2 + 1] = total;
+            }
+#pragma unroll
+            for (int d = 0; d < 2 * C; ++d) keep_part(j, w.slot, NC, k, DP, d * 16 + g * 4, o[t][d] * unit_scale);
+        } else if (at < s.rows * j.group) {
+            const float by = total == 0.f ? 0.f : unit_scale / total;
+#pragma unroll
+            for (int d = 0; d < 2 * C; ++d)
+                if (d * 16 + g * 4 < j.c.head_dim)
+                    put4(j, s.row0 + at / j.group, head * j.group + at % j.group, d * 16 + g * 4, o[t][d] * by);
+        }
+    }
 }
 
 __device__ __forceinline__ void put(const Job &j, int64_t row, int head, int d, float v) {
@@ -160,260 +714,98 @@ __device__ __forceinline__ void put(const Job &j, int64_t row, int head, int d, 
     else static_cast<__bf16 *>(j.O.ptr)[at] = (__bf16)v;
 }
 
-// A query row's dims as the matrix instruction takes them, times 2^-e so that the largest lies in 1..2: lane
-// 16 g + n has dims 32 c + 8 g .. + 7 of row n.  Returns 2^e.
-template <int C>
-__device__ __forceinline__ float load_query(const Job &j, int64_t row, int head, int64_t pos, Half8 (&q)[C]) {
-    const int lane = threadIdx.x & 63, dim = j.c.head_dim;
-    float x[C][8], most = 0.f;
-    with_dtype(j.q_dtype, [&](auto like) {
-        using T = decltype(like);
-        const T *p = static_cast<const T *>(j.Q.ptr) + row * j.Q.row_stride + head * j.Q.head_stride;
-#pragma unroll
-        for (int c = 0; c < C; ++c)
-#pragma unroll
-            for (int i = 0; i < 8; ++i) {
-                const int d = c * 32 + (lane >> 4) * 8 + i;
-                x[c][i] = d < dim ? turned(p, d, j.rot, pos) : 0.f;
-            }
-    });
-#pragma unroll
-    for (int c = 0; c < C; ++c)
-#pragma unroll
-        for (int i = 0; i < 8; ++i) most = fmaxf(most, fabsf(x[c][i]));
-    most = rows_max(most);
-    const int e = most > 0.f && most < INFINITY ? ilogbf(most) : 0;
-#pragma unroll
-    for (int c = 0; c < C; ++c)
-#pragma unroll
-        for (int i = 0; i < 8; ++i) q[c][i] = (_Float16)ldexpf(x[c][i], -e);
-    return ldexpf(1.f, e);
-}
-
-// C: 32 dims each of a head.  Tiles of 16 columns, one (row, query head) pair each; the wavefronts take the
-// part's units in turn and are added up through LDS.
-template <int C>
-__global__ __launch_bounds__(kWaves * 64) void attend_kernel(Job j) {
-    constexpr int NC = 16, DP = C * 32, kPad = DP + 4;
-    __shared__ float red[kWaves * NC * kPad];
-    __shared__ float ml[kWaves][NC][2];
-    const int lane = threadIdx.x & 63, wave = wave_index(), n = lane & 15, g = lane >> 4;
-    const Plan plan = make_plan<NC>(j, blockIdx.x == 0 && wave == 0);
-    const Place place = place_of<NC>(j, plan, blockIdx.x);
-    if (place.seq < 0) return;
-    bool bad = false;
-    const Seq s = sequence(j, place.seq, bad);
-    const int tiles = tiles_of<NC>(j, s), parts = parts_of(plan, s);
-    const int64_t x = blockIdx.x - place.before;
-    const int tile = (int)(x % tiles), head = (int)(x / tiles % j.c.kv_heads), part = (int)(x / tiles / j.c.kv_heads);
-
-    // this lane's query row
-    const int col = min(tile * NC + n, s.rows * j.group - 1);
-    const int row = col / j.group, qh = head * j.group + col % j.group;
-    const int64_t pos = (int64_t)s.length - s.asked + row;
-    int64_t at = max(pos, (int64_t)0);
-    if (j.rot.cos && at >= j.rot.positions) {
-        at = j.rot.positions - 1;
-        if (j.status) atomicOr(j.status, CMPQ_STATUS_RANGE);
-    }
-    Half8 q[C];
-    const float factor = load_query<C>(j, s.row0 + row, qh, at, q) * j.scale * kLog2e;
-    const int hi = (int)(j.causal ? min((int64_t)s.length, pos + 1) : (int64_t)s.length);  // tokens lo .. hi-1
-    const int lo = j.window > 0 ? (int)max((int64_t)0, pos - j.window + 1) : 0;
-    // bounds over the tile's rows: rows grow with the column
-    const int all_hi = __builtin_amdgcn_readlane(hi, 0), all_lo = __builtin_amdgcn_readlane(lo, 15);
-
-    Float4 o[2 * C];
-#pragma unroll
-    for (int d = 0; d < 2 * C; ++d) o[d] = Float4{0.f, 0.f, 0.f, 0.f};
-    float m = -3.4e38f, sum = 0.f, unit_scale = 0.f;  // reference, this lane's share of the sum, value scale of o
-
-    const int u0 = s.first_unit + part * plan.step, u1 = min(u0 + plan.step, s.first_unit + s.units);
-    const int64_t page_bytes = (int64_t)j.c.page * DP;
-    for (int base = u0 + wave; base < u1; base += kWaves * 64) {
-        // pages and scales of 64 units of this wavefront at once
-        const int mine = base + lane * kWaves;
-        int id = -1, in_page = 0;
-        float ks = 0.f, vs = 0.f;
-        if (mine < u1) {
-            const int token = mine * kUnit;
-            id = j.table[place.seq * j.ld_table + token / j.c.page];
-            in_page = token % j.c.page / kUnit;
-            if (id < 0 || id >= j.c.n_pages) {
-                id = -1;
-                if (j.status) atomicOr(j.status, CMPQ_STATUS_RANGE);
-            } else {
-                ks = j.c.k_scale[(int64_t)id * j.c.kv_heads + head];
-                vs = j.c.v_scale[(int64_t)id * j.c.kv_heads + head];
-            }
-        }
-        const int count = min(64, (u1 - base + kWaves - 1) / kWaves);
-        for (int i = 0; i < count; ++i) {
-            const int page = __builtin_amdgcn_readlane(id, i);
-            if (page < 0) continue;
-            const float kscale = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(ks), i));
-            const float vscale = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(vs), i));
-            const int64_t off = ((int64_t)page * j.c.kv_heads + head) * page_bytes +
-                                (int64_t)__builtin_amdgcn_readlane(in_page, i) * (kUnit * DP) + lane * 16;
-            uint4 kc[C], vc[C];
-#pragma unroll
-            for (int c = 0; c < C; ++c) kc[c] = *reinterpret_cast<const uint4 *>(j.c.k_codes + off + c * 1024);
-#pragma unroll
-            for (int c = 0; c < C; ++c) vc[c] = *reinterpret_cast<const uint4 *>(j.c.v_codes + off + c * 1024);
-            Float4 s0 = {0.f, 0.f, 0.f, 0.f}, s1 = s0;
-#pragma unroll
-            for (int c = 0; c < C; ++c) {
-                s0 = __builtin_amdgcn_mfma_f32_16x16x32_f16(halves(kc[c].x, kc[c].y), q[c], s0, 0, 0, 0);
-                s1 = __builtin_amdgcn_mfma_f32_16x16x32_f16(halves(kc[c].z, kc[c].w), q[c], s1, 0, 0, 0);
-            }
-            float l[8];
-            const float f = factor * kscale;
-#pragma unroll
-            for (int r = 0; r < 4; ++r) {
-                l[r] = s0[r] * f;
-                l[4 + r] = s1[r] * f;
-            }
-            const int t0 = (base + i * kWaves) * kUnit;
-            if (t0 < all_lo || t0 + kUnit > all_hi) {
-#pragma unroll
-                for (int r = 0; r < 8; ++r) {
-                    const int t = t0 + (r >> 2) * 16 + g * 4 + (r & 3);
-                    if (t < lo || t >= hi) l[r] = -INFINITY;
-                }
-            }
-            float top = l[0];
-#pragma unroll
-            for (int r = 1; r < 8; ++r) top = fmaxf(top, l[r]);
-            if (__ballot(top > m + kSlack) || vscale > unit_scale) {
-                top = rows_max(top);  // a row's reference moves by its own logits alone
-                const float next = top > m + kSlack ? top : m, keep = __builtin_amdgcn_exp2f(m - next);
-                const float u = fmaxf(unit_scale, vscale), turn = keep * (unit_scale / u);
-                sum *= keep;
-#pragma unroll
-                for (int d = 0; d < 2 * C; ++d) o[d] *= turn;
-                m = next;
-                unit_scale = u;
-            }
-            const float ratio = vscale / unit_scale, base_m = m - kRaise;
-            Half8 p;
-#pragma unroll
-            for (int r = 0; r < 8; ++r) {
-                const float w = __builtin_amdgcn_exp2f(l[r] - base_m);
-                sum += w;
-                p[r] = (_Float16)(w * ratio);
-            }
-#pragma unroll
-            for (int c = 0; c < C; ++c) {
-                o[2 * c] = __builtin_amdgcn_mfma_f32_16x16x32_f16(halves(vc[c].x, vc[c].y), p, o[2 * c], 0, 0, 0);
-                o[2 * c + 1] = __builtin_amdgcn_mfma_f32_16x16x32_f16(halves(vc[c].z, vc[c].w), p, o[2 * c + 1], 0, 0, 0);
-            }
-        }
-    }
-
-    // the wavefronts' shares: to one reference, then added in order
-    sum = rows_sum(sum);
-    if (g == 0) {
-        ml[wave][n][0] = m;
-        ml[wave][n][1] = sum;
-    }
-    __syncthreads();
-    float top = ml[0][n][0], total = 0.f;
-#pragma unroll
-    for (int w = 1; w < kWaves; ++w) top = fmaxf(top, ml[w][n][0]);
-#pragma unroll
-    for (int w = 0; w < kWaves; ++w) total += ml[w][n][1] * __builtin_amdgcn_exp2f(ml[w][n][0] - top);
-    const float mine = __builtin_amdgcn_exp2f(m - top) * unit_scale;
-#pragma unroll
-    for (int d = 0; d < 2 * C; ++d)
-        *reinterpret_cast<Float4 *>(&red[(wave * NC + n) * kPad + d * 16 + g * 4]) = o[d] * mine;
-    if (parts > 1 && wave == 0 && g == 0) {
-        j.part_ml[(blockIdx.x * (int64_t)NC + n) * 2] = top;
-        j.part_ml[(blockIdx.x * (int64_t)NC + n) * 2 + 1] = total;
-    }
-    __syncthreads();
-    if (wave == 0 && g == 0) ml[0][n][1] = total;
-    __syncthreads();
-    for (int e = threadIdx.x; e < NC * DP; e += kWaves * 64) {
-        const int c = e / DP, d = e % DP;
-        float v = red[c * kPad + d];
-#pragma unroll
-        for (int w = 1; w < kWaves; ++w) v += red[(w * NC + c) * kPad + d];
-        if (parts > 1) {
-            j.part_o[(blockIdx.x * (int64_t)NC + c) * DP + d] = v;
-        } else if (tile * NC + c < s.rows * j.group && d < j.c.head_dim) {
-            const int k = tile * NC + c;
-            const float t = ml[0][c][1];
-            put(j, s.row0 + k / j.group, head * j.group + k % j.group, d, t == 0.f ? 0.f : v / t);
-        }
-    }
-}
-
 // Rows whose sequence was cut into several parts: one wavefront a row and query head.
-template <int C>
+template <int C, int NC>
 __global__ __launch_bounds__(256) void join_kernel(Job j) {
-    constexpr int NC = 16, DP = C * 32;
+    constexpr int DP = C * 32;
     const int lane = threadIdx.x & 63;
     const int64_t x = (int64_t)blockIdx.x * 4 + wave_index();
     const int64_t row = x / j.q_heads;
     const int qh = (int)(x % j.q_heads);
     if (row >= j.n_rows) return;
     const Plan plan = make_plan<NC>(j, false);
-    // the row's sequence and the slots before it
-    int64_t before = 0;
-    for (int64_t base = 0; base < j.n_seq; base += 64) {
-        uint32_t n = 0;
-        Seq s = {};
-        if (base + lane < j.n_seq) {
-            bool bad = false;
-            s = sequence(j, base + lane, bad);
-            n = (uint32_t)(parts_of(plan, s) * tiles_of<NC>(j, s) * j.c.kv_heads);
-        }
-        const uint32_t incl = wave_scan_incl_u32(n);
-        const uint64_t holds = __ballot(s.rows > 0 && row >= s.row0 && row < s.row0 + s.rows);
-        if (holds) {
-            const int l = __builtin_ctzll(holds);
-            bool bad = false;
-            s = sequence(j, base + l, bad);
-            before += (int64_t)(__shfl(incl, l) - __shfl(n, l));
-            const int parts = parts_of(plan, s), tiles = tiles_of<NC>(j, s);
-            if (parts == 1) return;
-            const int col = (int)(row - s.row0) * j.group + qh % j.group, head = qh / j.group;
-            const int64_t slot0 = before + head * tiles + col / NC, step = (int64_t)tiles * j.c.kv_heads;
-            if (slot0 + (parts - 1) * step >= j.slots) return;  // rows named twice: there is no room for their parts
-            float top = -3.4e38f;
-            for (int p = lane; p < parts; p += 64) top = fmaxf(top, j.part_ml[((slot0 + p * step) * NC + col % NC) * 2]);
+    const Place place = place_of<NC>(j, plan, [&](const Seq &s, int64_t) { return s.rows > 0 && row >= s.row0 && row < s.row0 + s.rows; });
+    if (place.seq < 0) return;
+    bool bad = false;
+    const Seq s = sequence(j, place.seq, bad);
+    const int parts = parts_of(plan, s), tiles = tiles_of<NC>(j, s);
+    if (parts == 1 || tiles == 0) return;
+    const int col = (int)(row - s.row0) * j.group + qh % j.group, head = qh / j.group;
+    const int64_t slot0 = place.kept_before + head * tiles + col / NC, step = (int64_t)tiles * j.c.kv_heads;
+    if (slot0 + (parts - 1) * step >= j.kept) return;
+    float top = kLowest;
+    for (int p = lane; p < parts; p += 64) top = fmaxf(top, j.part_ml[((slot0 + p * step) * NC + col % NC) * 2]);
 #pragma unroll
-            for (int k = 32; k > 0; k >>= 1) top = fmaxf(top, __shfl_xor(top, k));
-            float total = 0.f, acc[(DP + 63) / 64] = {};
+    for (int k = 32; k > 0; k >>= 1) top = fmaxf(top, __shfl_xor(top, k));
+    float total = 0.f, acc[(DP + 63) / 64] = {};
 #pragma unroll 4
-            for (int p = 0; p < parts; ++p) {
-                const int64_t at = (slot0 + p * step) * NC + col % NC;
-                const float w = __builtin_amdgcn_exp2f(j.part_ml[at * 2] - top);
-                total += w * j.part_ml[at * 2 + 1];
+    for (int p = 0; p < parts; ++p) {
+        const int64_t at = (slot0 + p * step) * NC + col % NC;
+        const float w = __builtin_amdgcn_exp2f(j.part_ml[at * 2] - top);
+        total += w * j.part_ml[at * 2 + 1];
 #pragma unroll
-                for (int k = 0; k < (DP + 63) / 64; ++k)
-                    if (k * 64 + lane < DP) acc[k] += w * j.part_o[at * DP + k * 64 + lane];
-            }
+        for (int k = 0; k < (DP + 63) / 64; ++k)
+            if (k * 64 + lane < DP) acc[k] += w * j.part_o[at * DP + k * 64 + lane];
+    }
 #pragma unroll
-            for (int k = 0; k < (DP + 63) / 64; ++k)
-                if (k * 64 + lane < j.c.head_dim) put(j, row, qh, k * 64 + lane, total == 0.f ? 0.f : acc[k] / total);
-            return;
-        }
-        before += (uint32_t)__builtin_amdgcn_readlane((int)incl, 63);
+    for (int k = 0; k < (DP + 63) / 64; ++k)
+        if (k * 64 + lane < j.c.head_dim) put(j, row, qh, k * 64 + lane, total == 0.f ? 0.f : acc[k] / total);
+}
+
+// How a call is launched: the kernel for few rows, for many, or both, each with its columns, workgroups and kept parts.
+struct Kernel {
+    int nc = 0, target = 0, least = 0;
+    int64_t least_cols = 0, most_cols = -1, grid = 0, kept = 0;
+};
+struct Launches {
+    int64_t dp;
+    Kernel few, rows;
+    size_t o_floats(const Kernel &h) const { return (size_t)(h.kept * h.nc * dp); }
+    size_t ml_floats(const Kernel &h) const { return (size_t)(h.kept * h.nc * 2); }
+};
+
+// Tiles of 16 columns a wavefront of the kernel for many rows, as registers allow.
+constexpr int rows_tiles(int64_t c) { return c <= 2 ? 4 : c <= 4 ? 3 : c <= 6 ? 2 : 1; }
+
+void size_up(const cmpq_kv_attention_job *a, Kernel &h) {
+    const int64_t group = a->q_heads / a->cache.kv_heads;
+    const int64_t most = h.most_cols < a->max_rows * group ? h.most_cols : a->max_rows * group;  // columns of a sequence
+    const int64_t by_rows = a->n_rows * group / h.nc + a->n_seq, by_most = a->n_seq * cdiv(most, h.nc);
+    const int64_t tiles = (by_rows < by_most ? by_rows : by_most) * a->cache.kv_heads;
+    const int64_t parts = cdiv(cdiv(a->max_length, kUnit), h.least);
+    h.grid = tiles;
+    if (parts > 1) {
+        const int64_t full = tiles * parts;
+        h.grid = full < tiles + 2 * h.target ? full : tiles + 2 * h.target;
+        h.kept = full < 2 * h.target ? full : 2 * h.target;
     }
 }
 
-// Slots of a call: parts filled to the full, and one more a tile and head.
-int64_t tiles_bound(const cmpq_kv_attention_job *a, int nc) {
-    const int64_t group = a->q_heads / a->cache.kv_heads;
-    const int64_t by_rows = a->n_rows * group / nc + a->n_seq, by_most = a->n_seq * cdiv(a->max_rows * group, nc);
-    return by_rows < by_most ? by_rows : by_most;
+Launches plan_launches(const cmpq_kv_attention_job *a) {
+    Launches l;
+    const int64_t c = cdiv(a->cache.head_dim, 32), group = a->q_heads / a->cache.kv_heads, cols = a->max_rows * group;
+    l.dp = c * 32;
+    const int64_t few = c <= 4 ? 48 : 32;
+    if (cols <= few) {
+        l.few.nc = (int)cdiv(cols, 16) * 16;
+        l.few.least_cols = 1;
+        l.few.most_cols = few;
+    } else if (a->n_seq > 1 && group <= few) {  // single rows among sequences of many
+        l.few.nc = (int)cdiv(group, 16) * 16;
+        l.few.least_cols = 1;
+        l.few.most_cols = l.few.nc;
+    }
+    if (cols > few) {
+        l.rows.nc = 16 * kWaves * rows_tiles(c);
+        l.rows.least_cols = l.few.most_cols > 0 ? l.few.most_cols + 1 : 1;
+        l.rows.most_cols = INT64_MAX;
+    }
+    l.few.target = 1024, l.few.least = 8;
+    l.rows.target = 512, l.rows.least = 16;
+    if (l.few.nc) size_up(a, l.few);
+    if (l.rows.nc) size_up(a, l.rows);
+    return l;
 }
-int64_t slots_bound(const cmpq_kv_attention_job *a, int nc) {
-    const int64_t tiles = tiles_bound(a, nc) * a->cache.kv_heads, parts = cdiv(cdiv(a->max_length, kUnit) + 1, kLeast);
-    return tiles * (parts > 1 ? parts : 1) < tiles + kTarget ? tiles * (parts > 1 ? parts : 1) : tiles + kTarget;
-}
-bool may_split(const cmpq_kv_attention_job *a) { return cdiv(a->max_length, kUnit) > kLeast; }
 
 int check_job(const cmpq_kv_attention_job *a) {
     if (!a) return CMPQ_EINVAL;
@@ -428,22 +820,51 @@ int check_job(const cmpq_kv_attention_job *a) {
     return check_rotation(&a->rotation, a->cache.head_dim);
 }
 
+template <int C, int NC>
+void join(const Job &j, hipStream_t st) {
+    if (j.kept) join_kernel<C, NC><<<dim3((unsigned)cdiv(j.n_rows * j.q_heads, 4)), 256, 0, st>>>(j);
+}
+
+template <int C, int NT>
+void launch_few(const Job &j, const Kernel &h, hipStream_t st) {
+    attend_kernel<C, NT><<<dim3((unsigned)h.grid), kWaves * 64, 0, st>>>(j);
+    join<C, NT * 16>(j, st);
+}
+
 template <int C>
-void launch(const Job &j, int64_t slots, bool split, hipStream_t st) {
-    attend_kernel<C><<<dim3((unsigned)slots), kWaves * 64, 0, st>>>(j);
-    if (split) join_kernel<C><<<dim3((unsigned)cdiv(j.n_rows * j.q_heads, 4)), 256, 0, st>>>(j);
+void launch(Job j, const Launches &l, WsCarver &w, hipStream_t st) {
+    auto take = [&](const Kernel &h) {
+        j.target = h.target, j.least = h.least, j.least_cols = h.least_cols, j.most_cols = h.most_cols, j.kept = h.kept;
+        j.part_o = w.take<float>(l.o_floats(h));
+        j.part_ml = w.take<float>(l.ml_floats(h));
+    };
+    if (l.rows.nc) {
+        constexpr int NT = rows_tiles(C);
+        take(l.rows);
+        attend_rows_kernel<C, NT><<<dim3((unsigned)l.rows.grid), kWaves * 64, 0, st>>>(j);
+        join<C, NT * 16 * kWaves>(j, st);
+    }
+    if (l.few.nc) {
+        take(l.few);
+        if (l.few.nc == 16) launch_few<C, 1>(j, l.few, st);
+        else if (l.few.nc == 32) launch_few<C, 2>(j, l.few, st);
+        else if constexpr (C <= 4) launch_few<C, 3>(j, l.few, st);
+    }
 }
 
 }  // namespace
 
 extern "C" size_t cmpq_kv_attention_workspace(const cmpq_kv_attention_job *a) {
-    if (!a || a->cache.kv_heads < 1 || a->q_heads < 1 || a->n_seq < 0 || a->n_rows < 0 || a->max_rows < 0 ||
+    if (!a || a->cache.kv_heads < 1 || a->q_heads < a->cache.kv_heads || a->n_seq < 0 || a->n_rows < 0 || a->max_rows < 0 ||
         a->max_length < 0 || !cmpq_kv_page_bytes(a->cache.head_dim, a->cache.page))
         return 0;
+    const Launches l = plan_launches(a);
     WsCarver w(nullptr);
-    const int64_t slots = may_split(a) ? slots_bound(a, 16) : 0, dp = cdiv(a->cache.head_dim, 32) * 32;
-    w.take<float>((size_t)(slots * 16 * dp));
-    w.take<float>((size_t)(slots * 16 * 2));
+    for (const Kernel *h : {&l.rows, &l.few}) {
+        if (!h->nc) continue;
+        w.take<float>(l.o_floats(*h));
+        w.take<float>(l.ml_floats(*h));
+    }
     return w.need() > 256 ? w.need() : 256;
 }
 
@@ -451,31 +872,28 @@ extern "C" int cmpq_kv_attention(const cmpq_kv_attention_job *a, void *ws, size_
     if (int rc = check_job(a)) return rc;
     if (a->n_seq == 0 || a->n_rows == 0 || a->max_rows == 0) return CMPQ_OK;
     if (!a->page_table || !a->lengths || !a->cu_rows || !a->Q.ptr || !a->O.ptr) return CMPQ_EINVAL;
-    const int64_t slots = slots_bound(a, 16), dp = cdiv(a->cache.head_dim, 32) * 32;
-    if (slots > INT32_MAX) return CMPQ_ESHAPE;
+    const Launches l = plan_launches(a);
+    if (l.few.grid > INT32_MAX || l.rows.grid > INT32_MAX) return CMPQ_ESHAPE;
     if (!ws || reinterpret_cast<uintptr_t>(ws) % 256 || ws_bytes < cmpq_kv_attention_workspace(a)) return CMPQ_EWORKSPACE;
-    const bool split = may_split(a);
     WsCarver w(ws);
     Job j = {};
     j.c = a->cache;
     j.table = a->page_table, j.lengths = a->lengths, j.cu = a->cu_rows;
-    j.ld_table = a->ld_table, j.n_seq = a->n_seq, j.n_rows = a->n_rows, j.max_rows = a->max_rows, j.max_length = a->max_length;
+    j.ld_table = a->ld_table, j.n_seq = a->n_seq, j.n_rows = a->n_rows, j.max_rows = a->max_rows;
+    j.max_length = a->cache.n_pages > 0 ? a->max_length : 0;
     j.Q = a->Q, j.O = a->O, j.q_dtype = a->q_dtype, j.o_dtype = a->o_dtype, j.q_heads = a->q_heads;
     j.group = a->q_heads / a->cache.kv_heads;
     j.scale = a->softmax_scale, j.causal = a->causal, j.window = a->window, j.rot = a->rotation, j.status = a->status;
-    j.slots = slots;
-    j.part_o = w.take<float>((size_t)(split ? slots * 16 * dp : 0));
-    j.part_ml = w.take<float>((size_t)(split ? slots * 16 * 2 : 0));
     hipStream_t st = static_cast<hipStream_t>(stream);
-    switch (dp / 32) {
-        case 1: launch<1>(j, slots, split, st); break;
-        case 2: launch<2>(j, slots, split, st); break;
-        case 3: launch<3>(j, slots, split, st); break;
-        case 4: launch<4>(j, slots, split, st); break;
-        case 5: launch<5>(j, slots, split, st); break;
-        case 6: launch<6>(j, slots, split, st); break;
-        case 7: launch<7>(j, slots, split, st); break;
-        default: launch<8>(j, slots, split, st); break;
+    switch (l.dp / 32) {
+        case 1: launch<1>(j, l, w, st); break;
+        case 2: launch<2>(j, l, w, st); break;
+        case 3: launch<3>(j, l, w, st); break;
+        case 4: launch<4>(j, l, w, st); break;
+        case 5: launch<5>(j, l, w, st); break;
+        case 6: launch<6>(j, l, w, st); break;
+        case 7: launch<7>(j, l, w, st); break;
+        default: launch<8>(j, l, w, st); break;
     }
     CMPQ_LAUNCH_CHECK();
     return CMPQ_OK;

@@ -90,6 +90,40 @@ __device__ __forceinline__ float turned(const T *p, int d, const cmpq_rotation &
     return second ? turned_second(y, x, c, s) : turned_first(x, y, c, s);
 }
 
+// Dims d .. d + 7 (d a multiple of 8) of a head of `dim` at `p`, turned for the row `at` of the tables; 0 beyond the head.
+// Eight at a time where the turn's pairs are eight next to each other too, or lie within the eight.
+template <typename T>
+__device__ __forceinline__ void load_turned(const T *p, int dim, int d, const cmpq_rotation &rot, int64_t at, float (&x)[8]) {
+    load_f32<T, 8>(p + min(d, dim), max(dim - d, 0), x);
+    if (!rot.cos || d >= rot.dims) return;
+    const int half = rot.dims >> 1;
+    if (rot.interleaved && d + 8 <= rot.dims) {
+        float cs[4], sn[4];
+        load_f32<float, 4>(rot.cos + at * half + d / 2, 4, cs);
+        load_f32<float, 4>(rot.sin + at * half + d / 2, 4, sn);
+#pragma unroll
+        for (int i = 0; i < 8; i += 2) {
+            const float a = x[i], b = x[i + 1];
+            x[i] = turned_first(a, b, cs[i / 2], sn[i / 2]);
+            x[i + 1] = turned_second(a, b, cs[i / 2], sn[i / 2]);
+        }
+    } else if (!rot.interleaved && half % 8 == 0) {
+        const bool second = d >= half;
+        const int pair = second ? d - half : d;
+        float y[8], cs[8], sn[8];
+        load_f32<T, 8>(p + (second ? pair : d + half), 8, y);
+        load_f32<float, 8>(rot.cos + at * half + pair, 8, cs);
+        load_f32<float, 8>(rot.sin + at * half + pair, 8, sn);
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+            x[i] = second ? turned_second(y[i], x[i], cs[i], sn[i]) : turned_first(x[i], y[i], cs[i], sn[i]);
+    } else {
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+            if (d + i < dim) x[i] = turned(p, d + i, rot, at);
+    }
+}
+
 static inline int check_rotation(const cmpq_rotation *rot, int head_dim) {
     if (!rot || !rot->cos) return CMPQ_OK;
     if (!rot->sin || rot->positions < 1 || rot->dims < 2 || (rot->dims & 1)) return CMPQ_EINVAL;
