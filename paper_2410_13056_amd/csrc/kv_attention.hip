@@ -24,7 +24,7 @@ constexpr float kLog2e = 1.44269504088896340736f;
 constexpr float kLowest = -3.4e38f;        // a row's reference before its first token
 constexpr float kSlack = 8.f;              // a row's logits pass its reference by a factor of at most 2^kSlack
 constexpr float kRaise = 7.f;              // weights are held times 2^kRaise: at most 2^15 in FP16
-constexpr float kLeastRatio = 0x1p-60f;    // value scales below the largest so far by more count as this
+constexpr float kLeastLog = -60.f, kMostInverse = 0x1p60f;  // value scales further below the largest so far count as this
 
 struct Job {
     cmpq_kv_cache c;
@@ -67,8 +67,8 @@ __device__ __forceinline__ Seq sequence(const Job &j, int64_t i, bool &bad) {
     return s;
 }
 
-// How the call's work is cut up: a tile is NC (row, query head of the group) pairs of a sequence, a part at most `step`
-// units of it.  Every wavefront works this out for itself from the lengths, 64 sequences at a time.
+// How the call's work is cut up: a tile is NC (row, query head of the group) pairs of a sequence, its units go in equal
+// parts of at most `step`.  Every wavefront works this out for itself from the lengths, 64 sequences at a time.
 struct Plan {
     int step;
 };
@@ -94,7 +94,7 @@ __device__ __forceinline__ Plan make_plan(const Job &j, bool look) {
     // every sequence's last part is a short one, so that many workgroups are left over for them
     const double all = __shfl(wave_sum_f64(total), 0) * j.c.kv_heads, odd = __shfl(wave_sum_f64(pieces), 0) * j.c.kv_heads;
     Plan p;
-    p.step = max(j.least, (int)ceil(all / max((double)j.target - odd, 0.5 * j.target)));
+    p.step = __builtin_amdgcn_readfirstlane(max(j.least, (int)ceil(all / max((double)j.target - odd, 0.5 * j.target))));
     return p;
 }
 
@@ -106,9 +106,9 @@ struct Place {
     int64_t seq, before, kept_before;
 };
 
-// The sequence that `is` tells apart, given its data and the workgroups up to and with it; seq < 0: none.
+// The sequence `wanted`, or that `is` tells apart, given its data and the workgroups up to and with it; seq < 0: none.
 template <int NC, typename F>
-__device__ __forceinline__ Place place_of(const Job &j, const Plan &p, F is) {
+__device__ __forceinline__ Place place_of(const Job &j, const Plan &p, F is, int64_t wanted = -1) {
     const int lane = threadIdx.x & 63;
     int64_t before = 0, kept = 0;
     for (int64_t base = 0; base < j.n_seq; base += 64) {
@@ -122,10 +122,11 @@ __device__ __forceinline__ Place place_of(const Job &j, const Plan &p, F is) {
             k = parts > 1 ? n : 0;
         }
         const uint32_t incl = wave_scan_incl_u32(n), kept_incl = wave_scan_incl_u32(k);
-        const uint64_t found = __ballot(is(s, before + incl));
+        const uint64_t found = __ballot(is(s, before + incl) || base + lane == wanted);
         if (found) {
             const int l = __builtin_ctzll(found);
-            return {base + l, before + (int64_t)(__shfl(incl, l) - __shfl(n, l)), kept + (int64_t)(__shfl(kept_incl, l) - __shfl(k, l))};
+            return {base + l, before + (uint32_t)__builtin_amdgcn_readlane((int)(incl - n), l),
+                    kept + (uint32_t)__builtin_amdgcn_readlane((int)(kept_incl - k), l)};
         }
         before += (uint32_t)__builtin_amdgcn_readlane((int)incl, 63);
         kept += (uint32_t)__builtin_amdgcn_readlane((int)kept_incl, 63);
@@ -137,7 +138,7 @@ __device__ __forceinline__ Place place_of(const Job &j, const Plan &p, F is) {
 struct Share {
     Seq s;
     int64_t seq, slot;
-    int tile, head, part, parts;
+    int tile, head, parts, u0, u1;  // units u0 .. u1-1
 };
 
 template <int NC>
@@ -153,7 +154,9 @@ __device__ __forceinline__ bool share_of(const Job &j, const Plan &plan, int64_t
     w.slot = place.kept_before + x;
     w.tile = (int)(x % tiles);
     w.head = (int)(x / tiles % j.c.kv_heads);
-    w.part = (int)(x / tiles / j.c.kv_heads);
+    const int64_t part = x / tiles / j.c.kv_heads;
+    w.u0 = w.s.first_unit + (int)(w.s.units * part / w.parts);
+    w.u1 = w.s.first_unit + (int)(w.s.units * (part + 1) / w.parts);
     return w.parts == 1 || w.slot < j.kept;  // rows named twice: there is no room for their parts
 }
 
@@ -284,11 +287,11 @@ __device__ __forceinline__ int take_query(const float *from, float (&x)[C][8], f
 // The page of a unit of a sequence, -1 if the table names none, and its scales.
 struct PageOf {
     int id, in_page;
-    float ks, vs;
+    float ks, vs, log_vs, inv_vs;
 };
 
 __device__ __forceinline__ PageOf page_of(const Job &j, int64_t seq, int head, int unit, int end) {
-    PageOf p = {-1, 0, 0.f, 0.f};
+    PageOf p = {-1, 0, 0.f, 0.f, 0.f, 1.f};
     if (unit >= end) return p;
     const int token = unit * kUnit;
     p.id = j.table[seq * j.ld_table + token / j.c.page];
@@ -299,6 +302,8 @@ __device__ __forceinline__ PageOf page_of(const Job &j, int64_t seq, int head, i
     } else {
         p.ks = j.c.k_scale[(int64_t)p.id * j.c.kv_heads + head];
         p.vs = j.c.v_scale[(int64_t)p.id * j.c.kv_heads + head];
+        p.log_vs = log2f(p.vs);
+        p.inv_vs = 1.f / p.vs;
     }
     return p;
 }
@@ -311,18 +316,57 @@ struct State {
     float m, sum;
 };
 
-// The weights of a unit's 8 tokens in this lane: logits l to FP16, times the unit's value scale over `unit_scale`.
-__device__ __forceinline__ Half8 weigh(const float (&l)[8], State &st, float log_ratio, float inv_ratio) {
+// The value scale that a wavefront's outputs are held in: the largest so far, its logarithm.
+struct UnitScale {
+    float scale, log;
+};
+
+// Logits that a unit's products s stand for (s times f), each row's largest; -infinity where the row does not see the token.
+__device__ __forceinline__ float largest(const float (&s)[8], float f) {
+    float top = s[0];
+#pragma unroll
+    for (int r = 1; r < 8; ++r) top = fmaxf(top, s[r]);
+    return top * f;
+}
+
+// What turns a row's products with a page's codes into logits: above 0, so that -infinity stays it; NaN stays NaN.
+__device__ __forceinline__ float logit_factor(float of_row, float kscale) {
+    const float f = of_row * kscale;
+    return f < 0x1p-126f ? 0x1p-126f : f;
+}
+
+// Moves the rows whose logits pass their reference, and the unit scale, and what is held in them.  A row's reference moves
+// by its own logits alone: results do not depend on the rows beside it.
+template <int C, int NT>
+__device__ __forceinline__ void move_up(State (&st)[NT], const float (&top)[NT], Float4 (&o)[NT][2 * C], UnitScale &u, bool there,
+                                        float vscale, float log_vscale) {
+    const bool wider = there && vscale > u.scale;
+    const float change = wider ? u.scale / vscale : 1.f;
+#pragma unroll
+    for (int t = 0; t < NT; ++t) {
+        const float now = row_max(top[t]);
+        const float next = now > st[t].m + kSlack ? now : st[t].m, keep = __builtin_amdgcn_exp2f(st[t].m - next);
+        st[t].sum *= keep;
+        const float turn = keep * change;
+#pragma unroll
+        for (int d = 0; d < 2 * C; ++d) o[t][d] *= turn;
+        st[t].m = next;
+    }
+    if (wider) u = {vscale, log_vscale};
+}
+
+// The weights of a unit's 8 tokens in this lane to FP16, times the unit's value scale over the scale that outputs are held in.
+__device__ __forceinline__ Half8 weigh(const float (&s)[8], float f, State &st, float log_ratio, float inv_ratio) {
     const float base = st.m - kRaise - log_ratio;
     Half8 p;
     float part = 0.f;
 #pragma unroll
     for (int r = 0; r < 8; ++r) {
-        const float w = __builtin_amdgcn_exp2f(l[r] - base);
+        const float w = __builtin_amdgcn_exp2f(fmaf(s[r], f, -base));
         part += w;
         p[r] = (_Float16)w;
     }
-    st.sum += part * inv_ratio;
+    st.sum = fmaf(part, inv_ratio, st.sum);
     return p;
 }
 
@@ -344,7 +388,7 @@ __global__ __launch_bounds__(kWaves * 64, C * NT <= 4 ? 3 : C * NT <= 8 ? 2 : 1)
     Share w;
     if (!share_of<NC>(j, plan, blockIdx.x, w)) return;
     const Seq &s = w.s;
-    const int tile = w.tile, head = w.head, part = w.part, parts = w.parts;
+    const int tile = w.tile, head = w.head, parts = w.parts;
 
     Int4 qh[NT][(C + 1) / 2], ql[NT][(C + 1) / 2];
     float factor[NT];
@@ -359,7 +403,7 @@ __global__ __launch_bounds__(kWaves * 64, C * NT <= 4 ? 3 : C * NT <= 8 ? 2 : 1)
         float v[C][8], top;
         const int e = take_query<C>(red, v, top);
         const float sign = j.scale < 0.f ? -1.f : 1.f, to = top > 0.f ? sign * 32639.f / top : 0.f;  // NaN: 0
-        factor[t] = ldexpf(top * (1.f / 32639.f) * (sign * j.scale * kLog2e), e);                    // not below 0
+        factor[t] = col.lo < col.hi ? ldexpf(top * (1.f / 32639.f) * (sign * j.scale * kLog2e), e) : 0.f;  // not below 0
 #pragma unroll
         for (int c = 0; c < (C + 1) / 2 * 2; ++c) {
             uint32_t h[2] = {0, 0}, l[2] = {0, 0};
@@ -386,9 +430,9 @@ __global__ __launch_bounds__(kWaves * 64, C * NT <= 4 ? 3 : C * NT <= 8 ? 2 : 1)
 #pragma unroll
         for (int d = 0; d < 2 * C; ++d) o[t][d] = Float4{0.f, 0.f, 0.f, 0.f};
     }
-    float unit_scale = 0.f;  // value scale that o is held in
+    UnitScale u = {0.f, 0.f};
 
-    const int u0 = s.first_unit + part * plan.step, u1 = min(u0 + plan.step, s.first_unit + s.units);
+    const int u0 = w.u0, u1 = w.u1;
     const int64_t page_bytes = (int64_t)j.c.page * DP;
     for (int base = u0 + wave; base < u1; base += kWaves * 64) {
         const PageOf mine = page_of(j, w.seq, head, base + lane * kWaves, u1);  // 64 units of this wavefront at once
@@ -418,9 +462,11 @@ __global__ __launch_bounds__(kWaves * 64, C * NT <= 4 ? 3 : C * NT <= 8 ? 2 : 1)
             }
             load(j.c.k_codes, i + 1, kc);
             float l[NT][8], top[NT];
+            const int t0 = (base + i * kWaves) * kUnit;
+            const bool edge = !there || t0 < all_lo || t0 + kUnit > all_hi;
+            bool past = there && vscale > u.scale;
 #pragma unroll
             for (int t = 0; t < NT; ++t) {
-                const float f = factor[t] * kscale;
                 Int4 sum[2];
 #pragma unroll
                 for (int h = 0; h < 2; ++h) {
@@ -433,45 +479,20 @@ __global__ __launch_bounds__(kWaves * 64, C * NT <= 4 ? 3 : C * NT <= 8 ? 2 : 1)
                     sum[h] = high * 256 + low;
                 }
 #pragma unroll
-                for (int r = 0; r < 8; ++r) l[t][r] = (float)sum[r >> 2][r & 3] * f;
-            }
-            const int t0 = (base + i * kWaves) * kUnit;
-            if (!there || t0 < all_lo || t0 + kUnit > all_hi) {
-#pragma unroll
-                for (int t = 0; t < NT; ++t)
-#pragma unroll
-                    for (int r = 0; r < 8; ++r) {
-                        const int at = t0 + (r >> 2) * 16 + g * 4 + (r & 3);
-                        if (!there || at < lo[t] || at >= hi[t]) l[t][r] = -INFINITY;
-                    }
-            }
-            bool past = there && vscale > unit_scale;
-#pragma unroll
-            for (int t = 0; t < NT; ++t) {
-                top[t] = l[t][0];
-#pragma unroll
-                for (int r = 1; r < 8; ++r) top[t] = fmaxf(top[t], l[t][r]);
+                for (int r = 0; r < 8; ++r) {
+                    const int at = t0 + (r >> 2) * 16 + g * 4 + (r & 3);
+                    l[t][r] = (float)sum[r >> 2][r & 3];
+                    if (edge && (!there || at < lo[t] || at >= hi[t])) l[t][r] = -INFINITY;
+                }
+                top[t] = largest(l[t], logit_factor(factor[t], kscale));
                 past |= top[t] > st[t].m + kSlack;
             }
-            if (__ballot(past)) {
-                const float u = there ? fmaxf(unit_scale, vscale) : unit_scale, change = u > 0.f ? unit_scale / u : 1.f;
-#pragma unroll
-                for (int t = 0; t < NT; ++t) {
-                    const float now = row_max(top[t]);  // a row's reference moves by its own logits alone
-                    const float next = now > st[t].m + kSlack ? now : st[t].m, keep = __builtin_amdgcn_exp2f(st[t].m - next);
-                    st[t].sum *= keep;
-                    const float turn = keep * change;
-#pragma unroll
-                    for (int d = 0; d < 2 * C; ++d) o[t][d] *= turn;
-                    st[t].m = next;
-                }
-                unit_scale = u;
-            }
-            const float ratio = unit_scale > 0.f ? fmaxf(vscale / unit_scale, kLeastRatio) : 1.f;
-            const float log_ratio = __builtin_amdgcn_logf(ratio), inv_ratio = 1.f / ratio;
+            if (__ballot(past)) move_up<C, NT>(st, top, o, u, there, vscale, lane_value(mine.log_vs, i));
+            const float log_ratio = fmaxf(lane_value(mine.log_vs, i) - u.log, kLeastLog);
+            const float inv_ratio = fminf(u.scale * lane_value(mine.inv_vs, i), kMostInverse);
             Half8 p[NT];
 #pragma unroll
-            for (int t = 0; t < NT; ++t) p[t] = weigh(l[t], st[t], log_ratio, inv_ratio);
+            for (int t = 0; t < NT; ++t) p[t] = weigh(l[t], logit_factor(factor[t], kscale), st[t], log_ratio, inv_ratio);
 #pragma unroll
             for (int c = 0; c < C; ++c) {
                 const Half8 v0 = halves(vc[c].x, vc[c].y), v1 = halves(vc[c].z, vc[c].w);
@@ -500,7 +521,7 @@ __global__ __launch_bounds__(kWaves * 64, C * NT <= 4 ? 3 : C * NT <= 8 ? 2 : 1)
         float top = kLowest;
 #pragma unroll
         for (int v = 0; v < kWaves; ++v) top = fmaxf(top, ml[v][t * 16 + n][0]);
-        const float mine = __builtin_amdgcn_exp2f(st[t].m - top) * unit_scale;
+        const float mine = __builtin_amdgcn_exp2f(st[t].m - top) * u.scale;
         if (t > 0) __syncthreads();  // the columns before these have been read
 #pragma unroll
         for (int d = 0; d < 2 * C; ++d)
@@ -544,7 +565,7 @@ __global__ __launch_bounds__(kWaves * 64, 2) void attend_rows_kernel(Job j) {
     Share w;
     if (!share_of<NC>(j, plan, blockIdx.x, w)) return;
     const Seq &s = w.s;
-    const int tile = w.tile, head = w.head, part = w.part, parts = w.parts;
+    const int tile = w.tile, head = w.head, parts = w.parts;
 
     Half8 q[NT][C];
     float factor[NT];
@@ -558,19 +579,19 @@ __global__ __launch_bounds__(kWaves * 64, 2) void attend_rows_kernel(Job j) {
         stage_queries<C>(j, s, head, col0 + t * 16, mine, lane, 64);
         __syncthreads();
         const int e = take_query<C>(mine, v, top);
-        factor[t] = ldexpf(j.scale * kLog2e, e);
+        const float sign = j.scale < 0.f ? -1.f : 1.f;
+        factor[t] = ldexpf(sign * j.scale * kLog2e, e);  // not below 0
         (void)top;
 #pragma unroll
         for (int c = 0; c < C; ++c)
 #pragma unroll
-            for (int i = 0; i < 8; ++i) q[t][c][i] = (_Float16)v[c][i];
+            for (int i = 0; i < 8; ++i) q[t][c][i] = (_Float16)(sign * v[c][i]);
         __syncthreads();
     }
     const int all_hi = __builtin_amdgcn_readlane(hi[0], 0), all_lo = __builtin_amdgcn_readlane(lo[NT - 1], 15);
     // units that some column of the workgroup sees
     const Column first = column(j, s, head, tile * NC), last = column(j, s, head, tile * NC + NC - 1);
-    const int u0 = max(s.first_unit + part * plan.step, first.lo / kUnit);
-    const int u1 = min(min(s.first_unit + (part + 1) * plan.step, s.first_unit + s.units), (max(last.hi, 0) + kUnit - 1) / kUnit);
+    const int u0 = max(w.u0, first.lo / kUnit), u1 = min(w.u1, (max(last.hi, 0) + kUnit - 1) / kUnit);
 
     Float4 o[NT][2 * C];
     State st[NT];
@@ -580,7 +601,7 @@ __global__ __launch_bounds__(kWaves * 64, 2) void attend_rows_kernel(Job j) {
 #pragma unroll
         for (int d = 0; d < 2 * C; ++d) o[t][d] = Float4{0.f, 0.f, 0.f, 0.f};
     }
-    float unit_scale = 0.f;
+    UnitScale u = {0.f, 0.f};
     const int64_t page_bytes = (int64_t)j.c.page * DP;
 
     // A unit's codes come into registers a unit ahead and go into LDS as FP16: operand 2 c + h of the keys, then the values.
@@ -613,14 +634,16 @@ __global__ __launch_bounds__(kWaves * 64, 2) void attend_rows_kernel(Job j) {
     if (u0 < u1) {
         load(u0);
         store(0);
+        mine = ahead;
+        if (u0 + 1 < u1) load(u0 + 1);
     }
     __syncthreads();
     for (int unit = u0; unit < u1; ++unit) {
         const int buf = (unit - u0) & 1, i = (unit - u0) % 64;
-        if (i == 0) mine = ahead;
-        const bool more = unit + 1 < u1, there = __builtin_amdgcn_readlane(mine.id, i) >= 0;
+        const bool there = __builtin_amdgcn_readlane(mine.id, i) >= 0;
         const float kscale = lane_value(mine.ks, i), vscale = lane_value(mine.vs, i);
-        if (more) load(unit + 1);
+        if (unit + 1 < u1) store(buf ^ 1);
+        if (unit + 2 < u1) load(unit + 2);
         const Half8 *from = unit_at(buf);
         Float4 sum[NT][2];
 #pragma unroll
@@ -637,12 +660,11 @@ __global__ __launch_bounds__(kWaves * 64, 2) void attend_rows_kernel(Job j) {
         float l[NT][8], top[NT];
         const int t0 = unit * kUnit;
         const bool edge = !there || t0 < all_lo || t0 + kUnit > all_hi;
-        bool past = there && vscale > unit_scale;
+        bool past = there && vscale > u.scale;
 #pragma unroll
         for (int t = 0; t < NT; ++t) {
-            const float f = factor[t] * kscale;
 #pragma unroll
-            for (int r = 0; r < 8; ++r) l[t][r] = sum[t][r >> 2][r & 3] * f;
+            for (int r = 0; r < 8; ++r) l[t][r] = sum[t][r >> 2][r & 3];
             if (edge) {
 #pragma unroll
                 for (int r = 0; r < 8; ++r) {
@@ -650,30 +672,15 @@ __global__ __launch_bounds__(kWaves * 64, 2) void attend_rows_kernel(Job j) {
                     if (!there || at < lo[t] || at >= hi[t]) l[t][r] = -INFINITY;
                 }
             }
-            top[t] = l[t][0];
-#pragma unroll
-            for (int r = 1; r < 8; ++r) top[t] = fmaxf(top[t], l[t][r]);
+            top[t] = largest(l[t], logit_factor(factor[t], kscale));
             past |= top[t] > st[t].m + kSlack;
         }
-        if (__ballot(past)) {
-            const float u = there ? fmaxf(unit_scale, vscale) : unit_scale, change = u > 0.f ? unit_scale / u : 1.f;
-#pragma unroll
-            for (int t = 0; t < NT; ++t) {
-                const float now = row_max(top[t]);
-                const float next = now > st[t].m + kSlack ? now : st[t].m, keep = __builtin_amdgcn_exp2f(st[t].m - next);
-                st[t].sum *= keep;
-                const float turn = keep * change;
-#pragma unroll
-                for (int d = 0; d < 2 * C; ++d) o[t][d] *= turn;
-                st[t].m = next;
-            }
-            unit_scale = u;
-        }
-        const float ratio = unit_scale > 0.f ? fmaxf(vscale / unit_scale, kLeastRatio) : 1.f;
-        const float log_ratio = __builtin_amdgcn_logf(ratio), inv_ratio = 1.f / ratio;
+        if (__ballot(past)) move_up<C, NT>(st, top, o, u, there, vscale, lane_value(mine.log_vs, i));
+        const float log_ratio = fmaxf(lane_value(mine.log_vs, i) - u.log, kLeastLog);
+        const float inv_ratio = fminf(u.scale * lane_value(mine.inv_vs, i), kMostInverse);
         Half8 p[NT];
 #pragma unroll
-        for (int t = 0; t < NT; ++t) p[t] = weigh(l[t], st[t], log_ratio, inv_ratio);
+        for (int t = 0; t < NT; ++t) p[t] = weigh(l[t], logit_factor(factor[t], kscale), st[t], log_ratio, inv_ratio);
 #pragma unroll
         for (int c = 0; c < C; ++c) {
             const Half8 v0 = from[kHalf / 16 + c * 128], v1 = from[kHalf / 16 + c * 128 + 64];
@@ -683,7 +690,7 @@ __global__ __launch_bounds__(kWaves * 64, 2) void attend_rows_kernel(Job j) {
                 o[t][2 * c + 1] = __builtin_amdgcn_mfma_f32_16x16x32_f16(v1, p[t], o[t][2 * c + 1], 0, 0, 0);
             }
         }
-        if (more) store(buf ^ 1);
+        if (i == 63) mine = ahead;
         __syncthreads();
     }
 
@@ -697,9 +704,9 @@ __global__ __launch_bounds__(kWaves * 64, 2) void attend_rows_kernel(Job j) {
                 j.part_ml[(w.slot * NC + k) * 2 + 1] = total;
             }
 #pragma unroll
-            for (int d = 0; d < 2 * C; ++d) keep_part(j, w.slot, NC, k, DP, d * 16 + g * 4, o[t][d] * unit_scale);
+            for (int d = 0; d < 2 * C; ++d) keep_part(j, w.slot, NC, k, DP, d * 16 + g * 4, o[t][d] * u.scale);
         } else if (at < s.rows * j.group) {
-            const float by = total == 0.f ? 0.f : unit_scale / total;
+            const float by = total == 0.f ? 0.f : u.scale / total;
 #pragma unroll
             for (int d = 0; d < 2 * C; ++d)
                 if (d * 16 + g * 4 < j.c.head_dim)
@@ -708,20 +715,88 @@ __global__ __launch_bounds__(kWaves * 64, 2) void attend_rows_kernel(Job j) {
     }
 }
 
-__device__ __forceinline__ void put(const Job &j, int64_t row, int head, int d, float v) {
-    const int64_t at = row * j.O.row_stride + head * j.O.head_stride + d;
-    if (j.o_dtype == CMPQ_F16) static_cast<_Float16 *>(j.O.ptr)[at] = (_Float16)v;
-    else static_cast<__bf16 *>(j.O.ptr)[at] = (__bf16)v;
+// Adds up the parts first, first + step, ... below `parts` of a column, `slot0` being its first part's place and `stride` the way to
+// the next: a lane has four dims of every PAR-th of them.  `top` is the largest reference of all parts.
+template <int C, int NC>
+__device__ __forceinline__ float add_parts(const Job &j, int64_t slot0, int64_t stride, int col, int first, int step, int parts,
+                                           float top, Float4 &acc) {
+    constexpr int DP = C * 32, PAR = 64 / (C * 8);
+    const int lane = threadIdx.x & 63, mine = lane / (C * 8), d = lane % (C * 8) * 4;
+    float total = 0.f;
+    acc = Float4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll 4
+    for (int p = first; p < parts; p += step * PAR) {
+        const int at = p + mine * step;
+        if (mine >= PAR || at >= parts) continue;
+        const int64_t place = (slot0 + at * stride) * NC + col;
+        const float w = __builtin_amdgcn_exp2f(j.part_ml[place * 2] - top);
+        const Float4 v = *reinterpret_cast<const Float4 *>(j.part_o + place * DP + d);
+        total += w * j.part_ml[place * 2 + 1];
+#pragma unroll
+        for (int r = 0; r < 4; ++r) acc[r] += w > 0.f ? w * v[r] : 0.f;  // a part without tokens has no output
+    }
+#pragma unroll
+    for (int k = 1; k < PAR; ++k) {  // the other lanes of these dims, in order
+        total += __shfl(total, (lane + k * C * 8) & 63);
+#pragma unroll
+        for (int r = 0; r < 4; ++r) acc[r] += __shfl(acc[r], (lane + k * C * 8) & 63);
+    }
+    return total;
 }
 
-// Rows whose sequence was cut into several parts: one wavefront a row and query head.
-template <int C, int NC>
-__global__ __launch_bounds__(256) void join_kernel(Job j) {
-    constexpr int DP = C * 32;
+template <int NC>
+__device__ __forceinline__ float top_of_parts(const Job &j, int64_t slot0, int64_t stride, int col, int parts) {
     const int lane = threadIdx.x & 63;
-    const int64_t x = (int64_t)blockIdx.x * 4 + wave_index();
-    const int64_t row = x / j.q_heads;
-    const int qh = (int)(x % j.q_heads);
+    float top = kLowest;
+    for (int p = lane; p < parts; p += 64) top = fmaxf(top, j.part_ml[((slot0 + p * stride) * NC + col) * 2]);
+#pragma unroll
+    for (int k = 32; k > 0; k >>= 1) top = fmaxf(top, __shfl_xor(top, k));
+    return top;
+}
+
+// Joins the parts of few rows: SPLIT wavefronts (4 or 1) have a row and query head and share its parts.  `rows_each`: rows that a
+// sequence of this kernel has at most.
+template <int C, int NC, int SPLIT>
+__global__ __launch_bounds__(256) void join_kernel(Job j, int rows_each) {
+    __shared__ Float4 outs[4][C * 8];
+    __shared__ float sums[4];
+    const int lane = threadIdx.x & 63, wave = wave_index();
+    const int64_t item = SPLIT == 4 ? (int64_t)blockIdx.x : (int64_t)blockIdx.x * 4 + wave, seq = item / ((int64_t)rows_each * j.q_heads);
+    const int in = (int)(item - seq * rows_each * j.q_heads), r = in / j.q_heads, qh = in % j.q_heads;
+    if (seq >= j.n_seq) return;
+    bool bad = false;
+    const Seq s = sequence(j, seq, bad);
+    const int tiles = tiles_of<NC>(j, s);
+    if (r >= s.rows || tiles == 0) return;
+    const Plan plan = make_plan<NC>(j, false);
+    const int parts = parts_of(plan, s);
+    if (parts == 1) return;
+    const Place place = place_of<NC>(j, plan, [&](const Seq &, int64_t) { return false; }, seq);
+    const int index = r * j.group + qh % j.group, col = index % NC;
+    const int64_t slot0 = place.kept_before + qh / j.group * tiles + index / NC, stride = (int64_t)tiles * j.c.kv_heads;
+    if (slot0 + (parts - 1) * stride >= j.kept) return;
+    const float top = top_of_parts<NC>(j, slot0, stride, col, parts);
+    Float4 acc;
+    const float total = add_parts<C, NC>(j, slot0, stride, col, SPLIT == 4 ? wave : 0, SPLIT, parts, top, acc);
+    if (SPLIT == 1) {
+        if (lane < C * 8 && lane * 4 < j.c.head_dim) put4(j, s.row0 + r, qh, lane * 4, total == 0.f ? Float4{0.f, 0.f, 0.f, 0.f} : acc / total);
+        return;
+    }
+    if (lane < C * 8) outs[wave][lane] = acc;
+    if (lane == 0) sums[wave] = total;
+    __syncthreads();
+    if (wave != 0 || lane >= C * 8 || lane * 4 >= j.c.head_dim) return;
+    const float all = sums[0] + sums[1] + sums[2] + sums[3];
+    const Float4 o = outs[0][lane] + outs[1][lane] + outs[2][lane] + outs[3][lane];
+    put4(j, s.row0 + r, qh, lane * 4, all == 0.f ? Float4{0.f, 0.f, 0.f, 0.f} : o / all);
+}
+
+// Of many rows: a wavefront has a row and key / value head, and goes through the query heads.
+template <int C, int NC>
+__global__ __launch_bounds__(256) void join_rows_kernel(Job j) {
+    const int lane = threadIdx.x & 63;
+    const int64_t x = (int64_t)blockIdx.x * 4 + wave_index(), row = x / j.c.kv_heads;
+    const int head = (int)(x % j.c.kv_heads);
     if (row >= j.n_rows) return;
     const Plan plan = make_plan<NC>(j, false);
     const Place place = place_of<NC>(j, plan, [&](const Seq &s, int64_t) { return s.rows > 0 && row >= s.row0 && row < s.row0 + s.rows; });
@@ -730,26 +805,16 @@ __global__ __launch_bounds__(256) void join_kernel(Job j) {
     const Seq s = sequence(j, place.seq, bad);
     const int parts = parts_of(plan, s), tiles = tiles_of<NC>(j, s);
     if (parts == 1 || tiles == 0) return;
-    const int col = (int)(row - s.row0) * j.group + qh % j.group, head = qh / j.group;
-    const int64_t slot0 = place.kept_before + head * tiles + col / NC, step = (int64_t)tiles * j.c.kv_heads;
-    if (slot0 + (parts - 1) * step >= j.kept) return;
-    float top = kLowest;
-    for (int p = lane; p < parts; p += 64) top = fmaxf(top, j.part_ml[((slot0 + p * step) * NC + col % NC) * 2]);
-#pragma unroll
-    for (int k = 32; k > 0; k >>= 1) top = fmaxf(top, __shfl_xor(top, k));
-    float total = 0.f, acc[(DP + 63) / 64] = {};
-#pragma unroll 4
-    for (int p = 0; p < parts; ++p) {
-        const int64_t at = (slot0 + p * step) * NC + col % NC;
-        const float w = __builtin_amdgcn_exp2f(j.part_ml[at * 2] - top);
-        total += w * j.part_ml[at * 2 + 1];
-#pragma unroll
-        for (int k = 0; k < (DP + 63) / 64; ++k)
-            if (k * 64 + lane < DP) acc[k] += w * j.part_o[at * DP + k * 64 + lane];
+    const int64_t slot = place.kept_before + head * tiles, stride = (int64_t)tiles * j.c.kv_heads;
+    if (slot + tiles + (parts - 1) * stride > j.kept) return;
+    for (int g = 0; g < j.group; ++g) {
+        const int index = (int)(row - s.row0) * j.group + g, col = index % NC;
+        const float top = top_of_parts<NC>(j, slot + index / NC, stride, col, parts);
+        Float4 acc;
+        const float total = add_parts<C, NC>(j, slot + index / NC, stride, col, 0, 1, parts, top, acc);
+        if (lane < C * 8 && lane * 4 < j.c.head_dim)
+            put4(j, row, head * j.group + g, lane * 4, total == 0.f ? Float4{0.f, 0.f, 0.f, 0.f} : acc / total);
     }
-#pragma unroll
-    for (int k = 0; k < (DP + 63) / 64; ++k)
-        if (k * 64 + lane < j.c.head_dim) put(j, row, qh, k * 64 + lane, total == 0.f ? 0.f : acc[k] / total);
 }
 
 // How a call is launched: the kernel for few rows, for many, or both, each with its columns, workgroups and kept parts.
@@ -815,20 +880,20 @@ int check_job(const cmpq_kv_attention_job *a) {
     if (!serving_dtype(a->q_dtype) || (a->o_dtype != CMPQ_F16 && a->o_dtype != CMPQ_BF16)) return CMPQ_EINVAL;
     if (a->q_heads < 1 || a->q_heads % a->cache.kv_heads) return CMPQ_EINVAL;
     if (a->n_seq > INT32_MAX || a->n_rows > INT32_MAX || a->max_length > INT32_MAX - kUnit || a->q_heads > 65535 ||
-        a->ld_table > INT32_MAX || a->max_rows > INT32_MAX || a->n_rows * a->q_heads > ((int64_t)1 << 33))
+        a->ld_table > INT32_MAX || a->max_rows > INT32_MAX || a->n_rows * a->q_heads > ((int64_t)1 << 32))
         return CMPQ_ESHAPE;
     return check_rotation(&a->rotation, a->cache.head_dim);
-}
-
-template <int C, int NC>
-void join(const Job &j, hipStream_t st) {
-    if (j.kept) join_kernel<C, NC><<<dim3((unsigned)cdiv(j.n_rows * j.q_heads, 4)), 256, 0, st>>>(j);
 }
 
 template <int C, int NT>
 void launch_few(const Job &j, const Kernel &h, hipStream_t st) {
     attend_kernel<C, NT><<<dim3((unsigned)h.grid), kWaves * 64, 0, st>>>(j);
-    join<C, NT * 16>(j, st);
+    if (!h.kept) return;
+    const int64_t each = h.most_cols / j.group < j.max_rows ? h.most_cols / j.group : j.max_rows;
+    const int64_t items = j.n_seq * each * j.q_heads;
+    // us, 4 wavefronts and 1: 2 sequences of 64 heads (up to 80 parts) 9.0 and 12.4, 64 of them (3 parts) 12.5 and 6.6
+    if (items < 2048) join_kernel<C, NT * 16, 4><<<dim3((unsigned)items), 256, 0, st>>>(j, (int)each);
+    else join_kernel<C, NT * 16, 1><<<dim3((unsigned)cdiv(items, 4)), 256, 0, st>>>(j, (int)each);
 }
 
 template <int C>
@@ -842,7 +907,7 @@ void launch(Job j, const Launches &l, WsCarver &w, hipStream_t st) {
         constexpr int NT = rows_tiles(C);
         take(l.rows);
         attend_rows_kernel<C, NT><<<dim3((unsigned)l.rows.grid), kWaves * 64, 0, st>>>(j);
-        join<C, NT * 16 * kWaves>(j, st);
+        if (l.rows.kept) join_rows_kernel<C, NT * 16 * kWaves><<<dim3((unsigned)cdiv(j.n_rows * j.c.kv_heads, 4)), 256, 0, st>>>(j);
     }
     if (l.few.nc) {
         take(l.few);
@@ -873,7 +938,7 @@ extern "C" int cmpq_kv_attention(const cmpq_kv_attention_job *a, void *ws, size_
     if (a->n_seq == 0 || a->n_rows == 0 || a->max_rows == 0) return CMPQ_OK;
     if (!a->page_table || !a->lengths || !a->cu_rows || !a->Q.ptr || !a->O.ptr) return CMPQ_EINVAL;
     const Launches l = plan_launches(a);
-    if (l.few.grid > INT32_MAX || l.rows.grid > INT32_MAX) return CMPQ_ESHAPE;
+    if (l.few.grid > INT32_MAX || l.rows.grid > INT32_MAX || a->n_seq * 48 * a->q_heads > INT32_MAX) return CMPQ_ESHAPE;
     if (!ws || reinterpret_cast<uintptr_t>(ws) % 256 || ws_bytes < cmpq_kv_attention_workspace(a)) return CMPQ_EWORKSPACE;
     WsCarver w(ws);
     Job j = {};
