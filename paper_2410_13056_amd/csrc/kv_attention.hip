@@ -237,23 +237,31 @@ __device__ __forceinline__ Column column(const Job &j, const Seq &s, int kv_head
     return c;
 }
 
-// Columns `index` .. + 15 of a head's queries, turned, into LDS: 16 rows of DP + 4 floats.  Threads first, first + step, ... of the
-// 2 DP that have eight dims each; in a loop, since all of them at once take more registers than the kernels have left.
+// `count` columns of a head's queries from `index` on, turned, into LDS: rows of DP + 4 floats.  Threads first, first + step, ... take
+// eight dims each; in a loop, since all of them at once take more registers than the kernels have left.
 template <int C>
-__device__ __forceinline__ void stage_queries(const Job &j, const Seq &s, int kv_head, int index, float *to, int first, int step) {
+__device__ __forceinline__ void stage_queries(const Job &j, const Seq &s, int kv_head, int index, int count, float *to, int first,
+                                              int step) {
     constexpr int DP = C * 32;
+    const bool by_eight = turns_by_eight(j.rot);
 #pragma unroll 1
-    for (int e = first; e < 2 * DP; e += step) {
+    for (int e = first; e < count * (DP / 8); e += step) {
         const int n = e / (DP / 8), d = e % (DP / 8) * 8;
         const Column col = column(j, s, kv_head, index + n);
-        float x[8];
+        float *row = to + n * (DP + 4) + d;
         with_dtype(j.q_dtype, [&](auto like) {
             using T = decltype(like);
-            load_turned(static_cast<const T *>(j.Q.ptr) + col.row * j.Q.row_stride + col.head * j.Q.head_stride, j.c.head_dim, d, j.rot, col.at, x);
+            const T *p = static_cast<const T *>(j.Q.ptr) + col.row * j.Q.row_stride + col.head * j.Q.head_stride;
+            if (by_eight && d + 8 <= j.c.head_dim) {
+                float x[8];
+                load_turned(p, d, j.rot, col.at, x);
+                *reinterpret_cast<Float4 *>(row) = Float4{x[0], x[1], x[2], x[3]};
+                *reinterpret_cast<Float4 *>(row + 4) = Float4{x[4], x[5], x[6], x[7]};
+            } else {
+#pragma unroll 1
+                for (int i = 0; i < 8; ++i) row[i] = d + i < j.c.head_dim ? turned(p, d + i, j.rot, col.at) : 0.f;
+            }
         });
-        float *row = to + n * (DP + 4) + d;
-        *reinterpret_cast<Float4 *>(row) = Float4{x[0], x[1], x[2], x[3]};
-        *reinterpret_cast<Float4 *>(row + 4) = Float4{x[4], x[5], x[6], x[7]};
     }
 }
 
@@ -390,6 +398,9 @@ __global__ __launch_bounds__(kWaves * 64, C * NT <= 4 ? 3 : C * NT <= 8 ? 2 : 1)
     const Seq &s = w.s;
     const int tile = w.tile, head = w.head, parts = w.parts;
 
+    static_assert(NT <= kWaves, "room for the queries");
+    stage_queries<C>(j, s, head, tile * NC, NC, red, threadIdx.x, kWaves * 64);
+    __syncthreads();
     Int4 qh[NT][(C + 1) / 2], ql[NT][(C + 1) / 2];
     float factor[NT];
     int lo[NT], hi[NT];
@@ -397,11 +408,8 @@ __global__ __launch_bounds__(kWaves * 64, C * NT <= 4 ? 3 : C * NT <= 8 ? 2 : 1)
     for (int t = 0; t < NT; ++t) {
         const Column col = column(j, s, head, tile * NC + t * 16 + n);
         lo[t] = col.lo, hi[t] = col.hi;
-        if (t > 0) __syncthreads();
-        stage_queries<C>(j, s, head, tile * NC + t * 16, red, threadIdx.x, kWaves * 64);
-        __syncthreads();
         float v[C][8], top;
-        const int e = take_query<C>(red, v, top);
+        const int e = take_query<C>(red + t * 16 * kPad, v, top);
         const float sign = j.scale < 0.f ? -1.f : 1.f, to = top > 0.f ? sign * 32639.f / top : 0.f;  // NaN: 0
         factor[t] = col.lo < col.hi ? ldexpf(top * (1.f / 32639.f) * (sign * j.scale * kLog2e), e) : 0.f;  // not below 0
 #pragma unroll
@@ -576,7 +584,7 @@ __global__ __launch_bounds__(kWaves * 64, 2) void attend_rows_kernel(Job j) {
         const Column col = column(j, s, head, col0 + t * 16 + n);
         lo[t] = col.lo, hi[t] = col.hi;
         float v[C][8], top, *mine = staged + wave * 16 * (DP + 4);
-        stage_queries<C>(j, s, head, col0 + t * 16, mine, lane, 64);
+        stage_queries<C>(j, s, head, col0 + t * 16, 16, mine, lane, 64);
         __syncthreads();
         const int e = take_query<C>(mine, v, top);
         const float sign = j.scale < 0.f ? -1.f : 1.f;

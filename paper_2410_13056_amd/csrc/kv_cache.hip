@@ -71,67 +71,142 @@ __device__ __forceinline__ bool looks_over() {
     return (blockIdx.x | blockIdx.y | blockIdx.z) == 0 && wave_index() == 0;
 }
 
-// Token and dim of byte j of the 8-byte half `h` of the 16 bytes that lane l has of a piece.
+// An item is four tokens next to each other by eight dims, a lane's share: in the stored order its keys are four runs of 8
+// bytes, its values eight of 4 bytes, which no other item has a part in.
+struct Item {
+    int tok, d;      // first of each
+    uint8_t *at;     // keys: of the first token (the others 16 bytes apart); values: of the first dim (16 bytes apart)
+};
+
 template <bool KEYS>
-__device__ __forceinline__ int token_in_piece(int l, int h, int j) {
-    return KEYS ? 16 * h + (l & 15) : 16 * (j >> 2) + 4 * (l >> 4) + (j & 3);
-}
-template <bool KEYS>
-__device__ __forceinline__ int dim_in_piece(int l, int h, int j) {
-    return KEYS ? 8 * (l >> 4) + j : 16 * h + (l & 15);
+__device__ __forceinline__ Item item_of(int e, int octets, int chunks, uint8_t *codes) {
+    Item it;
+    it.tok = e / octets * 4;
+    it.d = e % octets * 8;
+    const int t = it.tok % 32, d = it.d % 32;
+    it.at = codes + (it.tok / 32 * chunks + it.d / 32) * 1024 +
+            (KEYS ? d / 8 * 256 + t % 16 * 16 + t / 16 * 8 : t % 16 / 4 * 256 + d % 16 * 16 + d / 16 * 8 + t / 16 * 4);
+    return it;
 }
 
-template <typename T, bool KEYS>
-__device__ void append_page(const cmpq_kv_cache &c, const Page &pg, int64_t id, int head, const cmpq_heads &in,
-                            const cmpq_rotation &rot, int32_t *status, float *scratch) {
-    const int dim = c.head_dim, chunks = (dim + 31) / 32;
+// The new values of an item: 0 for tokens that are not new and for dims beyond the head.  WHOLE: eight dims are all there or
+// none, and turn by eight.
+template <typename T, bool KEYS, bool WHOLE>
+__device__ __forceinline__ void load_item(const cmpq_kv_cache &c, const Page &pg, const cmpq_heads &in, const cmpq_rotation &rot,
+                                          int head, const Item &it, float (&x)[4][8]) {
     const T *base = static_cast<const T *>(in.ptr) + head * in.head_stride;
-    auto value = [&](int tok, int d) {
-        const int64_t at = pg.begin + tok;
-        const T *p = base + (pg.row0 + at - pg.first) * in.row_stride;
-        return KEYS ? turned(p, d, rot, min(at, rot.positions - 1)) : (float)p[d];
-    };
-    float most = 0.f;
-    bool bad = false;
-    const int n = pg.to - pg.from;
-    for (int e = threadIdx.x; e < n * dim; e += kThreads) most = fmaxf(most, finite_abs(value(pg.from + e / dim, e % dim), bad));
-    if (bad && status) atomicOr(status, CMPQ_STATUS_NONFINITE);
-    if (KEYS && rot.cos && threadIdx.x == 0 && status && pg.begin + pg.to > rot.positions)
-        atomicOr(status, CMPQ_STATUS_RANGE);
-    most = block_max(most, scratch);
-    float *scale = (KEYS ? c.k_scale : c.v_scale) + id * c.kv_heads + head;
-    const float old = pg.from > 0 ? *scale : 0.f;
-    const float now = fmaxf(old, code_scale(most)), inv = 1.f / now, again = old * inv;
-    __syncthreads();  // everybody has the old scale
-    if (threadIdx.x == 0) *scale = now;
-    uint8_t *codes = (KEYS ? c.k_codes : c.v_codes) + (id * c.kv_heads + head) * (int64_t)(c.page * chunks * 32);
-    const bool grown = pg.from > 0 && now != old;
-    const int pieces = c.page / 32 * chunks;
-    for (int e = threadIdx.x; e < pieces * 128; e += kThreads) {  // 8 bytes a step
-        const int h = e & 1, l = (e >> 1) & 63, piece = e >> 7;
-        const int t0 = piece / chunks * 32, d0 = piece % chunks * 32;
-        int lowest = t0 + token_in_piece<KEYS>(l, h, 0), highest = t0 + token_in_piece<KEYS>(l, h, 7);
-        if (lowest >= pg.to || (highest < pg.from && !grown)) continue;
-        uint2 *at = reinterpret_cast<uint2 *>(codes + piece * 1024 + l * 16 + h * 8);
-        uint2 had = make_uint2(0x80808080u, 0x80808080u);
-        if (lowest < pg.from || highest >= pg.to) had = *at;
-        uint32_t w[2] = {had.x, had.y};
 #pragma unroll
-        for (int j = 0; j < 8; ++j) {
-            const int tok = t0 + token_in_piece<KEYS>(l, h, j), d = d0 + dim_in_piece<KEYS>(l, h, j);
-            int code = (int)((w[j >> 2] >> (8 * (j & 3))) & 255) - 128;
-            if (tok < pg.from) code = grown ? (int)rintf((float)code * again) : code;
-            else if (tok < pg.to) code = d < dim ? code_of(value(tok, d), inv) : 0;
-            w[j >> 2] = (w[j >> 2] & ~(255u << (8 * (j & 3)))) | (uint32_t)((code + 128) & 255) << (8 * (j & 3));
+    for (int r = 0; r < 4; ++r) {
+        const int tok = it.tok + r;
+        const int64_t at = pg.begin + tok, turn = min(at, rot.positions - 1);
+        const T *p = base + (pg.row0 + at - pg.first) * in.row_stride;
+        const bool is_new = tok >= pg.from && tok < pg.to;
+        if (WHOLE && is_new && it.d < c.head_dim) {
+            if (KEYS) load_turned(p, it.d, rot, turn, x[r]);
+            else load_f32<T, 8>(p + it.d, x[r]);
+        } else {
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                x[r][i] = 0.f;
+                if (!WHOLE && is_new && it.d + i < c.head_dim) x[r][i] = KEYS ? turned(p, it.d + i, rot, turn) : (float)p[it.d + i];
+            }
         }
-        *at = make_uint2(w[0], w[1]);
     }
 }
 
-template <typename T>
+// Codes of an item's new tokens into the page; the bytes of others stay.
+template <bool KEYS>
+__device__ __forceinline__ void store_item(const Page &pg, const Item &it, const float (&x)[4][8], float inv) {
+    uint32_t w[8];  // keys: two words a token; values: one a dim
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+        w[i] = 0;
+#pragma unroll
+        for (int b = 0; b < 4; ++b)
+            w[i] |= (uint32_t)(code_of(KEYS ? x[i / 2][i % 2 * 4 + b] : x[b][i], inv) + 128) << (8 * b);
+    }
+    if (KEYS) {
+#pragma unroll
+        for (int r = 0; r < 4; ++r)
+            if (it.tok + r >= pg.from && it.tok + r < pg.to) *reinterpret_cast<uint2 *>(it.at + r * 16) = make_uint2(w[2 * r], w[2 * r + 1]);
+    } else {
+        uint32_t keep = 0;
+#pragma unroll
+        for (int r = 0; r < 4; ++r)
+            if (it.tok + r < pg.from || it.tok + r >= pg.to) keep |= 255u << (8 * r);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            uint32_t *at = reinterpret_cast<uint32_t *>(it.at + i * 16);
+            *at = keep ? (*at & keep) | (w[i] & ~keep) : w[i];
+        }
+    }
+}
+
+// Codes of an item's tokens before the new ones, times `again`.
+template <bool KEYS>
+__device__ __forceinline__ void hold_item(const Page &pg, const Item &it, float again) {
+    const int n = min(4, pg.from - it.tok);  // tokens
+#pragma unroll 1
+    for (int i = 0; i < 8; ++i) {
+        uint32_t *at = reinterpret_cast<uint32_t *>(it.at + (KEYS ? i / 2 * 16 + i % 2 * 4 : i * 16));
+        if (KEYS && i / 2 >= n) break;
+        const uint32_t had = *at;
+        uint32_t w = 0;
+#pragma unroll
+        for (int b = 0; b < 4; ++b) {
+            const int code = (int)((had >> (8 * b)) & 255) - 128;
+            w |= (uint32_t)((KEYS || b < n ? (int)rintf((float)code * again) : code) + 128) << (8 * b);
+        }
+        *at = w;
+    }
+}
+
+// The new values are read once where each lane has at most one item, else again for their codes.
+template <typename T, bool KEYS, bool WHOLE>
+__device__ __forceinline__ void append_page(const cmpq_kv_cache &c, const Page &pg, int64_t id, int head, const cmpq_heads &in,
+                            const cmpq_rotation &rot, int32_t *status, float *scratch) {
+    const int chunks = (c.head_dim + 31) / 32, octets = chunks * 4;
+    uint8_t *codes = (KEYS ? c.k_codes : c.v_codes) + (id * c.kv_heads + head) * (int64_t)(c.page * chunks * 32);
+    float *scale = (KEYS ? c.k_scale : c.v_scale) + id * c.kv_heads + head;
+    if (threadIdx.x == 0) scratch[kThreads / 64] = pg.from > 0 ? *scale : 0.f;
+    const int e0 = pg.from / 4 * octets, e1 = (pg.to + 3) / 4 * octets;
+    const bool once = e1 - e0 <= kThreads;
+    float x[4][8], most = 0.f, inv = 0.f;
+    bool bad = false;
+#pragma unroll 1
+    for (int pass = 0; pass < 2; ++pass) {
+        for (int e = e0 + threadIdx.x; e < e1; e += kThreads) {
+            const Item it = item_of<KEYS>(e, octets, chunks, codes);
+            if (pass == 0 || !once) load_item<T, KEYS, WHOLE>(c, pg, in, rot, head, it, x);
+            if (pass == 0) {
+#pragma unroll
+                for (int r = 0; r < 4; ++r)
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) most = fmaxf(most, finite_abs(x[r][i], bad));
+            } else {
+                store_item<KEYS>(pg, it, x, inv);
+            }
+        }
+        if (pass == 1) break;
+        if (bad && status) atomicOr(status, CMPQ_STATUS_NONFINITE);
+        if (KEYS && rot.cos && threadIdx.x == 0 && status && pg.begin + pg.to > rot.positions)
+            atomicOr(status, CMPQ_STATUS_RANGE);
+        most = block_max(most, scratch);
+        const float old = scratch[kThreads / 64], now = fmaxf(old, code_scale(most));
+        inv = 1.f / now;
+        if (threadIdx.x == 0) *scale = now;
+        if (pg.from > 0 && now != old) {
+            for (int e = threadIdx.x; e < (pg.from + 3) / 4 * octets; e += kThreads)
+                hold_item<KEYS>(pg, item_of<KEYS>(e, octets, chunks, codes), old * inv);
+            __syncthreads();  // an item of both is held first, by whichever lane
+        }
+    }
+}
+
+template <typename T, bool WHOLE>
 __global__ __launch_bounds__(kThreads) void append_kernel(cmpq_kv_cache c, cmpq_kv_rows r, cmpq_heads K, cmpq_heads V,
                                                           cmpq_rotation rot, int32_t *status) {
-    __shared__ float scratch[kThreads / 64];
+    __shared__ float scratch[kThreads / 64 + 1];
     const Page pg = find_page(r, c.page, blockIdx.x, looks_over() ? status : nullptr);
     if (pg.seq < 0) return;
     const int64_t id = r.page_table[pg.seq * r.ld_table + pg.begin / c.page];
@@ -139,22 +214,44 @@ __global__ __launch_bounds__(kThreads) void append_kernel(cmpq_kv_cache c, cmpq_
         if (threadIdx.x == 0 && status) atomicOr(status, CMPQ_STATUS_RANGE);
         return;
     }
-    if (blockIdx.z == 0) append_page<T, true>(c, pg, id, blockIdx.y, K, rot, status, scratch);
-    else append_page<T, false>(c, pg, id, blockIdx.y, V, rot, status, scratch);
+    if (blockIdx.z == 0) append_page<T, true, WHOLE>(c, pg, id, blockIdx.y, K, rot, status, scratch);
+    else append_page<T, false, WHOLE>(c, pg, id, blockIdx.y, V, rot, status, scratch);
 }
 
 template <typename T, bool KEYS>
 __device__ void read_page(const cmpq_kv_cache &c, const Page &pg, int64_t id, int head, const cmpq_heads &out) {
-    const int dim = c.head_dim, chunks = (dim + 31) / 32, n = pg.to - pg.from;
-    const uint8_t *codes = (KEYS ? c.k_codes : c.v_codes) + (id * c.kv_heads + head) * (int64_t)(c.page * chunks * 32);
+    const int dim = c.head_dim, chunks = (dim + 31) / 32, octets = chunks * 4;
+    uint8_t *codes = (KEYS ? c.k_codes : c.v_codes) + (id * c.kv_heads + head) * (int64_t)(c.page * chunks * 32);
     const float scale = (KEYS ? c.k_scale : c.v_scale)[id * c.kv_heads + head];
     T *base = static_cast<T *>(out.ptr) + head * out.head_stride;
-    for (int e = threadIdx.x; e < n * dim; e += kThreads) {
-        const int tok = pg.from + e / dim, d = e % dim, t = tok % 32, x = d % 32;
-        const int byte = KEYS ? (x >> 3) * 256 + (t & 15) * 16 + (t >> 4) * 8 + (x & 7)
-                              : ((t & 15) >> 2) * 256 + (x & 15) * 16 + (x >> 4) * 8 + (t >> 4) * 4 + (t & 3);
-        const int code = (int)codes[(tok / 32 * chunks + d / 32) * 1024 + byte] - 128;
-        base[(pg.row0 + pg.begin + tok - pg.first) * out.row_stride + d] = (T)((float)code * scale);
+    const int e0 = pg.from / 4 * octets, e1 = (pg.to + 3) / 4 * octets;
+    for (int e = e0 + threadIdx.x; e < e1; e += kThreads) {
+        const Item it = item_of<KEYS>(e, octets, chunks, codes);
+        uint32_t w[8];
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+            w[i] = *reinterpret_cast<const uint32_t *>(it.at + (KEYS ? i / 2 * 16 + i % 2 * 4 : i * 16));
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+            const int tok = it.tok + r;
+            if (tok < pg.from || tok >= pg.to) continue;
+            T *p = base + (pg.row0 + pg.begin + tok - pg.first) * out.row_stride + it.d;
+            typedef T T8 __attribute__((ext_vector_type(8)));
+            typedef T8 Any __attribute__((aligned(sizeof(T))));
+            T8 v;
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                const uint32_t code = KEYS ? w[2 * r + i / 4] >> (8 * (i & 3)) : w[i] >> (8 * r);
+                v[i] = (T)((float)((int)(code & 255) - 128) * scale);
+            }
+            if (it.d + 8 <= dim) {
+                *reinterpret_cast<Any *>(p) = v;
+            } else {
+#pragma unroll
+                for (int i = 0; i < 8; ++i)
+                    if (it.d + i < dim) p[i] = v[i];
+            }
+        }
     }
 }
 
@@ -204,9 +301,14 @@ extern "C" int cmpq_kv_append(const cmpq_kv_cache *cache, const cmpq_kv_rows *ro
     const cmpq_rotation rot = rotation ? *rotation : cmpq_rotation{};
     const dim3 grid = page_grid(*cache, *rows);
     hipStream_t st = static_cast<hipStream_t>(stream);
-    if (dtype == CMPQ_F16) append_kernel<_Float16><<<grid, kThreads, 0, st>>>(*cache, *rows, *K, *V, rot, status);
-    else if (dtype == CMPQ_BF16) append_kernel<__bf16><<<grid, kThreads, 0, st>>>(*cache, *rows, *K, *V, rot, status);
-    else append_kernel<float><<<grid, kThreads, 0, st>>>(*cache, *rows, *K, *V, rot, status);
+    auto launch = [&](auto like) {
+        using T = decltype(like);
+        if (cache->head_dim % 8 == 0 && turns_by_eight(rot)) append_kernel<T, true><<<grid, kThreads, 0, st>>>(*cache, *rows, *K, *V, rot, status);
+        else append_kernel<T, false><<<grid, kThreads, 0, st>>>(*cache, *rows, *K, *V, rot, status);
+    };
+    if (dtype == CMPQ_F16) launch(_Float16());
+    else if (dtype == CMPQ_BF16) launch(__bf16());
+    else launch(float());
     CMPQ_LAUNCH_CHECK();
     return CMPQ_OK;
 }

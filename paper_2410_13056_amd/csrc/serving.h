@@ -22,19 +22,14 @@ __device__ __forceinline__ void with_dtype(int dtype, F fn) {
 static inline bool serving_dtype(int dtype) { return dtype == CMPQ_F16 || dtype == CMPQ_BF16 || dtype == CMPQ_F32; }
 static inline size_t dtype_bytes(int dtype) { return dtype == CMPQ_F32 ? 4 : 2; }
 
-// N consecutive elements in 32 bits, `valid` of them there (the others read 0).
+// N elements next to each other in 32 bits, at any alignment of their type.
 template <typename T, int N>
-__device__ __forceinline__ void load_f32(const T *p, int valid, float (&x)[N]) {
-    if (valid >= N) {
-        typedef T V __attribute__((ext_vector_type(N)));
-        typedef V Any __attribute__((aligned(sizeof(T))));
-        const V v = *reinterpret_cast<const Any *>(p);
+__device__ __forceinline__ void load_f32(const T *p, float (&x)[N]) {
+    typedef T V __attribute__((ext_vector_type(N)));
+    typedef V Any __attribute__((aligned(sizeof(T))));
+    const V v = *reinterpret_cast<const Any *>(p);
 #pragma unroll
-        for (int i = 0; i < N; ++i) x[i] = (float)v[i];
-    } else {
-#pragma unroll
-        for (int i = 0; i < N; ++i) x[i] = i < valid ? (float)p[i] : 0.f;
-    }
+    for (int i = 0; i < N; ++i) x[i] = (float)v[i];
 }
 
 // |x| where it is finite, else 0; `bad` remembers that one was not.
@@ -90,37 +85,39 @@ __device__ __forceinline__ float turned(const T *p, int d, const cmpq_rotation &
     return second ? turned_second(y, x, c, s) : turned_first(x, y, c, s);
 }
 
-// Dims d .. d + 7 (d a multiple of 8) of a head of `dim` at `p`, turned for the row `at` of the tables; 0 beyond the head.
-// Eight at a time where the turn's pairs are eight next to each other too, or lie within the eight.
+// Whether the turn's pairs are eight next to each other, like the eight dims they are taken for, or lie within the eight.
+__host__ __device__ __forceinline__ bool turns_by_eight(const cmpq_rotation &rot) {
+    return !rot.cos || (rot.interleaved ? rot.dims % 8 == 0 : rot.dims % 16 == 0);
+}
+
+// Dims d .. d + 7 (d a multiple of 8, all within the head) at `p`, turned by eight for the row `at` of the tables.
 template <typename T>
-__device__ __forceinline__ void load_turned(const T *p, int dim, int d, const cmpq_rotation &rot, int64_t at, float (&x)[8]) {
-    load_f32<T, 8>(p + min(d, dim), max(dim - d, 0), x);
+__device__ __forceinline__ void load_turned(const T *p, int d, const cmpq_rotation &rot, int64_t at, float (&x)[8]) {
+    load_f32<T, 8>(p + d, x);
     if (!rot.cos || d >= rot.dims) return;
     const int half = rot.dims >> 1;
-    if (rot.interleaved && d + 8 <= rot.dims) {
+    if (rot.interleaved) {
         float cs[4], sn[4];
-        load_f32<float, 4>(rot.cos + at * half + d / 2, 4, cs);
-        load_f32<float, 4>(rot.sin + at * half + d / 2, 4, sn);
+        load_f32<float, 4>(rot.cos + at * half + d / 2, cs);
+        load_f32<float, 4>(rot.sin + at * half + d / 2, sn);
 #pragma unroll
         for (int i = 0; i < 8; i += 2) {
             const float a = x[i], b = x[i + 1];
             x[i] = turned_first(a, b, cs[i / 2], sn[i / 2]);
             x[i + 1] = turned_second(a, b, cs[i / 2], sn[i / 2]);
         }
-    } else if (!rot.interleaved && half % 8 == 0) {
+    } else {
         const bool second = d >= half;
         const int pair = second ? d - half : d;
         float y[8], cs[8], sn[8];
-        load_f32<T, 8>(p + (second ? pair : d + half), 8, y);
-        load_f32<float, 8>(rot.cos + at * half + pair, 8, cs);
-        load_f32<float, 8>(rot.sin + at * half + pair, 8, sn);
+        load_f32<T, 8>(p + (second ? pair : d + half), y);
+        load_f32<float, 8>(rot.cos + at * half + pair, cs);
+        load_f32<float, 8>(rot.sin + at * half + pair, sn);
 #pragma unroll
-        for (int i = 0; i < 8; ++i)
-            x[i] = second ? turned_second(y[i], x[i], cs[i], sn[i]) : turned_first(x[i], y[i], cs[i], sn[i]);
-    } else {
-#pragma unroll
-        for (int i = 0; i < 8; ++i)
-            if (d + i < dim) x[i] = turned(p, d + i, rot, at);
+        for (int i = 0; i < 8; ++i) {
+            const float first = turned_first(x[i], y[i], cs[i], sn[i]);
+            x[i] = second ? turned_second(y[i], x[i], cs[i], sn[i]) : first;
+        }
     }
 }
 
