@@ -15,7 +15,7 @@ import torch
 _HERE = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.path.join(_HERE, "libcmpq.so")
 
-OK = 0
+OK, EWORKSPACE = 0, -5
 F16, F32, BF16 = 0, 1, 2
 KMAX = 16
 PROTECTED = 16
@@ -698,18 +698,40 @@ def int8_prepare(W: torch.Tensor, codes: torch.Tensor, scale: torch.Tensor,
                                    _ptr(status), _stream()), "cmpq_int8_prepare")
 
 
+class Int8ProductCall:
+    """``cmpq_int8_product`` for one prepared weight: what stays the same from call to call is kept.  Holds the tensors
+    it points into."""
+
+    def __init__(self, d_in: int, d_out: int, codes: torch.Tensor, scale: torch.Tensor):
+        if codes.dtype != torch.int8 or not codes.is_contiguous() or codes.numel() != int8_weight_bytes(d_out, d_in):
+            raise ValueError("codes must be contiguous int8 of int8_weight_bytes(d_out, d_in)")
+        if scale.dtype != torch.float32 or not scale.is_contiguous() or scale.numel() != d_out:
+            raise ValueError("scale must be contiguous float32 [d_out]")
+        self._keep = (codes, scale)
+        self.d_in, self.d_out, self._codes, self._scale = int(d_in), int(d_out), _ptr(codes), _ptr(scale)
+        self._fn = lib().cmpq_int8_product
+
+    def __call__(self, X: torch.Tensor, Y: torch.Tensor, ws: Workspace, status: Optional[torch.Tensor] = None) -> None:
+        m, d_in, ldx = _rows(X)
+        my, d_out, ldy = _rows(Y)
+        if my != m or d_in != self.d_in or d_out != self.d_out:
+            raise ValueError("X must be [m, d_in] and Y [m, d_out] of the prepared weight")
+        x, xt, y, yt = _ptr(X), serving_dtype(X.dtype), _ptr(Y), serving_dtype(Y.dtype)
+        for _ in range(2):          # asks for the workspace's size only where what is there does not do
+            buf = ws.buf
+            rc = self._fn(x, xt, m, d_in, ldx, self._codes, self._scale, d_out, y, yt, ldy, buf.data_ptr(), buf.numel(),
+                          _ptr(status), _stream())
+            if rc != EWORKSPACE:
+                break
+            ws.get(workspace_bytes(OP_INT8_PRODUCT, d_in, d_out, m))
+        if rc:
+            _check(rc, "cmpq_int8_product")
+
+
 def int8_product(X: torch.Tensor, codes: torch.Tensor, scale: torch.Tensor, Y: torch.Tensor, ws: Workspace,
                  status: Optional[torch.Tensor] = None) -> None:
     """Y [m, d_out] = X [m, d_in] times a weight of `int8_prepare`, X in 8 bits with a scale per token on the way."""
-    m, d_in, ldx = _rows(X)
-    my, d_out, ldy = _rows(Y)
-    if my != m or scale.numel() != d_out or codes.numel() != int8_weight_bytes(d_out, d_in):
-        raise ValueError("X must be [m, d_in] and Y [m, d_out] of the prepared weight")
-    buf = ws.get(workspace_bytes(OP_INT8_PRODUCT, d_in, d_out, m))
-    rc = lib().cmpq_int8_product(_ptr(X), serving_dtype(X.dtype), m, d_in, ldx, _ptr(codes), _ptr(scale), d_out, _ptr(Y),
-                                 serving_dtype(Y.dtype), ldy, _ptr(buf), buf.numel(), _ptr(status), _stream())
-    if rc:
-        _check(rc, "cmpq_int8_product")
+    Int8ProductCall(_rows(X)[1], scale.numel(), codes, scale)(X, Y, ws, status)
 
 
 def kv_cache_view(k: torch.Tensor, v: torch.Tensor, k_scale: torch.Tensor, v_scale: torch.Tensor, page: int,
@@ -726,47 +748,64 @@ def kv_cache_view(k: torch.Tensor, v: torch.Tensor, k_scale: torch.Tensor, v_sca
                          (k_scale, torch.float32, (n_pages, heads)), (v_scale, torch.float32, (n_pages, heads))):
         if t.dtype != dt or tuple(t.shape) != shape or not t.is_contiguous():
             raise ValueError("codes are contiguous uint8 [n_pages, kv_heads, kv_page_bytes], scales float32")
-    return KvCacheView(_ptr(k), _ptr(v), _ptr(k_scale), _ptr(v_scale), n_pages, heads, int(head_dim), int(page))
+    view = KvCacheView(_ptr(k), _ptr(v), _ptr(k_scale), _ptr(v_scale), n_pages, heads, int(head_dim), int(page))
+    # what the calls on this cache are filled into, one call at a time
+    view.keep, view.ref = (k, v, k_scale, v_scale), ctypes.byref(view)
+    view.rows, view.K, view.V, view.job = KvRows(), Heads(), Heads(), KvAttentionJob(cache=view)
+    view.rows_ref, view.K_ref, view.V_ref, view.job_ref = (ctypes.byref(t) for t in (view.rows, view.K, view.V, view.job))
+    view.Q, view.O = view.job.Q, view.job.O                        # the job's own
+    return view
 
 
 def rotation_view(cos: torch.Tensor, sin: torch.Tensor, interleaved: bool) -> RotationView:
     for t in (cos, sin):
         if t.dtype != torch.float32 or t.dim() != 2 or not t.is_contiguous() or t.shape != cos.shape:
             raise ValueError("cos and sin must be contiguous float32 [positions, dims / 2]")
-    return RotationView(_ptr(cos), _ptr(sin), cos.shape[0], 2 * cos.shape[1], int(bool(interleaved)))
+    view = RotationView(_ptr(cos), _ptr(sin), cos.shape[0], 2 * cos.shape[1], int(bool(interleaved)))
+    view.keep, view.ref = (cos, sin), ctypes.byref(view)
+    return view
 
 
-def heads_view(t: torch.Tensor, n_heads: int, head_dim: int) -> Heads:
-    """A tensor [rows, heads, dims] of any row and head stride."""
-    if t.dim() != 3 or t.shape[1] != n_heads or t.shape[2] != head_dim or (head_dim > 1 and t.stride(2) != 1):
+def _heads(view: Heads, t: torch.Tensor, n_heads: int, head_dim: int) -> int:
+    """Fills in a tensor [rows, heads, dims] of any row and head stride; the number of rows."""
+    shape = t.shape
+    if len(shape) != 3 or shape[1] != n_heads or shape[2] != head_dim or (head_dim > 1 and t.stride(2) != 1):
         raise ValueError(f"expected [rows, {n_heads}, {head_dim}] with unit stride along the dims")
-    return Heads(_ptr(t), t.stride(0), t.stride(1))
+    view.ptr = _ptr(t)
+    view.row_stride, view.head_stride, _ = t.stride()
+    return shape[0]
 
 
-def _i32_table(t: torch.Tensor, shape, what: str) -> int:
-    if t.dtype != torch.int32 or tuple(t.shape) != tuple(shape) or not t.is_contiguous():
+def _i32_table(t: torch.Tensor, shape: tuple, what: str) -> int:
+    if t.dtype != torch.int32 or t.shape != shape or not t.is_contiguous():
         raise ValueError(f"{what} must be contiguous int32 {list(shape)}")
     return _ptr(t)
 
 
-def _kv_rows(page_table: torch.Tensor, first: torch.Tensor, cu_rows: torch.Tensor, n_rows: int) -> KvRows:
+def _table_shape(page_table: torch.Tensor):
     if page_table.dim() != 2:
         raise ValueError("page_table must be [n_seq, pages]")
-    n_seq, ld = page_table.shape
-    return KvRows(_i32_table(page_table, (n_seq, ld), "page_table"), ld, _i32_table(first, (n_seq,), "first"),
-                  _i32_table(cu_rows, (n_seq + 1,), "cu_rows"), n_seq, n_rows)
+    return page_table.shape
+
+
+def _fill_rows(cache: KvCacheView, page_table: torch.Tensor, first: torch.Tensor, cu_rows: torch.Tensor, K: torch.Tensor,
+               V: torch.Tensor) -> int:
+    n = _heads(cache.K, K, cache.kv_heads, cache.head_dim)
+    if _heads(cache.V, V, cache.kv_heads, cache.head_dim) != n or K.dtype != V.dtype:
+        raise ValueError("K and V must have the same rows and dtype")
+    n_seq, ld = shape = _table_shape(page_table)
+    r = cache.rows
+    r.page_table, r.ld_table, r.n_seq, r.n_rows = _i32_table(page_table, shape, "page_table"), ld, n_seq, n
+    r.first, r.cu_rows = _i32_table(first, (n_seq,), "first"), _i32_table(cu_rows, (n_seq + 1,), "cu_rows")
+    return serving_dtype(K.dtype)
 
 
 def kv_append(cache: KvCacheView, page_table: torch.Tensor, first: torch.Tensor, cu_rows: torch.Tensor, K: torch.Tensor,
               V: torch.Tensor, rotation: Optional[RotationView] = None, status: Optional[torch.Tensor] = None) -> None:
     """`cmpq_kv_append`: K and V [rows, kv_heads, head_dim] behind the first[i] tokens of each sequence."""
-    k, v = heads_view(K, cache.kv_heads, cache.head_dim), heads_view(V, cache.kv_heads, cache.head_dim)
-    if K.shape[0] != V.shape[0] or K.dtype != V.dtype:
-        raise ValueError("K and V must have the same rows and dtype")
-    rows = _kv_rows(page_table, first, cu_rows, K.shape[0])
-    rc = lib().cmpq_kv_append(ctypes.byref(cache), ctypes.byref(rows), ctypes.byref(k), ctypes.byref(v),
-                              serving_dtype(K.dtype), ctypes.byref(rotation) if rotation is not None else None,
-                              _ptr(status), _stream())
+    dtype = _fill_rows(cache, page_table, first, cu_rows, K, V)
+    rc = _lib.cmpq_kv_append(cache.ref, cache.rows_ref, cache.K_ref, cache.V_ref, dtype,
+                             None if rotation is None else rotation.ref, _ptr(status), _stream())
     if rc:
         _check(rc, "cmpq_kv_append")
 
@@ -774,14 +813,13 @@ def kv_append(cache: KvCacheView, page_table: torch.Tensor, first: torch.Tensor,
 def kv_read(cache: KvCacheView, page_table: torch.Tensor, first: torch.Tensor, cu_rows: torch.Tensor, K: torch.Tensor,
             V: torch.Tensor, status: Optional[torch.Tensor] = None) -> None:
     """`cmpq_kv_read`: the values that tokens first[i], first[i]+1, ... of each sequence stand for, into K and V."""
-    k, v = heads_view(K, cache.kv_heads, cache.head_dim), heads_view(V, cache.kv_heads, cache.head_dim)
-    if K.shape[0] != V.shape[0] or K.dtype != V.dtype:
-        raise ValueError("K and V must have the same rows and dtype")
-    rows = _kv_rows(page_table, first, cu_rows, K.shape[0])
-    rc = lib().cmpq_kv_read(ctypes.byref(cache), ctypes.byref(rows), ctypes.byref(k), ctypes.byref(v),
-                            serving_dtype(K.dtype), _ptr(status), _stream())
+    dtype = _fill_rows(cache, page_table, first, cu_rows, K, V)
+    rc = _lib.cmpq_kv_read(cache.ref, cache.rows_ref, cache.K_ref, cache.V_ref, dtype, _ptr(status), _stream())
     if rc:
         _check(rc, "cmpq_kv_read")
+
+
+_NO_ROTATION = RotationView()
 
 
 def kv_attention(cache: KvCacheView, page_table: torch.Tensor, lengths: torch.Tensor, cu_rows: torch.Tensor,
@@ -789,17 +827,23 @@ def kv_attention(cache: KvCacheView, page_table: torch.Tensor, lengths: torch.Te
                  ws: Workspace, causal: bool = True, window: int = 0, rotation: Optional[RotationView] = None,
                  status: Optional[torch.Tensor] = None) -> None:
     """`cmpq_kv_attention`: Q [rows, q_heads, head_dim] over the cache, into O of the same shape."""
-    if O.shape != Q.shape or page_table.dim() != 2 or Q.dim() != 3:
-        raise ValueError("Q and O must be [rows, q_heads, head_dim], page_table [n_seq, pages]")
-    n_seq, ld = page_table.shape
-    job = KvAttentionJob(cache, _i32_table(page_table, (n_seq, ld), "page_table"), ld,
-                         _i32_table(lengths, (n_seq,), "lengths"), _i32_table(cu_rows, (n_seq + 1,), "cu_rows"),
-                         n_seq, Q.shape[0], int(max_rows), int(max_length), heads_view(Q, Q.shape[1], cache.head_dim),
-                         heads_view(O, Q.shape[1], cache.head_dim), serving_dtype(Q.dtype), serving_dtype(O.dtype),
-                         Q.shape[1], float(softmax_scale), int(bool(causal)), int(window),
-                         rotation if rotation is not None else RotationView(), _ptr(status))
-    ref = ctypes.byref(job)
-    buf = ws.get(lib().cmpq_kv_attention_workspace(ref))
-    rc = lib().cmpq_kv_attention(ref, _ptr(buf), buf.numel(), _stream())
+    if O.shape != Q.shape or Q.dim() != 3:
+        raise ValueError("Q and O must be [rows, q_heads, head_dim]")
+    n_seq, ld = shape = _table_shape(page_table)
+    j, heads = cache.job, Q.shape[1]
+    j.page_table, j.ld_table, j.n_seq = _i32_table(page_table, shape, "page_table"), ld, n_seq
+    j.lengths, j.cu_rows = _i32_table(lengths, (n_seq,), "lengths"), _i32_table(cu_rows, (n_seq + 1,), "cu_rows")
+    j.n_rows = _heads(cache.Q, Q, heads, cache.head_dim)
+    _heads(cache.O, O, heads, cache.head_dim)
+    j.q_dtype, j.o_dtype, j.q_heads = serving_dtype(Q.dtype), serving_dtype(O.dtype), heads
+    j.max_rows, j.max_length, j.window = max_rows, max_length, window
+    j.softmax_scale, j.causal, j.status = softmax_scale, 1 if causal else 0, _ptr(status)
+    j.rotation = _NO_ROTATION if rotation is None else rotation
+    for _ in range(2):              # asks for the workspace's size only where what is there does not do
+        buf = ws.buf
+        rc = _lib.cmpq_kv_attention(cache.job_ref, buf.data_ptr(), buf.numel(), _stream())
+        if rc != EWORKSPACE:
+            break
+        ws.get(_lib.cmpq_kv_attention_workspace(cache.job_ref))
     if rc:
         _check(rc, "cmpq_kv_attention")

@@ -386,11 +386,11 @@ __device__ __forceinline__ void keep_part(const Job &j, int64_t slot, int nc, in
 // Few rows.  C: 32 dims each of a head.  Tiles of 16 NT columns, one (row, query head) pair each; the wavefronts take the
 // part's units in turn and are added up through LDS.  Keys go into the integer matrix instruction as they are; a query
 // is held in 16 bits fixed point, 256 high + low, of its row's largest magnitude, two instructions for one.
-template <int C, int NT>
-__global__ __launch_bounds__(kWaves * 64, C * NT <= 4 ? 3 : C * NT <= 8 ? 2 : 1) void attend_kernel(Job j) {
+template <int C, int NT, int WAVES>
+__global__ __launch_bounds__(WAVES * 64, WAVES == 8 ? 2 : C * NT <= 4 ? 3 : C * NT <= 8 ? 2 : 1) void attend_kernel(Job j) {
     constexpr int NC = 16 * NT, DP = C * 32, kPad = DP + 4;
-    __shared__ float red[kWaves * 16 * kPad];
-    __shared__ float ml[kWaves][NC][2];
+    __shared__ __align__(16) float red[4 * 16 * kPad];
+    __shared__ float ml[WAVES][NC][2];
     const int lane = threadIdx.x & 63, wave = wave_index(), n = lane & 15, g = lane >> 4;
     const Plan plan = make_plan<NC>(j, blockIdx.x == 0 && wave == 0);
     Share w;
@@ -398,8 +398,8 @@ __global__ __launch_bounds__(kWaves * 64, C * NT <= 4 ? 3 : C * NT <= 8 ? 2 : 1)
     const Seq &s = w.s;
     const int tile = w.tile, head = w.head, parts = w.parts;
 
-    static_assert(NT <= kWaves, "room for the queries");
-    stage_queries<C>(j, s, head, tile * NC, NC, red, threadIdx.x, kWaves * 64);
+    static_assert(NT <= 4 && (WAVES == 4 || WAVES == 8), "room for the queries, shares of outputs");
+    stage_queries<C>(j, s, head, tile * NC, NC, red, threadIdx.x, WAVES * 64);
     __syncthreads();
     Int4 qh[NT][(C + 1) / 2], ql[NT][(C + 1) / 2];
     float factor[NT];
@@ -442,9 +442,9 @@ __global__ __launch_bounds__(kWaves * 64, C * NT <= 4 ? 3 : C * NT <= 8 ? 2 : 1)
 
     const int u0 = w.u0, u1 = w.u1;
     const int64_t page_bytes = (int64_t)j.c.page * DP;
-    for (int base = u0 + wave; base < u1; base += kWaves * 64) {
-        const PageOf mine = page_of(j, w.seq, head, base + lane * kWaves, u1);  // 64 units of this wavefront at once
-        const int count = min(64, (u1 - base + kWaves - 1) / kWaves);
+    for (int base = u0 + wave; base < u1; base += WAVES * 64) {
+        const PageOf mine = page_of(j, w.seq, head, base + lane * WAVES, u1);  // 64 units of this wavefront at once
+        const int count = min(64, (u1 - base + WAVES - 1) / WAVES);
         auto offset = [&](int i) {
             return ((int64_t)max(__builtin_amdgcn_readlane(mine.id, i), 0) * j.c.kv_heads + head) * page_bytes +
                    (int64_t)__builtin_amdgcn_readlane(mine.in_page, i) * (kUnit * DP) + lane * 16;
@@ -470,7 +470,7 @@ __global__ __launch_bounds__(kWaves * 64, C * NT <= 4 ? 3 : C * NT <= 8 ? 2 : 1)
             }
             load(j.c.k_codes, i + 1, kc);
             float l[NT][8], top[NT];
-            const int t0 = (base + i * kWaves) * kUnit;
+            const int t0 = (base + i * WAVES) * kUnit;
             const bool edge = !there || t0 < all_lo || t0 + kUnit > all_hi;
             bool past = there && vscale > u.scale;
 #pragma unroll
@@ -528,23 +528,30 @@ __global__ __launch_bounds__(kWaves * 64, C * NT <= 4 ? 3 : C * NT <= 8 ? 2 : 1)
     for (int t = 0; t < NT; ++t) {
         float top = kLowest;
 #pragma unroll
-        for (int v = 0; v < kWaves; ++v) top = fmaxf(top, ml[v][t * 16 + n][0]);
+        for (int v = 0; v < WAVES; ++v) top = fmaxf(top, ml[v][t * 16 + n][0]);
         const float mine = __builtin_amdgcn_exp2f(st[t].m - top) * u.scale;
         if (t > 0) __syncthreads();  // the columns before these have been read
+        auto share = [&](int of) { return reinterpret_cast<Float4 *>(&red[(of * 16 + n) * kPad + g * 4]); };
+        if (WAVES == 8) {  // the upper four first, the others on top
+            if (wave >= 4)
 #pragma unroll
-        for (int d = 0; d < 2 * C; ++d)
-            *reinterpret_cast<Float4 *>(&red[(wave * 16 + n) * kPad + d * 16 + g * 4]) = o[t][d] * mine;
+                for (int d = 0; d < 2 * C; ++d) share(wave - 4)[d * 4] = o[t][d] * mine;
+            __syncthreads();
+        }
+        if (wave < 4)
+#pragma unroll
+            for (int d = 0; d < 2 * C; ++d) share(wave)[d * 4] = WAVES == 8 ? o[t][d] * mine + share(wave)[d * 4] : o[t][d] * mine;
         __syncthreads();
-        for (int e = threadIdx.x; e < 16 * DP / 4; e += kWaves * 64) {
+        for (int e = threadIdx.x; e < 16 * DP / 4; e += WAVES * 64) {
             const int c = e / (DP / 4), d = e % (DP / 4) * 4, k = t * 16 + c;
             Float4 v = *reinterpret_cast<const Float4 *>(&red[c * kPad + d]);
 #pragma unroll
-            for (int q = 1; q < kWaves; ++q) v += *reinterpret_cast<const Float4 *>(&red[(q * 16 + c) * kPad + d]);
+            for (int q = 1; q < 4; ++q) v += *reinterpret_cast<const Float4 *>(&red[(q * 16 + c) * kPad + d]);
             float high = kLowest, total = 0.f;
 #pragma unroll
-            for (int q = 0; q < kWaves; ++q) high = fmaxf(high, ml[q][k][0]);
+            for (int q = 0; q < WAVES; ++q) high = fmaxf(high, ml[q][k][0]);
 #pragma unroll
-            for (int q = 0; q < kWaves; ++q) total += ml[q][k][1] * __builtin_amdgcn_exp2f(ml[q][k][0] - high);
+            for (int q = 0; q < WAVES; ++q) total += ml[q][k][1] * __builtin_amdgcn_exp2f(ml[q][k][0] - high);
             if (parts > 1) {
                 keep_part(j, w.slot, NC, k, DP, d, v);
                 if (d == 0) {
@@ -828,6 +835,7 @@ __global__ __launch_bounds__(256) void join_rows_kernel(Job j) {
 // How a call is launched: the kernel for few rows, for many, or both, each with its columns, workgroups and kept parts.
 struct Kernel {
     int nc = 0, target = 0, least = 0;
+    bool wide = false;  // 8 wavefronts a workgroup
     int64_t least_cols = 0, most_cols = -1, grid = 0, kept = 0;
 };
 struct Launches {
@@ -840,12 +848,23 @@ struct Launches {
 // Tiles of 16 columns a wavefront of the kernel for many rows, as registers allow.
 constexpr int rows_tiles(int64_t c) { return c <= 2 ? 4 : c <= 4 ? 3 : c <= 6 ? 2 : 1; }
 
-void size_up(const cmpq_kv_attention_job *a, Kernel &h) {
+// Units that a sequence's rows see at most.
+int64_t most_units(const cmpq_kv_attention_job *a) {
+    const int64_t all = cdiv(a->max_length, kUnit);
+    if (a->window == 0) return all;
+    const int64_t seen = (a->window + a->max_rows) / kUnit + 2;  // of those of any place in a unit
+    return seen < all ? seen : all;
+}
+
+int64_t most_tiles(const cmpq_kv_attention_job *a, const Kernel &h) {
     const int64_t group = a->q_heads / a->cache.kv_heads;
     const int64_t most = h.most_cols < a->max_rows * group ? h.most_cols : a->max_rows * group;  // columns of a sequence
     const int64_t by_rows = a->n_rows * group / h.nc + a->n_seq, by_most = a->n_seq * cdiv(most, h.nc);
-    const int64_t tiles = (by_rows < by_most ? by_rows : by_most) * a->cache.kv_heads;
-    const int64_t parts = cdiv(cdiv(a->max_length, kUnit), h.least);
+    return (by_rows < by_most ? by_rows : by_most) * a->cache.kv_heads;
+}
+
+void size_up(const cmpq_kv_attention_job *a, Kernel &h) {
+    const int64_t tiles = most_tiles(a, h), parts = cdiv(most_units(a), h.least);
     h.grid = tiles;
     if (parts > 1) {
         const int64_t full = tiles * parts;
@@ -874,6 +893,12 @@ Launches plan_launches(const cmpq_kv_attention_job *a) {
         l.rows.most_cols = INT64_MAX;
     }
     l.few.target = 1024, l.few.least = 8;
+    // Short sequences in one part, by 8 wavefronts where that leaves compute units free: a part more costs the launch that
+    // joins them.
+    if (l.few.nc && most_units(a) <= 64) {
+        l.few.least = 64;
+        l.few.wide = most_tiles(a, l.few) < 512;
+    }
     l.rows.target = 512, l.rows.least = 16;
     if (l.few.nc) size_up(a, l.few);
     if (l.rows.nc) size_up(a, l.rows);
@@ -895,7 +920,12 @@ int check_job(const cmpq_kv_attention_job *a) {
 
 template <int C, int NT>
 void launch_few(const Job &j, const Kernel &h, hipStream_t st) {
-    attend_kernel<C, NT><<<dim3((unsigned)h.grid), kWaves * 64, 0, st>>>(j);
+    if constexpr (C * NT <= 8) {
+        if (h.wide) attend_kernel<C, NT, 8><<<dim3((unsigned)h.grid), 512, 0, st>>>(j);
+        else attend_kernel<C, NT, 4><<<dim3((unsigned)h.grid), 256, 0, st>>>(j);
+    } else {
+        attend_kernel<C, NT, 4><<<dim3((unsigned)h.grid), 256, 0, st>>>(j);
+    }
     if (!h.kept) return;
     const int64_t each = h.most_cols / j.group < j.max_rows ? h.most_cols / j.group : j.max_rows;
     const int64_t items = j.n_seq * each * j.q_heads;
@@ -925,13 +955,7 @@ void launch(Job j, const Launches &l, WsCarver &w, hipStream_t st) {
     }
 }
 
-}  // namespace
-
-extern "C" size_t cmpq_kv_attention_workspace(const cmpq_kv_attention_job *a) {
-    if (!a || a->cache.kv_heads < 1 || a->q_heads < a->cache.kv_heads || a->n_seq < 0 || a->n_rows < 0 || a->max_rows < 0 ||
-        a->max_length < 0 || !cmpq_kv_page_bytes(a->cache.head_dim, a->cache.page))
-        return 0;
-    const Launches l = plan_launches(a);
+size_t workspace_of(const Launches &l) {
     WsCarver w(nullptr);
     for (const Kernel *h : {&l.rows, &l.few}) {
         if (!h->nc) continue;
@@ -941,13 +965,22 @@ extern "C" size_t cmpq_kv_attention_workspace(const cmpq_kv_attention_job *a) {
     return w.need() > 256 ? w.need() : 256;
 }
 
+}  // namespace
+
+extern "C" size_t cmpq_kv_attention_workspace(const cmpq_kv_attention_job *a) {
+    if (!a || a->cache.kv_heads < 1 || a->q_heads < a->cache.kv_heads || a->n_seq < 0 || a->n_rows < 0 || a->max_rows < 0 ||
+        a->max_length < 0 || !cmpq_kv_page_bytes(a->cache.head_dim, a->cache.page))
+        return 0;
+    return workspace_of(plan_launches(a));
+}
+
 extern "C" int cmpq_kv_attention(const cmpq_kv_attention_job *a, void *ws, size_t ws_bytes, void *stream) {
     if (int rc = check_job(a)) return rc;
     if (a->n_seq == 0 || a->n_rows == 0 || a->max_rows == 0) return CMPQ_OK;
     if (!a->page_table || !a->lengths || !a->cu_rows || !a->Q.ptr || !a->O.ptr) return CMPQ_EINVAL;
     const Launches l = plan_launches(a);
     if (l.few.grid > INT32_MAX || l.rows.grid > INT32_MAX || a->n_seq * 48 * a->q_heads > INT32_MAX) return CMPQ_ESHAPE;
-    if (!ws || reinterpret_cast<uintptr_t>(ws) % 256 || ws_bytes < cmpq_kv_attention_workspace(a)) return CMPQ_EWORKSPACE;
+    if (!ws || reinterpret_cast<uintptr_t>(ws) % 256 || ws_bytes < workspace_of(l)) return CMPQ_EWORKSPACE;
     WsCarver w(ws);
     Job j = {};
     j.c = a->cache;

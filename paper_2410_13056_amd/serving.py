@@ -31,6 +31,9 @@ class Int8Weight:
     codes: torch.Tensor     # int8, in the order of the matrix instruction's operands
     scale: torch.Tensor     # [d_out] fp32
 
+    def __post_init__(self):
+        self._call = B.Int8ProductCall(self.d_in, self.d_out, self.codes, self.scale)
+
 
 def prepare_int8(W: torch.Tensor, status: Optional[torch.Tensor] = None) -> Int8Weight:
     """A weight [d_out, d_in] (the framework layout) in 8 bits with a scale per output channel."""
@@ -46,10 +49,9 @@ def int8_product(w: Int8Weight, X: torch.Tensor, ws: Optional[B.Workspace] = Non
                  status: Optional[torch.Tensor] = None) -> torch.Tensor:
     """Y [m, d_out] = X [m, d_in] times the weight, X in 8 bits with a scale per token on the way.  `out_dtype`
     defaults to X's."""
-    ws = ws or B.Workspace(X.device)
     if out is None:
         out = torch.empty((X.shape[0], w.d_out), dtype=out_dtype or X.dtype, device=X.device)
-    B.int8_product(X, w.codes, w.scale, out, ws, status)
+    w._call(X, out, ws or B.Workspace(X.device), status)
     return out
 
 
@@ -79,7 +81,8 @@ def make_rotation(positions: int, dims: int, base: float = 10000.0, interleaved:
 @dataclasses.dataclass
 class KvCache:
     """Keys and values in pages of `page` tokens, 8 bits a value, a scale per page and head (device tensors).
-    Which page belongs to which sequence is the caller's: every call takes a table of them."""
+    Which page belongs to which sequence is the caller's: every call takes a table of them.  One call on a cache object
+    at a time: its arguments are filled into structures that the object keeps."""
     k: torch.Tensor         # uint8 [n_pages, kv_heads, kv_page_bytes(head_dim, page)]: code + 128
     v: torch.Tensor
     k_scale: torch.Tensor   # fp32 [n_pages, kv_heads]
@@ -119,8 +122,8 @@ def kv_read(cache: KvCache, page_table: torch.Tensor, first: torch.Tensor, cu_ro
             status: Optional[torch.Tensor] = None) -> Tuple[torch.Tensor, torch.Tensor]:
     """Keys and values [n_rows, kv_heads, head_dim] that the tokens first[i], first[i]+1, ... of each sequence stand
     for, cu_rows[i+1] - cu_rows[i] of them.  Rows that name no token of the cache are left as they come."""
-    shape = (n_rows, cache.kv_heads, cache.head_dim)
-    K, V = (torch.empty(shape, dtype=dtype, device=cache.k.device) for _ in range(2))
+    K = torch.empty((n_rows, cache.kv_heads, cache.head_dim), dtype=dtype, device=cache.k.device)
+    V = torch.empty_like(K)
     B.kv_read(cache._view, page_table, first, cu_rows, K, V, status)
     return K, V
 
@@ -135,13 +138,12 @@ def kv_attention(cache: KvCache, Q: torch.Tensor, page_table: torch.Tensor, leng
     to its own (all of them unless `causal`), the last `window` of those where window > 0; one that sees none gives
     zeros.  `softmax_scale` defaults to head_dim^-0.5; the output is float16 or bfloat16, by default Q's type
     (float16 for float32)."""
-    ws = ws or B.Workspace(Q.device)
     if out is None:
         out = torch.empty(Q.shape, dtype=out_dtype or (torch.float16 if Q.dtype == torch.float32 else Q.dtype),
                           device=Q.device)
     B.kv_attention(cache._view, page_table, lengths, cu_rows, Q, out, max_rows, max_length,
-                   cache.head_dim ** -0.5 if softmax_scale is None else softmax_scale, ws, causal, window,
-                   None if rotation is None else rotation._view, status)
+                   cache.head_dim ** -0.5 if softmax_scale is None else softmax_scale, ws or B.Workspace(Q.device), causal,
+                   window, None if rotation is None else rotation._view, status)
     return out
 
 
