@@ -82,6 +82,7 @@ __device__ __forceinline__ int tiles_of(const Job &j, const Seq &s) {
 template <int NC>
 __device__ __forceinline__ Plan make_plan(const Job &j, bool look) {
     const int lane = threadIdx.x & 63;
+    if (j.kept == 0 && !look) return {1 << 30};
     double total = 0, pieces = 0;
     for (int64_t base = 0; base < j.n_seq; base += 64) {
         if (base + lane >= j.n_seq) continue;
@@ -95,6 +96,7 @@ __device__ __forceinline__ Plan make_plan(const Job &j, bool look) {
     const double all = __shfl(wave_sum_f64(total), 0) * j.c.kv_heads, odd = __shfl(wave_sum_f64(pieces), 0) * j.c.kv_heads;
     Plan p;
     p.step = __builtin_amdgcn_readfirstlane(max(j.least, (int)ceil(all / max((double)j.target - odd, 0.5 * j.target))));
+    if (j.kept == 0) p.step = 1 << 30;
     return p;
 }
 
@@ -299,21 +301,24 @@ struct PageOf {
 };
 
 __device__ __forceinline__ PageOf page_of(const Job &j, int64_t seq, int head, int unit, int end) {
-    PageOf p = {-1, 0, 0.f, 0.f, 0.f, 1.f};
+    PageOf p = {-1, 0, 0.f, 1.f, 0.f, 1.f};
     if (unit >= end) return p;
-    const int token = unit * kUnit;
-    p.id = j.table[seq * j.ld_table + token / j.c.page];
-    p.in_page = token % j.c.page / kUnit;
+    const int token = unit * kUnit, nth = token / j.c.page;
+    p.id = j.table[seq * j.ld_table + nth];
+    p.in_page = (token - nth * j.c.page) / kUnit;
     if (p.id < 0 || p.id >= j.c.n_pages) {
         p.id = -1;
         if (j.status) atomicOr(j.status, CMPQ_STATUS_RANGE);
     } else {
         p.ks = j.c.k_scale[(int64_t)p.id * j.c.kv_heads + head];
         p.vs = j.c.v_scale[(int64_t)p.id * j.c.kv_heads + head];
-        p.log_vs = log2f(p.vs);
-        p.inv_vs = 1.f / p.vs;
     }
     return p;
+}
+// The rest of it: apart, so that loads of the codes need not wait for the scales.
+__device__ __forceinline__ void finish(PageOf &p) {
+    p.log_vs = log2f(p.vs);
+    p.inv_vs = 1.f / p.vs;
 }
 __device__ __forceinline__ float lane_value(float v, int lane) {
     return __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(v), lane));
@@ -399,6 +404,27 @@ __global__ __launch_bounds__(WAVES * 64, WAVES == 8 ? 2 : C * NT <= 4 ? 3 : C * 
     const int tile = w.tile, head = w.head, parts = w.parts;
 
     static_assert(NT <= 4 && (WAVES == 4 || WAVES == 8), "room for the queries, shares of outputs");
+    const int u0 = w.u0, u1 = w.u1;
+    const int64_t page_bytes = (int64_t)j.c.page * DP;
+    // pages of 64 units of this wavefront at once, and the codes of the unit to come: both before the queries, which take
+    // their time as well
+    int base = u0 + wave, count = 0;
+    PageOf mine;
+    uint4 kc[C], vc[C];
+    auto load = [&](const uint8_t *from, int i, uint4 (&to)[C]) {
+        const int k = min(i, count - 1);
+        const int64_t off = ((int64_t)max(__builtin_amdgcn_readlane(mine.id, k), 0) * j.c.kv_heads + head) * page_bytes +
+                            (int64_t)__builtin_amdgcn_readlane(mine.in_page, k) * (kUnit * DP) + lane * 16;
+#pragma unroll
+        for (int c = 0; c < C; ++c) to[c] = load16_stream(from + off + c * 1024);
+    };
+    auto begin = [&]() {
+        mine = page_of(j, w.seq, head, base + lane * WAVES, u1);
+        count = min(64, (u1 - base + WAVES - 1) / WAVES);
+        load(j.c.k_codes, 0, kc);
+        load(j.c.v_codes, 0, vc);
+    };
+    if (base < u1) begin();
     stage_queries<C>(j, s, head, tile * NC, NC, red, threadIdx.x, WAVES * 64);
     __syncthreads();
     Int4 qh[NT][(C + 1) / 2], ql[NT][(C + 1) / 2];
@@ -440,23 +466,9 @@ __global__ __launch_bounds__(WAVES * 64, WAVES == 8 ? 2 : C * NT <= 4 ? 3 : C * 
     }
     UnitScale u = {0.f, 0.f};
 
-    const int u0 = w.u0, u1 = w.u1;
-    const int64_t page_bytes = (int64_t)j.c.page * DP;
-    for (int base = u0 + wave; base < u1; base += WAVES * 64) {
-        const PageOf mine = page_of(j, w.seq, head, base + lane * WAVES, u1);  // 64 units of this wavefront at once
-        const int count = min(64, (u1 - base + WAVES - 1) / WAVES);
-        auto offset = [&](int i) {
-            return ((int64_t)max(__builtin_amdgcn_readlane(mine.id, i), 0) * j.c.kv_heads + head) * page_bytes +
-                   (int64_t)__builtin_amdgcn_readlane(mine.in_page, i) * (kUnit * DP) + lane * 16;
-        };
-        uint4 kc[C], vc[C];
-        auto load = [&](const uint8_t *from, int i, uint4 (&to)[C]) {
-            const int64_t off = offset(min(i, count - 1));
-#pragma unroll
-            for (int c = 0; c < C; ++c) to[c] = load16_stream(from + off + c * 1024);
-        };
-        load(j.c.k_codes, 0, kc);
-        load(j.c.v_codes, 0, vc);
+    for (bool first = true; base < u1; base += WAVES * 64, first = false) {
+        if (!first) begin();
+        finish(mine);
         for (int i = 0; i < count; ++i) {
             const bool there = __builtin_amdgcn_readlane(mine.id, i) >= 0;
             const float kscale = lane_value(mine.ks, i), vscale = lane_value(mine.vs, i);
@@ -623,7 +635,10 @@ __global__ __launch_bounds__(kWaves * 64, 2) void attend_rows_kernel(Job j) {
     uint4 kc[kShare], vc[kShare];
     PageOf ahead = {}, mine = {};
     auto load = [&](int unit) {
-        if ((unit - u0) % 64 == 0) ahead = page_of(j, w.seq, head, unit + lane, u1);
+        if ((unit - u0) % 64 == 0) {
+            ahead = page_of(j, w.seq, head, unit + lane, u1);
+            finish(ahead);
+        }
         const int i = (unit - u0) % 64;
         const int64_t off = ((int64_t)max(__builtin_amdgcn_readlane(ahead.id, i), 0) * j.c.kv_heads + head) * page_bytes +
                             (int64_t)__builtin_amdgcn_readlane(ahead.in_page, i) * (kUnit * DP) + lane * 16;
