@@ -5,7 +5,6 @@
 
 namespace {
 
-constexpr int kThreads = 256;
 
 struct Page {
     int64_t seq;     // sequence, -1: there is no such page
@@ -162,20 +161,20 @@ __device__ __forceinline__ void hold_item(const Page &pg, const Item &it, float 
 }
 
 // The new values are read once where each lane has at most one item, else again for their codes.
-template <typename T, bool KEYS, bool WHOLE>
+template <typename T, bool KEYS, bool WHOLE, int THREADS>
 __device__ __forceinline__ void append_page(const cmpq_kv_cache &c, const Page &pg, int64_t id, int head, const cmpq_heads &in,
                             const cmpq_rotation &rot, int32_t *status, float *scratch) {
     const int chunks = (c.head_dim + 31) / 32, octets = chunks * 4;
     uint8_t *codes = (KEYS ? c.k_codes : c.v_codes) + (id * c.kv_heads + head) * (int64_t)(c.page * chunks * 32);
     float *scale = (KEYS ? c.k_scale : c.v_scale) + id * c.kv_heads + head;
-    if (threadIdx.x == 0) scratch[kThreads / 64] = pg.from > 0 ? *scale : 0.f;
+    if (threadIdx.x == 0) scratch[THREADS / 64] = pg.from > 0 ? *scale : 0.f;
     const int e0 = pg.from / 4 * octets, e1 = (pg.to + 3) / 4 * octets;
-    const bool once = e1 - e0 <= kThreads;
+    const bool once = e1 - e0 <= THREADS;
     float x[4][8], most = 0.f, inv = 0.f;
     bool bad = false;
 #pragma unroll 1
     for (int pass = 0; pass < 2; ++pass) {
-        for (int e = e0 + threadIdx.x; e < e1; e += kThreads) {
+        for (int e = e0 + threadIdx.x; e < e1; e += THREADS) {
             const Item it = item_of<KEYS>(e, octets, chunks, codes);
             if (pass == 0 || !once) load_item<T, KEYS, WHOLE>(c, pg, in, rot, head, it, x);
             if (pass == 0) {
@@ -192,21 +191,21 @@ __device__ __forceinline__ void append_page(const cmpq_kv_cache &c, const Page &
         if (KEYS && rot.cos && threadIdx.x == 0 && status && pg.begin + pg.to > rot.positions)
             atomicOr(status, CMPQ_STATUS_RANGE);
         most = block_max(most, scratch);
-        const float old = scratch[kThreads / 64], now = fmaxf(old, code_scale(most));
+        const float old = scratch[THREADS / 64], now = fmaxf(old, code_scale(most));
         inv = 1.f / now;
         if (threadIdx.x == 0) *scale = now;
         if (pg.from > 0 && now != old) {
-            for (int e = threadIdx.x; e < (pg.from + 3) / 4 * octets; e += kThreads)
+            for (int e = threadIdx.x; e < (pg.from + 3) / 4 * octets; e += THREADS)
                 hold_item<KEYS>(pg, item_of<KEYS>(e, octets, chunks, codes), old * inv);
             __syncthreads();  // an item of both is held first, by whichever lane
         }
     }
 }
 
-template <typename T, bool WHOLE>
-__global__ __launch_bounds__(kThreads) void append_kernel(cmpq_kv_cache c, cmpq_kv_rows r, cmpq_heads K, cmpq_heads V,
+template <typename T, bool WHOLE, int THREADS>
+__global__ __launch_bounds__(THREADS) void append_kernel(cmpq_kv_cache c, cmpq_kv_rows r, cmpq_heads K, cmpq_heads V,
                                                           cmpq_rotation rot, int32_t *status) {
-    __shared__ float scratch[kThreads / 64 + 1];
+    __shared__ float scratch[THREADS / 64 + 1];
     const Page pg = find_page(r, c.page, blockIdx.x, looks_over() ? status : nullptr);
     if (pg.seq < 0) return;
     const int64_t id = r.page_table[pg.seq * r.ld_table + pg.begin / c.page];
@@ -214,18 +213,18 @@ __global__ __launch_bounds__(kThreads) void append_kernel(cmpq_kv_cache c, cmpq_
         if (threadIdx.x == 0 && status) atomicOr(status, CMPQ_STATUS_RANGE);
         return;
     }
-    if (blockIdx.z == 0) append_page<T, true, WHOLE>(c, pg, id, blockIdx.y, K, rot, status, scratch);
-    else append_page<T, false, WHOLE>(c, pg, id, blockIdx.y, V, rot, status, scratch);
+    if (blockIdx.z == 0) append_page<T, true, WHOLE, THREADS>(c, pg, id, blockIdx.y, K, rot, status, scratch);
+    else append_page<T, false, WHOLE, THREADS>(c, pg, id, blockIdx.y, V, rot, status, scratch);
 }
 
-template <typename T, bool KEYS>
+template <typename T, bool KEYS, int THREADS>
 __device__ void read_page(const cmpq_kv_cache &c, const Page &pg, int64_t id, int head, const cmpq_heads &out) {
     const int dim = c.head_dim, chunks = (dim + 31) / 32, octets = chunks * 4;
     uint8_t *codes = (KEYS ? c.k_codes : c.v_codes) + (id * c.kv_heads + head) * (int64_t)(c.page * chunks * 32);
     const float scale = (KEYS ? c.k_scale : c.v_scale)[id * c.kv_heads + head];
     T *base = static_cast<T *>(out.ptr) + head * out.head_stride;
     const int e0 = pg.from / 4 * octets, e1 = (pg.to + 3) / 4 * octets;
-    for (int e = e0 + threadIdx.x; e < e1; e += kThreads) {
+    for (int e = e0 + threadIdx.x; e < e1; e += THREADS) {
         const Item it = item_of<KEYS>(e, octets, chunks, codes);
         uint32_t w[8];
 #pragma unroll
@@ -255,8 +254,8 @@ __device__ void read_page(const cmpq_kv_cache &c, const Page &pg, int64_t id, in
     }
 }
 
-template <typename T>
-__global__ __launch_bounds__(kThreads) void read_kernel(cmpq_kv_cache c, cmpq_kv_rows r, cmpq_heads K, cmpq_heads V,
+template <typename T, int THREADS>
+__global__ __launch_bounds__(THREADS) void read_kernel(cmpq_kv_cache c, cmpq_kv_rows r, cmpq_heads K, cmpq_heads V,
                                                         int32_t *status) {
     const Page pg = find_page(r, c.page, blockIdx.x, looks_over() ? status : nullptr);
     if (pg.seq < 0) return;
@@ -265,8 +264,8 @@ __global__ __launch_bounds__(kThreads) void read_kernel(cmpq_kv_cache c, cmpq_kv
         if (threadIdx.x == 0 && status) atomicOr(status, CMPQ_STATUS_RANGE);
         return;
     }
-    if (blockIdx.z == 0) read_page<T, true>(c, pg, id, blockIdx.y, K);
-    else read_page<T, false>(c, pg, id, blockIdx.y, V);
+    if (blockIdx.z == 0) read_page<T, true, THREADS>(c, pg, id, blockIdx.y, K);
+    else read_page<T, false, THREADS>(c, pg, id, blockIdx.y, V);
 }
 
 int check_rows(const cmpq_kv_cache *c, const cmpq_kv_rows *r, const cmpq_heads *K, const cmpq_heads *V, int dtype) {
@@ -303,8 +302,10 @@ extern "C" int cmpq_kv_append(const cmpq_kv_cache *cache, const cmpq_kv_rows *ro
     hipStream_t st = static_cast<hipStream_t>(stream);
     auto launch = [&](auto like) {
         using T = decltype(like);
-        if (cache->head_dim % 8 == 0 && turns_by_eight(rot)) append_kernel<T, true><<<grid, kThreads, 0, st>>>(*cache, *rows, *K, *V, rot, status);
-        else append_kernel<T, false><<<grid, kThreads, 0, st>>>(*cache, *rows, *K, *V, rot, status);
+        const bool whole = cache->head_dim % 8 == 0 && turns_by_eight(rot);
+        if (!whole) append_kernel<T, false, 256><<<grid, 256, 0, st>>>(*cache, *rows, *K, *V, rot, status);
+        else if (rows->n_rows > 4 * rows->n_seq) append_kernel<T, true, 256><<<grid, 256, 0, st>>>(*cache, *rows, *K, *V, rot, status);
+        else append_kernel<T, true, 64><<<grid, 64, 0, st>>>(*cache, *rows, *K, *V, rot, status);
     };
     if (dtype == CMPQ_F16) launch(_Float16());
     else if (dtype == CMPQ_BF16) launch(__bf16());
@@ -319,9 +320,9 @@ extern "C" int cmpq_kv_read(const cmpq_kv_cache *cache, const cmpq_kv_rows *rows
     if (rows->n_seq == 0 || rows->n_rows == 0 || rows->ld_table == 0) return CMPQ_OK;
     const dim3 grid = page_grid(*cache, *rows);
     hipStream_t st = static_cast<hipStream_t>(stream);
-    if (dtype == CMPQ_F16) read_kernel<_Float16><<<grid, kThreads, 0, st>>>(*cache, *rows, *K, *V, status);
-    else if (dtype == CMPQ_BF16) read_kernel<__bf16><<<grid, kThreads, 0, st>>>(*cache, *rows, *K, *V, status);
-    else read_kernel<float><<<grid, kThreads, 0, st>>>(*cache, *rows, *K, *V, status);
+    if (dtype == CMPQ_F16) read_kernel<_Float16, 256><<<grid, 256, 0, st>>>(*cache, *rows, *K, *V, status);
+    else if (dtype == CMPQ_BF16) read_kernel<__bf16, 256><<<grid, 256, 0, st>>>(*cache, *rows, *K, *V, status);
+    else read_kernel<float, 256><<<grid, 256, 0, st>>>(*cache, *rows, *K, *V, status);
     CMPQ_LAUNCH_CHECK();
     return CMPQ_OK;
 }
