@@ -368,18 +368,18 @@ __device__ __forceinline__ void move_up(State (&st)[NT], const float (&top)[NT],
     if (wider) u = {vscale, log_vscale};
 }
 
-// The weights of a unit's 8 tokens in this lane to FP16, times the unit's value scale over the scale that outputs are held in.
-__device__ __forceinline__ Half8 weigh(const float (&s)[8], float f, State &st, float log_ratio, float inv_ratio) {
-    const float base = st.m - kRaise - log_ratio;
+// The weights of a unit's 8 tokens in this lane to FP16, against reference m, times the unit's value scale over the scale that
+// outputs are held in; `part`: their sum.
+__device__ __forceinline__ Half8 weigh(const float (&s)[8], float f, float m, float log_ratio, float &part) {
+    const float base = m - kRaise - log_ratio;
     Half8 p;
-    float part = 0.f;
+    float w[8];
 #pragma unroll
     for (int r = 0; r < 8; ++r) {
-        const float w = __builtin_amdgcn_exp2f(fmaf(s[r], f, -base));
-        part += w;
-        p[r] = (_Float16)w;
+        w[r] = __builtin_amdgcn_exp2f(fmaf(s[r], f, -base));
+        p[r] = (_Float16)w[r];
     }
-    st.sum = fmaf(part, inv_ratio, st.sum);
+    part = ((w[0] + w[1]) + (w[2] + w[3])) + ((w[4] + w[5]) + (w[6] + w[7]));
     return p;
 }
 
@@ -512,7 +512,11 @@ __global__ __launch_bounds__(WAVES * 64, WAVES == 8 ? 2 : C * NT <= 4 ? 3 : C * 
             const float inv_ratio = fminf(u.scale * lane_value(mine.inv_vs, i), kMostInverse);
             Half8 p[NT];
 #pragma unroll
-            for (int t = 0; t < NT; ++t) p[t] = weigh(l[t], logit_factor(factor[t], kscale), st[t], log_ratio, inv_ratio);
+            for (int t = 0; t < NT; ++t) {
+                float part;
+                p[t] = weigh(l[t], logit_factor(factor[t], kscale), st[t].m, log_ratio, part);
+                st[t].sum = fmaf(part, inv_ratio, st[t].sum);
+            }
 #pragma unroll
             for (int c = 0; c < C; ++c) {
                 const Half8 v0 = halves(vc[c].x, vc[c].y), v1 = halves(vc[c].z, vc[c].w);
@@ -588,47 +592,15 @@ __global__ __launch_bounds__(kWaves * 64, 2) void attend_rows_kernel(Job j) {
     static_assert(sizeof(staged) >= 4 * kHalf, "two units");
     const int lane = threadIdx.x & 63, wave = wave_index(), n = lane & 15, g = lane >> 4;
     auto unit_at = [&](int buf) { return reinterpret_cast<Half8 *>(staged) + buf * (2 * kHalf / 16) + lane; };
+    float *const of_wave = staged + wave * 16 * (DP + 4);
     const Plan plan = make_plan<NC>(j, blockIdx.x == 0 && wave == 0);
     Share w;
     if (!share_of<NC>(j, plan, blockIdx.x, w)) return;
     const Seq &s = w.s;
     const int tile = w.tile, head = w.head, parts = w.parts;
-
-    Half8 q[NT][C];
-    float factor[NT];
-    int lo[NT], hi[NT];
-    const int col0 = tile * NC + wave * NT * 16;
-#pragma unroll
-    for (int t = 0; t < NT; ++t) {
-        const Column col = column(j, s, head, col0 + t * 16 + n);
-        lo[t] = col.lo, hi[t] = col.hi;
-        float v[C][8], top, *mine = staged + wave * 16 * (DP + 4);
-        stage_queries<C>(j, s, head, col0 + t * 16, 16, mine, lane, 64);
-        __syncthreads();
-        const int e = take_query<C>(mine, v, top);
-        const float sign = j.scale < 0.f ? -1.f : 1.f;
-        factor[t] = ldexpf(sign * j.scale * kLog2e, e);  // not below 0
-        (void)top;
-#pragma unroll
-        for (int c = 0; c < C; ++c)
-#pragma unroll
-            for (int i = 0; i < 8; ++i) q[t][c][i] = (_Float16)(sign * v[c][i]);
-        __syncthreads();
-    }
-    const int all_hi = __builtin_amdgcn_readlane(hi[0], 0), all_lo = __builtin_amdgcn_readlane(lo[NT - 1], 15);
     // units that some column of the workgroup sees
     const Column first = column(j, s, head, tile * NC), last = column(j, s, head, tile * NC + NC - 1);
     const int u0 = max(w.u0, first.lo / kUnit), u1 = min(w.u1, (max(last.hi, 0) + kUnit - 1) / kUnit);
-
-    Float4 o[NT][2 * C];
-    State st[NT];
-#pragma unroll
-    for (int t = 0; t < NT; ++t) {
-        st[t] = {kLowest, 0.f};
-#pragma unroll
-        for (int d = 0; d < 2 * C; ++d) o[t][d] = Float4{0.f, 0.f, 0.f, 0.f};
-    }
-    UnitScale u = {0.f, 0.f};
     const int64_t page_bytes = (int64_t)j.c.page * DP;
 
     // A unit's codes come into registers a unit ahead and go into LDS as FP16: operand 2 c + h of the keys, then the values.
@@ -661,8 +633,47 @@ __global__ __launch_bounds__(kWaves * 64, 2) void attend_rows_kernel(Job j) {
             to[kHalf / 16 + 64] = halves(vc[k].z, vc[k].w);
         }
     };
+    if (u0 < u1) load(u0);  // on its way while the queries come
+
+    Half8 q[NT][C];
+    float factor[NT];
+    int lo[NT], hi[NT];
+#pragma unroll 1
+    for (int tt = 0; tt < NT; ++tt) {  // not unrolled: the code would be long before its first unit
+        const int index = tile * NC + (wave * NT + tt) * 16;
+        const Column col = column(j, s, head, index + n);
+        stage_queries<C>(j, s, head, index, 16, of_wave, lane, 64);
+        __syncthreads();
+        float v[C][8], top;
+        const int e = take_query<C>(of_wave, v, top);
+        const float sign = j.scale < 0.f ? -1.f : 1.f;
+        Half8 h[C];
+#pragma unroll
+        for (int c = 0; c < C; ++c)
+#pragma unroll
+            for (int i = 0; i < 8; ++i) h[c][i] = (_Float16)(sign * v[c][i]);
+#pragma unroll
+        for (int t = 0; t < NT; ++t) {
+            if (t != tt) continue;
+            lo[t] = col.lo, hi[t] = col.hi;
+            factor[t] = ldexpf(sign * j.scale * kLog2e, e);  // not below 0
+#pragma unroll
+            for (int c = 0; c < C; ++c) q[t][c] = h[c];
+        }
+        __syncthreads();
+    }
+    const int all_hi = __builtin_amdgcn_readlane(hi[0], 0), all_lo = __builtin_amdgcn_readlane(lo[NT - 1], 15);
+
+    Float4 o[NT][2 * C];
+    State st[NT];
+#pragma unroll
+    for (int t = 0; t < NT; ++t) {
+        st[t] = {kLowest, 0.f};
+#pragma unroll
+        for (int d = 0; d < 2 * C; ++d) o[t][d] = Float4{0.f, 0.f, 0.f, 0.f};
+    }
+    UnitScale u = {0.f, 0.f};
     if (u0 < u1) {
-        load(u0);
         store(0);
         mine = ahead;
         if (u0 + 1 < u1) load(u0 + 1);
@@ -675,6 +686,7 @@ __global__ __launch_bounds__(kWaves * 64, 2) void attend_rows_kernel(Job j) {
         if (unit + 1 < u1) store(buf ^ 1);
         if (unit + 2 < u1) load(unit + 2);
         const Half8 *from = unit_at(buf);
+        __builtin_amdgcn_s_setprio(1);
         Float4 sum[NT][2];
 #pragma unroll
         for (int t = 0; t < NT; ++t) sum[t][0] = sum[t][1] = Float4{0.f, 0.f, 0.f, 0.f};
@@ -687,6 +699,7 @@ __global__ __launch_bounds__(kWaves * 64, 2) void attend_rows_kernel(Job j) {
                 sum[t][1] = __builtin_amdgcn_mfma_f32_16x16x32_f16(k1, q[t][c], sum[t][1], 0, 0, 0);
             }
         }
+        __builtin_amdgcn_s_setprio(0);
         float l[NT][8], top[NT];
         const int t0 = unit * kUnit;
         const bool edge = !there || t0 < all_lo || t0 + kUnit > all_hi;
@@ -710,7 +723,11 @@ __global__ __launch_bounds__(kWaves * 64, 2) void attend_rows_kernel(Job j) {
         const float inv_ratio = fminf(u.scale * lane_value(mine.inv_vs, i), kMostInverse);
         Half8 p[NT];
 #pragma unroll
-        for (int t = 0; t < NT; ++t) p[t] = weigh(l[t], logit_factor(factor[t], kscale), st[t], log_ratio, inv_ratio);
+        for (int t = 0; t < NT; ++t) {
+            float part;
+            p[t] = weigh(l[t], logit_factor(factor[t], kscale), st[t].m, log_ratio, part);
+            st[t].sum = fmaf(part, inv_ratio, st[t].sum);
+        }
 #pragma unroll
         for (int c = 0; c < C; ++c) {
             const Half8 v0 = from[kHalf / 16 + c * 128], v1 = from[kHalf / 16 + c * 128 + 64];
@@ -724,24 +741,26 @@ __global__ __launch_bounds__(kWaves * 64, 2) void attend_rows_kernel(Job j) {
         __syncthreads();
     }
 
+    // a tile at a time through LDS, so that rows go out whole
 #pragma unroll
     for (int t = 0; t < NT; ++t) {
-        const float total = row_sum(st[t].sum);
-        const int k = wave * NT * 16 + t * 16 + n, at = tile * NC + k;
-        if (parts > 1) {
-            if (g == 0) {
-                j.part_ml[(w.slot * NC + k) * 2] = st[t].m;
-                j.part_ml[(w.slot * NC + k) * 2 + 1] = total;
-            }
-#pragma unroll
-            for (int d = 0; d < 2 * C; ++d) keep_part(j, w.slot, NC, k, DP, d * 16 + g * 4, o[t][d] * u.scale);
-        } else if (at < s.rows * j.group) {
-            const float by = total == 0.f ? 0.f : u.scale / total;
-#pragma unroll
-            for (int d = 0; d < 2 * C; ++d)
-                if (d * 16 + g * 4 < j.c.head_dim)
-                    put4(j, s.row0 + at / j.group, head * j.group + at % j.group, d * 16 + g * 4, o[t][d] * by);
+        const float total = row_sum(st[t].sum), by = parts > 1 ? u.scale : total == 0.f ? 0.f : u.scale / total;
+        const int first_col = (wave * NT + t) * 16;
+        if (parts > 1 && g == 0) {
+            j.part_ml[(w.slot * NC + first_col + n) * 2] = st[t].m;
+            j.part_ml[(w.slot * NC + first_col + n) * 2 + 1] = total;
         }
+#pragma unroll
+        for (int d = 0; d < 2 * C; ++d) *reinterpret_cast<Float4 *>(of_wave + n * (DP + 4) + d * 16 + g * 4) = o[t][d] * by;
+        __syncthreads();
+#pragma unroll 1
+        for (int e = lane; e < 16 * DP / 4; e += 64) {
+            const int c = e / (DP / 4), d = e % (DP / 4) * 4, k = first_col + c, at = tile * NC + k;
+            const Float4 v = *reinterpret_cast<const Float4 *>(of_wave + c * (DP + 4) + d);
+            if (parts > 1) keep_part(j, w.slot, NC, k, DP, d, v);
+            else if (at < s.rows * j.group) put4(j, s.row0 + at / j.group, head * j.group + at % j.group, d, v);
+        }
+        __syncthreads();
     }
 }
 
@@ -821,12 +840,12 @@ __global__ __launch_bounds__(256) void join_kernel(Job j, int rows_each) {
     put4(j, s.row0 + r, qh, lane * 4, all == 0.f ? Float4{0.f, 0.f, 0.f, 0.f} : o / all);
 }
 
-// Of many rows: a wavefront has a row and key / value head, and goes through the query heads.
+// Of many rows: a wavefront has `each` of a row's query heads that share a key / value head.
 template <int C, int NC>
-__global__ __launch_bounds__(256) void join_rows_kernel(Job j) {
-    const int lane = threadIdx.x & 63;
-    const int64_t x = (int64_t)blockIdx.x * 4 + wave_index(), row = x / j.c.kv_heads;
-    const int head = (int)(x % j.c.kv_heads);
+__global__ __launch_bounds__(256) void join_rows_kernel(Job j, int each) {
+    const int lane = threadIdx.x & 63, runs = (j.group + each - 1) / each;
+    const int64_t x = (int64_t)blockIdx.x * 4 + wave_index(), row = x / (j.c.kv_heads * runs);
+    const int in = (int)(x - row * (j.c.kv_heads * runs)), head = in / runs, g0 = in % runs * each;
     if (row >= j.n_rows) return;
     const Plan plan = make_plan<NC>(j, false);
     const Place place = place_of<NC>(j, plan, [&](const Seq &s, int64_t) { return s.rows > 0 && row >= s.row0 && row < s.row0 + s.rows; });
@@ -837,7 +856,7 @@ __global__ __launch_bounds__(256) void join_rows_kernel(Job j) {
     if (parts == 1 || tiles == 0) return;
     const int64_t slot = place.kept_before + head * tiles, stride = (int64_t)tiles * j.c.kv_heads;
     if (slot + tiles + (parts - 1) * stride > j.kept) return;
-    for (int g = 0; g < j.group; ++g) {
+    for (int g = g0; g < min(g0 + each, j.group); ++g) {
         const int index = (int)(row - s.row0) * j.group + g, col = index % NC;
         const float top = top_of_parts<NC>(j, slot + index / NC, stride, col, parts);
         Float4 acc;
@@ -960,7 +979,11 @@ void launch(Job j, const Launches &l, WsCarver &w, hipStream_t st) {
         constexpr int NT = rows_tiles(C);
         take(l.rows);
         attend_rows_kernel<C, NT><<<dim3((unsigned)l.rows.grid), kWaves * 64, 0, st>>>(j);
-        if (l.rows.kept) join_rows_kernel<C, NT * 16 * kWaves><<<dim3((unsigned)cdiv(j.n_rows * j.c.kv_heads, 4)), 256, 0, st>>>(j);
+        if (l.rows.kept) {  // heads one after the other only where there are wavefronts enough all the same
+            const int64_t all = cdiv(j.n_rows * j.q_heads, 4096), each = all < j.group ? all : j.group;
+            const int64_t waves = j.n_rows * j.c.kv_heads * cdiv(j.group, each);
+            join_rows_kernel<C, NT * 16 * kWaves><<<dim3((unsigned)cdiv(waves, 4)), 256, 0, st>>>(j, (int)each);
+        }
     }
     if (l.few.nc) {
         take(l.few);
