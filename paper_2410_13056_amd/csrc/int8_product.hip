@@ -33,13 +33,26 @@ struct Sixteen {
             for (int i = 0; i < 16; ++i) v[i] = i < valid ? p[i] : (T)0.f;
         }
     }
-    __device__ __forceinline__ uint4 codes(float inv) const {
+    __device__ __forceinline__ void look(Largest &l) const {
+#pragma unroll
+        for (int i = 0; i < 16; ++i) l.add((float)v[i]);
+    }
+    __device__ __forceinline__ void look_again(Largest &l) const {
+#pragma unroll
+        for (int i = 0; i < 16; ++i) l.add_finite((float)v[i]);
+    }
+    // `clean`: none is a NaN.
+    __device__ __forceinline__ uint4 codes(float inv, bool clean) const {
         uint32_t w[4];
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-            w[i] = 0;
+            float x[4];
 #pragma unroll
-            for (int j = 0; j < 4; ++j) w[i] |= (uint32_t)(code_of((float)v[4 * i + j], inv) & 255) << (8 * j);
+            for (int k = 0; k < 4; ++k) {
+                x[k] = (float)v[4 * i + k];
+                if (!clean) x[k] = no_nan(x[k]);
+            }
+            w[i] = low_bytes(code_byte<0>(x[0], inv), code_byte<0>(x[1], inv), code_byte<0>(x[2], inv), code_byte<0>(x[3], inv));
         }
         return make_uint4(w[0], w[1], w[2], w[3]);
     }
@@ -62,15 +75,19 @@ __global__ __launch_bounds__(256) void code_rows_kernel(const T *__restrict__ X,
         return;
     }
     const T *x = X + row * ld;
-    float most = 0.f;
-    bool bad = false;
+    Largest largest;
     Sixteen<T> kept[KEPT > 0 ? KEPT : 1];
-    auto look = [&](const Sixteen<T> &s) {
+    auto each = [&](auto fn) {  // fn(sixteen inputs, their number), from registers where they were kept
+        if (KEPT > 0) {
 #pragma unroll
-        for (int i = 0; i < 16; ++i) most = fmaxf(most, finite_abs((float)s.v[i], bad));
-    };
-    auto code = [&](const Sixteen<T> &s, int c, float inv) {
-        *reinterpret_cast<uint4 *>(out + c / 4 * kPiece + c % 4 * 256) = s.codes(inv);
+            for (int k = 0; k < KEPT; ++k)
+                if ((int)threadIdx.x + k * 256 < groups) fn(kept[k], (int)threadIdx.x + k * 256);
+        } else {
+            for (int c = threadIdx.x; c < groups; c += 256) {
+                kept[0].load(x + c * 16, d - c * 16);
+                fn(kept[0], c);
+            }
+        }
     };
     if (KEPT > 0) {
 #pragma unroll
@@ -78,28 +95,21 @@ __global__ __launch_bounds__(256) void code_rows_kernel(const T *__restrict__ X,
             const int c = threadIdx.x + k * 256;
             kept[k].load(x + c * 16, c < groups ? d - c * 16 : 0);
         }
-#pragma unroll
-        for (int k = 0; k < KEPT; ++k) look(kept[k]);
-    } else {
-        for (int c = threadIdx.x; c < groups; c += 256) {
-            kept[0].load(x + c * 16, d - c * 16);
-            look(kept[0]);
-        }
     }
-    most = block_max(most, scratch);
-    const float s = code_scale(most), inv = 1.f / s;
+    each([&](const Sixteen<T> &s, int) { s.look(largest); });
+    const bool bad = __ballot(largest.bad()) != 0;
+    if (bad) {
+        largest.most = 0.f;
+        each([&](const Sixteen<T> &s, int) { s.look_again(largest); });
+        if (status) atomicOr(status, CMPQ_STATUS_NONFINITE);
+    }
+    const float s = code_scale(block_max(largest.most, scratch)), inv = 1.f / s;
     if (threadIdx.x == 0) scale[row] = s;
-    if (bad && status) atomicOr(status, CMPQ_STATUS_NONFINITE);
-    if (KEPT > 0) {
-#pragma unroll
-        for (int k = 0; k < KEPT; ++k)
-            if (threadIdx.x + k * 256 < groups) code(kept[k], threadIdx.x + k * 256, inv);
-    } else {
-        for (int c = threadIdx.x; c < groups; c += 256) {
-            kept[0].load(x + c * 16, d - c * 16);
-            code(kept[0], c, inv);
-        }
-    }
+    auto put = [&](const Sixteen<T> &s, int c, bool clean) {
+        *reinterpret_cast<uint4 *>(out + c / 4 * kPiece + c % 4 * 256) = s.codes(inv, clean);
+    };
+    if (bad) each([&](const Sixteen<T> &s, int c) { put(s, c, false); });
+    else each([&](const Sixteen<T> &s, int c) { put(s, c, true); });
 }
 
 template <typename T>
@@ -256,9 +266,14 @@ __global__ __launch_bounds__(kFewWaves * 64) void few_tokens_kernel(const uint8_
     bool bad = false;
 #pragma unroll
     for (int t = 0; t < M; ++t) {
-        float v = 0.f;
-#pragma unroll
-        for (int i = 0; i < 16; ++i) v = fmaxf(v, finite_abs((float)x[t].v[i], bad));
+        Largest largest;
+        x[t].look(largest);
+        if (__ballot(largest.bad())) {
+            bad = true;
+            largest.most = 0.f;
+            x[t].look_again(largest);
+        }
+        float v = largest.most;
 #pragma unroll
         for (int s = 32; s > 0; s >>= 1) v = fmaxf(v, __shfl_xor(v, s, CMPQ_WAVE));
         if (lane == 0) most[t][wave] = v;
@@ -272,7 +287,7 @@ __global__ __launch_bounds__(kFewWaves * 64) void few_tokens_kernel(const uint8_
         for (int q = 1; q < kFewWaves; ++q) v = fmaxf(v, most[t][q]);
         const float s = code_scale(v), inv = 1.f / s;
         if (threadIdx.x == 0) scales[t] = s;
-        if (c < chunks) *reinterpret_cast<uint4 *>(codes + t * kFewDepth + c * 16) = x[t].codes(inv);
+        if (c < chunks) *reinterpret_cast<uint4 *>(codes + t * kFewDepth + c * 16) = x[t].codes(inv, !bad);
     }
     __syncthreads();
     Int4 acc = {};

@@ -113,16 +113,16 @@ __device__ __forceinline__ void load_item(const cmpq_kv_cache &c, const Page &pg
     }
 }
 
-// Codes of an item's new tokens into the page; the bytes of others stay.
+// Codes of an item's new tokens, none of them NaN, into the page; the bytes of others stay.
 template <bool KEYS>
 __device__ __forceinline__ void store_item(const Page &pg, const Item &it, const float (&x)[4][8], float inv) {
     uint32_t w[8];  // keys: two words a token; values: one a dim
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
-        w[i] = 0;
+        uint32_t b[4];
 #pragma unroll
-        for (int b = 0; b < 4; ++b)
-            w[i] |= (uint32_t)(code_of(KEYS ? x[i / 2][i % 2 * 4 + b] : x[b][i], inv) + 128) << (8 * b);
+        for (int k = 0; k < 4; ++k) b[k] = code_byte<128>(KEYS ? x[i / 2][i % 2 * 4 + k] : x[k][i], inv);
+        w[i] = low_bytes(b[0], b[1], b[2], b[3]);
     }
     if (KEYS) {
 #pragma unroll
@@ -170,7 +170,8 @@ __device__ __forceinline__ void append_page(const cmpq_kv_cache &c, const Page &
     if (threadIdx.x == 0) scratch[THREADS / 64] = pg.from > 0 ? *scale : 0.f;
     const int e0 = pg.from / 4 * octets, e1 = (pg.to + 3) / 4 * octets;
     const bool once = e1 - e0 <= THREADS;
-    float x[4][8], most = 0.f, inv = 0.f;
+    float x[4][8], inv = 0.f;
+    Largest largest;
     bool bad = false;
 #pragma unroll 1
     for (int pass = 0; pass < 2; ++pass) {
@@ -178,11 +179,26 @@ __device__ __forceinline__ void append_page(const cmpq_kv_cache &c, const Page &
             const Item it = item_of<KEYS>(e, octets, chunks, codes);
             if (pass == 0 || !once) load_item<T, KEYS, WHOLE>(c, pg, in, rot, head, it, x);
             if (pass == 0) {
+                Largest here;
 #pragma unroll
                 for (int r = 0; r < 4; ++r)
 #pragma unroll
-                    for (int i = 0; i < 8; ++i) most = fmaxf(most, finite_abs(x[r][i], bad));
+                    for (int i = 0; i < 8; ++i) here.add(x[r][i]);
+                if (__ballot(here.bad())) {
+                    bad = true;
+                    here.most = 0.f;
+#pragma unroll
+                    for (int r = 0; r < 4; ++r)
+#pragma unroll
+                        for (int i = 0; i < 8; ++i) here.add_finite(x[r][i]);
+                }
+                largest.most = fmaxf(largest.most, here.most);
             } else {
+                if (bad)
+#pragma unroll
+                    for (int r = 0; r < 4; ++r)
+#pragma unroll
+                        for (int i = 0; i < 8; ++i) x[r][i] = no_nan(x[r][i]);
                 store_item<KEYS>(pg, it, x, inv);
             }
         }
@@ -190,8 +206,7 @@ __device__ __forceinline__ void append_page(const cmpq_kv_cache &c, const Page &
         if (bad && status) atomicOr(status, CMPQ_STATUS_NONFINITE);
         if (KEYS && rot.cos && threadIdx.x == 0 && status && pg.begin + pg.to > rot.positions)
             atomicOr(status, CMPQ_STATUS_RANGE);
-        most = block_max(most, scratch);
-        const float old = scratch[THREADS / 64], now = fmaxf(old, code_scale(most));
+        const float most = block_max(largest.most, scratch), old = scratch[THREADS / 64], now = fmaxf(old, code_scale(most));
         inv = 1.f / now;
         if (threadIdx.x == 0) *scale = now;
         if (pg.from > 0 && now != old) {

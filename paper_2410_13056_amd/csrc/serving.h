@@ -32,21 +32,34 @@ __device__ __forceinline__ void load_f32(const T *p, float (&x)[N]) {
     for (int i = 0; i < N; ++i) x[i] = (float)v[i];
 }
 
-// |x| where it is finite, else 0; `bad` remembers that one was not.
-__device__ __forceinline__ float finite_abs(float x, bool &bad) {
-    const float a = fabsf(x);
-    const bool fine = a < INFINITY;
-    bad |= !fine;
-    return fine ? a : 0.f;
-}
+// Largest magnitude of values, and whether all were finite.  Two instructions a value; where one was not (bad()), the
+// magnitudes are looked over again and the infinite ones left out.
+struct Largest {
+    float most = 0.f, zero = 0.f;
+    __device__ __forceinline__ void add(float x) {
+        most = fmaxf(most, fabsf(x));
+        zero = fmaf(x, 0.f, zero);  // NaN from the first infinity or NaN on
+    }
+    __device__ __forceinline__ void add_finite(float x) {
+        const float a = fabsf(x);
+        most = a < INFINITY ? fmaxf(most, a) : most;
+    }
+    __device__ __forceinline__ bool bad() const { return !(zero == 0.f); }
+};
 
 __device__ __forceinline__ float code_scale(float most) { return fmaxf(most / 127.f, kSmallestScale); }
 
-// rint(x * inv) within -127..127, NaN to 0.
-__device__ __forceinline__ int code_of(float x, float inv) {
-    const float t = rintf(__builtin_amdgcn_fmed3f(x * inv, -127.f, 127.f));
-    return x == x ? (int)t : 0;
+// x * inv within -127..127, rounded to even, in the low byte (two's complement; OFFSET more): adding 3 * 2^22 rounds and
+// leaves the number there.  x is no NaN.
+template <int OFFSET>
+__device__ __forceinline__ uint32_t code_byte(float x, float inv) {
+    return __float_as_uint(__builtin_amdgcn_fmed3f(x * inv, -127.f, 127.f) + (float)(12582912 + OFFSET));
 }
+// The low bytes of four words next to each other.
+__device__ __forceinline__ uint32_t low_bytes(uint32_t a, uint32_t b, uint32_t c, uint32_t d) {
+    return __builtin_amdgcn_perm(b, a, 0x0c0c0400u) | __builtin_amdgcn_perm(d, c, 0x04000c0cu);
+}
+__device__ __forceinline__ float no_nan(float x) { return x == x ? x : 0.f; }
 
 // Largest of non-negative values over the workgroup, in every lane.  `scratch`: one float a wavefront.  Has barriers.
 __device__ __forceinline__ float block_max(float v, float *scratch) {
