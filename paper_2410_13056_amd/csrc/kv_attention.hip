@@ -585,7 +585,7 @@ __global__ __launch_bounds__(WAVES * 64, WAVES == 8 ? 2 : C * NT <= 4 ? 3 : C * 
 // Many rows.  A workgroup has 16 NT columns a wavefront; it goes through the part's units together, two units of FP16 in
 // LDS, one being read while the next is put there.
 template <int C, int NT>
-__global__ __launch_bounds__(kWaves * 64, 2) void attend_rows_kernel(Job j) {
+__global__ __launch_bounds__(kWaves * 64, NT == 1 && C <= 4 ? 4 : 2) void attend_rows_kernel(Job j) {
     constexpr int NC = 16 * NT * kWaves, DP = C * 32, kHalf = 2 * C * 1024;  // bytes of a unit's keys, or values
     constexpr int kShare = (C + kWaves - 1) / kWaves;                        // pieces that a wavefront brings, of either
     __shared__ __align__(16) float staged[kWaves * 16 * (DP + 4)];  // queries first, then units: a little less
@@ -907,6 +907,12 @@ void size_up(const cmpq_kv_attention_job *a, Kernel &h) {
     }
 }
 
+// Where the kernel for many rows takes all the columns that registers allow: from so many units of such tiles on.  Below, one
+// tile of 16 a wavefront and four wavefronts a SIMD in place of two; us, 48 columns and 16: chunks of 700 rows over
+// 8000 tokens, three of them (180 000 units), 250 and 291, 1000 over 16384 (86 000) 305 and 390, 1024 over 4096 (44 000) 226 and
+// 200, 256 over 8192 (22 500) 118 and 121, 512 over 512 of 32 heads (1500) 43 and 24.
+constexpr int64_t kManyUnits = 50000;
+
 Launches plan_launches(const cmpq_kv_attention_job *a) {
     Launches l;
     const int64_t c = cdiv(a->cache.head_dim, 32), group = a->q_heads / a->cache.kv_heads, cols = a->max_rows * group;
@@ -925,6 +931,7 @@ Launches plan_launches(const cmpq_kv_attention_job *a) {
         l.rows.nc = 16 * kWaves * rows_tiles(c);
         l.rows.least_cols = l.few.most_cols > 0 ? l.few.most_cols + 1 : 1;
         l.rows.most_cols = INT64_MAX;
+        if (most_tiles(a, l.rows) * most_units(a) < kManyUnits) l.rows.nc = 16 * kWaves;
     }
     l.few.target = 1024, l.few.least = 8;
     // Short sequences in one part, by 8 wavefronts where that leaves compute units free: a part more costs the launch that
@@ -933,7 +940,7 @@ Launches plan_launches(const cmpq_kv_attention_job *a) {
         l.few.least = 64;
         l.few.wide = most_tiles(a, l.few) < 512;
     }
-    l.rows.target = 512, l.rows.least = 16;
+    l.rows.target = l.rows.nc == 16 * kWaves && c <= 4 ? 1024 : 512, l.rows.least = 16;
     if (l.few.nc) size_up(a, l.few);
     if (l.rows.nc) size_up(a, l.rows);
     return l;
@@ -968,6 +975,16 @@ void launch_few(const Job &j, const Kernel &h, hipStream_t st) {
     else join_kernel<C, NT * 16, 1><<<dim3((unsigned)cdiv(items, 4)), 256, 0, st>>>(j, (int)each);
 }
 
+template <int C, int NT>
+void launch_rows(const Job &j, const Kernel &h, hipStream_t st) {
+    attend_rows_kernel<C, NT><<<dim3((unsigned)h.grid), kWaves * 64, 0, st>>>(j);
+    if (!h.kept) return;
+    // heads one after the other only where there are wavefronts enough all the same
+    const int64_t all = cdiv(j.n_rows * j.q_heads, 4096), each = all < j.group ? all : j.group;
+    const int64_t waves = j.n_rows * j.c.kv_heads * cdiv(j.group, each);
+    join_rows_kernel<C, NT * 16 * kWaves><<<dim3((unsigned)cdiv(waves, 4)), 256, 0, st>>>(j, (int)each);
+}
+
 template <int C>
 void launch(Job j, const Launches &l, WsCarver &w, hipStream_t st) {
     auto take = [&](const Kernel &h) {
@@ -976,14 +993,9 @@ void launch(Job j, const Launches &l, WsCarver &w, hipStream_t st) {
         j.part_ml = w.take<float>(l.ml_floats(h));
     };
     if (l.rows.nc) {
-        constexpr int NT = rows_tiles(C);
         take(l.rows);
-        attend_rows_kernel<C, NT><<<dim3((unsigned)l.rows.grid), kWaves * 64, 0, st>>>(j);
-        if (l.rows.kept) {  // heads one after the other only where there are wavefronts enough all the same
-            const int64_t all = cdiv(j.n_rows * j.q_heads, 4096), each = all < j.group ? all : j.group;
-            const int64_t waves = j.n_rows * j.c.kv_heads * cdiv(j.group, each);
-            join_rows_kernel<C, NT * 16 * kWaves><<<dim3((unsigned)cdiv(waves, 4)), 256, 0, st>>>(j, (int)each);
-        }
+        if (l.rows.nc == 16 * kWaves) launch_rows<C, 1>(j, l.rows, st);
+        else if constexpr (rows_tiles(C) > 1) launch_rows<C, rows_tiles(C)>(j, l.rows, st);
     }
     if (l.few.nc) {
         take(l.few);
