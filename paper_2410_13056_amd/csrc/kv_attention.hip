@@ -92,7 +92,7 @@ __device__ __forceinline__ Plan make_plan(const Job &j, bool look) {
         total += (double)s.units * tiles_of<NC>(j, s);
         pieces += (double)tiles_of<NC>(j, s);
     }
-    // every sequence's last part is a short one, so that many workgroups are left over for them
+    // a sequence's parts are rounded up: up to one workgroup a piece more than its share
     const double all = __shfl(wave_sum_f64(total), 0) * j.c.kv_heads, odd = __shfl(wave_sum_f64(pieces), 0) * j.c.kv_heads;
     Plan p;
     p.step = __builtin_amdgcn_readfirstlane(max(j.least, (int)ceil(all / max((double)j.target - odd, 0.5 * j.target))));
@@ -907,11 +907,17 @@ void size_up(const cmpq_kv_attention_job *a, Kernel &h) {
     }
 }
 
-// Where the kernel for many rows takes all the columns that registers allow: from so many units of such tiles on.  Below, one
-// tile of 16 a wavefront and four wavefronts a SIMD in place of two; us, 48 columns and 16: chunks of 700 rows over
-// 8000 tokens, three of them (180 000 units), 250 and 291, 1000 over 16384 (86 000) 305 and 390, 1024 over 4096 (44 000) 226 and
-// 200, 256 over 8192 (22 500) 118 and 121, 512 over 512 of 32 heads (1500) 43 and 24.
+// Where the kernel for many rows takes all the columns that registers allow: from so many units of such tiles on.  Below,
+// one tile of 16 a wavefront and four wavefronts a SIMD in place of two.  us, 48 columns and 16: 1000 rows over 16384
+// tokens, heads 4 to 1 (86 000 units), 305 and 390; 1024 over 4096, 8 to 1 (44 000), 226 and 200; 512 over 512 of 32 heads
+// (1500) 43 and 24.
 constexpr int64_t kManyUnits = 50000;
+
+// Where sequences of single rows among ones of many have the kernel for few rows: from so many units of theirs on.  Below, its
+// two launches cost more than it saves.  us, with it and without: a sequence of 3000 tokens beside 700 rows (750 units)
+// 133 and 119, 8 of up to 4096 beside 8 chunks (15 000) 118 and 107, 16 beside 16 (32 000) 134 and 165, 16 of up to 8192
+// beside 16 of 64 rows (63 000) 156 and 225.
+constexpr int64_t kApartUnits = 20000;
 
 Launches plan_launches(const cmpq_kv_attention_job *a) {
     Launches l;
@@ -922,7 +928,7 @@ Launches plan_launches(const cmpq_kv_attention_job *a) {
         l.few.nc = (int)cdiv(cols, 16) * 16;
         l.few.least_cols = 1;
         l.few.most_cols = few;
-    } else if (a->n_seq > 1 && group <= few) {  // single rows among sequences of many
+    } else if (group <= few && (a->n_seq - 1) * a->cache.kv_heads * most_units(a) >= kApartUnits) {
         l.few.nc = (int)cdiv(group, 16) * 16;
         l.few.least_cols = 1;
         l.few.most_cols = l.few.nc;

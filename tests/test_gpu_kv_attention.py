@@ -377,3 +377,44 @@ def test_attention_block_runs_the_operators_together(S):
         want = np.concatenate(parts).reshape(sum(new), -1) @ W["o"].double().cpu().numpy().T
         rel = np.linalg.norm(got.double().cpu().numpy() - want) / np.linalg.norm(want)
         assert rel <= 2.0 ** -9
+
+
+class Bounded(Setup):
+    """Calls with a bound on the lengths far above them: the work is cut up as for long sequences."""
+
+    def run(self, Q, rows, ws=None, **kw):
+        from paper_2410_13056_amd import binding as B
+        cu = _i32([0] + list(np.cumsum(rows)))
+        return self.S.kv_attention(self.cache, Q, self.table, _i32(self.tokens), cu, max(rows), 1 << 26, ws or B.Workspace(DEV), **kw)
+
+
+@pytest.mark.parametrize("dim", [1, 32, 40, 64, 96, 128, 160, 192, 224, 256])
+@pytest.mark.parametrize("rows,tokens", [([150], [700]), ([3, 90, 1, 17], [3, 130, 700, 65])])
+def test_dims_cut_up_as_for_long_sequences(S, dim, rows, tokens):
+    _check(S, Bounded(S, tokens, 2, dim, 32, dim + 1), rows, 6, torch.float16, dim,
+           rotation=S.make_rotation(max(tokens), dim // 2 * 2, device=DEV) if dim > 1 else None)
+
+
+@pytest.mark.parametrize("group,kv", [(1, 3), (5, 2), (8, 1), (16, 1), (17, 1), (49, 1)])
+def test_groups_cut_up_as_for_long_sequences(S, group, kv):
+    _check(S, Bounded(S, [200, 33, 64, 95, 0], kv, 64, 32, group), [77, 1, 2, 60, 3], group * kv, torch.float16, group)
+
+
+@pytest.mark.parametrize("causal", [True, False])
+@pytest.mark.parametrize("window", [0, 1 << 24])
+@pytest.mark.parametrize("tokens", [1, 31, 32, 33, 63, 64, 65, 2049])
+def test_lengths_cut_up_as_for_long_sequences(S, causal, window, tokens):
+    _check(S, Bounded(S, [tokens, 1, tokens], 2, 128, 64, tokens), [min(100, tokens), 1, 1], 8, torch.bfloat16, causal=causal,
+           window=window)
+
+
+def test_long_sequences_of_many_rows_beside_single_ones(S):
+    tokens = [9000, 5, 400, 7000, 33, 2000]
+    _check(S, Bounded(S, tokens, 3, 128, 64, 5), [200, 1, 4, 1, 33, 64], 12, torch.bfloat16, 2,
+           rotation=S.make_rotation(9000, 128, device=DEV))
+
+
+def test_many_sequences_cut_up_as_for_long_ones(S):
+    rng = np.random.default_rng(8)
+    tokens, rows = rng.integers(0, 400, 130).tolist(), [int(rng.choice([0, 1, 1, 2, 70])) for _ in range(130)]
+    _check(S, Bounded(S, tokens, 1, 32, 32, 9), rows, 2, torch.float16, 4)
