@@ -651,7 +651,8 @@ int cmpq_int8_prepare(const void *W, int dtype, int64_t d_out, int64_t d_in, int
 /*
  * Y[t,o] = (sum_i cx[t,i] * cw[o,i]) * sx[t] * sw[o]: X [m, d_in] (ldx) is coded with a scale per token on the
  * way, the sum is exact, its fp32 value is multiplied by the smaller scale, then by the larger (so that nothing
- * on the way leaves the range that the result is in), and rounded once more to y_dtype.  Y [m, d_out] (ldy).  codes, scale: from cmpq_int8_prepare.
+ * on the way leaves the range that the result is in), and rounded once more to y_dtype.  Y [m, d_out] (ldy).
+ * codes, scale: from cmpq_int8_prepare.
  * Workspace: CMPQ_OP_INT8_PRODUCT with n = m.  Limits: m < 2^24 and those of cmpq_int8_prepare.
  */
 int cmpq_int8_product(const void *X, int dtype, int64_t m, int64_t d_in, int64_t ldx, const int8_t *codes,
@@ -738,9 +739,11 @@ int cmpq_kv_read(const cmpq_kv_cache *cache, const cmpq_kv_rows *rows, const cmp
  *   Q  [n_rows, q_heads, head_dim] of q_dtype;  O  [n_rows, q_heads, head_dim] of o_dtype, CMPQ_F16 or CMPQ_BF16.
  *   max_rows, max_length  host bounds of the rows and the length of any sequence: rows beyond are not
  *       written, tokens beyond are left out, and either raises CMPQ_STATUS_RANGE.
- * Logits, their maximum, the weights' sum and the output are held in fp32; queries (scaled by a power of two per
- * row) and weights are rounded to FP16 for the matrix instruction, codes are exact in it.  The order of all
- * additions depends on sizes and lengths alone: results are reproducible bit for bit.
+ * Logits, their maximum, the weights' sum and the output are held in fp32.  A turned query is rounded to 16 bits fixed
+ * point of its row's largest magnitude, its products with codes are exact; weights are rounded to FP16 for their products
+ * with the values; a page's value scale below 2^-60 of a sequence's largest so far counts as that.  A query that holds
+ * a NaN or an infinity gives NaN for its row and head alone.  The order of all additions depends on sizes, lengths and
+ * the host bounds alone: results are reproducible bit for bit.
  * Workspace: cmpq_kv_attention_workspace(job) (a function of the sizes, not of the pointers).
  */
 typedef struct cmpq_kv_attention_job {

@@ -6,9 +6,16 @@
 // codes are stored in the order of the instructions' operands, 16 bytes a lane and 1 KB a load.  A page's key scale
 // multiplies its logits, its value scale goes into its weights' exponent.
 //
-// Two kernels.  For few rows (attend_kernel) the cache's bytes are what counts: the wavefronts of a workgroup share the tokens
-// and read codes straight from memory.  For many rows (attend_rows_kernel) multiplications and exponentials count: the
-// wavefronts share the rows, and codes become FP16 once a workgroup, on their way into LDS.
+// A row's weights are held against its reference, a running maximum that moves only when a logit passes it by a factor
+// of 2^8, so that sums and outputs are rarely multiplied again; what it is cancels in the quotient.
+//
+// Two kernels.  For few rows (attend_kernel) the cache's bytes are what counts: the wavefronts of a workgroup share the
+// tokens and read codes straight from memory.  For many rows (attend_rows_kernel) multiplications and exponentials
+// count: the wavefronts share the rows, and a workgroup's codes go through LDS.  A long sequence's units are cut into parts,
+// which a second launch joins.
+//
+// Roundings: queries to 16 bits fixed point (fixed_query), their products with codes exact; weights to FP16 for the matrix
+// instruction (their sum is taken before, in fp32); the output once to its type.  All else is fp32.
 #include "serving.h"
 
 namespace {
@@ -294,6 +301,33 @@ __device__ __forceinline__ int take_query(const float *from, float (&x)[C][8], f
     return e;
 }
 
+// A staged row for the integer matrix instruction: 16 bits fixed point of the row's largest magnitude, 256 high + low, and
+// what turns its products with codes into logits in base 2 (never below 0: the sign of softmax_scale goes into the
+// row).  Keys then need no conversion, and two instructions of 64 dims do what two of 32 in FP16 would.  An element is
+// off by at most 2^-16 of the row's largest, less than FP16 rounds the larger half of them by.
+template <int C>
+__device__ __forceinline__ float fixed_query(const float *from, float scale, bool seen, Int4 (&high)[(C + 1) / 2],
+                                             Int4 (&low)[(C + 1) / 2]) {
+    float v[C][8], top;
+    const int e = take_query<C>(from, v, top);
+    const float sign = scale < 0.f ? -1.f : 1.f, to = top > 0.f ? sign * 32639.f / top : 0.f;  // NaN: 0
+#pragma unroll
+    for (int c = 0; c < (C + 1) / 2 * 2; ++c) {
+        uint32_t h[2] = {0, 0}, l[2] = {0, 0};
+        if (c < C) {
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                const int q = (int)rintf(v[c < C ? c : 0][i] * to), up = (q + 128) >> 8;
+                h[i >> 2] |= (uint32_t)(up & 255) << (8 * (i & 3));
+                l[i >> 2] |= (uint32_t)((q - 256 * up) & 255) << (8 * (i & 3));
+            }
+        }
+        high[c / 2][c % 2 * 2] = (int)h[0], high[c / 2][c % 2 * 2 + 1] = (int)h[1];
+        low[c / 2][c % 2 * 2] = (int)l[0], low[c / 2][c % 2 * 2 + 1] = (int)l[1];
+    }
+    return seen ? ldexpf(top * (1.f / 32639.f) * (sign * scale * kLog2e), e) : 0.f;
+}
+
 // The page of a unit of a sequence, -1 if the table names none, and its scales.
 struct PageOf {
     int id, in_page;
@@ -389,8 +423,10 @@ __device__ __forceinline__ void keep_part(const Job &j, int64_t slot, int nc, in
 }
 
 // Few rows.  C: 32 dims each of a head.  Tiles of 16 NT columns, one (row, query head) pair each; the wavefronts take the
-// part's units in turn and are added up through LDS.  Keys go into the integer matrix instruction as they are; a query
-// is held in 16 bits fixed point, 256 high + low, of its row's largest magnitude, two instructions for one.
+// part's units in turn and are added up through LDS.  Bound by the cache's bytes: 64 sequences of one row, 184 000 tokens,
+// 8 heads of 128 dims in 76 us, 2 sequences of 172 000 tokens in 75 us (4.9 and 4.7 TB/s; a large copy reaches 4.8).  Where there
+// is little to read, by what comes one after the other: 11 us for 777 tokens of 32 heads.  Hence codes straight
+// into registers a unit ahead, no barrier before the last unit, and the pages' numbers 64 at a time.
 template <int C, int NT, int WAVES>
 __global__ __launch_bounds__(WAVES * 64, WAVES == 8 ? 2 : C * NT <= 4 ? 3 : C * NT <= 8 ? 2 : 1) void attend_kernel(Job j) {
     constexpr int NC = 16 * NT, DP = C * 32, kPad = DP + 4;
@@ -434,24 +470,7 @@ __global__ __launch_bounds__(WAVES * 64, WAVES == 8 ? 2 : C * NT <= 4 ? 3 : C * 
     for (int t = 0; t < NT; ++t) {
         const Column col = column(j, s, head, tile * NC + t * 16 + n);
         lo[t] = col.lo, hi[t] = col.hi;
-        float v[C][8], top;
-        const int e = take_query<C>(red + t * 16 * kPad, v, top);
-        const float sign = j.scale < 0.f ? -1.f : 1.f, to = top > 0.f ? sign * 32639.f / top : 0.f;  // NaN: 0
-        factor[t] = col.lo < col.hi ? ldexpf(top * (1.f / 32639.f) * (sign * j.scale * kLog2e), e) : 0.f;  // not below 0
-#pragma unroll
-        for (int c = 0; c < (C + 1) / 2 * 2; ++c) {
-            uint32_t h[2] = {0, 0}, l[2] = {0, 0};
-            if (c < C) {
-#pragma unroll
-                for (int i = 0; i < 8; ++i) {
-                    const int q = (int)rintf(v[c < C ? c : 0][i] * to), high = (q + 128) >> 8;
-                    h[i >> 2] |= (uint32_t)(high & 255) << (8 * (i & 3));
-                    l[i >> 2] |= (uint32_t)((q - 256 * high) & 255) << (8 * (i & 3));
-                }
-            }
-            qh[t][c / 2][c % 2 * 2] = (int)h[0], qh[t][c / 2][c % 2 * 2 + 1] = (int)h[1];
-            ql[t][c / 2][c % 2 * 2] = (int)l[0], ql[t][c / 2][c % 2 * 2 + 1] = (int)l[1];
-        }
+        factor[t] = fixed_query<C>(red + t * 16 * kPad, j.scale, col.lo < col.hi, qh[t], ql[t]);
     }
     // bounds over the tile's columns: rows grow with the column
     const int all_hi = __builtin_amdgcn_readlane(hi[0], 0), all_lo = __builtin_amdgcn_readlane(lo[NT - 1], 15);
@@ -582,16 +601,21 @@ __global__ __launch_bounds__(WAVES * 64, WAVES == 8 ? 2 : C * NT <= 4 ? 3 : C * 
     }
 }
 
-// Many rows.  A workgroup has 16 NT columns a wavefront; it goes through the part's units together, two units of FP16 in
-// LDS, one being read while the next is put there.
+// Many rows.  A workgroup has 16 NT columns a wavefront; it goes through the part's units together, two units in LDS
+// (keys as bytes, values as FP16, converted once a workgroup), one being read while the next is put there.  Bound by
+// issue: of a unit's 32 x 16 weights at 128 dims the matrix instructions take 280 clocks, all else some 250 (a conversion, a
+// shift, a fused multiplication, an exponential, half a rounding to FP16 and an addition each), and the wavefronts of a SIMD
+// overlap the two in part.  758 rows of 64 heads over 12 000 tokens 250 us, 0.72 PFLOP/s.  Queries in FP16 would save
+// the shift and the conversion (235 us) at twice the rounding errors in the output (4.3e-4 of it, 2.8e-4 now).
 template <int C, int NT>
 __global__ __launch_bounds__(kWaves * 64, NT == 1 && C <= 4 ? 4 : 2) void attend_rows_kernel(Job j) {
-    constexpr int NC = 16 * NT * kWaves, DP = C * 32, kHalf = 2 * C * 1024;  // bytes of a unit's keys, or values
+    constexpr int NC = 16 * NT * kWaves, DP = C * 32, H = (C + 1) / 2;
+    constexpr int kKeys = 2 * H * 1024, kUnitBytes = kKeys + 2 * C * 1024;  // of a unit's keys, with its values
     constexpr int kShare = (C + kWaves - 1) / kWaves;                        // pieces that a wavefront brings, of either
     __shared__ __align__(16) float staged[kWaves * 16 * (DP + 4)];  // queries first, then units: a little less
-    static_assert(sizeof(staged) >= 4 * kHalf, "two units");
+    static_assert(sizeof(staged) >= 2 * kUnitBytes, "two units");
     const int lane = threadIdx.x & 63, wave = wave_index(), n = lane & 15, g = lane >> 4;
-    auto unit_at = [&](int buf) { return reinterpret_cast<Half8 *>(staged) + buf * (2 * kHalf / 16) + lane; };
+    auto unit_at = [&](int buf) { return reinterpret_cast<uint8_t *>(staged) + buf * kUnitBytes + lane * 16; };
     float *const of_wave = staged + wave * 16 * (DP + 4);
     const Plan plan = make_plan<NC>(j, blockIdx.x == 0 && wave == 0);
     Share w;
@@ -626,16 +650,17 @@ __global__ __launch_bounds__(kWaves * 64, NT == 1 && C <= 4 ? 4 : 2) void attend
         for (int k = 0; k < kShare; ++k) {
             const int c = wave + k * kWaves;
             if (c >= C) break;
-            Half8 *to = unit_at(buf) + c * 128;
-            to[0] = halves(kc[k].x, kc[k].y);
-            to[64] = halves(kc[k].z, kc[k].w);
-            to[kHalf / 16] = halves(vc[k].x, vc[k].y);
-            to[kHalf / 16 + 64] = halves(vc[k].z, vc[k].w);
+            constexpr uint32_t flip = 0x80808080u;  // code + 128 to the code's own byte
+            uint8_t *keys = unit_at(buf) + c / 2 * 2048 + c % 2 * 8, *values = unit_at(buf) + kKeys + c * 2048;
+            *reinterpret_cast<uint2 *>(keys) = make_uint2(kc[k].x ^ flip, kc[k].y ^ flip);
+            *reinterpret_cast<uint2 *>(keys + 1024) = make_uint2(kc[k].z ^ flip, kc[k].w ^ flip);
+            *reinterpret_cast<Half8 *>(values) = halves(vc[k].x, vc[k].y);
+            *reinterpret_cast<Half8 *>(values + 1024) = halves(vc[k].z, vc[k].w);
         }
     };
     if (u0 < u1) load(u0);  // on its way while the queries come
 
-    Half8 q[NT][C];
+    Int4 qh[NT][H], ql[NT][H];
     float factor[NT];
     int lo[NT], hi[NT];
 #pragma unroll 1
@@ -644,21 +669,15 @@ __global__ __launch_bounds__(kWaves * 64, NT == 1 && C <= 4 ? 4 : 2) void attend
         const Column col = column(j, s, head, index + n);
         stage_queries<C>(j, s, head, index, 16, of_wave, lane, 64);
         __syncthreads();
-        float v[C][8], top;
-        const int e = take_query<C>(of_wave, v, top);
-        const float sign = j.scale < 0.f ? -1.f : 1.f;
-        Half8 h[C];
-#pragma unroll
-        for (int c = 0; c < C; ++c)
-#pragma unroll
-            for (int i = 0; i < 8; ++i) h[c][i] = (_Float16)(sign * v[c][i]);
+        Int4 high[H], low[H];
+        const float f = fixed_query<C>(of_wave, j.scale, col.lo < col.hi, high, low);
 #pragma unroll
         for (int t = 0; t < NT; ++t) {
             if (t != tt) continue;
             lo[t] = col.lo, hi[t] = col.hi;
-            factor[t] = ldexpf(sign * j.scale * kLog2e, e);  // not below 0
+            factor[t] = f;
 #pragma unroll
-            for (int c = 0; c < C; ++c) q[t][c] = h[c];
+            for (int c = 0; c < H; ++c) qh[t][c] = high[c], ql[t][c] = low[c];
         }
         __syncthreads();
     }
@@ -673,6 +692,10 @@ __global__ __launch_bounds__(kWaves * 64, NT == 1 && C <= 4 ? 4 : 2) void attend
         for (int d = 0; d < 2 * C; ++d) o[t][d] = Float4{0.f, 0.f, 0.f, 0.f};
     }
     UnitScale u = {0.f, 0.f};
+    if (C % 2 && wave == 0)  // no dims there: zeros, though the queries are zeros as well
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+            *reinterpret_cast<uint2 *>(unit_at(i / 2) + C / 2 * 2048 + 8 + i % 2 * 1024) = make_uint2(0, 0);
     if (u0 < u1) {
         store(0);
         mine = ahead;
@@ -685,29 +708,37 @@ __global__ __launch_bounds__(kWaves * 64, NT == 1 && C <= 4 ? 4 : 2) void attend
         const float kscale = lane_value(mine.ks, i), vscale = lane_value(mine.vs, i);
         if (unit + 1 < u1) store(buf ^ 1);
         if (unit + 2 < u1) load(unit + 2);
-        const Half8 *from = unit_at(buf);
+        const uint8_t *from = unit_at(buf);
         __builtin_amdgcn_s_setprio(1);
-        Float4 sum[NT][2];
+        float l[NT][8], top[NT];
 #pragma unroll
-        for (int t = 0; t < NT; ++t) sum[t][0] = sum[t][1] = Float4{0.f, 0.f, 0.f, 0.f};
+        for (int h = 0; h < 2; ++h) {
+            Int4 k[H], sum[NT];
 #pragma unroll
-        for (int c = 0; c < C; ++c) {
-            const Half8 k0 = from[c * 128], k1 = from[c * 128 + 64];
+            for (int c = 0; c < H; ++c) k[c] = *reinterpret_cast<const Int4 *>(from + c * 2048 + h * 1024);
 #pragma unroll
             for (int t = 0; t < NT; ++t) {
-                sum[t][0] = __builtin_amdgcn_mfma_f32_16x16x32_f16(k0, q[t][c], sum[t][0], 0, 0, 0);
-                sum[t][1] = __builtin_amdgcn_mfma_f32_16x16x32_f16(k1, q[t][c], sum[t][1], 0, 0, 0);
+                sum[t] = Int4{0, 0, 0, 0};
+#pragma unroll
+                for (int c = 0; c < H; ++c) sum[t] = __builtin_amdgcn_mfma_i32_16x16x64_i8(k[c], qh[t][c], sum[t], 0, 0, 0);
             }
+#pragma unroll
+            for (int t = 0; t < NT; ++t) {
+                sum[t] *= 256;
+#pragma unroll
+                for (int c = 0; c < H; ++c) sum[t] = __builtin_amdgcn_mfma_i32_16x16x64_i8(k[c], ql[t][c], sum[t], 0, 0, 0);
+            }
+#pragma unroll
+            for (int t = 0; t < NT; ++t)
+#pragma unroll
+                for (int r = 0; r < 4; ++r) l[t][h * 4 + r] = (float)sum[t][r];
         }
         __builtin_amdgcn_s_setprio(0);
-        float l[NT][8], top[NT];
         const int t0 = unit * kUnit;
         const bool edge = !there || t0 < all_lo || t0 + kUnit > all_hi;
         bool past = there && vscale > u.scale;
 #pragma unroll
         for (int t = 0; t < NT; ++t) {
-#pragma unroll
-            for (int r = 0; r < 8; ++r) l[t][r] = sum[t][r >> 2][r & 3];
             if (edge) {
 #pragma unroll
                 for (int r = 0; r < 8; ++r) {
@@ -730,7 +761,8 @@ __global__ __launch_bounds__(kWaves * 64, NT == 1 && C <= 4 ? 4 : 2) void attend
         }
 #pragma unroll
         for (int c = 0; c < C; ++c) {
-            const Half8 v0 = from[kHalf / 16 + c * 128], v1 = from[kHalf / 16 + c * 128 + 64];
+            const Half8 *of = reinterpret_cast<const Half8 *>(from + kKeys + c * 2048);
+            const Half8 v0 = of[0], v1 = of[64];
 #pragma unroll
             for (int t = 0; t < NT; ++t) {
                 o[t][2 * c] = __builtin_amdgcn_mfma_f32_16x16x32_f16(v0, p[t], o[t][2 * c], 0, 0, 0);
@@ -879,8 +911,10 @@ struct Launches {
     size_t ml_floats(const Kernel &h) const { return (size_t)(h.kept * h.nc * 2); }
 };
 
-// Tiles of 16 columns a wavefront of the kernel for many rows, as registers allow.
-constexpr int rows_tiles(int64_t c) { return c <= 2 ? 4 : c <= 4 ? 3 : c <= 6 ? 2 : 1; }
+// Tiles of 16 columns a wavefront of the kernel for many rows has at most.  Heads of up to 64 and of more than 128 dims are as
+// fast or faster with one (us, 1000 rows of 32 heads, 4 to 1: 64 dims, 16384 tokens, 4 tiles 310 and one 299; 192
+// dims, 8000 tokens, 2 tiles 331 and one 292).
+constexpr int rows_tiles(int64_t c) { return c == 3 || c == 4 ? 3 : 1; }
 
 // Units that a sequence's rows see at most.
 int64_t most_units(const cmpq_kv_attention_job *a) {
@@ -907,10 +941,9 @@ void size_up(const cmpq_kv_attention_job *a, Kernel &h) {
     }
 }
 
-// Where the kernel for many rows takes all the columns that registers allow: from so many units of such tiles on.  Below,
-// one tile of 16 a wavefront and four wavefronts a SIMD in place of two.  us, 48 columns and 16: 1000 rows over 16384
-// tokens, heads 4 to 1 (86 000 units), 305 and 390; 1024 over 4096, 8 to 1 (44 000), 226 and 200; 512 over 512 of 32 heads
-// (1500) 43 and 24.
+// Where the kernel for many rows takes those tiles: from so many units of theirs on.  Below, one a wavefront and four
+// wavefronts a SIMD in place of two.  us, three tiles and one, heads of 128 dims: 1000 rows over 16384 tokens, 4 to 1 (86 000
+// units), 320 and 385; 1024 over 4096, 8 to 1 (44 000), 239 and 200; 2048 over 2048 of 32 heads (22 500) 164 and 133.
 constexpr int64_t kManyUnits = 50000;
 
 // Where sequences of single rows among ones of many have the kernel for few rows: from so many units of theirs on.  Below, its
@@ -946,7 +979,8 @@ Launches plan_launches(const cmpq_kv_attention_job *a) {
         l.few.least = 64;
         l.few.wide = most_tiles(a, l.few) < 512;
     }
-    l.rows.target = l.rows.nc == 16 * kWaves && c <= 4 ? 1024 : 512, l.rows.least = 16;
+    l.rows.target = l.rows.nc == 16 * kWaves && c <= 4 ? 1024 : 512;  // workgroups that run at once
+    l.rows.least = 16;
     if (l.few.nc) size_up(a, l.few);
     if (l.rows.nc) size_up(a, l.rows);
     return l;
