@@ -113,10 +113,9 @@ __device__ __forceinline__ void load_item(const cmpq_kv_cache &c, const Page &pg
     }
 }
 
-// Codes of an item's new tokens, none of them NaN, into the page; the bytes of others stay.
+// Codes of an item, none of them NaN: for keys two words a token, for values one a dim.
 template <bool KEYS>
-__device__ __forceinline__ void store_item(const Page &pg, const Item &it, const float (&x)[4][8], float inv) {
-    uint32_t w[8];  // keys: two words a token; values: one a dim
+__device__ __forceinline__ void code_item(const float (&x)[4][8], float inv, uint32_t (&w)[8]) {
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
         uint32_t b[4];
@@ -124,6 +123,25 @@ __device__ __forceinline__ void store_item(const Page &pg, const Item &it, const
         for (int k = 0; k < 4; ++k) b[k] = code_byte<128>(KEYS ? x[i / 2][i % 2 * 4 + k] : x[k][i], inv);
         w[i] = low_bytes(b[0], b[1], b[2], b[3]);
     }
+}
+
+// Where byte `at` of staged codes lies in LDS: 16 bytes stay together, other lanes' of one instruction go to other banks.
+__device__ __forceinline__ int staged_at(int at) { return at ^ (at >> 4 & 0xf0); }
+
+template <bool KEYS>
+__device__ __forceinline__ void stage_item(uint8_t *staged, int at, const uint32_t (&w)[8]) {
+    if (KEYS) {
+#pragma unroll
+        for (int r = 0; r < 4; ++r) *reinterpret_cast<uint2 *>(staged + staged_at(at + r * 16)) = make_uint2(w[2 * r], w[2 * r + 1]);
+    } else {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) *reinterpret_cast<uint32_t *>(staged + staged_at(at + i * 16)) = w[i];
+    }
+}
+
+// Codes of an item's new tokens into the page; the bytes of others stay.
+template <bool KEYS>
+__device__ __forceinline__ void store_item(const Page &pg, const Item &it, const uint32_t (&w)[8]) {
     if (KEYS) {
 #pragma unroll
         for (int r = 0; r < 4; ++r)
@@ -160,47 +178,73 @@ __device__ __forceinline__ void hold_item(const Page &pg, const Item &it, float 
     }
 }
 
-// The new values are read once where each lane has at most one item, else again for their codes.
+// Blocks of 32 tokens that a workgroup takes at once, one item a lane.
+template <int THREADS>
+__device__ __forceinline__ int blocks_at_once(int chunks) {
+    return max(1, THREADS / (32 * chunks));
+}
+
+// The new values are read once where each lane has at most one item, else again for their codes.  Codes of whole blocks of 32
+// tokens go out through LDS, 1 KB in order a wavefront; written from the lanes that make them, 4 or 8 bytes each, they
+// would take up a line of the cache behind each time.
 template <typename T, bool KEYS, bool WHOLE, int THREADS>
 __device__ __forceinline__ void append_page(const cmpq_kv_cache &c, const Page &pg, int64_t id, int head, const cmpq_heads &in,
-                            const cmpq_rotation &rot, int32_t *status, float *scratch) {
-    const int chunks = (c.head_dim + 31) / 32, octets = chunks * 4;
+                                            const cmpq_rotation &rot, int32_t *status, float *scratch, uint8_t *staged) {
+    constexpr bool kStaged = THREADS == 256;
+    const int chunks = (c.head_dim + 31) / 32, octets = chunks * 4, block_items = chunks * 32, block_bytes = chunks * 1024;
     uint8_t *codes = (KEYS ? c.k_codes : c.v_codes) + (id * c.kv_heads + head) * (int64_t)(c.page * chunks * 32);
     float *scale = (KEYS ? c.k_scale : c.v_scale) + id * c.kv_heads + head;
     if (threadIdx.x == 0) scratch[THREADS / 64] = pg.from > 0 ? *scale : 0.f;
-    const int e0 = pg.from / 4 * octets, e1 = (pg.to + 3) / 4 * octets;
-    const bool once = e1 - e0 <= THREADS;
+    const int step = kStaged ? blocks_at_once<THREADS>(chunks) * block_items : THREADS;
+    const int start = kStaged ? pg.from / 32 * block_items : pg.from / 4 * octets, e0 = pg.from / 4 * octets;
+    const int e1 = (pg.to + 3) / 4 * octets;
+    const bool once = e1 - start <= step;
+    auto whole = [&](int block) { return block * 32 >= pg.from && block * 32 + 32 <= pg.to; };
     float x[4][8], inv = 0.f;
     Largest largest;
     bool bad = false;
 #pragma unroll 1
     for (int pass = 0; pass < 2; ++pass) {
-        for (int e = e0 + threadIdx.x; e < e1; e += THREADS) {
-            const Item it = item_of<KEYS>(e, octets, chunks, codes);
-            if (pass == 0 || !once) load_item<T, KEYS, WHOLE>(c, pg, in, rot, head, it, x);
-            if (pass == 0) {
-                Largest here;
-#pragma unroll
-                for (int r = 0; r < 4; ++r)
-#pragma unroll
-                    for (int i = 0; i < 8; ++i) here.add(x[r][i]);
-                if (__ballot(here.bad())) {
-                    bad = true;
-                    here.most = 0.f;
+#pragma unroll 1
+        for (int base = start; base < e1; base += step) {
+            const int e = base + threadIdx.x;
+            if ((int)threadIdx.x < step && e >= e0 && e < e1) {
+                const Item it = item_of<KEYS>(e, octets, chunks, codes);
+                if (pass == 0 || !once) load_item<T, KEYS, WHOLE>(c, pg, in, rot, head, it, x);
+                if (pass == 0) {
+                    Largest here;
 #pragma unroll
                     for (int r = 0; r < 4; ++r)
 #pragma unroll
-                        for (int i = 0; i < 8; ++i) here.add_finite(x[r][i]);
+                        for (int i = 0; i < 8; ++i) here.add(x[r][i]);
+                    if (__ballot(here.bad())) {
+                        bad = true;
+                        here.most = 0.f;
+#pragma unroll
+                        for (int r = 0; r < 4; ++r)
+#pragma unroll
+                            for (int i = 0; i < 8; ++i) here.add_finite(x[r][i]);
+                    }
+                    largest.most = fmaxf(largest.most, here.most);
+                } else {
+                    if (bad)
+#pragma unroll
+                        for (int r = 0; r < 4; ++r)
+#pragma unroll
+                            for (int i = 0; i < 8; ++i) x[r][i] = no_nan(x[r][i]);
+                    uint32_t w[8];
+                    code_item<KEYS>(x, inv, w);
+                    if (kStaged && whole(it.tok / 32)) stage_item<KEYS>(staged, (int)(it.at - codes) - base / block_items * block_bytes, w);
+                    else store_item<KEYS>(pg, it, w);
                 }
-                largest.most = fmaxf(largest.most, here.most);
-            } else {
-                if (bad)
-#pragma unroll
-                    for (int r = 0; r < 4; ++r)
-#pragma unroll
-                        for (int i = 0; i < 8; ++i) x[r][i] = no_nan(x[r][i]);
-                store_item<KEYS>(pg, it, x, inv);
             }
+            if (!kStaged || pass == 0) continue;
+            __syncthreads();
+            const int first = base / block_items;
+            for (int at = threadIdx.x * 16; at < step / block_items * block_bytes; at += THREADS * 16)
+                if (whole(first + at / block_bytes))
+                    *reinterpret_cast<uint4 *>(codes + first * block_bytes + at) = *reinterpret_cast<const uint4 *>(staged + staged_at(at));
+            __syncthreads();
         }
         if (pass == 1) break;
         if (bad && status) atomicOr(status, CMPQ_STATUS_NONFINITE);
@@ -221,6 +265,7 @@ template <typename T, bool WHOLE, int THREADS>
 __global__ __launch_bounds__(THREADS) void append_kernel(cmpq_kv_cache c, cmpq_kv_rows r, cmpq_heads K, cmpq_heads V,
                                                           cmpq_rotation rot, int32_t *status) {
     __shared__ float scratch[THREADS / 64 + 1];
+    __shared__ __align__(16) uint8_t staged[THREADS == 256 ? 8192 : 16];
     const Page pg = find_page(r, c.page, blockIdx.x, looks_over() ? status : nullptr);
     if (pg.seq < 0) return;
     const int64_t id = r.page_table[pg.seq * r.ld_table + pg.begin / c.page];
@@ -228,8 +273,8 @@ __global__ __launch_bounds__(THREADS) void append_kernel(cmpq_kv_cache c, cmpq_k
         if (threadIdx.x == 0 && status) atomicOr(status, CMPQ_STATUS_RANGE);
         return;
     }
-    if (blockIdx.z == 0) append_page<T, true, WHOLE, THREADS>(c, pg, id, blockIdx.y, K, rot, status, scratch);
-    else append_page<T, false, WHOLE, THREADS>(c, pg, id, blockIdx.y, V, rot, status, scratch);
+    if (blockIdx.z == 0) append_page<T, true, WHOLE, THREADS>(c, pg, id, blockIdx.y, K, rot, status, scratch, staged);
+    else append_page<T, false, WHOLE, THREADS>(c, pg, id, blockIdx.y, V, rot, status, scratch, staged);
 }
 
 template <typename T, bool KEYS, int THREADS>
