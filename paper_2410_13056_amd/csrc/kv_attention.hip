@@ -263,7 +263,7 @@ __device__ __forceinline__ void stage_queries(const Job &j, const Seq &s, int kv
             const T *p = static_cast<const T *>(j.Q.ptr) + col.row * j.Q.row_stride + col.head * j.Q.head_stride;
             if (by_eight && d + 8 <= j.c.head_dim) {
                 float x[8];
-                load_turned(p, d, j.rot, col.at, x);
+                load_turned(p, d, j.rot, col.at * (j.rot.dims >> 1), x);
                 *reinterpret_cast<Float4 *>(row) = Float4{x[0], x[1], x[2], x[3]};
                 *reinterpret_cast<Float4 *>(row + 4) = Float4{x[4], x[5], x[6], x[7]};
             } else {

@@ -77,13 +77,20 @@ struct Item {
     uint8_t *at;     // keys: of the first token (the others 16 bytes apart); values: of the first dim (16 bytes apart)
 };
 
+// Items e -> (four tokens, octet of dims), without a division: e * octets stays below 2^18 (1024 tokens of 256 dims), so the
+// product by 2^20 / octets, rounded up, has the right whole part.
+struct Octets {
+    uint32_t n, inverse;
+    __device__ __forceinline__ explicit Octets(int head_dim) : n((head_dim + 31) / 32 * 4), inverse((1u << 20) / n + 1) {}
+};
+
 template <bool KEYS>
-__device__ __forceinline__ Item item_of(int e, int octets, int chunks, uint8_t *codes) {
+__device__ __forceinline__ Item item_of(uint32_t e, const Octets &octets, uint8_t *codes) {
+    const uint32_t four = e * octets.inverse >> 20, tok = four * 4, dim = (e - four * octets.n) * 8, t = tok % 32, d = dim % 32;
     Item it;
-    it.tok = e / octets * 4;
-    it.d = e % octets * 8;
-    const int t = it.tok % 32, d = it.d % 32;
-    it.at = codes + (it.tok / 32 * chunks + it.d / 32) * 1024 +
+    it.tok = (int)tok;
+    it.d = (int)dim;
+    it.at = codes + (tok / 32 * (octets.n / 4) + dim / 32) * 1024 +
             (KEYS ? d / 8 * 256 + t % 16 * 16 + t / 16 * 8 : t % 16 / 4 * 256 + d % 16 * 16 + d / 16 * 8 + t / 16 * 4);
     return it;
 }
@@ -93,21 +100,23 @@ __device__ __forceinline__ Item item_of(int e, int octets, int chunks, uint8_t *
 template <typename T, bool KEYS, bool WHOLE>
 __device__ __forceinline__ void load_item(const cmpq_kv_cache &c, const Page &pg, const cmpq_heads &in, const cmpq_rotation &rot,
                                           int head, const Item &it, float (&x)[4][8]) {
-    const T *base = static_cast<const T *>(in.ptr) + head * in.head_stride;
+    const int64_t t0 = pg.begin + it.tok, turn = min(t0, rot.positions - 1), half = rot.dims >> 1;
+    const int more = (int)min((int64_t)3, rot.positions - 1 - turn);  // rows of the tables after this one
+    const T *p0 = static_cast<const T *>(in.ptr) + head * in.head_stride + (pg.row0 + t0 - pg.first) * in.row_stride;
+    const int64_t row = turn * half;
 #pragma unroll
     for (int r = 0; r < 4; ++r) {
         const int tok = it.tok + r;
-        const int64_t at = pg.begin + tok, turn = min(at, rot.positions - 1);
-        const T *p = base + (pg.row0 + at - pg.first) * in.row_stride;
+        const T *p = p0 + r * in.row_stride;
         const bool is_new = tok >= pg.from && tok < pg.to;
         if (WHOLE && is_new && it.d < c.head_dim) {
-            if (KEYS) load_turned(p, it.d, rot, turn, x[r]);
+            if (KEYS) load_turned(p, it.d, rot, row + min(r, more) * (int)half, x[r]);
             else load_f32<T, 8>(p + it.d, x[r]);
         } else {
 #pragma unroll
             for (int i = 0; i < 8; ++i) {
                 x[r][i] = 0.f;
-                if (!WHOLE && is_new && it.d + i < c.head_dim) x[r][i] = KEYS ? turned(p, it.d + i, rot, turn) : (float)p[it.d + i];
+                if (!WHOLE && is_new && it.d + i < c.head_dim) x[r][i] = KEYS ? turned(p, it.d + i, rot, turn + min(r, more)) : (float)p[it.d + i];
             }
         }
     }
@@ -191,25 +200,27 @@ template <typename T, bool KEYS, bool WHOLE, int THREADS>
 __device__ __forceinline__ void append_page(const cmpq_kv_cache &c, const Page &pg, int64_t id, int head, const cmpq_heads &in,
                                             const cmpq_rotation &rot, int32_t *status, float *scratch, uint8_t *staged) {
     constexpr bool kStaged = THREADS == 256;
-    const int chunks = (c.head_dim + 31) / 32, octets = chunks * 4, block_items = chunks * 32, block_bytes = chunks * 1024;
+    const Octets octets(c.head_dim);
+    const int chunks = (int)octets.n / 4, block_items = chunks * 32, block_bytes = chunks * 1024;
     uint8_t *codes = (KEYS ? c.k_codes : c.v_codes) + (id * c.kv_heads + head) * (int64_t)(c.page * chunks * 32);
     float *scale = (KEYS ? c.k_scale : c.v_scale) + id * c.kv_heads + head;
     if (threadIdx.x == 0) scratch[THREADS / 64] = pg.from > 0 ? *scale : 0.f;
     const int step = kStaged ? blocks_at_once<THREADS>(chunks) * block_items : THREADS;
-    const int start = kStaged ? pg.from / 32 * block_items : pg.from / 4 * octets, e0 = pg.from / 4 * octets;
-    const int e1 = (pg.to + 3) / 4 * octets;
+    const int start = kStaged ? pg.from / 32 * block_items : pg.from / 4 * (int)octets.n, e0 = pg.from / 4 * (int)octets.n;
+    const int e1 = (pg.to + 3) / 4 * (int)octets.n;
     const bool once = e1 - start <= step;
-    auto whole = [&](int block) { return block * 32 >= pg.from && block * 32 + 32 <= pg.to; };
+    const int staged_bytes = step / 32 * 1024;
+    const int whole0 = (pg.from + 31) / 32, whole1 = pg.to / 32;  // whole blocks
     float x[4][8], inv = 0.f;
     Largest largest;
     bool bad = false;
 #pragma unroll 1
     for (int pass = 0; pass < 2; ++pass) {
 #pragma unroll 1
-        for (int base = start; base < e1; base += step) {
+        for (int base = start, byte = start / 32 * 1024; base < e1; base += step, byte += staged_bytes) {  // its codes begin there
             const int e = base + threadIdx.x;
             if ((int)threadIdx.x < step && e >= e0 && e < e1) {
-                const Item it = item_of<KEYS>(e, octets, chunks, codes);
+                const Item it = item_of<KEYS>(e, octets, codes);
                 if (pass == 0 || !once) load_item<T, KEYS, WHOLE>(c, pg, in, rot, head, it, x);
                 if (pass == 0) {
                     Largest here;
@@ -234,16 +245,15 @@ __device__ __forceinline__ void append_page(const cmpq_kv_cache &c, const Page &
                             for (int i = 0; i < 8; ++i) x[r][i] = no_nan(x[r][i]);
                     uint32_t w[8];
                     code_item<KEYS>(x, inv, w);
-                    if (kStaged && whole(it.tok / 32)) stage_item<KEYS>(staged, (int)(it.at - codes) - base / block_items * block_bytes, w);
+                    if (kStaged && it.tok / 32 >= whole0 && it.tok / 32 < whole1) stage_item<KEYS>(staged, (int)(it.at - codes) - byte, w);
                     else store_item<KEYS>(pg, it, w);
                 }
             }
             if (!kStaged || pass == 0) continue;
             __syncthreads();
-            const int first = base / block_items;
-            for (int at = threadIdx.x * 16; at < step / block_items * block_bytes; at += THREADS * 16)
-                if (whole(first + at / block_bytes))
-                    *reinterpret_cast<uint4 *>(codes + first * block_bytes + at) = *reinterpret_cast<const uint4 *>(staged + staged_at(at));
+            const int end = min(staged_bytes, whole1 * block_bytes - byte);
+            for (int at = max(0, whole0 * block_bytes - byte) + threadIdx.x * 16; at < end; at += THREADS * 16)
+                *reinterpret_cast<uint4 *>(codes + byte + at) = *reinterpret_cast<const uint4 *>(staged + staged_at(at));
             __syncthreads();
         }
         if (pass == 1) break;
@@ -254,8 +264,8 @@ __device__ __forceinline__ void append_page(const cmpq_kv_cache &c, const Page &
         inv = 1.f / now;
         if (threadIdx.x == 0) *scale = now;
         if (pg.from > 0 && now != old) {
-            for (int e = threadIdx.x; e < (pg.from + 3) / 4 * octets; e += THREADS)
-                hold_item<KEYS>(pg, item_of<KEYS>(e, octets, chunks, codes), old * inv);
+            for (int e = threadIdx.x; e < (pg.from + 3) / 4 * (int)octets.n; e += THREADS)
+                hold_item<KEYS>(pg, item_of<KEYS>(e, octets, codes), old * inv);
             __syncthreads();  // an item of both is held first, by whichever lane
         }
     }
@@ -279,13 +289,14 @@ __global__ __launch_bounds__(THREADS) void append_kernel(cmpq_kv_cache c, cmpq_k
 
 template <typename T, bool KEYS, int THREADS>
 __device__ void read_page(const cmpq_kv_cache &c, const Page &pg, int64_t id, int head, const cmpq_heads &out) {
-    const int dim = c.head_dim, chunks = (dim + 31) / 32, octets = chunks * 4;
+    const Octets octets(c.head_dim);
+    const int dim = c.head_dim, chunks = (int)octets.n / 4;
     uint8_t *codes = (KEYS ? c.k_codes : c.v_codes) + (id * c.kv_heads + head) * (int64_t)(c.page * chunks * 32);
     const float scale = (KEYS ? c.k_scale : c.v_scale)[id * c.kv_heads + head];
     T *base = static_cast<T *>(out.ptr) + head * out.head_stride;
-    const int e0 = pg.from / 4 * octets, e1 = (pg.to + 3) / 4 * octets;
+    const int e0 = pg.from / 4 * (int)octets.n, e1 = (pg.to + 3) / 4 * (int)octets.n;
     for (int e = e0 + threadIdx.x; e < e1; e += THREADS) {
-        const Item it = item_of<KEYS>(e, octets, chunks, codes);
+        const Item it = item_of<KEYS>(e, octets, codes);
         uint32_t w[8];
 #pragma unroll
         for (int i = 0; i < 8; ++i)

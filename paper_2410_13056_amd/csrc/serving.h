@@ -103,16 +103,17 @@ __host__ __device__ __forceinline__ bool turns_by_eight(const cmpq_rotation &rot
     return !rot.cos || (rot.interleaved ? rot.dims % 8 == 0 : rot.dims % 16 == 0);
 }
 
-// Dims d .. d + 7 (d a multiple of 8, all within the head) at `p`, turned by eight for the row `at` of the tables.
+// Dims d .. d + 7 (d a multiple of 8, all within the head) at `p`, turned by eight for the row of the tables that begins at
+// element `row`.
 template <typename T>
-__device__ __forceinline__ void load_turned(const T *p, int d, const cmpq_rotation &rot, int64_t at, float (&x)[8]) {
+__device__ __forceinline__ void load_turned(const T *p, int d, const cmpq_rotation &rot, int64_t row, float (&x)[8]) {
     load_f32<T, 8>(p + d, x);
     if (!rot.cos || d >= rot.dims) return;
     const int half = rot.dims >> 1;
     if (rot.interleaved) {
         float cs[4], sn[4];
-        load_f32<float, 4>(rot.cos + at * half + d / 2, cs);
-        load_f32<float, 4>(rot.sin + at * half + d / 2, sn);
+        load_f32<float, 4>(rot.cos + row + d / 2, cs);
+        load_f32<float, 4>(rot.sin + row + d / 2, sn);
 #pragma unroll
         for (int i = 0; i < 8; i += 2) {
             const float a = x[i], b = x[i + 1];
@@ -122,15 +123,13 @@ __device__ __forceinline__ void load_turned(const T *p, int d, const cmpq_rotati
     } else {
         const bool second = d >= half;
         const int pair = second ? d - half : d;
+        const uint32_t flip = second ? 0x80000000u : 0;  // b cos + a sin = b cos - a (-sin), bit for bit
         float y[8], cs[8], sn[8];
         load_f32<T, 8>(p + (second ? pair : d + half), y);
-        load_f32<float, 8>(rot.cos + at * half + pair, cs);
-        load_f32<float, 8>(rot.sin + at * half + pair, sn);
+        load_f32<float, 8>(rot.cos + row + pair, cs);
+        load_f32<float, 8>(rot.sin + row + pair, sn);
 #pragma unroll
-        for (int i = 0; i < 8; ++i) {
-            const float first = turned_first(x[i], y[i], cs[i], sn[i]);
-            x[i] = second ? turned_second(y[i], x[i], cs[i], sn[i]) : first;
-        }
+        for (int i = 0; i < 8; ++i) x[i] = turned_first(x[i], y[i], cs[i], __uint_as_float(__float_as_uint(sn[i]) ^ flip));
     }
 }
 
