@@ -99,11 +99,11 @@ __global__ __launch_bounds__(256) void code_rows_kernel(const T *__restrict__ X,
     each([&](const Sixteen<T> &s, int) { s.look(largest); });
     const bool bad = __ballot(largest.bad()) != 0;
     if (bad) {
-        largest.most = 0.f;
+        largest.bits = 0;
         each([&](const Sixteen<T> &s, int) { s.look_again(largest); });
         if (status) atomicOr(status, CMPQ_STATUS_NONFINITE);
     }
-    const float s = code_scale(block_max(largest.most, scratch)), inv = 1.f / s;
+    const float s = code_scale(block_max(largest.most(), scratch)), inv = 1.f / s;
     if (threadIdx.x == 0) scale[row] = s;
     auto put = [&](const Sixteen<T> &s, int c, bool clean) {
         *reinterpret_cast<uint4 *>(out + c / 4 * kPiece + c % 4 * 256) = s.codes(inv, clean);
@@ -270,10 +270,10 @@ __global__ __launch_bounds__(kFewWaves * 64) void few_tokens_kernel(const uint8_
         x[t].look(largest);
         if (__ballot(largest.bad())) {
             bad = true;
-            largest.most = 0.f;
+            largest.bits = 0;
             x[t].look_again(largest);
         }
-        float v = largest.most;
+        float v = largest.most();
 #pragma unroll
         for (int s = 32; s > 0; s >>= 1) v = fmaxf(v, __shfl_xor(v, s, CMPQ_WAVE));
         if (lane == 0) most[t][wave] = v;

@@ -211,62 +211,75 @@ __device__ __forceinline__ void append_page(const cmpq_kv_cache &c, const Page &
     const bool once = e1 - start <= step;
     const int staged_bytes = step / 32 * 1024;
     const int whole0 = (pg.from + 31) / 32, whole1 = pg.to / 32;  // whole blocks
-    float x[4][8], inv = 0.f;
+    float x[4][8];
     Largest largest;
     bool bad = false;
-#pragma unroll 1
-    for (int pass = 0; pass < 2; ++pass) {
-#pragma unroll 1
-        for (int base = start, byte = start / 32 * 1024; base < e1; base += step, byte += staged_bytes) {  // its codes begin there
-            const int e = base + threadIdx.x;
-            if ((int)threadIdx.x < step && e >= e0 && e < e1) {
-                const Item it = item_of<KEYS>(e, octets, codes);
-                if (pass == 0 || !once) load_item<T, KEYS, WHOLE>(c, pg, in, rot, head, it, x);
-                if (pass == 0) {
-                    Largest here;
+    auto has = [&](int e) { return (int)threadIdx.x < step && e >= e0 && e < e1; };
+    auto look = [&](int e) {
+        load_item<T, KEYS, WHOLE>(c, pg, in, rot, head, item_of<KEYS>(e, octets, codes), x);
+        Largest here;
 #pragma unroll
-                    for (int r = 0; r < 4; ++r)
+        for (int r = 0; r < 4; ++r)
 #pragma unroll
-                        for (int i = 0; i < 8; ++i) here.add(x[r][i]);
-                    if (__ballot(here.bad())) {
-                        bad = true;
-                        here.most = 0.f;
+            for (int i = 0; i < 8; ++i) here.add(x[r][i]);
+        if (here.bad()) {
+            bad = true;
+            here.bits = 0;
 #pragma unroll
-                        for (int r = 0; r < 4; ++r)
+            for (int r = 0; r < 4; ++r)
 #pragma unroll
-                            for (int i = 0; i < 8; ++i) here.add_finite(x[r][i]);
-                    }
-                    largest.most = fmaxf(largest.most, here.most);
-                } else {
-                    if (bad)
-#pragma unroll
-                        for (int r = 0; r < 4; ++r)
-#pragma unroll
-                            for (int i = 0; i < 8; ++i) x[r][i] = no_nan(x[r][i]);
-                    uint32_t w[8];
-                    code_item<KEYS>(x, inv, w);
-                    if (kStaged && it.tok / 32 >= whole0 && it.tok / 32 < whole1) stage_item<KEYS>(staged, (int)(it.at - codes) - byte, w);
-                    else store_item<KEYS>(pg, it, w);
-                }
-            }
-            if (!kStaged || pass == 0) continue;
-            __syncthreads();
-            const int end = min(staged_bytes, whole1 * block_bytes - byte);
-            for (int at = max(0, whole0 * block_bytes - byte) + threadIdx.x * 16; at < end; at += THREADS * 16)
-                *reinterpret_cast<uint4 *>(codes + byte + at) = *reinterpret_cast<const uint4 *>(staged + staged_at(at));
-            __syncthreads();
+                for (int i = 0; i < 8; ++i) here.add_finite(x[r][i]);
         }
-        if (pass == 1) break;
-        if (bad && status) atomicOr(status, CMPQ_STATUS_NONFINITE);
-        if (KEYS && rot.cos && threadIdx.x == 0 && status && pg.begin + pg.to > rot.positions)
-            atomicOr(status, CMPQ_STATUS_RANGE);
-        const float most = block_max(largest.most, scratch), old = scratch[THREADS / 64], now = fmaxf(old, code_scale(most));
-        inv = 1.f / now;
-        if (threadIdx.x == 0) *scale = now;
-        if (pg.from > 0 && now != old) {
-            for (int e = threadIdx.x; e < (pg.from + 3) / 4 * (int)octets.n; e += THREADS)
-                hold_item<KEYS>(pg, item_of<KEYS>(e, octets, codes), old * inv);
-            __syncthreads();  // an item of both is held first, by whichever lane
+        largest.bits = max(largest.bits, here.bits);
+    };
+    if (once) {
+        if (has(start + threadIdx.x)) look(start + threadIdx.x);
+    } else {
+#pragma unroll 1
+        for (int base = start; base < e1; base += step)
+            if (has(base + threadIdx.x)) look(base + threadIdx.x);
+    }
+    if (bad && status) atomicOr(status, CMPQ_STATUS_NONFINITE);
+    if (KEYS && rot.cos && threadIdx.x == 0 && status && pg.begin + pg.to > rot.positions) atomicOr(status, CMPQ_STATUS_RANGE);
+    const float most = block_max(largest.most(), scratch), old = scratch[THREADS / 64], now = fmaxf(old, code_scale(most));
+    const float inv = 1.f / now;
+    if (threadIdx.x == 0) *scale = now;
+    if (pg.from > 0 && now != old) {
+        for (int e = threadIdx.x; e < (pg.from + 3) / 4 * (int)octets.n; e += THREADS)
+            hold_item<KEYS>(pg, item_of<KEYS>(e, octets, codes), old * inv);
+        __syncthreads();  // an item of both is held first, by whichever lane
+    }
+    auto put = [&](int e, int byte) {
+        const Item it = item_of<KEYS>(e, octets, codes);
+        if (bad)
+#pragma unroll
+            for (int r = 0; r < 4; ++r)
+#pragma unroll
+                for (int i = 0; i < 8; ++i) x[r][i] = no_nan(x[r][i]);
+        uint32_t w[8];
+        code_item<KEYS>(x, inv, w);
+        if (kStaged && it.tok / 32 >= whole0 && it.tok / 32 < whole1) stage_item<KEYS>(staged, (int)(it.at - codes) - byte, w);
+        else store_item<KEYS>(pg, it, w);
+    };
+    auto copy_out = [&](int byte) {
+        __syncthreads();
+        const int end = min(staged_bytes, whole1 * block_bytes - byte);
+        for (int at = max(0, whole0 * block_bytes - byte) + threadIdx.x * 16; at < end; at += THREADS * 16)
+            *reinterpret_cast<uint4 *>(codes + byte + at) = *reinterpret_cast<const uint4 *>(staged + staged_at(at));
+    };
+    if (once) {
+        if (has(start + threadIdx.x)) put(start + threadIdx.x, start / 32 * 1024);
+        if (kStaged) copy_out(start / 32 * 1024);
+    } else {
+#pragma unroll 1
+        for (int base = start, byte = start / 32 * 1024; base < e1; base += step, byte += staged_bytes) {  // codes begin there
+            if (has(base + threadIdx.x)) {
+                load_item<T, KEYS, WHOLE>(c, pg, in, rot, head, item_of<KEYS>(base + threadIdx.x, octets, codes), x);
+                put(base + threadIdx.x, byte);
+            }
+            if (!kStaged) continue;
+            copy_out(byte);
+            __syncthreads();
         }
     }
 }

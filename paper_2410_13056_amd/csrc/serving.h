@@ -32,19 +32,18 @@ __device__ __forceinline__ void load_f32(const T *p, float (&x)[N]) {
     for (int i = 0; i < N; ++i) x[i] = (float)v[i];
 }
 
-// Largest magnitude of values, and whether all were finite.  Two instructions a value; where one was not (bad()), the
-// magnitudes are looked over again and the infinite ones left out.
+// Largest magnitude of values, and whether all were finite: magnitudes are ordered as their bits are, infinity and NaN
+// above the rest.  Where one was not finite (bad()), they are looked over again without those.
 struct Largest {
-    float most = 0.f, zero = 0.f;
-    __device__ __forceinline__ void add(float x) {
-        most = fmaxf(most, fabsf(x));
-        zero = fmaf(x, 0.f, zero);  // NaN from the first infinity or NaN on
-    }
+    uint32_t bits = 0;
+    static constexpr uint32_t kInfinity = 0x7f800000u;
+    __device__ __forceinline__ void add(float x) { bits = max(bits, __float_as_uint(x) & 0x7fffffffu); }
     __device__ __forceinline__ void add_finite(float x) {
-        const float a = fabsf(x);
-        most = a < INFINITY ? fmaxf(most, a) : most;
+        const uint32_t a = __float_as_uint(x) & 0x7fffffffu;
+        bits = a < kInfinity ? max(bits, a) : bits;
     }
-    __device__ __forceinline__ bool bad() const { return !(zero == 0.f); }
+    __device__ __forceinline__ bool bad() const { return bits >= kInfinity; }
+    __device__ __forceinline__ float most() const { return __uint_as_float(bits); }
 };
 
 __device__ __forceinline__ float code_scale(float most) { return fmaxf(most / 127.f, kSmallestScale); }
