@@ -1,10 +1,15 @@
 // The paged cache in 8 bits: new tokens in (keys turned by position on the way) and values back.
 // A workgroup takes one page of one sequence for one head, keys or values: a scale belongs to a page and head, so
-// whoever finds the page's new largest magnitude also writes its codes, and nobody else touches them.
+// whoever finds the page's new largest magnitude also writes its codes, and nobody else touches them.  The new values are
+// in registers between the two: they are read once from memory.
+//
+// Bound.  Prompts: 5701 tokens of 32 heads, 128 dims, FP16, 140 MB in 47 us (3.0 TB/s): vector instructions
+// keep the units busy for three quarters of it (25 a value: turn, magnitude, code, addresses, and the search for the
+// page), stores in whole lines took 5 us off.  Read back: 30 us, 4.7 TB/s, what a large copy reaches.  Steps: 64 sequences of
+// one token, 8 heads, 6.6 us and 9 us back: a chain of loads (lengths, page table, scale, codes).
 #include "serving.h"
 
 namespace {
-
 
 struct Page {
     int64_t seq;     // sequence, -1: there is no such page
@@ -284,6 +289,7 @@ __device__ __forceinline__ void append_page(const cmpq_kv_cache &c, const Page &
     }
 }
 
+// THREADS: 256, or a wavefront where sequences have up to 4 rows on average (64 sequences of one token 7.4 us, with 256 8.6).
 template <typename T, bool WHOLE, int THREADS>
 __global__ __launch_bounds__(THREADS) void append_kernel(cmpq_kv_cache c, cmpq_kv_rows r, cmpq_heads K, cmpq_heads V,
                                                           cmpq_rotation rot, int32_t *status) {
