@@ -364,9 +364,8 @@ __global__ __launch_bounds__(WO * WT * 64, 2) void tile_kernel(const uint8_t *__
         constexpr int kUnder = (BUFS - 2) * kLoads;
         static_assert(kUnder < 64, "the count of loads still under way");
         __builtin_amdgcn_sched_barrier(0);
-        __builtin_amdgcn_s_waitcnt((kUnder & 15) | (kUnder >> 4) << 14 | 7 << 4);  // vmcnt(kUnder) lgkmcnt(0)
-        __builtin_amdgcn_s_barrier();
-        asm volatile("" ::: "memory");
+        __builtin_amdgcn_s_waitcnt((kUnder & 15) | (kUnder >> 4) << 14 | 7 << 4);  // the same wait, for the compiler to count on
+        asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"(kUnder) : "memory");
     };
     // Multiplies a step while the next one's operands come from LDS and a later one's pieces from memory, a share of
     // each at a time: issued together, the loads fill the memory pipeline's queue and hold up all behind them.
