@@ -147,21 +147,28 @@ __device__ __forceinline__ float scaled(int sum, float sx, float sw) {
     return (float)sum * fminf(sx, sw) * fmaxf(sx, sw);
 }
 
+__device__ __forceinline__ float token_scale(const Scaled &y, int64_t t) { return t < y.m ? y.sx[t] : 0.f; }
+
+// Of outputs o .. o + 3.
+__device__ __forceinline__ float4 output_scales(const Scaled &y, int64_t o) {
+    if (o + 4 <= y.d_out && y.aligned) return *reinterpret_cast<const float4 *>(y.sw + o);
+    const auto one = [&](int64_t i) { return i < y.d_out ? y.sw[i] : 0.f; };
+    return make_float4(one(o), one(o + 1), one(o + 2), one(o + 3));
+}
+
 // Four outputs next to each other, o .. o + 3, of token t.
 template <typename T>
-__device__ __forceinline__ void put4(const Scaled &y, int64_t t, int64_t o, const Int4 &acc) {
+__device__ __forceinline__ void put4(const Scaled &y, int64_t t, int64_t o, const Int4 &acc, float sx, const float4 &sw) {
     if (t >= y.m || o >= y.d_out) return;
-    const float sx = y.sx[t];
     T *p = static_cast<T *>(y.Y) + t * y.ldy + o;
+    typedef T T4 __attribute__((ext_vector_type(4)));
+    const T4 v = {(T)scaled(acc[0], sx, sw.x), (T)scaled(acc[1], sx, sw.y), (T)scaled(acc[2], sx, sw.z), (T)scaled(acc[3], sx, sw.w)};
     if (o + 4 <= y.d_out && y.aligned) {
-        typedef T T4 __attribute__((ext_vector_type(4)));
-        const float4 sw = *reinterpret_cast<const float4 *>(y.sw + o);
-        *reinterpret_cast<T4 *>(p) = T4{(T)scaled(acc[0], sx, sw.x), (T)scaled(acc[1], sx, sw.y),
-                                        (T)scaled(acc[2], sx, sw.z), (T)scaled(acc[3], sx, sw.w)};
+        *reinterpret_cast<T4 *>(p) = v;
     } else {
 #pragma unroll
         for (int r = 0; r < 4; ++r)
-            if (o + r < y.d_out) p[r] = (T)scaled(acc[r], sx, y.sw[o + r]);
+            if (o + r < y.d_out) p[r] = v[r];
     }
 }
 
@@ -189,6 +196,17 @@ __global__ __launch_bounds__(WAVES * 64) void shared_depth_kernel(const uint8_t 
     for (int i = 0; i < OP; ++i) w[i] = W + min(o0 + i, last_o) * deep * kPiece + lane * 16;
 #pragma unroll
     for (int i = 0; i < TP; ++i) x[i] = X + min(t0 + i, last_t) * deep * kPiece + lane * 16;
+    // the scales that the results will take, on their way meanwhile
+    constexpr int kMine = (OP * TP + WAVES - 1) / WAVES;
+    const int64_t t = t0 * kRows + (lane & 15), o = o0 * kRows + (lane >> 4) * 4;
+    float sx[kMine];
+    float4 sw[kMine];
+#pragma unroll
+    for (int i = 0; i < kMine; ++i) {
+        const int q = wave + i * WAVES;
+        sx[i] = token_scale(y, t + q % TP * kRows);
+        sw[i] = output_scales(y, o + q / TP * kRows);
+    }
     Int4 acc[OP][TP] = {};
     const int k0 = (int)((int64_t)deep * wave / WAVES), k1 = (int)((int64_t)deep * (wave + 1) / WAVES);
     Int4 a[2][kAhead][OP], b[2][kAhead][TP];
@@ -231,11 +249,14 @@ __global__ __launch_bounds__(WAVES * 64) void shared_depth_kernel(const uint8_t 
 #pragma unroll
         for (int j = 0; j < TP; ++j) red[wave][i * TP + j][lane] = acc[i][j];
     __syncthreads();
-    for (int q = wave; q < OP * TP; q += WAVES) {
+#pragma unroll
+    for (int i = 0; i < kMine; ++i) {
+        const int q = wave + i * WAVES;
+        if (q >= OP * TP) break;
         Int4 sum = red[0][q][lane];
 #pragma unroll
         for (int v = 1; v < WAVES; ++v) sum += red[v][q][lane];
-        put4<T>(y, (t0 + q % TP) * kRows + (lane & 15), (o0 + q / TP) * kRows + (lane >> 4) * 4, sum);
+        put4<T>(y, t + q % TP * kRows, o + q / TP * kRows, sum, sx[i], sw[i]);
     }
 }
 
@@ -307,10 +328,12 @@ __global__ __launch_bounds__(kFewWaves * 64) void few_tokens_kernel(const uint8_
     red[wave][lane] = acc;
     __syncthreads();
     if (wave != 0) return;
-#pragma unroll
+#pragma unroll 5  // more at once would take the registers of a second workgroup a unit
     for (int v = 1; v < kFewWaves; ++v) acc += red[v][lane];
-    y.sx = scales;
-    with_dtype(dtype, [&](auto like) { put4<decltype(like)>(y, lane & 15, (int64_t)blockIdx.x * kRows + (lane >> 4) * 4, acc); });
+    const int64_t o = (int64_t)blockIdx.x * kRows + (lane >> 4) * 4;
+    const float sx = scales[min(lane & 15, m - 1)];
+    const float4 sw = output_scales(y, o);
+    with_dtype(dtype, [&](auto like) { put4<decltype(like)>(y, lane & 15, o, acc, sx, sw); });
 }
 
 __device__ __forceinline__ void load_lds16(const uint8_t *src, uint8_t *dst) {
@@ -397,11 +420,17 @@ __global__ __launch_bounds__(WO * WT * 64, 2) void tile_kernel(const uint8_t *__
         turn(step + 1, 1);
     }
     asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");  // what nothing reads ends before the LDS does
+    const int64_t t = (t0 + wt) * kRows + (lane & 15), o = (o0 + wo) * kRows + (lane >> 4) * 4;
+    float sx[B];
+    float4 sw[A];
+#pragma unroll
+    for (int q = 0; q < B; ++q) sx[q] = token_scale(y, t + q * kRows);
+#pragma unroll
+    for (int p = 0; p < A; ++p) sw[p] = output_scales(y, o + p * kRows);
 #pragma unroll
     for (int q = 0; q < B; ++q)
 #pragma unroll
-        for (int p = 0; p < A; ++p)
-            put4<T>(y, (t0 + wt + q) * kRows + (lane & 15), (o0 + wo + p) * kRows + (lane >> 4) * 4, acc[p][q]);
+        for (int p = 0; p < A; ++p) put4<T>(y, t + q * kRows, o + p * kRows, acc[p][q], sx[q], sw[p]);
 }
 
 template <typename T, int OT, int TT, int WO, int WT, int BUFS>
