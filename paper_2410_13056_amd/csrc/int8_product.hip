@@ -262,8 +262,8 @@ __global__ __launch_bounds__(WAVES * 64) void shared_depth_kernel(const uint8_t 
 
 // One or two tokens in one launch: every workgroup codes the tokens for itself, 16 inputs a lane, while the first pieces
 // of its 16 outputs' weights are on their way; the wavefronts share the depth.  Against coding them in a launch of
-// its own, us: 1 token 8192 -> 1024 5.7 and 9.1, -> 28672 34.3 and 39.2; 2 tokens 8192 -> 8192 17.0 and 19.2; 4
-// tokens 25.8 and 19.3, which is why it ends there.  Small ones are bound by what comes one after the other (the token,
+// its own, us: 1 token 8192 -> 1024 5.2 and 8.2, -> 28672 34.6 and 38.5; 2 tokens 8192 -> 8192 11.8 and 15.4; 4
+// tokens 20.5 and 15.4, which is why it ends there.  Small ones are bound by what comes one after the other (the token,
 // its largest, two barriers, the products, the join), large ones by the weights' bytes.
 constexpr int kFewWaves = 16, kFewDepth = kFewWaves * 64 * 16;
 
@@ -344,8 +344,8 @@ __device__ __forceinline__ void load_lds16(const uint8_t *src, uint8_t *dst) {
 // Tiles of OT x TT pieces a workgroup, WO x WT wavefronts.  Pieces reach LDS by direct loads in the order in which they
 // are read (no conflicts), BUFS steps of 64 inputs in a ring; while a step is multiplied its operands are in
 // registers, those of the next are on their way from LDS and the steps after it from memory.  Bound by the matrix
-// instructions at 256 x 256: 4096 tokens 8192 -> 28672 in 735 us with the codes (29), 2.6 POP/s, the instructions busy for two
-// thirds of the clocks, the rest at the barrier of a step.  64 x 64 (333 tokens 4099 -> 3001, 17 us): 128 steps at the
+// instructions at 256 x 256: 4096 tokens 8192 -> 28672 in 737 us with the codes (29), 2.6 POP/s, the instructions busy for two
+// thirds of the clocks, the rest at the barrier of a step.  64 x 64 (333 tokens 4099 -> 3001, 16 us): 128 steps at the
 // latency of the caches, one tile a compute unit, matrix instructions 14 %.  Bands keep the inputs of a die's tiles in its
 // cache while the weights pass once a band.
 constexpr int kBand = 4;
@@ -448,13 +448,13 @@ void launch_shared(const uint8_t *W, const uint8_t *X, int deep, const Scaled &y
 int64_t tiles_of(const Scaled &y, int ot, int tt) { return cdiv(y.d_out, ot * kRows) * cdiv(y.m, tt * kRows); }
 
 // Which kernel: the largest tile that fills the chip.  A tile of 256 x 256 or 256 x 128 takes a compute unit for itself, so
-// its last round has to be two thirds full, or one of many.  us (4096 tokens 8192 -> 28672; 2048 tokens 4096 ->
-// 4096; 1024 tokens 4096 -> 4096; 512 tokens 4096 -> 11008): 256 x 256 759, 61, 59, 64; 256 x 128 877, 44, 37, 42; 128 x
-// 128 916, 45, 29, 48; 64 x 64 (333 tokens 4099 -> 3001 22.4, 128 x 128 32.5; 48 tokens 4096 -> 11008 17.1, 25.4).  Fewer than
-// 150 tiles of 64 x 64, and up to 32 tokens: wavefronts share the depth (512 tokens 8192 -> 1024 18.8, 64 x 64
-// 22.9; 64 tokens 4096 -> 4096 10.7, 13.4).  Up to 16 tokens: two pieces of outputs a workgroup where there are many
-// (16 tokens 5120 -> 13824 19.8, one piece 22.5), 8 wavefronts for some (8192 -> 8192 19.0, 16 wavefronts 20.4), 16
-// for few (1 token 8192 -> 1024 9.1, 8 wavefronts 10.8).
+// its last round has to be two thirds full, or one of many.  us (4096 tokens 8192 -> 28672; 2048 tokens 4096 -> 4096; 1024
+// tokens 4096 -> 4096; 512 tokens 4096 -> 11008): 256 x 256 737, 60, 53, 53; 256 x 128 860, 43.1, 36, 34.8; 128 x 128 901,
+// 44.0, 28, 35.4; 64 x 64 (333 tokens 4099 -> 3001 20.4, 128 x 128 25.5; 48 tokens 4096 -> 11008 14.0, 21.3).  Fewer than 150
+// tiles of 64 x 64, and up to 32 tokens: wavefronts share the depth (512 tokens 8192 -> 1024 18.6, 64 x 64 23.0; 64 tokens
+// 4096 -> 4096 9.4, 12.3).  Up to 16 tokens: two pieces of outputs a workgroup where there are many (16 tokens 5120 -> 13824
+// 16.0, one piece 17.9), 8 wavefronts for some (8192 -> 8192 15.8, 16 wavefronts 16.4), 16 for few (8 tokens 8192 -> 1024
+// 8.6, 8 wavefronts 9.8).
 template <typename T>
 int launch_product(const uint8_t *W, const uint8_t *X, int deep, const Scaled &y, hipStream_t st) {
     constexpr int64_t kUnits = 256;  // compute units
