@@ -344,8 +344,8 @@ __device__ __forceinline__ void load_lds16(const uint8_t *src, uint8_t *dst) {
 // Tiles of OT x TT pieces a workgroup, WO x WT wavefronts.  Pieces reach LDS by direct loads in the order in which they
 // are read (no conflicts), BUFS steps of 64 inputs in a ring; while a step is multiplied its operands are in
 // registers, those of the next are on their way from LDS and the steps after it from memory.  Bound by the matrix
-// instructions at 256 x 256: 4096 tokens 8192 -> 28672 in 737 us with the codes (29), 2.6 POP/s, the instructions busy for two
-// thirds of the clocks, the rest at the barrier of a step.  64 x 64 (333 tokens 4099 -> 3001, 16 us): 128 steps at the
+// instructions at 256 x 256: 4096 tokens 8192 -> 28672 in 737 us with the codes (29), 2.6 POP/s, the instructions busy for 69 %
+// of the clocks, the rest at the barrier of a step.  64 x 64 (333 tokens 4099 -> 3001, 16 us): 66 steps at the
 // latency of the caches, one tile a compute unit, matrix instructions 14 %.  Bands keep the inputs of a die's tiles in its
 // cache while the weights pass once a band.
 constexpr int kBand = 4;

@@ -956,6 +956,9 @@ Launches plan_launches(const cmpq_kv_attention_job *a) {
     Launches l;
     const int64_t c = cdiv(a->cache.head_dim, 32), group = a->q_heads / a->cache.kv_heads, cols = a->max_rows * group;
     l.dp = c * 32;
+    // Columns that the kernel for few rows takes at most, as registers allow.  us, it and the one for many rows: 48 columns of 128
+    // dims, 8 heads, 8000 tokens 26.6 and 30.4, 32 such sequences 123 and 153 (64 of 1000 tokens 46.6 and 41.1); 32 columns of
+    // 192 dims 26.9 and 39.4.
     const int64_t few = c <= 4 ? 48 : 32;
     if (cols <= few) {
         l.few.nc = (int)cdiv(cols, 16) * 16;
@@ -974,9 +977,10 @@ Launches plan_launches(const cmpq_kv_attention_job *a) {
     }
     l.few.target = 1024, l.few.least = 8;
     // Short sequences in one part, by 8 wavefronts where that leaves compute units free: a part more costs the launch that
-    // joins them.
-    if (l.few.nc && most_units(a) <= 64) {
-        l.few.least = 64;
+    // joins them.  us, one part and several: 32 heads, 1000 tokens 11.8 and 13.5, 1300 13.0 and 13.9, 2000 15.8 and 14.1; 32
+    // sequences of up to 1300 15.0 and 20.7.  8 wavefronts and 4: 2000 tokens 15.8 and 17.8, 64 sequences (512 tiles) 28.5 and 26.4.
+    if (l.few.nc && most_units(a) <= 48) {
+        l.few.least = 48;
         l.few.wide = most_tiles(a, l.few) < 512;
     }
     l.rows.target = l.rows.nc == 16 * kWaves && c <= 4 ? 1024 : 512;  // workgroups that run at once
