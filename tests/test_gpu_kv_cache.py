@@ -296,3 +296,26 @@ def test_refusals(S):
     assert e.value.code == -2
     S.kv_append(cache, K[:0], K[:0], t, h, _i32([0, 0]))          # nothing to do
     assert S.kv_read(cache, t, h, _i32([0, 0]), 0)[0].shape == (0, 2, 64)
+
+
+@pytest.mark.parametrize("dim", [8, 40, 72, 128, 160, 176, 208, 256])
+@pytest.mark.parametrize("page", [32, 160, 1024])
+def test_blocks_of_32_tokens_that_are_new_as_a_whole_or_in_part(S, dim, page):
+    """Appends that begin and end at, before and behind the edges of blocks and pages, with rows that are no numbers."""
+    from paper_2410_13056_amd import binding as B
+    g = torch.Generator(device=DEV).manual_seed(dim + page)
+    rounds = [[page, 33], [31, 1], [1, 62], [64, 97], [page - 1, page + 2]]
+    both = Both(S, 2, -(-max(sum(r[i] for r in rounds) for i in range(2)) // page), 2, dim, page, dim)
+    rotation = S.make_rotation(4 * page + 300, dim // 16 * 16, device=DEV) if dim >= 16 else None
+    for k, new in enumerate(rounds):
+        x = torch.randn((sum(new), 2, 2, dim), generator=g, device=DEV) * (1.0 + k % 3)
+        status = torch.zeros(1, dtype=torch.int32, device=DEV)
+        both.append(x[:, 0].half(), x[:, 1].half(), new, rotation, status)
+        both.check()
+        assert int(status) == 0
+    bad = torch.randn((40, 2, 2, dim), generator=g, device=DEV).half()
+    bad[37, 1, 0, dim // 2], bad[2, 1, 1, 0] = float("nan"), float("-inf")
+    both.held = [0, 0]
+    both.append(bad[:, 0], bad[:, 1], [39, 1], rotation, status)
+    both.check()
+    assert int(status) == B.STATUS_NONFINITE
