@@ -816,11 +816,13 @@ __device__ __forceinline__ float add_parts(const Job &j, int64_t slot0, int64_t 
 #pragma unroll
         for (int r = 0; r < 4; ++r) acc[r] += w > 0.f ? w * v[r] : 0.f;  // a part without tokens has no output
     }
+    const float mine_total = total;
+    const Float4 mine_acc = acc;
 #pragma unroll
-    for (int k = 1; k < PAR; ++k) {  // the other lanes of these dims, in order
-        total += __shfl(total, (lane + k * C * 8) & 63);
+    for (int k = 1; k < PAR; ++k) {  // the other lanes of these dims, in order behind this one's
+        total += __shfl(mine_total, (lane + k * C * 8) & 63);
 #pragma unroll
-        for (int r = 0; r < 4; ++r) acc[r] += __shfl(acc[r], (lane + k * C * 8) & 63);
+        for (int r = 0; r < 4; ++r) acc[r] += __shfl(mine_acc[r], (lane + k * C * 8) & 63);
     }
     return total;
 }
