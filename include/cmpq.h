@@ -741,9 +741,10 @@ int cmpq_kv_read(const cmpq_kv_cache *cache, const cmpq_kv_rows *rows, const cmp
  *       written, tokens beyond are left out, and either raises CMPQ_STATUS_RANGE.
  * Logits, their maximum, the weights' sum and the output are held in fp32.  A turned query is rounded to 16 bits fixed
  * point of its row's largest magnitude, its products with codes are exact; weights are rounded to FP16 for their products
- * with the values; a page's value scale below 2^-60 of a sequence's largest so far counts as that.  A query that holds
+ * with the values, after the page's value scale has gone into them and relative to the row's largest such product so far (its
+ * largest weight is kept apart).  A value scale below 2^-100 of the quotient of the two counts as that.  A query that holds
  * a NaN or an infinity gives NaN for its row and head alone.  The order of all additions depends on sizes, lengths and
- * the host bounds alone: results are reproducible bit for bit.
+ * the host bounds alone: results are reproducible bit for bit, and a row's do not depend on the other rows' queries.
  * Workspace: cmpq_kv_attention_workspace(job) (a function of the sizes, not of the pointers).
  */
 typedef struct cmpq_kv_attention_job {

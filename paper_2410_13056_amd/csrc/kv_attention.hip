@@ -6,8 +6,11 @@
 // codes are stored in the order of the instructions' operands, 16 bytes a lane and 1 KB a load.  A page's key scale
 // multiplies its logits, its value scale goes into its weights' exponent.
 //
-// A row's weights are held against its reference, a running maximum that moves only when a logit passes it by a factor
-// of 2^8, so that sums and outputs are rarely multiplied again; what it is cancels in the quotient.
+// A row has two references, both running maxima over the tokens that it sees: m of its logits, against which the weights' sum
+// is held, and m + d of its logits plus the logarithms of their value scales, against which its output is.  So the
+// weights that a matrix instruction takes are near the top of FP16 where they matter for the output, whatever the scales
+// of other pages.  A reference moves only when it is passed by a factor of 2^8, so that sums and outputs are rarely
+// multiplied again; m cancels in the quotient, 2^d multiplies it at the end.
 //
 // Two kernels.  For few rows (attend_kernel) the cache's bytes are what counts: the wavefronts of a workgroup share the
 // tokens and read codes straight from memory.  For many rows (attend_rows_kernel) multiplications and exponentials
@@ -31,7 +34,7 @@ constexpr float kLog2e = 1.44269504088896340736f;
 constexpr float kLowest = -3.4e38f;        // a row's reference before its first token
 constexpr float kSlack = 8.f;              // a row's logits pass its reference by a factor of at most 2^kSlack
 constexpr float kRaise = 7.f;              // weights are held times 2^kRaise: at most 2^15 in FP16
-constexpr float kLeastLog = -60.f, kMostInverse = 0x1p60f;  // value scales further below the largest so far count as this
+constexpr float kMostBelow = 100.f;        // value scales further below 2^d count as 2^(d - kMostBelow)
 
 struct Job {
     cmpq_kv_cache c;
@@ -44,7 +47,7 @@ struct Job {
     int64_t window;
     cmpq_rotation rot;
     int32_t *status;
-    float *part_o, *part_ml;   // [kept, columns, dims], [kept, columns, 2]
+    float *part_o, *part_ml;   // [kept, columns, dims], [kept, columns, 3]: outputs; m, d, sums
     int64_t kept;              // parts that there is room for
     int target, least;         // workgroups that fill the chip, units of a part at least
     int64_t least_cols, most_cols;  // sequences of that many (row, query head of the group) pairs are this kernel's
@@ -331,11 +334,11 @@ __device__ __forceinline__ float fixed_query(const float *from, float scale, boo
 // The page of a unit of a sequence, -1 if the table names none, and its scales.
 struct PageOf {
     int id, in_page;
-    float ks, vs, log_vs, inv_vs;
+    float ks, vs, log_vs;
 };
 
 __device__ __forceinline__ PageOf page_of(const Job &j, int64_t seq, int head, int unit, int end) {
-    PageOf p = {-1, 0, 0.f, 1.f, 0.f, 1.f};
+    PageOf p = {-1, 0, 0.f, 1.f, 0.f};
     if (unit >= end) return p;
     const int token = unit * kUnit, nth = token / j.c.page;
     p.id = j.table[seq * j.ld_table + nth];
@@ -350,22 +353,14 @@ __device__ __forceinline__ PageOf page_of(const Job &j, int64_t seq, int head, i
     return p;
 }
 // The rest of it: apart, so that loads of the codes need not wait for the scales.
-__device__ __forceinline__ void finish(PageOf &p) {
-    p.log_vs = log2f(p.vs);
-    p.inv_vs = 1.f / p.vs;
-}
+__device__ __forceinline__ void finish(PageOf &p) { p.log_vs = log2f(p.vs); }
 __device__ __forceinline__ float lane_value(float v, int lane) {
     return __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(v), lane));
 }
 
-// A tile's running state of one column in a lane: reference, this lane's share of the sum.
+// A tile's running state of one column in a lane: the references m and d, this lane's share of the sum.
 struct State {
-    float m, sum;
-};
-
-// The value scale that a wavefront's outputs are held in: the largest so far, its logarithm.
-struct UnitScale {
-    float scale, log;
+    float m, d, sum;
 };
 
 // Logits that a unit's products s stand for (s times f), each row's largest; -infinity where the row does not see the token.
@@ -382,30 +377,32 @@ __device__ __forceinline__ float logit_factor(float of_row, float kscale) {
     return f < 0x1p-126f ? 0x1p-126f : f;
 }
 
-// Moves the rows whose logits pass their reference, and the unit scale, and what is held in them.  A row's reference moves
-// by its own logits alone: results do not depend on the rows beside it.
-template <int C, int NT>
-__device__ __forceinline__ void move_up(State (&st)[NT], const float (&top)[NT], Float4 (&o)[NT][2 * C], UnitScale &u, bool there,
-                                        float vscale, float log_vscale) {
-    const bool wider = there && vscale > u.scale;
-    const float change = wider ? u.scale / vscale : 1.f;
-#pragma unroll
-    for (int t = 0; t < NT; ++t) {
-        const float now = row_max(top[t]);
-        const float next = now > st[t].m + kSlack ? now : st[t].m, keep = __builtin_amdgcn_exp2f(st[t].m - next);
-        st[t].sum *= keep;
-        const float turn = keep * change;
-#pragma unroll
-        for (int d = 0; d < 2 * C; ++d) o[t][d] *= turn;
-        st[t].m = next;
-    }
-    if (wider) u = {vscale, log_vscale};
+// Whether a unit's largest logit passes a reference of its row by more than the slack.
+__device__ __forceinline__ bool passes(const State &st, float top, float log_vs) {
+    return top - st.m > kSlack + fminf(0.f, st.d - log_vs);
 }
 
-// The weights of a unit's 8 tokens in this lane to FP16, against reference m, times the unit's value scale over the scale that
-// outputs are held in; `part`: their sum.
-__device__ __forceinline__ Half8 weigh(const float (&s)[8], float f, float m, float log_ratio, float &part) {
-    const float base = m - kRaise - log_ratio;
+// Moves the references that are passed, and what is held against them: by the row's own logits and pages alone, so results
+// do not depend on the rows beside it.
+template <int C, int NT>
+__device__ __forceinline__ void move_up(State (&st)[NT], const float (&top)[NT], Float4 (&o)[NT][2 * C], float log_vs) {
+#pragma unroll
+    for (int t = 0; t < NT; ++t) {
+        const float now = row_max(top[t]), rise = now - st[t].m, below = st[t].d - log_vs;
+        const bool up = rise > kSlack, out_up = rise - below > kSlack;
+        st[t].sum *= up ? __builtin_amdgcn_exp2f(-rise) : 1.f;
+        const float turn = out_up ? __builtin_amdgcn_exp2f(below - rise) : 1.f;
+#pragma unroll
+        for (int d = 0; d < 2 * C; ++d) o[t][d] *= turn;
+        st[t].d = out_up ? log_vs + (up ? 0.f : rise) : st[t].d - (up ? rise : 0.f);
+        st[t].m = up ? now : st[t].m;
+    }
+}
+
+// The weights of a unit's 8 tokens in this lane to FP16, against m + d and with the unit's value scale; adds them to the sum,
+// against m and without it.
+__device__ __forceinline__ Half8 weigh(const float (&s)[8], float f, State &st, float log_vs) {
+    const float below = fminf(st.d - log_vs, kMostBelow), base = st.m - kRaise + below;
     Half8 p;
     float w[8];
 #pragma unroll
@@ -413,13 +410,24 @@ __device__ __forceinline__ Half8 weigh(const float (&s)[8], float f, float m, fl
         w[r] = __builtin_amdgcn_exp2f(fmaf(s[r], f, -base));
         p[r] = (_Float16)w[r];
     }
-    part = ((w[0] + w[1]) + (w[2] + w[3])) + ((w[4] + w[5]) + (w[6] + w[7]));
+    const float part = ((w[0] + w[1]) + (w[2] + w[3])) + ((w[4] + w[5]) + (w[6] + w[7]));
+    st.sum = fmaf(part, __builtin_amdgcn_exp2f(below), st.sum);
     return p;
 }
 
-// What a part leaves: its output in absolute units and (reference, sum) into the workspace, or the output itself.
+// Output over sum, times 2^d, in two steps: 2^d may pass fp32's range where the result does not.
+__device__ __forceinline__ Float4 quotient(const Float4 &o, float total, float d) {
+    const float half = __builtin_amdgcn_exp2f(0.5f * d), by = total == 0.f ? 0.f : half / total;
+    return o * by * half;
+}
+
+// What a part leaves of a column's output in the workspace, and beside it.
 __device__ __forceinline__ void keep_part(const Job &j, int64_t slot, int nc, int col, int dims, int d, const Float4 &v) {
     *reinterpret_cast<Float4 *>(j.part_o + (slot * nc + col) * dims + d) = v;
+}
+__device__ __forceinline__ void keep_sum(const Job &j, int64_t slot, int nc, int col, float m, float d, float sum) {
+    float *p = j.part_ml + (slot * nc + col) * 3;
+    p[0] = m, p[1] = d, p[2] = sum;
 }
 
 // Few rows.  C: 32 dims each of a head.  Tiles of 16 NT columns, one (row, query head) pair each; the wavefronts take the
@@ -431,7 +439,7 @@ template <int C, int NT, int WAVES>
 __global__ __launch_bounds__(WAVES * 64, WAVES == 8 ? 2 : C * NT <= 4 ? 3 : C * NT <= 8 ? 2 : 1) void attend_kernel(Job j) {
     constexpr int NC = 16 * NT, DP = C * 32, kPad = DP + 4;
     __shared__ __align__(16) float red[4 * 16 * kPad];
-    __shared__ float ml[WAVES][NC][2];
+    __shared__ float ml[WAVES][NC][3];
     const int lane = threadIdx.x & 63, wave = wave_index(), n = lane & 15, g = lane >> 4;
     const Plan plan = make_plan<NC>(j, blockIdx.x == 0 && wave == 0);
     Share w;
@@ -479,18 +487,17 @@ __global__ __launch_bounds__(WAVES * 64, WAVES == 8 ? 2 : C * NT <= 4 ? 3 : C * 
     State st[NT];
 #pragma unroll
     for (int t = 0; t < NT; ++t) {
-        st[t] = {kLowest, 0.f};
+        st[t] = {kLowest, 0.f, 0.f};
 #pragma unroll
         for (int d = 0; d < 2 * C; ++d) o[t][d] = Float4{0.f, 0.f, 0.f, 0.f};
     }
-    UnitScale u = {0.f, 0.f};
 
     for (bool first = true; base < u1; base += WAVES * 64, first = false) {
         if (!first) begin();
         finish(mine);
         for (int i = 0; i < count; ++i) {
             const bool there = __builtin_amdgcn_readlane(mine.id, i) >= 0;
-            const float kscale = lane_value(mine.ks, i), vscale = lane_value(mine.vs, i);
+            const float kscale = lane_value(mine.ks, i), log_vs = lane_value(mine.log_vs, i);
             Int4 a[2][(C + 1) / 2];
 #pragma unroll
             for (int c = 0; c < (C + 1) / 2; ++c) {
@@ -503,7 +510,7 @@ __global__ __launch_bounds__(WAVES * 64, WAVES == 8 ? 2 : C * NT <= 4 ? 3 : C * 
             float l[NT][8], top[NT];
             const int t0 = (base + i * WAVES) * kUnit;
             const bool edge = !there || t0 < all_lo || t0 + kUnit > all_hi;
-            bool past = there && vscale > u.scale;
+            bool past = false;
 #pragma unroll
             for (int t = 0; t < NT; ++t) {
                 Int4 sum[2];
@@ -524,18 +531,12 @@ __global__ __launch_bounds__(WAVES * 64, WAVES == 8 ? 2 : C * NT <= 4 ? 3 : C * 
                     if (edge && (!there || at < lo[t] || at >= hi[t])) l[t][r] = -INFINITY;
                 }
                 top[t] = largest(l[t], logit_factor(factor[t], kscale));
-                past |= top[t] > st[t].m + kSlack;
+                past |= passes(st[t], top[t], log_vs);
             }
-            if (__ballot(past)) move_up<C, NT>(st, top, o, u, there, vscale, lane_value(mine.log_vs, i));
-            const float log_ratio = fmaxf(lane_value(mine.log_vs, i) - u.log, kLeastLog);
-            const float inv_ratio = fminf(u.scale * lane_value(mine.inv_vs, i), kMostInverse);
+            if (__ballot(past)) move_up<C, NT>(st, top, o, log_vs);
             Half8 p[NT];
 #pragma unroll
-            for (int t = 0; t < NT; ++t) {
-                float part;
-                p[t] = weigh(l[t], logit_factor(factor[t], kscale), st[t].m, log_ratio, part);
-                st[t].sum = fmaf(part, inv_ratio, st[t].sum);
-            }
+            for (int t = 0; t < NT; ++t) p[t] = weigh(l[t], logit_factor(factor[t], kscale), st[t], log_vs);
 #pragma unroll
             for (int c = 0; c < C; ++c) {
                 const Half8 v0 = halves(vc[c].x, vc[c].y), v1 = halves(vc[c].z, vc[c].w);
@@ -555,16 +556,24 @@ __global__ __launch_bounds__(WAVES * 64, WAVES == 8 ? 2 : C * NT <= 4 ? 3 : C * 
         st[t].sum = row_sum(st[t].sum);
         if (g == 0) {
             ml[wave][t * 16 + n][0] = st[t].m;
-            ml[wave][t * 16 + n][1] = st[t].sum;
+            ml[wave][t * 16 + n][1] = st[t].d;
+            ml[wave][t * 16 + n][2] = st[t].sum;
         }
     }
     __syncthreads();
 #pragma unroll
     for (int t = 0; t < NT; ++t) {
-        float top = kLowest;
+        // the references of a column's shares together: its largest m, and what then is the largest m + d less it
+        auto tops = [&](int k, float &top, float &scale) {
+            top = kLowest, scale = -INFINITY;
 #pragma unroll
-        for (int v = 0; v < WAVES; ++v) top = fmaxf(top, ml[v][t * 16 + n][0]);
-        const float mine = __builtin_amdgcn_exp2f(st[t].m - top) * u.scale;
+            for (int v = 0; v < WAVES; ++v) top = fmaxf(top, ml[v][k][0]);
+#pragma unroll
+            for (int v = 0; v < WAVES; ++v) scale = fmaxf(scale, ml[v][k][0] - top + ml[v][k][1]);
+        };
+        float top, scale;
+        tops(t * 16 + n, top, scale);
+        const float mine = __builtin_amdgcn_exp2f(st[t].m - top + st[t].d - scale);
         if (t > 0) __syncthreads();  // the columns before these have been read
         auto share = [&](int of) { return reinterpret_cast<Float4 *>(&red[(of * 16 + n) * kPad + g * 4]); };
         if (WAVES == 8) {  // the upper four first, the others on top
@@ -582,20 +591,16 @@ __global__ __launch_bounds__(WAVES * 64, WAVES == 8 ? 2 : C * NT <= 4 ? 3 : C * 
             Float4 v = *reinterpret_cast<const Float4 *>(&red[c * kPad + d]);
 #pragma unroll
             for (int q = 1; q < 4; ++q) v += *reinterpret_cast<const Float4 *>(&red[(q * 16 + c) * kPad + d]);
-            float high = kLowest, total = 0.f;
+            float high, total = 0.f, by;
+            tops(k, high, by);
 #pragma unroll
-            for (int q = 0; q < WAVES; ++q) high = fmaxf(high, ml[q][k][0]);
-#pragma unroll
-            for (int q = 0; q < WAVES; ++q) total += ml[q][k][1] * __builtin_amdgcn_exp2f(ml[q][k][0] - high);
+            for (int q = 0; q < WAVES; ++q) total += ml[q][k][2] * __builtin_amdgcn_exp2f(ml[q][k][0] - high);
             if (parts > 1) {
                 keep_part(j, w.slot, NC, k, DP, d, v);
-                if (d == 0) {
-                    j.part_ml[(w.slot * NC + k) * 2] = high;
-                    j.part_ml[(w.slot * NC + k) * 2 + 1] = total;
-                }
+                if (d == 0) keep_sum(j, w.slot, NC, k, high, by, total);
             } else if (tile * NC + k < s.rows * j.group) {
                 const int at = tile * NC + k;
-                put4(j, s.row0 + at / j.group, head * j.group + at % j.group, d, total == 0.f ? Float4{0.f, 0.f, 0.f, 0.f} : v / total);
+                put4(j, s.row0 + at / j.group, head * j.group + at % j.group, d, quotient(v, total, by));
             }
         }
     }
@@ -687,11 +692,10 @@ __global__ __launch_bounds__(kWaves * 64, NT == 1 && C <= 4 ? 4 : 2) void attend
     State st[NT];
 #pragma unroll
     for (int t = 0; t < NT; ++t) {
-        st[t] = {kLowest, 0.f};
+        st[t] = {kLowest, 0.f, 0.f};
 #pragma unroll
         for (int d = 0; d < 2 * C; ++d) o[t][d] = Float4{0.f, 0.f, 0.f, 0.f};
     }
-    UnitScale u = {0.f, 0.f};
     if (C % 2 && wave == 0)  // no dims there: zeros, though the queries are zeros as well
 #pragma unroll
         for (int i = 0; i < 4; ++i)
@@ -705,7 +709,7 @@ __global__ __launch_bounds__(kWaves * 64, NT == 1 && C <= 4 ? 4 : 2) void attend
     for (int unit = u0; unit < u1; ++unit) {
         const int buf = (unit - u0) & 1, i = (unit - u0) % 64;
         const bool there = __builtin_amdgcn_readlane(mine.id, i) >= 0;
-        const float kscale = lane_value(mine.ks, i), vscale = lane_value(mine.vs, i);
+        const float kscale = lane_value(mine.ks, i), log_vs = lane_value(mine.log_vs, i);
         if (unit + 1 < u1) store(buf ^ 1);
         if (unit + 2 < u1) load(unit + 2);
         const uint8_t *from = unit_at(buf);
@@ -736,7 +740,7 @@ __global__ __launch_bounds__(kWaves * 64, NT == 1 && C <= 4 ? 4 : 2) void attend
         __builtin_amdgcn_s_setprio(0);
         const int t0 = unit * kUnit;
         const bool edge = !there || t0 < all_lo || t0 + kUnit > all_hi;
-        bool past = there && vscale > u.scale;
+        bool past = false;
 #pragma unroll
         for (int t = 0; t < NT; ++t) {
             if (edge) {
@@ -747,18 +751,12 @@ __global__ __launch_bounds__(kWaves * 64, NT == 1 && C <= 4 ? 4 : 2) void attend
                 }
             }
             top[t] = largest(l[t], logit_factor(factor[t], kscale));
-            past |= top[t] > st[t].m + kSlack;
+            past |= passes(st[t], top[t], log_vs);
         }
-        if (__ballot(past)) move_up<C, NT>(st, top, o, u, there, vscale, lane_value(mine.log_vs, i));
-        const float log_ratio = fmaxf(lane_value(mine.log_vs, i) - u.log, kLeastLog);
-        const float inv_ratio = fminf(u.scale * lane_value(mine.inv_vs, i), kMostInverse);
+        if (__ballot(past)) move_up<C, NT>(st, top, o, log_vs);
         Half8 p[NT];
 #pragma unroll
-        for (int t = 0; t < NT; ++t) {
-            float part;
-            p[t] = weigh(l[t], logit_factor(factor[t], kscale), st[t].m, log_ratio, part);
-            st[t].sum = fmaf(part, inv_ratio, st[t].sum);
-        }
+        for (int t = 0; t < NT; ++t) p[t] = weigh(l[t], logit_factor(factor[t], kscale), st[t], log_vs);
 #pragma unroll
         for (int c = 0; c < C; ++c) {
             const Half8 *of = reinterpret_cast<const Half8 *>(from + kKeys + c * 2048);
@@ -776,14 +774,12 @@ __global__ __launch_bounds__(kWaves * 64, NT == 1 && C <= 4 ? 4 : 2) void attend
     // a tile at a time through LDS, so that rows go out whole
 #pragma unroll
     for (int t = 0; t < NT; ++t) {
-        const float total = row_sum(st[t].sum), by = parts > 1 ? u.scale : total == 0.f ? 0.f : u.scale / total;
+        const float total = row_sum(st[t].sum);
         const int first_col = (wave * NT + t) * 16;
-        if (parts > 1 && g == 0) {
-            j.part_ml[(w.slot * NC + first_col + n) * 2] = st[t].m;
-            j.part_ml[(w.slot * NC + first_col + n) * 2 + 1] = total;
-        }
+        if (parts > 1 && g == 0) keep_sum(j, w.slot, NC, first_col + n, st[t].m, st[t].d, total);
 #pragma unroll
-        for (int d = 0; d < 2 * C; ++d) *reinterpret_cast<Float4 *>(of_wave + n * (DP + 4) + d * 16 + g * 4) = o[t][d] * by;
+        for (int d = 0; d < 2 * C; ++d)
+            *reinterpret_cast<Float4 *>(of_wave + n * (DP + 4) + d * 16 + g * 4) = parts > 1 ? o[t][d] : quotient(o[t][d], total, st[t].d);
         __syncthreads();
 #pragma unroll 1
         for (int e = lane; e < 16 * DP / 4; e += 64) {
@@ -797,10 +793,10 @@ __global__ __launch_bounds__(kWaves * 64, NT == 1 && C <= 4 ? 4 : 2) void attend
 }
 
 // Adds up the parts first, first + step, ... below `parts` of a column, `slot0` being its first part's place and `stride` the way to
-// the next: a lane has four dims of every PAR-th of them.  `top` is the largest reference of all parts.
+// the next: a lane has four dims of every PAR-th of them.  `top` and `scale`: the references of all parts together.
 template <int C, int NC>
 __device__ __forceinline__ float add_parts(const Job &j, int64_t slot0, int64_t stride, int col, int first, int step, int parts,
-                                           float top, Float4 &acc) {
+                                           float top, float scale, Float4 &acc) {
     constexpr int DP = C * 32, PAR = 64 / (C * 8);
     const int lane = threadIdx.x & 63, mine = lane / (C * 8), d = lane % (C * 8) * 4;
     float total = 0.f;
@@ -810,9 +806,10 @@ __device__ __forceinline__ float add_parts(const Job &j, int64_t slot0, int64_t 
         const int at = p + mine * step;
         if (mine >= PAR || at >= parts) continue;
         const int64_t place = (slot0 + at * stride) * NC + col;
-        const float w = __builtin_amdgcn_exp2f(j.part_ml[place * 2] - top);
+        const float *ml = j.part_ml + place * 3;
+        const float rise = ml[0] - top, w = __builtin_amdgcn_exp2f(rise + ml[1] - scale);
         const Float4 v = *reinterpret_cast<const Float4 *>(j.part_o + place * DP + d);
-        total += w * j.part_ml[place * 2 + 1];
+        total += __builtin_amdgcn_exp2f(rise) * ml[2];
 #pragma unroll
         for (int r = 0; r < 4; ++r) acc[r] += w > 0.f ? w * v[r] : 0.f;  // a part without tokens has no output
     }
@@ -827,13 +824,19 @@ __device__ __forceinline__ float add_parts(const Job &j, int64_t slot0, int64_t 
     return total;
 }
 
+// The references of a column's parts together: their largest m, and what then is the largest m + d less it.
 template <int NC>
-__device__ __forceinline__ float top_of_parts(const Job &j, int64_t slot0, int64_t stride, int col, int parts) {
+__device__ __forceinline__ float top_of_parts(const Job &j, int64_t slot0, int64_t stride, int col, int parts, float &scale) {
     const int lane = threadIdx.x & 63;
+    auto of = [&](int p) { return j.part_ml + ((slot0 + p * stride) * NC + col) * 3; };
     float top = kLowest;
-    for (int p = lane; p < parts; p += 64) top = fmaxf(top, j.part_ml[((slot0 + p * stride) * NC + col) * 2]);
+    for (int p = lane; p < parts; p += 64) top = fmaxf(top, of(p)[0]);
 #pragma unroll
     for (int k = 32; k > 0; k >>= 1) top = fmaxf(top, __shfl_xor(top, k));
+    scale = -INFINITY;
+    for (int p = lane; p < parts; p += 64) scale = fmaxf(scale, of(p)[0] - top + of(p)[1]);
+#pragma unroll
+    for (int k = 32; k > 0; k >>= 1) scale = fmaxf(scale, __shfl_xor(scale, k));
     return top;
 }
 
@@ -858,11 +861,12 @@ __global__ __launch_bounds__(256) void join_kernel(Job j, int rows_each) {
     const int index = r * j.group + qh % j.group, col = index % NC;
     const int64_t slot0 = place.kept_before + qh / j.group * tiles + index / NC, stride = (int64_t)tiles * j.c.kv_heads;
     if (slot0 + (parts - 1) * stride >= j.kept) return;
-    const float top = top_of_parts<NC>(j, slot0, stride, col, parts);
+    float scale;
+    const float top = top_of_parts<NC>(j, slot0, stride, col, parts, scale);
     Float4 acc;
-    const float total = add_parts<C, NC>(j, slot0, stride, col, SPLIT == 4 ? wave : 0, SPLIT, parts, top, acc);
+    const float total = add_parts<C, NC>(j, slot0, stride, col, SPLIT == 4 ? wave : 0, SPLIT, parts, top, scale, acc);
     if (SPLIT == 1) {
-        if (lane < C * 8 && lane * 4 < j.c.head_dim) put4(j, s.row0 + r, qh, lane * 4, total == 0.f ? Float4{0.f, 0.f, 0.f, 0.f} : acc / total);
+        if (lane < C * 8 && lane * 4 < j.c.head_dim) put4(j, s.row0 + r, qh, lane * 4, quotient(acc, total, scale));
         return;
     }
     if (lane < C * 8) outs[wave][lane] = acc;
@@ -871,7 +875,7 @@ __global__ __launch_bounds__(256) void join_kernel(Job j, int rows_each) {
     if (wave != 0 || lane >= C * 8 || lane * 4 >= j.c.head_dim) return;
     const float all = sums[0] + sums[1] + sums[2] + sums[3];
     const Float4 o = outs[0][lane] + outs[1][lane] + outs[2][lane] + outs[3][lane];
-    put4(j, s.row0 + r, qh, lane * 4, all == 0.f ? Float4{0.f, 0.f, 0.f, 0.f} : o / all);
+    put4(j, s.row0 + r, qh, lane * 4, quotient(o, all, scale));
 }
 
 // Of many rows: a wavefront has `each` of a row's query heads that share a key / value head.
@@ -892,11 +896,12 @@ __global__ __launch_bounds__(256) void join_rows_kernel(Job j, int each) {
     if (slot + tiles + (parts - 1) * stride > j.kept) return;
     for (int g = g0; g < min(g0 + each, j.group); ++g) {
         const int index = (int)(row - s.row0) * j.group + g, col = index % NC;
-        const float top = top_of_parts<NC>(j, slot + index / NC, stride, col, parts);
+        float scale;
+        const float top = top_of_parts<NC>(j, slot + index / NC, stride, col, parts, scale);
         Float4 acc;
-        const float total = add_parts<C, NC>(j, slot + index / NC, stride, col, 0, 1, parts, top, acc);
+        const float total = add_parts<C, NC>(j, slot + index / NC, stride, col, 0, 1, parts, top, scale, acc);
         if (lane < C * 8 && lane * 4 < j.c.head_dim)
-            put4(j, row, head * j.group + g, lane * 4, total == 0.f ? Float4{0.f, 0.f, 0.f, 0.f} : acc / total);
+            put4(j, row, head * j.group + g, lane * 4, quotient(acc, total, scale));
     }
 }
 
@@ -910,7 +915,7 @@ struct Launches {
     int64_t dp;
     Kernel few, rows;
     size_t o_floats(const Kernel &h) const { return (size_t)(h.kept * h.nc * dp); }
-    size_t ml_floats(const Kernel &h) const { return (size_t)(h.kept * h.nc * 2); }
+    size_t ml_floats(const Kernel &h) const { return (size_t)(h.kept * h.nc * 3); }
 };
 
 // Tiles of 16 columns a wavefront of the kernel for many rows has at most.  Heads of up to 64 and of more than 128 dims are as
