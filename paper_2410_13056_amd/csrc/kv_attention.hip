@@ -50,6 +50,7 @@ struct Job {
     float *part_o, *part_ml;   // [kept, columns, dims], [kept, columns, 3]: outputs; m, d, sums
     int64_t kept;              // parts that there is room for
     int target, least;         // workgroups that fill the chip, units of a part at least
+    int most_parts;            // of a sequence, by the host's bounds: the grid and the kept parts have room for so many
     int64_t least_cols, most_cols;  // sequences of that many (row, query head of the group) pairs are this kernel's
 };
 
@@ -80,7 +81,7 @@ __device__ __forceinline__ Seq sequence(const Job &j, int64_t i, bool &bad) {
 // How the call's work is cut up: a tile is NC (row, query head of the group) pairs of a sequence, its units go in equal
 // parts of at most `step`.  Every wavefront works this out for itself from the lengths, 64 sequences at a time.
 struct Plan {
-    int step;
+    int step, most_parts;
 };
 
 template <int NC>
@@ -92,7 +93,7 @@ __device__ __forceinline__ int tiles_of(const Job &j, const Seq &s) {
 template <int NC>
 __device__ __forceinline__ Plan make_plan(const Job &j, bool look) {
     const int lane = threadIdx.x & 63;
-    if (j.kept == 0 && !look) return {1 << 30};
+    if (j.kept == 0 && !look) return {1 << 30, 1};
     double total = 0, pieces = 0;
     for (int64_t base = 0; base < j.n_seq; base += 64) {
         if (base + lane >= j.n_seq) continue;
@@ -107,10 +108,14 @@ __device__ __forceinline__ Plan make_plan(const Job &j, bool look) {
     Plan p;
     p.step = __builtin_amdgcn_readfirstlane(max(j.least, (int)ceil(all / max((double)j.target - odd, 0.5 * j.target))));
     if (j.kept == 0) p.step = 1 << 30;
+    p.most_parts = j.most_parts;
     return p;
 }
 
-__device__ __forceinline__ int parts_of(const Plan &p, const Seq &s) { return max(1, (s.units + p.step - 1) / p.step); }
+// A sequence that names more rows than `max_rows` may have more units in a window than the host counts with.
+__device__ __forceinline__ int parts_of(const Plan &p, const Seq &s) {
+    return min(max(1, (s.units + p.step - 1) / p.step), p.most_parts);
+}
 
 // A sequence's workgroups: those of the sequences before it, and how many of theirs leave parts to be joined (at most
 // 2 target in all: a sequence of more than `step` units has at most 2 units / step parts).
@@ -909,7 +914,7 @@ __global__ __launch_bounds__(256) void join_rows_kernel(Job j, int each) {
 struct Kernel {
     int nc = 0, target = 0, least = 0;
     bool wide = false;  // 8 wavefronts a workgroup
-    int64_t least_cols = 0, most_cols = -1, grid = 0, kept = 0;
+    int64_t least_cols = 0, most_cols = -1, grid = 0, kept = 0, parts = 1;
 };
 struct Launches {
     int64_t dp;
@@ -945,6 +950,7 @@ void size_up(const cmpq_kv_attention_job *a, Kernel &h) {
         const int64_t full = tiles * parts;
         h.grid = full < tiles + 2 * h.target ? full : tiles + 2 * h.target;
         h.kept = full < 2 * h.target ? full : 2 * h.target;
+        h.parts = parts;
     }
 }
 
@@ -1040,6 +1046,7 @@ template <int C>
 void launch(Job j, const Launches &l, WsCarver &w, hipStream_t st) {
     auto take = [&](const Kernel &h) {
         j.target = h.target, j.least = h.least, j.least_cols = h.least_cols, j.most_cols = h.most_cols, j.kept = h.kept;
+        j.most_parts = (int)h.parts;
         j.part_o = w.take<float>(l.o_floats(h));
         j.part_ml = w.take<float>(l.ml_floats(h));
     };
