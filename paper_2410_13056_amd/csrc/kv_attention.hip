@@ -56,8 +56,8 @@ struct Job {
 
 // A sequence: its rows and tokens, cut to what the call allows.
 struct Seq {
-    int64_t row0;
-    int rows, asked, length;   // `asked`: rows that the call names (the first `rows` of them are done)
+    int64_t row0, at0;         // first row, and its position
+    int rows, length;          // rows that are done of those that the call names
     int first_unit, units;     // those that some row attends to
 };
 
@@ -66,13 +66,13 @@ __device__ __forceinline__ Seq sequence(const Job &j, int64_t i, bool &bad) {
     const int64_t a = j.cu[i], b = j.cu[i + 1];
     s.row0 = min(max(a, (int64_t)0), j.n_rows);
     const int64_t end = min(max(b, s.row0), j.n_rows);
-    s.asked = (int)(end - s.row0);
-    s.rows = (int)min((int64_t)s.asked, j.max_rows);
-    const int64_t named = j.lengths[i];
-    const int64_t length = min(max(named, (int64_t)0), min(j.max_length, j.ld_table * j.c.page));
-    bad |= a != s.row0 || b != end || s.rows != s.asked || length != named;
+    const int64_t asked = end - s.row0, named = j.lengths[i], all = max(named, (int64_t)0);
+    s.rows = (int)min(asked, j.max_rows);
+    const int64_t length = min(all, min(j.max_length, j.ld_table * j.c.page));
+    bad |= a != s.row0 || b != end || s.rows != asked || length != named;
     s.length = (int)length;
-    const int64_t low = j.window > 0 ? max((int64_t)0, length - s.asked - j.window + 1) : 0;
+    s.at0 = all - asked;       // rows stay at their positions where tokens are left out
+    const int64_t low = j.window > 0 ? max((int64_t)0, s.at0 - j.window + 1) : 0;
     s.first_unit = (int)(low / kUnit);
     s.units = max(0, (int)((length + kUnit - 1) / kUnit) - s.first_unit);
     return s;
@@ -242,7 +242,7 @@ __device__ __forceinline__ Column column(const Job &j, const Seq &s, int kv_head
     Column c;
     c.row = col / j.group;
     c.head = kv_head * j.group + col % j.group;
-    const int64_t pos = (int64_t)s.length - s.asked + c.row;
+    const int64_t pos = s.at0 + c.row;
     c.row += s.row0;
     c.at = max(pos, (int64_t)0);
     if (j.rot.cos && c.at >= j.rot.positions) {
@@ -250,7 +250,7 @@ __device__ __forceinline__ Column column(const Job &j, const Seq &s, int kv_head
         if (j.status) atomicOr(j.status, CMPQ_STATUS_RANGE);
     }
     c.hi = (int)(j.causal ? min((int64_t)s.length, pos + 1) : (int64_t)s.length);
-    c.lo = j.window > 0 ? (int)max((int64_t)0, pos - j.window + 1) : 0;
+    c.lo = j.window > 0 ? (int)max((int64_t)0, pos - j.window + 1) : 0;  // may be past the last token that is not left out
     return c;
 }
 

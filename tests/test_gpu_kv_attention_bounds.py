@@ -65,3 +65,30 @@ def test_more_rows_than_the_bound_under_a_window(S, causal, most, beside):
         k, v = _tokens(s, i + 1, 3000)
         a, b = cu[i + 1], cu[i + 2]
         _near(out[a:b], R.attention(q[a:b], k, v, 0.125, causal, window)[0], v)
+
+
+@pytest.mark.parametrize("causal", [True, False])
+@pytest.mark.parametrize("window", [0, 40, 70, 4000])
+@pytest.mark.parametrize("rows", [1, 20, 70])
+def test_tokens_that_are_left_out_do_not_move_the_rows(S, rows, window, causal):
+    """A sequence of 300 tokens under bounds of 200 and 250, and of a table that ends at 256: its rows are the tokens
+    300 - rows .. 299 all the same, turned and masked as such."""
+    from paper_2410_13056_amd import binding as B
+    s = A.Setup(S, [300], 1, 64, 32, 4)
+    rotation = S.make_rotation(300, 64, device=DEV)
+    Q = torch.randn((rows, 2, 64), generator=torch.Generator(device=DEV).manual_seed(1), device=DEV).half() * 0.25
+    pos = 300 - rows + np.arange(rows)
+    q = R.turn(R.as_f32(Q), pos, R.as_f32(rotation.cos), R.as_f32(rotation.sin), False).astype(np.float64)
+    whole = s.table
+    for bound, pages in ((200, 10), (250, 10), (300, 8)):
+        s.table = whole[:, :pages].contiguous()
+        left = min(bound, pages * 32)
+        out, status = _call(S, s, Q, [0, rows], [300], rows, bound, rotation=rotation, causal=causal, window=window)
+        assert status == B.STATUS_RANGE
+        k, v = _tokens(s, 0, left)
+        for r in range(rows):
+            lo, hi = max(0, pos[r] - window + 1) if window else 0, min(left, pos[r] + 1) if causal else left
+            if lo >= hi:
+                assert (out[r] == 0).all()
+            else:
+                _near(out[r], R.attention(q[r:r + 1], k[lo:hi], v[lo:hi], 0.125, False, 0)[0][0], v)
