@@ -745,7 +745,9 @@ int cmpq_kv_read(const cmpq_kv_cache *cache, const cmpq_kv_rows *rows, const cmp
  * largest weight is kept apart).  A value scale below 2^-100 of the quotient of the two counts as that.  A query that holds
  * a NaN or an infinity gives NaN for its row and head alone.  The order of all additions depends on sizes, lengths and
  * the host bounds alone: results are reproducible bit for bit, and a row's do not depend on the other rows' queries.
- * Workspace: cmpq_kv_attention_workspace(job) (a function of the sizes, not of the pointers).
+ * Workspace: cmpq_kv_attention_workspace(job) (a function of the sizes, not of the pointers; 0 where they are refused).
+ * Limits: max_rows, ld_table and n_seq below 2^31, max_length below 2^31 - 32, q_heads <= 65535, n_rows * q_heads <= 2^32,
+ * min(n_rows, max_rows) * q_heads / kv_heads below 2^31 - 1024, 48 * n_seq * q_heads below 2^31.
  */
 typedef struct cmpq_kv_attention_job {
     cmpq_kv_cache cache;

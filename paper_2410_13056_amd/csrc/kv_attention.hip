@@ -928,11 +928,14 @@ struct Launches {
 // dims, 8000 tokens, 2 tiles 331 and one 292).
 constexpr int rows_tiles(int64_t c) { return c == 3 || c == 4 ? 3 : 1; }
 
+// A window that no length reaches is none.
+int64_t window_of(const cmpq_kv_attention_job *a) { return a->window > INT32_MAX ? 0 : a->window; }
+
 // Units that a sequence's rows see at most.
 int64_t most_units(const cmpq_kv_attention_job *a) {
-    const int64_t all = cdiv(a->max_length, kUnit);
-    if (a->window == 0) return all;
-    const int64_t seen = (a->window + a->max_rows) / kUnit + 2;  // of those of any place in a unit
+    const int64_t all = cdiv(a->max_length, kUnit), window = window_of(a);
+    if (window == 0) return all;
+    const int64_t seen = (window + a->max_rows) / kUnit + 2;  // of those of any place in a unit
     return seen < all ? seen : all;
 }
 
@@ -1003,16 +1006,25 @@ Launches plan_launches(const cmpq_kv_attention_job *a) {
     return l;
 }
 
-int check_job(const cmpq_kv_attention_job *a) {
-    if (!a) return CMPQ_EINVAL;
-    if (int rc = check_cache(a->cache)) return rc;
+// Sizes alone.  Columns of a tile, items of a join and workgroups are counted in 32 bits.
+int check_sizes(const cmpq_kv_attention_job *a) {
     if (a->n_seq < 0 || a->n_rows < 0 || a->max_rows < 0 || a->max_length < 0 || a->ld_table < 0 || a->window < 0)
         return CMPQ_EINVAL;
-    if (!serving_dtype(a->q_dtype) || (a->o_dtype != CMPQ_F16 && a->o_dtype != CMPQ_BF16)) return CMPQ_EINVAL;
-    if (a->q_heads < 1 || a->q_heads % a->cache.kv_heads) return CMPQ_EINVAL;
+    if (a->cache.kv_heads < 1 || a->q_heads < 1 || a->q_heads % a->cache.kv_heads) return CMPQ_EINVAL;
+    if (!cmpq_kv_page_bytes(a->cache.head_dim, a->cache.page)) return CMPQ_ESHAPE;
     if (a->n_seq > INT32_MAX || a->n_rows > INT32_MAX || a->max_length > INT32_MAX - kUnit || a->q_heads > 65535 ||
         a->ld_table > INT32_MAX || a->max_rows > INT32_MAX || a->n_rows * a->q_heads > ((int64_t)1 << 32))
         return CMPQ_ESHAPE;
+    const int64_t rows = a->max_rows < a->n_rows ? a->max_rows : a->n_rows;
+    if (rows * (a->q_heads / a->cache.kv_heads) > INT32_MAX - 1024 || a->n_seq * 48 * a->q_heads > INT32_MAX) return CMPQ_ESHAPE;
+    return CMPQ_OK;
+}
+
+int check_job(const cmpq_kv_attention_job *a) {
+    if (!a) return CMPQ_EINVAL;
+    if (int rc = check_cache(a->cache)) return rc;
+    if (!serving_dtype(a->q_dtype) || (a->o_dtype != CMPQ_F16 && a->o_dtype != CMPQ_BF16)) return CMPQ_EINVAL;
+    if (int rc = check_sizes(a)) return rc;
     return check_rotation(&a->rotation, a->cache.head_dim);
 }
 
@@ -1076,10 +1088,7 @@ size_t workspace_of(const Launches &l) {
 }  // namespace
 
 extern "C" size_t cmpq_kv_attention_workspace(const cmpq_kv_attention_job *a) {
-    if (!a || a->cache.kv_heads < 1 || a->q_heads < a->cache.kv_heads || a->n_seq < 0 || a->n_rows < 0 || a->max_rows < 0 ||
-        a->max_length < 0 || !cmpq_kv_page_bytes(a->cache.head_dim, a->cache.page))
-        return 0;
-    return workspace_of(plan_launches(a));
+    return a && check_sizes(a) == CMPQ_OK ? workspace_of(plan_launches(a)) : 0;
 }
 
 extern "C" int cmpq_kv_attention(const cmpq_kv_attention_job *a, void *ws, size_t ws_bytes, void *stream) {
@@ -1087,7 +1096,7 @@ extern "C" int cmpq_kv_attention(const cmpq_kv_attention_job *a, void *ws, size_
     if (a->n_seq == 0 || a->n_rows == 0 || a->max_rows == 0) return CMPQ_OK;
     if (!a->page_table || !a->lengths || !a->cu_rows || !a->Q.ptr || !a->O.ptr) return CMPQ_EINVAL;
     const Launches l = plan_launches(a);
-    if (l.few.grid > INT32_MAX || l.rows.grid > INT32_MAX || a->n_seq * 48 * a->q_heads > INT32_MAX) return CMPQ_ESHAPE;
+    if (l.few.grid > INT32_MAX || l.rows.grid > INT32_MAX) return CMPQ_ESHAPE;
     if (!ws || reinterpret_cast<uintptr_t>(ws) % 256 || ws_bytes < workspace_of(l)) return CMPQ_EWORKSPACE;
     WsCarver w(ws);
     Job j = {};
@@ -1097,7 +1106,7 @@ extern "C" int cmpq_kv_attention(const cmpq_kv_attention_job *a, void *ws, size_
     j.max_length = a->cache.n_pages > 0 ? a->max_length : 0;
     j.Q = a->Q, j.O = a->O, j.q_dtype = a->q_dtype, j.o_dtype = a->o_dtype, j.q_heads = a->q_heads;
     j.group = a->q_heads / a->cache.kv_heads;
-    j.scale = a->softmax_scale, j.causal = a->causal, j.window = a->window, j.rot = a->rotation, j.status = a->status;
+    j.scale = a->softmax_scale, j.causal = a->causal, j.window = window_of(a), j.rot = a->rotation, j.status = a->status;
     hipStream_t st = static_cast<hipStream_t>(stream);
     switch (l.dp / 32) {
         case 1: launch<1>(j, l, w, st); break;
