@@ -1093,7 +1093,8 @@ extern "C" size_t cmpq_kv_attention_workspace(const cmpq_kv_attention_job *a) {
 
 extern "C" int cmpq_kv_attention(const cmpq_kv_attention_job *a, void *ws, size_t ws_bytes, void *stream) {
     if (int rc = check_job(a)) return rc;
-    if (a->n_seq == 0 || a->n_rows == 0 || a->max_rows == 0) return CMPQ_OK;
+    if (a->n_seq == 0 || a->n_rows == 0 || a->max_rows == 0)
+        return cmpq_flag_named_rows(a->cu_rows, a->n_seq, a->status, static_cast<hipStream_t>(stream));
     if (!a->page_table || !a->lengths || !a->cu_rows || !a->Q.ptr || !a->O.ptr) return CMPQ_EINVAL;
     const Launches l = plan_launches(a);
     if (l.few.grid > INT32_MAX || l.rows.grid > INT32_MAX) return CMPQ_ESHAPE;

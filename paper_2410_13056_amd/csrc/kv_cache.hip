@@ -374,7 +374,19 @@ dim3 page_grid(const cmpq_kv_cache &c, const cmpq_kv_rows &r) {
     return dim3((unsigned)(most < r.n_rows ? most : r.n_rows), (unsigned)c.kv_heads, 2);
 }
 
+__global__ __launch_bounds__(64) void named_rows_kernel(const int32_t *cu, int64_t n_seq, int32_t *status) {
+    for (int64_t i = threadIdx.x; i < n_seq; i += 64)
+        if (cu[i + 1] > cu[i]) atomicOr(status, CMPQ_STATUS_RANGE);
+}
+
 }  // namespace
+
+int cmpq_flag_named_rows(const int32_t *cu, int64_t n_seq, int32_t *status, hipStream_t stream) {
+    if (!status || !cu || n_seq < 1) return CMPQ_OK;
+    named_rows_kernel<<<1, 64, 0, stream>>>(cu, n_seq, status);
+    CMPQ_LAUNCH_CHECK();
+    return CMPQ_OK;
+}
 
 extern "C" size_t cmpq_kv_page_bytes(int head_dim, int page) {
     if (head_dim < 1 || head_dim > 256 || page < 32 || page > 1024 || page % 32) return 0;
@@ -386,7 +398,8 @@ extern "C" int cmpq_kv_append(const cmpq_kv_cache *cache, const cmpq_kv_rows *ro
                               void *stream) {
     if (int rc = check_rows(cache, rows, K, V, dtype)) return rc;
     if (int rc = check_rotation(rotation, cache->head_dim)) return rc;
-    if (rows->n_seq == 0 || rows->n_rows == 0 || rows->ld_table == 0) return CMPQ_OK;
+    if (rows->n_seq == 0 || rows->n_rows == 0 || rows->ld_table == 0)
+        return cmpq_flag_named_rows(rows->cu_rows, rows->n_seq, status, static_cast<hipStream_t>(stream));
     const cmpq_rotation rot = rotation ? *rotation : cmpq_rotation{};
     const dim3 grid = page_grid(*cache, *rows);
     hipStream_t st = static_cast<hipStream_t>(stream);
@@ -407,7 +420,8 @@ extern "C" int cmpq_kv_append(const cmpq_kv_cache *cache, const cmpq_kv_rows *ro
 extern "C" int cmpq_kv_read(const cmpq_kv_cache *cache, const cmpq_kv_rows *rows, const cmpq_heads *K,
                             const cmpq_heads *V, int dtype, int32_t *status, void *stream) {
     if (int rc = check_rows(cache, rows, K, V, dtype)) return rc;
-    if (rows->n_seq == 0 || rows->n_rows == 0 || rows->ld_table == 0) return CMPQ_OK;
+    if (rows->n_seq == 0 || rows->n_rows == 0 || rows->ld_table == 0)
+        return cmpq_flag_named_rows(rows->cu_rows, rows->n_seq, status, static_cast<hipStream_t>(stream));
     const dim3 grid = page_grid(*cache, *rows);
     hipStream_t st = static_cast<hipStream_t>(stream);
     if (dtype == CMPQ_F16) read_kernel<_Float16, 256><<<grid, 256, 0, st>>>(*cache, *rows, *K, *V, status);

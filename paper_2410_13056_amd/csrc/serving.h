@@ -144,3 +144,6 @@ static inline int check_cache(const cmpq_kv_cache &c) {
     if (reinterpret_cast<uintptr_t>(c.k_codes) % 16 || reinterpret_cast<uintptr_t>(c.v_codes) % 16) return CMPQ_EINVAL;
     return CMPQ_OK;
 }
+
+// For calls that do no row: CMPQ_STATUS_RANGE where a sequence names one all the same.
+int cmpq_flag_named_rows(const int32_t *cu, int64_t n_seq, int32_t *status, hipStream_t stream);

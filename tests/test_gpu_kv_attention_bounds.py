@@ -92,3 +92,25 @@ def test_tokens_that_are_left_out_do_not_move_the_rows(S, rows, window, causal):
                 assert (out[r] == 0).all()
             else:
                 _near(out[r], R.attention(q[r:r + 1], k[lo:hi], v[lo:hi], 0.125, False, 0)[0][0], v)
+
+
+@pytest.mark.parametrize("seqs", [1, 70])
+def test_calls_without_room_for_rows_that_are_named_are_flagged(S, seqs):
+    from paper_2410_13056_amd import binding as B
+    s = A.Setup(S, [40] * seqs, 2, 64, 32, 3)
+    none, one = [0] * (seqs + 1), [0] * seqs + [1]
+    Q = torch.randn((1, 4, 64), device=DEV).half()
+    for cu, flag in ((none, 0), (one, B.STATUS_RANGE)):
+        for q, most in ((Q, 0), (Q[:0], 0), (Q[:0], 1)):
+            out, status = _call(S, s, q, cu, [40] * seqs, most, 40)
+            assert status == flag and (out == 5).all()
+        K, held = torch.randn((1, 2, 64), device=DEV), A._i32([3] * seqs)
+        for x, table in ((K[:0], s.table), (K, s.table[:, :0].contiguous())):
+            status = torch.zeros(1, dtype=torch.int32, device=DEV)
+            S.kv_append(s.cache, x, x, table, held, A._i32(cu), status=status)
+            torch.cuda.synchronize()
+            assert status.item() == flag
+            status.zero_()
+            B.kv_read(s.cache._view, table, held, A._i32(cu), x, x.clone(), status)
+            torch.cuda.synchronize()
+            assert status.item() == flag
