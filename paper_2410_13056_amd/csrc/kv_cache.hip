@@ -44,7 +44,7 @@ __device__ __forceinline__ Page find_page(const cmpq_kv_rows &r, int page, int64
             bad |= first < 0;
             if (first < 0) n = 0;
             const int64_t room = r.ld_table * page - first;  // tokens that the table has pages for
-            if (n > room) {
+            if (n > 0 && n > room) {
                 bad = true;
                 n = max(room, (int64_t)0);
             }
