@@ -8,7 +8,8 @@ weights (`pipeline.lut_matvec`, `pipeline.group_products`).
 * `attention_block`: the three together, as a decoder layer's attention runs them.
 
 Everything is enqueued on the current stream and nothing synchronises; there is no gradient, since
-codes have none.
+codes have none.  `status` ([1] int32, cleared by the caller) collects the flags of `binding.STATUS_*`: codes have no NaN
+and no infinity (they become 0 and +-127 codes), so without it such an input goes unnoticed.
 """
 from __future__ import annotations
 
@@ -152,11 +153,12 @@ def kv_attention(cache: KvCache, Q: torch.Tensor, page_table: torch.Tensor, leng
 Layer = Union[Int8Weight, P.Deployed, Callable[[torch.Tensor], torch.Tensor]]
 
 
-def apply_layer(layer: Layer, X: torch.Tensor, ws: B.Workspace) -> torch.Tensor:
+def apply_layer(layer: Layer, X: torch.Tensor, ws: B.Workspace, status: Optional[torch.Tensor] = None) -> torch.Tensor:
     """X [m, d_in] times a layer in whichever form it was prepared: 8-bit integers, the mixed-precision tables
-    (fp32 out of FP16 in), or any function."""
+    (fp32 out of FP16 in), or any function.  The last two carry a NaN or an infinity on into their outputs; 8-bit
+    integers raise it in `status`."""
     if isinstance(layer, Int8Weight):
-        return int8_product(layer, X, ws, out_dtype=torch.float32)
+        return int8_product(layer, X, ws, out_dtype=torch.float32, status=status)
     if isinstance(layer, P.Deployed):
         return P.lut_matvec(layer, X.to(torch.float16), ws)
     return layer(X)
@@ -169,10 +171,10 @@ def attention_block(cache: KvCache, X: torch.Tensor, q: Layer, k: Layer, v: Laye
     """A decoder layer's attention for new tokens X [rows, hidden] of several sequences (see `kv_append`; lengths[i] =
     held[i] + the sequence's rows): the three projections, keys and values into the cache, attention over it, the
     output projection [rows, hidden].  The projections may be of different kinds, for instance queries and outputs in
-    mixed precision and the short key and value layers in 8 bits."""
+    mixed precision and the short key and value layers in 8 bits.  `status` collects the flags of all of them."""
     rows = X.shape[0]
-    Q, K, V = (apply_layer(layer, X, ws).view(rows, -1, cache.head_dim) for layer in (q, k, v))
+    Q, K, V = (apply_layer(layer, X, ws, status).view(rows, -1, cache.head_dim) for layer in (q, k, v))
     kv_append(cache, K, V, page_table, held, cu_rows, rotation, status)
     O = kv_attention(cache, Q, page_table, lengths, cu_rows, max_rows, max_length, ws, causal=causal, window=window,
                      rotation=rotation, out_dtype=torch.float16, status=status)
-    return apply_layer(o, O.view(rows, -1), ws)
+    return apply_layer(o, O.view(rows, -1), ws, status)
