@@ -167,14 +167,20 @@ def apply_layer(layer: Layer, X: torch.Tensor, ws: B.Workspace, status: Optional
 def attention_block(cache: KvCache, X: torch.Tensor, q: Layer, k: Layer, v: Layer, o: Layer, page_table: torch.Tensor,
                     held: torch.Tensor, lengths: torch.Tensor, cu_rows: torch.Tensor, max_rows: int,
                     max_length: int, ws: B.Workspace, rotation: Optional[Rotation] = None, causal: bool = True,
-                    window: int = 0, status: Optional[torch.Tensor] = None) -> torch.Tensor:
+                    window: int = 0, status: Optional[torch.Tensor] = None,
+                    attention_dtype: Optional[torch.dtype] = None) -> torch.Tensor:
     """A decoder layer's attention for new tokens X [rows, hidden] of several sequences (see `kv_append`; lengths[i] =
     held[i] + the sequence's rows): the three projections, keys and values into the cache, attention over it, the
     output projection [rows, hidden].  The projections may be of different kinds, for instance queries and outputs in
-    mixed precision and the short key and value layers in 8 bits.  `status` collects the flags of all of them."""
+    mixed precision and the short key and value layers in 8 bits.  `status` collects the flags of all of them.
+    `attention_dtype`, float16 or bfloat16: what the attention hands to `o`.  By default bfloat16 for a bfloat16 X, whose
+    values may pass float16's range, unless `o` is in mixed precision, which reads float16; else float16."""
+    if attention_dtype is None:
+        wide = X.dtype == torch.bfloat16 and not isinstance(o, P.Deployed)
+        attention_dtype = torch.bfloat16 if wide else torch.float16
     rows = X.shape[0]
     Q, K, V = (apply_layer(layer, X, ws, status).view(rows, -1, cache.head_dim) for layer in (q, k, v))
     kv_append(cache, K, V, page_table, held, cu_rows, rotation, status)
     O = kv_attention(cache, Q, page_table, lengths, cu_rows, max_rows, max_length, ws, causal=causal, window=window,
-                     rotation=rotation, out_dtype=torch.float16, status=status)
+                     rotation=rotation, out_dtype=attention_dtype, status=status)
     return apply_layer(o, O.view(rows, -1), ws, status)

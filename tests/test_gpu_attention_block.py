@@ -60,3 +60,33 @@ def test_inputs_that_are_no_finite_numbers_are_flagged(S, kinds, new, value):
     X[0, 3] = value
     b.step(X[:2], [1, 1])
     assert b.status.item() == B.STATUS_NONFINITE
+
+
+@pytest.mark.parametrize("kinds", ["ffff", "fff8", "8888"])
+def test_values_beyond_float16_of_a_bfloat16_model(S, kinds):
+    """Values of some millions: finite, and right.  Rounded: X's codes not at all (the same codes on both sides), the attention's
+    output to bfloat16 (2^-9 of itself, and once more as 8-bit codes of the largest of a row where `o` has them, 2^-8 of the
+    largest, at most 4 times the row's norm / sqrt(256)), its weights to FP16."""
+    import numpy as np
+    b = Block(S, "ffff")
+    b.W["v"] *= 0
+    b.W["v"] += torch.randn((KV * DIM, HIDDEN), generator=torch.Generator(device=DEV).manual_seed(2), device=DEV).half() * 2048
+    b.layers = {n: S.prepare_int8(w) if kind == "8" else (lambda x, w=w: x.float() @ w.float().t()) for (n, w), kind in zip(b.W.items(), kinds)}
+    new = [30, 12]
+    X = torch.randn((42, HIDDEN), generator=torch.Generator(device=DEV).manual_seed(3), device=DEV).bfloat16() * 64
+    b.layers["q"] = lambda x: x.float() @ b.W["q"].float().t() / 64
+    got = b.step(X, new)
+    assert got.isfinite().all() and b.status.item() == 0
+    q, want, at = R.as_f32(b.layers["q"](X)).reshape(-1, HEADS, DIM), [], 0
+    for i, n in enumerate(new):
+        k, v = (t.double().cpu().numpy() for t in S.kv_read(b.cache, b.table[i:i + 1].contiguous(), _i32([0]), _i32([0, n]), n, torch.float32))
+        assert np.abs(v).max() > 1e5
+        x = R.turn(q[at:at + n], np.arange(n), R.as_f32(b.rot.cos), R.as_f32(b.rot.sin), False)
+        want.append(R.attention(x.astype(np.float64), k, v, DIM ** -0.5, True, 0)[0])
+        at += n
+    want = np.concatenate(want).reshape(42, -1) @ b.W["o"].double().cpu().numpy().T
+    rel = np.linalg.norm(got.double().cpu().numpy() - want) / np.linalg.norm(want)
+    assert rel <= 2.0 ** -8 + (2.0 ** -6 if kinds[3] == "8" else 0), rel
+    b.held = [0, 0]
+    half = b.step(X, new, attention_dtype=torch.float16)                # as asked for: infinite
+    assert kinds[3] == "8" and b.status.item() or not half.isfinite().all()
