@@ -164,6 +164,12 @@ def apply_layer(layer: Layer, X: torch.Tensor, ws: B.Workspace, status: Optional
     return layer(X)
 
 
+def _as_heads(Y: torch.Tensor, head_dim: int) -> torch.Tensor:
+    """[rows, heads * head_dim], of no rows as well, as [rows, heads, head_dim] with unit stride along the dims."""
+    Y = Y if Y.stride(1) == 1 else Y.contiguous()
+    return Y.reshape(Y.shape[0], Y.shape[1] // head_dim, head_dim)
+
+
 def attention_block(cache: KvCache, X: torch.Tensor, q: Layer, k: Layer, v: Layer, o: Layer, page_table: torch.Tensor,
                     held: torch.Tensor, lengths: torch.Tensor, cu_rows: torch.Tensor, max_rows: int,
                     max_length: int, ws: B.Workspace, rotation: Optional[Rotation] = None, causal: bool = True,
@@ -178,9 +184,8 @@ def attention_block(cache: KvCache, X: torch.Tensor, q: Layer, k: Layer, v: Laye
     if attention_dtype is None:
         wide = X.dtype == torch.bfloat16 and not isinstance(o, P.Deployed)
         attention_dtype = torch.bfloat16 if wide else torch.float16
-    rows = X.shape[0]
-    Q, K, V = (apply_layer(layer, X, ws, status).view(rows, -1, cache.head_dim) for layer in (q, k, v))
+    Q, K, V = (_as_heads(apply_layer(layer, X, ws, status), cache.head_dim) for layer in (q, k, v))
     kv_append(cache, K, V, page_table, held, cu_rows, rotation, status)
     O = kv_attention(cache, Q, page_table, lengths, cu_rows, max_rows, max_length, ws, causal=causal, window=window,
                      rotation=rotation, out_dtype=attention_dtype, status=status)
-    return apply_layer(o, O.view(rows, -1), ws, status)
+    return apply_layer(o, O.flatten(1), ws, status)

@@ -90,3 +90,16 @@ def test_values_beyond_float16_of_a_bfloat16_model(S, kinds):
     b.held = [0, 0]
     half = b.step(X, new, attention_dtype=torch.float16)                # as asked for: infinite
     assert kinds[3] == "8" and b.status.item() or not half.isfinite().all()
+
+
+@pytest.mark.parametrize("kinds", ["8888", "ffff"])
+def test_no_rows_and_layers_whose_outputs_are_views(S, kinds):
+    b = Block(S, kinds)
+    assert b.step(torch.empty((0, HIDDEN), device=DEV).half(), [0, 0]).shape == (0, HIDDEN)
+    X = torch.randn((9, HIDDEN), device=DEV).half()
+    want = b.step(X, [4, 5])
+    b.held = [0, 0]
+    plain = dict(b.layers)
+    for n in b.layers:                                                   # rows that lie apart, and columns
+        b.layers[n] = lambda x, n=n: S.apply_layer(plain[n], x, b.ws).t().contiguous().t()
+    assert torch.equal(b.step(X, [4, 5]), want) and b.status.item() == 0
