@@ -750,9 +750,9 @@ def kv_cache_view(k: torch.Tensor, v: torch.Tensor, k_scale: torch.Tensor, v_sca
             raise ValueError("codes are contiguous uint8 [n_pages, kv_heads, kv_page_bytes], scales float32")
     view = KvCacheView(_ptr(k), _ptr(v), _ptr(k_scale), _ptr(v_scale), n_pages, heads, int(head_dim), int(page))
     # what the calls on this cache are filled into, one call at a time
-    view.keep, view.ref = (k, v, k_scale, v_scale), ctypes.byref(view)
+    # (no ctypes.byref of it: one that a structure keeps of itself is a cycle that Python's collector does not see)
+    view.keep = (k, v, k_scale, v_scale)
     view.rows, view.K, view.V, view.job = KvRows(), Heads(), Heads(), KvAttentionJob(cache=view)
-    view.rows_ref, view.K_ref, view.V_ref, view.job_ref = (ctypes.byref(t) for t in (view.rows, view.K, view.V, view.job))
     view.Q, view.O = view.job.Q, view.job.O                        # the job's own
     return view
 
@@ -762,7 +762,7 @@ def rotation_view(cos: torch.Tensor, sin: torch.Tensor, interleaved: bool) -> Ro
         if t.dtype != torch.float32 or t.dim() != 2 or not t.is_contiguous() or t.shape != cos.shape:
             raise ValueError("cos and sin must be contiguous float32 [positions, dims / 2]")
     view = RotationView(_ptr(cos), _ptr(sin), cos.shape[0], 2 * cos.shape[1], int(bool(interleaved)))
-    view.keep, view.ref = (cos, sin), ctypes.byref(view)
+    view.keep = (cos, sin)
     return view
 
 
@@ -804,8 +804,7 @@ def kv_append(cache: KvCacheView, page_table: torch.Tensor, first: torch.Tensor,
               V: torch.Tensor, rotation: Optional[RotationView] = None, status: Optional[torch.Tensor] = None) -> None:
     """`cmpq_kv_append`: K and V [rows, kv_heads, head_dim] behind the first[i] tokens of each sequence."""
     dtype = _fill_rows(cache, page_table, first, cu_rows, K, V)
-    rc = _lib.cmpq_kv_append(cache.ref, cache.rows_ref, cache.K_ref, cache.V_ref, dtype,
-                             None if rotation is None else rotation.ref, _ptr(status), _stream())
+    rc = _lib.cmpq_kv_append(cache, cache.rows, cache.K, cache.V, dtype, rotation, _ptr(status), _stream())
     if rc:
         _check(rc, "cmpq_kv_append")
 
@@ -814,7 +813,7 @@ def kv_read(cache: KvCacheView, page_table: torch.Tensor, first: torch.Tensor, c
             V: torch.Tensor, status: Optional[torch.Tensor] = None) -> None:
     """`cmpq_kv_read`: the values that tokens first[i], first[i]+1, ... of each sequence stand for, into K and V."""
     dtype = _fill_rows(cache, page_table, first, cu_rows, K, V)
-    rc = _lib.cmpq_kv_read(cache.ref, cache.rows_ref, cache.K_ref, cache.V_ref, dtype, _ptr(status), _stream())
+    rc = _lib.cmpq_kv_read(cache, cache.rows, cache.K, cache.V, dtype, _ptr(status), _stream())
     if rc:
         _check(rc, "cmpq_kv_read")
 
@@ -841,9 +840,9 @@ def kv_attention(cache: KvCacheView, page_table: torch.Tensor, lengths: torch.Te
     j.rotation = _NO_ROTATION if rotation is None else rotation
     for _ in range(2):              # asks for the workspace's size only where what is there does not do
         buf = ws.buf
-        rc = _lib.cmpq_kv_attention(cache.job_ref, buf.data_ptr(), buf.numel(), _stream())
+        rc = _lib.cmpq_kv_attention(j, buf.data_ptr(), buf.numel(), _stream())
         if rc != EWORKSPACE:
             break
-        ws.get(_lib.cmpq_kv_attention_workspace(cache.job_ref))
+        ws.get(_lib.cmpq_kv_attention_workspace(j))
     if rc:
         _check(rc, "cmpq_kv_attention")
