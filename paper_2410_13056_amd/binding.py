@@ -749,11 +749,8 @@ def kv_cache_view(k: torch.Tensor, v: torch.Tensor, k_scale: torch.Tensor, v_sca
         if t.dtype != dt or tuple(t.shape) != shape or not t.is_contiguous():
             raise ValueError("codes are contiguous uint8 [n_pages, kv_heads, kv_page_bytes], scales float32")
     view = KvCacheView(_ptr(k), _ptr(v), _ptr(k_scale), _ptr(v_scale), n_pages, heads, int(head_dim), int(page))
-    # what the calls on this cache are filled into, one call at a time
     # (no ctypes.byref of it: one that a structure keeps of itself is a cycle that Python's collector does not see)
     view.keep = (k, v, k_scale, v_scale)
-    view.rows, view.K, view.V, view.job = KvRows(), Heads(), Heads(), KvAttentionJob(cache=view)
-    view.Q, view.O = view.job.Q, view.job.O                        # the job's own
     return view
 
 
@@ -766,14 +763,15 @@ def rotation_view(cos: torch.Tensor, sin: torch.Tensor, interleaved: bool) -> Ro
     return view
 
 
-def _heads(view: Heads, t: torch.Tensor, n_heads: int, head_dim: int) -> int:
-    """Fills in a tensor [rows, heads, dims] of any row and head stride; the number of rows."""
+# A call's arguments are its own structures: other threads may be in calls on the same cache.
+
+def _heads(t: torch.Tensor, n_heads: int, head_dim: int) -> Heads:
+    """A tensor [rows, heads, dims] of any row and head stride."""
     shape = t.shape
     if len(shape) != 3 or shape[1] != n_heads or shape[2] != head_dim or (head_dim > 1 and t.stride(2) != 1):
         raise ValueError(f"expected [rows, {n_heads}, {head_dim}] with unit stride along the dims")
-    view.ptr = _ptr(t)
-    view.row_stride, view.head_stride, _ = t.stride()
-    return shape[0]
+    row_stride, head_stride, _ = t.stride()
+    return Heads(_ptr(t), row_stride, head_stride)
 
 
 def _i32_table(t: torch.Tensor, shape: tuple, what: str) -> int:
@@ -788,23 +786,23 @@ def _table_shape(page_table: torch.Tensor):
     return page_table.shape
 
 
-def _fill_rows(cache: KvCacheView, page_table: torch.Tensor, first: torch.Tensor, cu_rows: torch.Tensor, K: torch.Tensor,
-               V: torch.Tensor) -> int:
-    n = _heads(cache.K, K, cache.kv_heads, cache.head_dim)
-    if _heads(cache.V, V, cache.kv_heads, cache.head_dim) != n or K.dtype != V.dtype:
+def _row_args(cache: KvCacheView, page_table: torch.Tensor, first: torch.Tensor, cu_rows: torch.Tensor, K: torch.Tensor,
+              V: torch.Tensor):
+    """What append and read are handed: rows, K, V, dtype."""
+    heads, dims = cache.kv_heads, cache.head_dim
+    k, v = _heads(K, heads, dims), _heads(V, heads, dims)
+    if V.shape[0] != K.shape[0] or K.dtype != V.dtype:
         raise ValueError("K and V must have the same rows and dtype")
     n_seq, ld = shape = _table_shape(page_table)
-    r = cache.rows
-    r.page_table, r.ld_table, r.n_seq, r.n_rows = _i32_table(page_table, shape, "page_table"), ld, n_seq, n
-    r.first, r.cu_rows = _i32_table(first, (n_seq,), "first"), _i32_table(cu_rows, (n_seq + 1,), "cu_rows")
-    return serving_dtype(K.dtype)
+    rows = KvRows(_i32_table(page_table, shape, "page_table"), ld, _i32_table(first, (n_seq,), "first"),
+                  _i32_table(cu_rows, (n_seq + 1,), "cu_rows"), n_seq, K.shape[0])
+    return rows, k, v, serving_dtype(K.dtype)
 
 
 def kv_append(cache: KvCacheView, page_table: torch.Tensor, first: torch.Tensor, cu_rows: torch.Tensor, K: torch.Tensor,
               V: torch.Tensor, rotation: Optional[RotationView] = None, status: Optional[torch.Tensor] = None) -> None:
     """`cmpq_kv_append`: K and V [rows, kv_heads, head_dim] behind the first[i] tokens of each sequence."""
-    dtype = _fill_rows(cache, page_table, first, cu_rows, K, V)
-    rc = _lib.cmpq_kv_append(cache, cache.rows, cache.K, cache.V, dtype, rotation, _ptr(status), _stream())
+    rc = _lib.cmpq_kv_append(cache, *_row_args(cache, page_table, first, cu_rows, K, V), rotation, _ptr(status), _stream())
     if rc:
         _check(rc, "cmpq_kv_append")
 
@@ -812,8 +810,7 @@ def kv_append(cache: KvCacheView, page_table: torch.Tensor, first: torch.Tensor,
 def kv_read(cache: KvCacheView, page_table: torch.Tensor, first: torch.Tensor, cu_rows: torch.Tensor, K: torch.Tensor,
             V: torch.Tensor, status: Optional[torch.Tensor] = None) -> None:
     """`cmpq_kv_read`: the values that tokens first[i], first[i]+1, ... of each sequence stand for, into K and V."""
-    dtype = _fill_rows(cache, page_table, first, cu_rows, K, V)
-    rc = _lib.cmpq_kv_read(cache, cache.rows, cache.K, cache.V, dtype, _ptr(status), _stream())
+    rc = _lib.cmpq_kv_read(cache, *_row_args(cache, page_table, first, cu_rows, K, V), _ptr(status), _stream())
     if rc:
         _check(rc, "cmpq_kv_read")
 
@@ -829,15 +826,11 @@ def kv_attention(cache: KvCacheView, page_table: torch.Tensor, lengths: torch.Te
     if O.shape != Q.shape or Q.dim() != 3:
         raise ValueError("Q and O must be [rows, q_heads, head_dim]")
     n_seq, ld = shape = _table_shape(page_table)
-    j, heads = cache.job, Q.shape[1]
-    j.page_table, j.ld_table, j.n_seq = _i32_table(page_table, shape, "page_table"), ld, n_seq
-    j.lengths, j.cu_rows = _i32_table(lengths, (n_seq,), "lengths"), _i32_table(cu_rows, (n_seq + 1,), "cu_rows")
-    j.n_rows = _heads(cache.Q, Q, heads, cache.head_dim)
-    _heads(cache.O, O, heads, cache.head_dim)
-    j.q_dtype, j.o_dtype, j.q_heads = serving_dtype(Q.dtype), serving_dtype(O.dtype), heads
-    j.max_rows, j.max_length, j.window = max_rows, max_length, window
-    j.softmax_scale, j.causal, j.status = softmax_scale, 1 if causal else 0, _ptr(status)
-    j.rotation = _NO_ROTATION if rotation is None else rotation
+    heads, dims = Q.shape[1], cache.head_dim
+    j = KvAttentionJob(cache, _i32_table(page_table, shape, "page_table"), ld, _i32_table(lengths, (n_seq,), "lengths"),
+                       _i32_table(cu_rows, (n_seq + 1,), "cu_rows"), n_seq, Q.shape[0], max_rows, max_length,
+                       _heads(Q, heads, dims), _heads(O, heads, dims), serving_dtype(Q.dtype), serving_dtype(O.dtype), heads,
+                       softmax_scale, 1 if causal else 0, window, _NO_ROTATION if rotation is None else rotation, _ptr(status))
     for _ in range(2):              # asks for the workspace's size only where what is there does not do
         buf = ws.buf
         rc = _lib.cmpq_kv_attention(j, buf.data_ptr(), buf.numel(), _stream())

@@ -82,8 +82,7 @@ def make_rotation(positions: int, dims: int, base: float = 10000.0, interleaved:
 @dataclasses.dataclass
 class KvCache:
     """Keys and values in pages of `page` tokens, 8 bits a value, a scale per page and head (device tensors).
-    Which page belongs to which sequence is the caller's: every call takes a table of them.  One call on a cache object
-    at a time: its arguments are filled into structures that the object keeps."""
+    Which page belongs to which sequence is the caller's: every call takes a table of them."""
     k: torch.Tensor         # uint8 [n_pages, kv_heads, kv_page_bytes(head_dim, page)]: code + 128
     v: torch.Tensor
     k_scale: torch.Tensor   # fp32 [n_pages, kv_heads]

@@ -33,3 +33,49 @@ def test_dropped_objects_give_their_memory_back(S):
         del thing
         gc.collect()
         assert [r() for r in held] == [None] * len(held), names
+
+
+def _calls(S, cache, n):
+    """Append, read and attention with n rows."""
+    i32 = lambda *v: torch.tensor(v, dtype=torch.int32)
+    x, table, zero, cu = torch.zeros((n, 2, 64)), torch.zeros((1, n), dtype=torch.int32), i32(0), i32(0, n)
+    return {"append": lambda: S.kv_append(cache, x, x, table, zero, cu),
+            "read": lambda: S.kv_read(cache, table, zero, cu, n, torch.float32),
+            "attention": lambda: S.kv_attention(cache, x, table, zero, cu, n, n, ws=_NoWorkspace())}
+
+
+class _NoWorkspace:
+    buf = torch.empty(0, dtype=torch.uint8)
+
+
+@pytest.mark.parametrize("kind", ["append", "read", "attention"])
+def test_threads_in_calls_on_one_cache_have_their_own_arguments(S, monkeypatch, kind):
+    """Two threads are in the library at once; each of its two calls reads its arguments when both have been handed them."""
+    import threading
+    from paper_2410_13056_amd import binding as B
+    meet, seen = threading.Barrier(2), {}
+
+    class Library:
+        def __getattr__(self, name):
+            def call(*args):
+                meet.wait(20)
+                got = args[0] if name == "cmpq_kv_attention" else args[1]
+                got = getattr(got, "_obj", got)
+                seen[threading.get_ident()] = (got.n_rows, got.ld_table)
+                meet.wait(20)
+                return 0
+            return call
+
+    cache, want, errors = S.make_cache(8, 2, 64, 32, "cpu"), {}, []
+    monkeypatch.setattr(B, "_lib", Library())
+
+    def run(n):
+        want[threading.get_ident()] = (n, n)
+        try:
+            _calls(S, cache, n)[kind]()
+        except Exception as e:
+            errors.append(e)
+    threads = [threading.Thread(target=run, args=(n,)) for n in (3, 5)]
+    [t.start() for t in threads]
+    [t.join() for t in threads]
+    assert not errors and seen == want
