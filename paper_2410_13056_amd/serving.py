@@ -22,18 +22,40 @@ from . import binding as B
 from . import pipeline as P
 
 
+class _Kept:
+    """An object whose fields calls are handed in a form that `_make` gives; that is made once, and again after a field is
+    assigned.  Copies make their own."""
+
+    def __post_init__(self):
+        self._args                          # refuses fields that do not fit
+
+    @property
+    def _args(self):
+        args = self.__dict__.get("_made")
+        if args is None:
+            args = self.__dict__["_made"] = self._make()
+        return args
+
+    def __setattr__(self, name, value):
+        self.__dict__[name] = value
+        self.__dict__.pop("_made", None)
+
+    def __getstate__(self):
+        return {k: v for k, v in self.__dict__.items() if k != "_made"}
+
+
 # ---- products --------------------------------------------------------------------------------
 
 @dataclasses.dataclass
-class Int8Weight:
+class Int8Weight(_Kept):
     """A linear layer as `int8_product` reads it (device tensors)."""
     d_in: int
     d_out: int
     codes: torch.Tensor     # int8, in the order of the matrix instruction's operands
     scale: torch.Tensor     # [d_out] fp32
 
-    def __post_init__(self):
-        self._call = B.Int8ProductCall(self.d_in, self.d_out, self.codes, self.scale)
+    def _make(self) -> B.Int8ProductCall:
+        return B.Int8ProductCall(self.d_in, self.d_out, self.codes, self.scale)
 
 
 def prepare_int8(W: torch.Tensor, status: Optional[torch.Tensor] = None) -> Int8Weight:
@@ -52,22 +74,22 @@ def int8_product(w: Int8Weight, X: torch.Tensor, ws: Optional[B.Workspace] = Non
     defaults to X's."""
     if out is None:
         out = torch.empty((X.shape[0], w.d_out), dtype=out_dtype or X.dtype, device=X.device)
-    w._call(X, out, ws or B.Workspace(X.device), status)
+    w._args(X, out, ws or B.Workspace(X.device), status)
     return out
 
 
 # ---- the cache -------------------------------------------------------------------------------
 
 @dataclasses.dataclass
-class Rotation:
+class Rotation(_Kept):
     """Turning by position: tables [positions, dims / 2] of the pairs' cosines and sines; the pairs are (j, j + dims / 2)
     of a head's first `dims` dims, or (2 j, 2 j + 1) where `interleaved`."""
     cos: torch.Tensor
     sin: torch.Tensor
     interleaved: bool = False
 
-    def __post_init__(self):
-        self._view = B.rotation_view(self.cos, self.sin, self.interleaved)
+    def _make(self) -> B.RotationView:
+        return B.rotation_view(self.cos, self.sin, self.interleaved)
 
 
 def make_rotation(positions: int, dims: int, base: float = 10000.0, interleaved: bool = False,
@@ -80,7 +102,7 @@ def make_rotation(positions: int, dims: int, base: float = 10000.0, interleaved:
 
 
 @dataclasses.dataclass
-class KvCache:
+class KvCache(_Kept):
     """Keys and values in pages of `page` tokens, 8 bits a value, a scale per page and head (device tensors).
     Which page belongs to which sequence is the caller's: every call takes a table of them."""
     k: torch.Tensor         # uint8 [n_pages, kv_heads, kv_page_bytes(head_dim, page)]: code + 128
@@ -90,8 +112,12 @@ class KvCache:
     page: int
     head_dim: int
 
-    def __post_init__(self):
-        self._view = B.kv_cache_view(self.k, self.v, self.k_scale, self.v_scale, self.page, self.head_dim)
+    def _make(self) -> B.KvCacheView:
+        return B.kv_cache_view(self.k, self.v, self.k_scale, self.v_scale, self.page, self.head_dim)
+
+    @property
+    def _view(self) -> B.KvCacheView:
+        return self._args
 
     @property
     def kv_heads(self) -> int:
@@ -114,7 +140,7 @@ def kv_append(cache: KvCache, K: torch.Tensor, V: torch.Tensor, page_table: torc
     """Rows cu_rows[i] .. cu_rows[i+1]-1 of K and V [rows, kv_heads, head_dim] become the tokens held[i], held[i]+1,
     ... of sequence i, keys turned by `rotation` at their position.  `page_table` [n_seq, pages] int32 names the
     sequences' pages; `held` [n_seq] and `cu_rows` [n_seq + 1] are int32 too.  K and V may be views."""
-    B.kv_append(cache._view, page_table, held, cu_rows, K, V, None if rotation is None else rotation._view, status)
+    B.kv_append(cache._args, page_table, held, cu_rows, K, V, None if rotation is None else rotation._args, status)
 
 
 def kv_read(cache: KvCache, page_table: torch.Tensor, first: torch.Tensor, cu_rows: torch.Tensor, n_rows: int,
@@ -124,7 +150,7 @@ def kv_read(cache: KvCache, page_table: torch.Tensor, first: torch.Tensor, cu_ro
     for, cu_rows[i+1] - cu_rows[i] of them.  Rows that name no token of the cache are left as they come."""
     K = torch.empty((n_rows, cache.kv_heads, cache.head_dim), dtype=dtype, device=cache.k.device)
     V = torch.empty_like(K)
-    B.kv_read(cache._view, page_table, first, cu_rows, K, V, status)
+    B.kv_read(cache._args, page_table, first, cu_rows, K, V, status)
     return K, V
 
 
@@ -141,9 +167,9 @@ def kv_attention(cache: KvCache, Q: torch.Tensor, page_table: torch.Tensor, leng
     if out is None:
         out = torch.empty(Q.shape, dtype=out_dtype or (torch.float16 if Q.dtype == torch.float32 else Q.dtype),
                           device=Q.device)
-    B.kv_attention(cache._view, page_table, lengths, cu_rows, Q, out, max_rows, max_length,
+    B.kv_attention(cache._args, page_table, lengths, cu_rows, Q, out, max_rows, max_length,
                    cache.head_dim ** -0.5 if softmax_scale is None else softmax_scale, ws or B.Workspace(Q.device), causal,
-                   window, None if rotation is None else rotation._view, status)
+                   window, None if rotation is None else rotation._args, status)
     return out
 
 

@@ -79,3 +79,35 @@ def test_threads_in_calls_on_one_cache_have_their_own_arguments(S, monkeypatch, 
     [t.start() for t in threads]
     [t.join() for t in threads]
     assert not errors and seen == want
+
+
+def test_assigned_fields_are_what_the_next_call_takes(S):
+    cache = S.make_cache(4, 2, 64, 32, "cpu")
+    names = {"k": "k_codes", "v": "v_codes", "k_scale": "k_scale", "v_scale": "v_scale"}
+    for name, field in names.items():
+        t = getattr(cache, name).clone()
+        setattr(cache, name, t)
+        assert getattr(cache._view, field) == t.data_ptr()
+    cache.k = cache.k[:3].contiguous()                                   # no cache any more
+    with pytest.raises(ValueError):
+        cache._view
+    weight = _weight(S)
+    weight.scale = weight.scale.clone()
+    assert weight._args._scale == weight.scale.data_ptr()
+    rotation = S.make_rotation(8, 64, device="cpu")
+    rotation.cos, rotation.sin = rotation.cos[:5].contiguous(), rotation.sin[:5].contiguous()
+    assert rotation._args.positions == 5 and rotation._args.cos == rotation.cos.data_ptr()
+
+
+def test_copies_are_copies(S, tmp_path):
+    import copy
+    import pickle
+    for thing, names in ((S.make_cache(2, 2, 64, 32, "cpu"), ("k", "v", "k_scale", "v_scale")),
+                         (S.make_rotation(8, 64, device="cpu"), ("cos", "sin")), (_weight(S), ("codes", "scale"))):
+        for other in (copy.deepcopy(thing), pickle.loads(pickle.dumps(thing))):
+            assert type(other) is type(thing) and other._args is not thing._args
+            for n in names:
+                a, b = getattr(thing, n), getattr(other, n)
+                assert torch.equal(a.nan_to_num(), b.nan_to_num()) and a.data_ptr() != b.data_ptr()
+        shallow = copy.copy(thing)
+        assert all(getattr(shallow, n) is getattr(thing, n) for n in names) and shallow._args is not thing._args
