@@ -95,6 +95,8 @@ class Rotation(_Kept):
 def make_rotation(positions: int, dims: int, base: float = 10000.0, interleaved: bool = False,
                   device="cuda") -> Rotation:
     """The tables of angle p * base^(-2 j / dims)."""
+    if dims < 2 or dims % 2 or positions < 1:
+        raise ValueError("dims are turned in pairs: an even number of them; there is at least one position")
     half = dims // 2
     freq = torch.pow(float(base), -torch.arange(half, dtype=torch.float64) / half)
     angle = torch.arange(positions, dtype=torch.float64)[:, None] * freq

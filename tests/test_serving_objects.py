@@ -111,3 +111,10 @@ def test_copies_are_copies(S, tmp_path):
                 assert torch.equal(a.nan_to_num(), b.nan_to_num()) and a.data_ptr() != b.data_ptr()
         shallow = copy.copy(thing)
         assert all(getattr(shallow, n) is getattr(thing, n) for n in names) and shallow._args is not thing._args
+
+
+def test_rotations_of_dims_that_are_no_pairs_are_refused(S):
+    for positions, dims in ((8, 7), (8, 1), (8, 0), (8, -2), (0, 64)):
+        with pytest.raises(ValueError):
+            S.make_rotation(positions, dims, device="cpu")
+    assert S.make_rotation(1, 2, device="cpu").cos.shape == (1, 1)
