@@ -751,6 +751,7 @@ def kv_cache_view(k: torch.Tensor, v: torch.Tensor, k_scale: torch.Tensor, v_sca
     view = KvCacheView(_ptr(k), _ptr(v), _ptr(k_scale), _ptr(v_scale), n_pages, heads, int(head_dim), int(page))
     # (no ctypes.byref of it: one that a structure keeps of itself is a cycle that Python's collector does not see)
     view.keep = (k, v, k_scale, v_scale)
+    view.free_rows, view.free_jobs = [], []         # argument structures that no call has at the moment
     return view
 
 
@@ -763,15 +764,15 @@ def rotation_view(cos: torch.Tensor, sin: torch.Tensor, interleaved: bool) -> Ro
     return view
 
 
-# A call's arguments are its own structures: other threads may be in calls on the same cache.
-
-def _heads(t: torch.Tensor, n_heads: int, head_dim: int) -> Heads:
-    """A tensor [rows, heads, dims] of any row and head stride."""
-    shape = t.shape
-    if len(shape) != 3 or shape[1] != n_heads or shape[2] != head_dim or (head_dim > 1 and t.stride(2) != 1):
-        raise ValueError(f"expected [rows, {n_heads}, {head_dim}] with unit stride along the dims")
-    row_stride, head_stride, _ = t.stride()
-    return Heads(_ptr(t), row_stride, head_stride)
+def _heads(view: Heads, t: torch.Tensor, n_heads: int, head_dim: int) -> int:
+    """Fills in a tensor [rows, heads, dims] of any row and head stride; the number of rows."""
+    if t.dim() == 3:
+        rows, heads, dims = t.shape
+        row_stride, head_stride, stride = t.stride()
+        if heads == n_heads and dims == head_dim and (stride == 1 or dims == 1):
+            view.ptr, view.row_stride, view.head_stride = _ptr(t), row_stride, head_stride
+            return rows
+    raise ValueError(f"expected [rows, {n_heads}, {head_dim}] with unit stride along the dims")
 
 
 def _i32_table(t: torch.Tensor, shape: tuple, what: str) -> int:
@@ -786,23 +787,43 @@ def _table_shape(page_table: torch.Tensor):
     return page_table.shape
 
 
-def _row_args(cache: KvCacheView, page_table: torch.Tensor, first: torch.Tensor, cu_rows: torch.Tensor, K: torch.Tensor,
-              V: torch.Tensor):
-    """What append and read are handed: rows, K, V, dtype."""
-    heads, dims = cache.kv_heads, cache.head_dim
-    k, v = _heads(K, heads, dims), _heads(V, heads, dims)
-    if V.shape[0] != K.shape[0] or K.dtype != V.dtype:
+# A call's arguments are its own while it runs, since other threads may be in calls on the same cache: it takes structures that
+# no call has (a list's pop and append are one step each), or makes some, and gives them back at its end.
+
+def _row_args(cache: KvCacheView):
+    try:
+        return cache.free_rows.pop()
+    except IndexError:
+        return KvRows(), Heads(), Heads()
+
+
+def _job_args(cache: KvCacheView):
+    try:
+        return cache.free_jobs.pop()
+    except IndexError:
+        j = KvAttentionJob(cache=cache)
+        return j, j.Q, j.O                          # the last two are the job's own
+
+
+def _fill_rows(cache: KvCacheView, args, page_table: torch.Tensor, first: torch.Tensor, cu_rows: torch.Tensor, K: torch.Tensor,
+               V: torch.Tensor) -> int:
+    r, k, v = args
+    n = _heads(k, K, cache.kv_heads, cache.head_dim)
+    if _heads(v, V, cache.kv_heads, cache.head_dim) != n or K.dtype != V.dtype:
         raise ValueError("K and V must have the same rows and dtype")
     n_seq, ld = shape = _table_shape(page_table)
-    rows = KvRows(_i32_table(page_table, shape, "page_table"), ld, _i32_table(first, (n_seq,), "first"),
-                  _i32_table(cu_rows, (n_seq + 1,), "cu_rows"), n_seq, K.shape[0])
-    return rows, k, v, serving_dtype(K.dtype)
+    r.page_table, r.ld_table, r.n_seq, r.n_rows = _i32_table(page_table, shape, "page_table"), ld, n_seq, n
+    r.first, r.cu_rows = _i32_table(first, (n_seq,), "first"), _i32_table(cu_rows, (n_seq + 1,), "cu_rows")
+    return serving_dtype(K.dtype)
 
 
 def kv_append(cache: KvCacheView, page_table: torch.Tensor, first: torch.Tensor, cu_rows: torch.Tensor, K: torch.Tensor,
               V: torch.Tensor, rotation: Optional[RotationView] = None, status: Optional[torch.Tensor] = None) -> None:
     """`cmpq_kv_append`: K and V [rows, kv_heads, head_dim] behind the first[i] tokens of each sequence."""
-    rc = _lib.cmpq_kv_append(cache, *_row_args(cache, page_table, first, cu_rows, K, V), rotation, _ptr(status), _stream())
+    args = _row_args(cache)
+    dtype = _fill_rows(cache, args, page_table, first, cu_rows, K, V)
+    rc = _lib.cmpq_kv_append(cache, *args, dtype, rotation, _ptr(status), _stream())
+    cache.free_rows.append(args)
     if rc:
         _check(rc, "cmpq_kv_append")
 
@@ -810,7 +831,10 @@ def kv_append(cache: KvCacheView, page_table: torch.Tensor, first: torch.Tensor,
 def kv_read(cache: KvCacheView, page_table: torch.Tensor, first: torch.Tensor, cu_rows: torch.Tensor, K: torch.Tensor,
             V: torch.Tensor, status: Optional[torch.Tensor] = None) -> None:
     """`cmpq_kv_read`: the values that tokens first[i], first[i]+1, ... of each sequence stand for, into K and V."""
-    rc = _lib.cmpq_kv_read(cache, *_row_args(cache, page_table, first, cu_rows, K, V), _ptr(status), _stream())
+    args = _row_args(cache)
+    dtype = _fill_rows(cache, args, page_table, first, cu_rows, K, V)
+    rc = _lib.cmpq_kv_read(cache, *args, dtype, _ptr(status), _stream())
+    cache.free_rows.append(args)
     if rc:
         _check(rc, "cmpq_kv_read")
 
@@ -826,16 +850,22 @@ def kv_attention(cache: KvCacheView, page_table: torch.Tensor, lengths: torch.Te
     if O.shape != Q.shape or Q.dim() != 3:
         raise ValueError("Q and O must be [rows, q_heads, head_dim]")
     n_seq, ld = shape = _table_shape(page_table)
-    heads, dims = Q.shape[1], cache.head_dim
-    j = KvAttentionJob(cache, _i32_table(page_table, shape, "page_table"), ld, _i32_table(lengths, (n_seq,), "lengths"),
-                       _i32_table(cu_rows, (n_seq + 1,), "cu_rows"), n_seq, Q.shape[0], max_rows, max_length,
-                       _heads(Q, heads, dims), _heads(O, heads, dims), serving_dtype(Q.dtype), serving_dtype(O.dtype), heads,
-                       softmax_scale, 1 if causal else 0, window, _NO_ROTATION if rotation is None else rotation, _ptr(status))
+    args = _job_args(cache)
+    (j, q, o), heads = args, Q.shape[1]
+    j.page_table, j.ld_table, j.n_seq = _i32_table(page_table, shape, "page_table"), ld, n_seq
+    j.lengths, j.cu_rows = _i32_table(lengths, (n_seq,), "lengths"), _i32_table(cu_rows, (n_seq + 1,), "cu_rows")
+    j.n_rows = _heads(q, Q, heads, cache.head_dim)
+    _heads(o, O, heads, cache.head_dim)
+    j.q_dtype, j.o_dtype, j.q_heads = serving_dtype(Q.dtype), serving_dtype(O.dtype), heads
+    j.max_rows, j.max_length, j.window = max_rows, max_length, window
+    j.softmax_scale, j.causal, j.status = softmax_scale, 1 if causal else 0, _ptr(status)
+    j.rotation = _NO_ROTATION if rotation is None else rotation
     for _ in range(2):              # asks for the workspace's size only where what is there does not do
         buf = ws.buf
         rc = _lib.cmpq_kv_attention(j, buf.data_ptr(), buf.numel(), _stream())
         if rc != EWORKSPACE:
             break
         ws.get(_lib.cmpq_kv_attention_workspace(j))
+    cache.free_jobs.append(args)
     if rc:
         _check(rc, "cmpq_kv_attention")

@@ -14,6 +14,7 @@ and no infinity (they become 0 and +-127 codes), so without it such an input goe
 from __future__ import annotations
 
 import dataclasses
+import functools
 from typing import Callable, Optional, Tuple, Union
 
 import torch
@@ -29,19 +30,16 @@ class _Kept:
     def __post_init__(self):
         self._args                          # refuses fields that do not fit
 
-    @property
+    @functools.cached_property
     def _args(self):
-        args = self.__dict__.get("_made")
-        if args is None:
-            args = self.__dict__["_made"] = self._make()
-        return args
+        return self._make()
 
     def __setattr__(self, name, value):
         self.__dict__[name] = value
-        self.__dict__.pop("_made", None)
+        self.__dict__.pop("_args", None)
 
     def __getstate__(self):
-        return {k: v for k, v in self.__dict__.items() if k != "_made"}
+        return {k: v for k, v in self.__dict__.items() if k != "_args"}
 
 
 # ---- products --------------------------------------------------------------------------------

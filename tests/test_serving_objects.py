@@ -118,3 +118,24 @@ def test_rotations_of_dims_that_are_no_pairs_are_refused(S):
         with pytest.raises(ValueError):
             S.make_rotation(positions, dims, device="cpu")
     assert S.make_rotation(1, 2, device="cpu").cos.shape == (1, 1)
+
+
+def test_objects_that_calls_were_made_with_give_their_memory_back(S, monkeypatch):
+    from paper_2410_13056_amd import binding as B
+    monkeypatch.setattr(B, "_lib", type("Library", (), {"__getattr__": lambda self, name: lambda *args: 0})())
+    real = S.make_cache
+    monkeypatch.setattr(B, "kv_page_bytes", lambda dim, page: 2048)
+    cache, rotation = real(8, 2, 64, 32, "cpu"), S.make_rotation(8, 64, device="cpu")
+    held = [weakref.ref(t) for t in (cache.k, cache.v_scale, rotation.cos)]
+    for n in (1, 2):
+        for call in _calls(S, cache, n).values():
+            call()
+    i32 = lambda *v: torch.tensor(v, dtype=torch.int32)
+    x = torch.zeros((1, 2, 64))
+    S.kv_append(cache, x, x, i32(0)[None], i32(0), i32(0, 1), rotation)
+    S.kv_attention(cache, x, i32(0)[None], i32(1), i32(0, 1), 1, 1, ws=_NoWorkspace(), rotation=rotation)
+    with pytest.raises(ValueError):
+        S.kv_append(cache, x[:, :1], x, i32(0)[None], i32(0), i32(0, 1))
+    del cache, rotation, call
+    gc.collect()
+    assert [r() for r in held] == [None] * 3
