@@ -103,3 +103,35 @@ def test_no_rows_and_layers_whose_outputs_are_views(S, kinds):
     for n in b.layers:                                                   # rows that lie apart, and columns
         b.layers[n] = lambda x, n=n: S.apply_layer(plain[n], x, b.ws).t().contiguous().t()
     assert torch.equal(b.step(X, [4, 5]), want) and b.status.item() == 0
+
+
+@pytest.mark.parametrize("dtype", [torch.float16, torch.bfloat16])
+@pytest.mark.parametrize("deployed", ["qo", "qkvo"])
+def test_layers_in_mixed_precision(S, dtype, deployed):
+    """Queries and outputs, or all, through the mixed-precision tables: a prompt and steps, against the same layers one by one.
+    Rounded apart from what both sides have: the query to 2^-16 of its row's largest, weights to FP16, the attention's output
+    to FP16 (what those layers read): 2^-10 in all."""
+    import numpy as np
+    from paper_2410_13056_amd import pipeline as P
+    b = Block(S, "8888")
+    g = torch.Generator(device=DEV).manual_seed(4)
+    for n in deployed:
+        d_in = b.W[n].shape[1]
+        X = torch.randn((512, d_in), generator=g, device=DEV).half()
+        _, sumsq = P.activation_stats(torch.randn((512, d_in), generator=g, device=DEV).half(), b.ws)
+        r = P.quantize_layer(b.W[n], sumsq, (2, 3, 4), 3.5, 4500, 10000, 5, b.ws)
+        b.layers[n] = P.prepare_deployment(r, b.ws)
+    for new in ([40, 7], [1, 1], [3, 2]):
+        X = torch.randn((sum(new), HIDDEN), generator=g, device=DEV).to(dtype)
+        got = b.step(X, new)
+        assert b.status.item() == 0
+        q, want, at = R.as_f32(S.apply_layer(b.layers["q"], X, b.ws)).reshape(-1, HEADS, DIM), [], 0
+        for i, n in enumerate(new):
+            t = b.held[i]
+            k, v = (x.double().cpu().numpy() for x in S.kv_read(b.cache, b.table[i:i + 1].contiguous(), _i32([0]), _i32([0, t]), t, torch.float32))
+            x = R.turn(q[at:at + n], t - n + np.arange(n), R.as_f32(b.rot.cos), R.as_f32(b.rot.sin), False)
+            want.append(R.attention(x.astype(np.float64), k, v, DIM ** -0.5, True, 0)[0])
+            at += n
+        attended = torch.from_numpy(np.concatenate(want)).flatten(1).to(DEV).half()
+        ref = S.apply_layer(b.layers["o"], attended, b.ws).double()
+        assert ((got.double() - ref).norm() / ref.norm()).item() <= 2.0 ** -10
