@@ -458,7 +458,7 @@ int64_t tiles_of(const Scaled &y, int ot, int tt) { return cdiv(y.d_out, ot * kR
 template <typename T>
 int launch_product(const uint8_t *W, const uint8_t *X, int deep, const Scaled &y, hipStream_t st) {
     constexpr int64_t kUnits = 256;  // compute units
-    auto fills = [](int64_t n) { return n >= 4 * kUnits || (n >= kUnits * 5 / 8 && (n + kUnits / 3) / kUnits * kUnits >= n); };
+    auto fills = [](int64_t n) { return n >= 4 * kUnits || (n + kUnits / 3) / kUnits * kUnits >= n; };  // 171 .. 256, 427 .. 512, ...
     const int64_t pieces = cdiv(y.d_out, kRows);
     if (tiles_of(y, 1, 1) > INT32_MAX) return CMPQ_ESHAPE;
     if (y.m <= 16 && pieces >= 768) launch_shared<T, 2, 1, 8>(W, X, deep, y, st);
