@@ -834,12 +834,16 @@ template <int NC>
 __device__ __forceinline__ float top_of_parts(const Job &j, int64_t slot0, int64_t stride, int col, int parts, float &scale) {
     const int lane = threadIdx.x & 63;
     auto of = [&](int p) { return j.part_ml + ((slot0 + p * stride) * NC + col) * 3; };
-    float top = kLowest;
-    for (int p = lane; p < parts; p += 64) top = fmaxf(top, of(p)[0]);
+    float m = kLowest, d = 0.f;  // of the first 64 parts, one a lane: read once
+    if (lane < parts) m = of(lane)[0], d = of(lane)[1];
+    float top = m;
+#pragma unroll 1
+    for (int p = lane + 64; p < parts; p += 64) top = fmaxf(top, of(p)[0]);
 #pragma unroll
     for (int k = 32; k > 0; k >>= 1) top = fmaxf(top, __shfl_xor(top, k));
-    scale = -INFINITY;
-    for (int p = lane; p < parts; p += 64) scale = fmaxf(scale, of(p)[0] - top + of(p)[1]);
+    scale = m - top + d;
+#pragma unroll 1
+    for (int p = lane + 64; p < parts; p += 64) scale = fmaxf(scale, of(p)[0] - top + of(p)[1]);
 #pragma unroll
     for (int k = 32; k > 0; k >>= 1) scale = fmaxf(scale, __shfl_xor(scale, k));
     return top;
