@@ -14,6 +14,7 @@ and again inside the timed steps - and the CPU oracle timed on a bounded sample 
 same workload.
 """
 import argparse
+import gc
 import json
 import os
 import sys
@@ -356,6 +357,10 @@ def main():
     for _ in range(args.warmup):
         out = step()
         del out
+    # The interpreter's one full collection over the objects that the imports leave (45 to 60 ms) comes due some 70 000
+    # allocations after them: before the timed steps rather than among them, where the GPU may run dry meanwhile.  Later ones wait
+    # until a quarter as many objects have been added.
+    gc.collect()
     torch.cuda.synchronize()
     # The timed region: K steps enqueued one after the other, as when a model is quantized block
     # after block; with several streams the queues of one step run on into the next and the
