@@ -354,13 +354,13 @@ def main():
         dst.copy_(src)                            # reads 1 GiB, writes 1 GiB
         torch.cuda.synchronize()
         del src, dst
+    # The interpreter's one full collection over the objects that the imports leave (45 to 60 ms) comes due some 70 000
+    # allocations after them: here rather than among the timed steps, where the GPU may run dry meanwhile.  Later ones wait
+    # until a quarter as many objects have been added.  (Not after the warm-up: the GPU's clocks fall in so long a pause.)
+    gc.collect()
     for _ in range(args.warmup):
         out = step()
         del out
-    # The interpreter's one full collection over the objects that the imports leave (45 to 60 ms) comes due some 70 000
-    # allocations after them: before the timed steps rather than among them, where the GPU may run dry meanwhile.  Later ones wait
-    # until a quarter as many objects have been added.
-    gc.collect()
     torch.cuda.synchronize()
     # The timed region: K steps enqueued one after the other, as when a model is quantized block
     # after block; with several streams the queues of one step run on into the next and the
