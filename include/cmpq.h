@@ -681,7 +681,8 @@ size_t cmpq_kv_page_bytes(int head_dim, int page); /* of one page and head: page
  * Rows of several sequences one after the other: rows cu_rows[i] .. cu_rows[i+1]-1 are the tokens first[i],
  * first[i]+1, ... of sequence i, whose token p lies in page page_table[i * ld_table + p / page], place p % page.
  * All arrays are device data, so the host cannot check them: a sequence with first[i] < 0, a row beyond n_rows,
- * a token beyond ld_table pages or in a page outside 0..n_pages-1 is left out and raises CMPQ_STATUS_RANGE.
+ * a token beyond ld_table pages or in a page outside 0..n_pages-1 is left out and raises CMPQ_STATUS_RANGE (also where n_rows
+ * or ld_table is 0, so that none is done).
  */
 typedef struct cmpq_kv_rows {
     const int32_t *page_table; /* device, [n_seq, ld_table] */
@@ -735,11 +736,11 @@ int cmpq_kv_read(const cmpq_kv_cache *cache, const cmpq_kv_rows *rows, const cmp
  * reads key / value head h / (q_heads / kv_heads),
  *   O = sum_t w_t v_t / sum_t w_t,  w_t = exp(softmax_scale * q . k_t),  q turned by `rotation` (nullable) at p,
  * over the tokens t with 0 <= t < lengths[i], and t <= p if `causal`, and t > p - window if window > 0.  A row that
- * has no such token (a sequence without tokens, or more rows than tokens) gives zeros.
+ * has no such token (a sequence without tokens; `causal` and p < 0, in a sequence with more rows than tokens) gives zeros.
  *   Q  [n_rows, q_heads, head_dim] of q_dtype;  O  [n_rows, q_heads, head_dim] of o_dtype, CMPQ_F16 or CMPQ_BF16.
  *   max_rows, max_length  host bounds of the rows and the length of any sequence: rows beyond are not
- *       written, tokens beyond are left out, and either raises CMPQ_STATUS_RANGE.
- * Logits, their maximum, the weights' sum and the output are held in fp32.  A turned query is rounded to 16 bits fixed
+ *       written, tokens beyond (and beyond ld_table pages) are left out, which moves no row, and either raises CMPQ_STATUS_RANGE.
+ * Logits, their maximum, the weights' sum and the output are held in fp32.  A query, once turned, is rounded to 16 bits fixed
  * point of its row's largest magnitude, its products with codes are exact; weights are rounded to FP16 for their products
  * with the values, after the page's value scale has gone into them and relative to the row's largest such product so far (its
  * largest weight is kept apart).  A value scale below 2^-100 of the quotient of the two counts as that.  A query that holds

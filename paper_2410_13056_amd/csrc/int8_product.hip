@@ -61,7 +61,8 @@ struct Sixteen {
 // One workgroup a row: its largest magnitude, then its codes, 16 inputs a lane and step.  Rows of up to KEPT * 4096
 // inputs stay in registers between the two, longer ones are read again.  The rows of a piece write 16 bytes each
 // of the same lines, so consecutive rows go to one die, whose cache puts the lines together.  Bound by bytes where rows are
-// many: 4096 rows of 8192 in FP16 29 us, 3.5 TB/s; by a row's latency where they are few: 333 rows 4 us.
+// many: 4096 rows of 8192 in FP16 29 us, 3.5 TB/s (three quarters of a copy's rate; vector instructions 38 %); by a row's latency
+// where they are few: 333 rows 4 us.
 template <typename T, int KEPT>
 __global__ __launch_bounds__(256) void code_rows_kernel(const T *__restrict__ X, int64_t n, int64_t d, int64_t ld,
                                                         int8_t *__restrict__ codes, float *__restrict__ scale,
@@ -344,9 +345,9 @@ __device__ __forceinline__ void load_lds16(const uint8_t *src, uint8_t *dst) {
 // Tiles of OT x TT pieces a workgroup, WO x WT wavefronts.  Pieces reach LDS by direct loads in the order in which they
 // are read (no conflicts), BUFS steps of 64 inputs in a ring; while a step is multiplied its operands are in
 // registers, those of the next are on their way from LDS and the steps after it from memory.  Bound by the matrix
-// instructions at 256 x 256: 4096 tokens 8192 -> 28672 in 737 us with the codes (29), 2.6 POP/s, the instructions busy for 69 %
-// of the clocks, the rest at the barrier of a step.  64 x 64 (333 tokens 4099 -> 3001, 16 us): 66 steps at the
-// latency of the caches, one tile a compute unit, matrix instructions 14 %.  Bands keep the inputs of a die's tiles in its
+// instructions at 256 x 256: 4096 tokens 8192 -> 28672 in 741 us with the codes (29), 2.6 POP/s, the instructions busy for 69 %
+// of the clocks, the rest at the barrier of a step.  64 x 64 (333 tokens 4099 -> 3001, 16 us): by what the caches deliver, 282 tiles
+// of 66 steps of 8 KB, 9.4 TB/s; matrix instructions 14 %.  Bands keep the inputs of a die's tiles in its
 // cache while the weights pass once a band.
 constexpr int kBand = 4;
 

@@ -438,7 +438,8 @@ __device__ __forceinline__ void keep_sum(const Job &j, int64_t slot, int nc, int
 // Few rows.  C: 32 dims each of a head.  Tiles of 16 NT columns, one (row, query head) pair each; the wavefronts take the
 // part's units in turn and are added up through LDS.  Bound by the cache's bytes: 64 sequences of one row, 184 000 tokens,
 // 8 heads of 128 dims in 76 us, 2 sequences of 172 000 tokens in 75 us (4.9 and 4.7 TB/s; a large copy reaches 4.8).  Where there
-// is little to read, by what comes one after the other: 11 us for 777 tokens of 32 heads.  Hence codes straight
+// is little to read, by what comes one after the other (lengths, pages, scales, queries, up to 4 units a wavefront, the join by
+// barriers) on a part of the compute units: 11 us for 777 tokens of 32 heads, 32 workgroups.  Hence codes straight
 // into registers a unit ahead, no barrier before the last unit, and the pages' numbers 64 at a time.
 template <int C, int NT, int WAVES>
 __global__ __launch_bounds__(WAVES * 64, WAVES == 8 ? 2 : C * NT <= 4 ? 3 : C * NT <= 8 ? 2 : 1) void attend_kernel(Job j) {
@@ -615,8 +616,10 @@ __global__ __launch_bounds__(WAVES * 64, WAVES == 8 ? 2 : C * NT <= 4 ? 3 : C * 
 // (keys as bytes, values as FP16, converted once a workgroup), one being read while the next is put there.  Bound by
 // issue: of a unit's 32 x 16 weights at 128 dims the matrix instructions take 280 clocks, all else some 250 (a conversion, a
 // shift, a fused multiplication, an exponential, half a rounding to FP16 and an addition each), and the wavefronts of a SIMD
-// overlap the two in part.  758 rows of 64 heads over 12 000 tokens 250 us, 0.72 PFLOP/s.  Queries in FP16 would save
-// the shift and the conversion (235 us) at twice the rounding errors in the output (4.3e-4 of it, 2.8e-4 now).
+// overlap the two in part.  758 rows of 64 heads over 12 000 tokens 251 us, 0.71 PFLOP/s.  Queries in FP16 would save
+// the shift and the conversion (13 us less) at twice the rounding errors in the output (4.3e-4 of it, 2.8e-4 now).  A row's second
+// reference is 3 us of it.  Prompts from their first token on are further from the floor, since a causal mask leaves
+// parts and tiles of different length: 2048 tokens of 32 heads 137 us, 0.25 PFLOP/s, 4096 375 us, 0.37, 16384 3137 us, 0.70.
 template <int C, int NT>
 __global__ __launch_bounds__(kWaves * 64, NT == 1 && C <= 4 ? 4 : 2) void attend_rows_kernel(Job j) {
     constexpr int NC = 16 * NT * kWaves, DP = C * 32, H = (C + 1) / 2;
@@ -637,7 +640,7 @@ __global__ __launch_bounds__(kWaves * 64, NT == 1 && C <= 4 ? 4 : 2) void attend
     const int u0 = max(w.u0, first.lo / kUnit), u1 = min(w.u1, (max(last.hi, 0) + kUnit - 1) / kUnit);
     const int64_t page_bytes = (int64_t)j.c.page * DP;
 
-    // A unit's codes come into registers a unit ahead and go into LDS as FP16: operand 2 c + h of the keys, then the values.
+    // A unit's codes come into registers a unit ahead and go into LDS in the order of the operands, keys as bytes, values as FP16.
     uint4 kc[kShare], vc[kShare];
     PageOf ahead = {}, mine = {};
     auto load = [&](int unit) {
