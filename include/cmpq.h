@@ -50,7 +50,7 @@ extern "C" {
 
 #define CMPQ_F16 0 /* IEEE binary16 */
 #define CMPQ_F32 1 /* IEEE binary32 */
-#define CMPQ_BF16 2 /* bfloat16: the calls of 8-bit serving alone (cmpq_int8_*, cmpq_kv_*) */
+#define CMPQ_BF16 2 /* bfloat16: the calls of serving alone (cmpq_int8_*, cmpq_kv_*, cmpq_rms_norm, cmpq_epilogue) */
 
 #define CMPQ_KMAX 16      /* levels per channel at the widest setting (4 bits)   */
 #define CMPQ_PROTECTED 16 /* bits[i] of a channel of O_act: kept whole in FP16   */
@@ -658,6 +658,106 @@ int cmpq_int8_prepare(const void *W, int dtype, int64_t d_out, int64_t d_in, int
 int cmpq_int8_product(const void *X, int dtype, int64_t m, int64_t d_in, int64_t ldx, const int8_t *codes,
                       const float *scale, int64_t d_out, void *Y, int y_dtype, int64_t ldy, void *ws,
                       size_t ws_bytes, int32_t *status, void *stream);
+
+/*
+ * What may follow a product, in this order, every step in fp32 and rounded, the result rounded once more to its type:
+ *   v = act(v + bias),  v = v * (times + times_bias),  v = v + residual;  what is null is left out.
+ *   SILU v / (1 + e^-v);  GELU v Phi(v), Phi the normal distribution's;  GELU_TANH v (1 + tanh(sqrt(2 / pi) (v + 0.044715
+ *   v^3))) / 2;  RELU v, or 0 where v < 0.  A NaN stays one, and SILU and both GELU of minus infinity are NaN.
+ */
+#define CMPQ_ACT_NONE 0
+#define CMPQ_ACT_SILU 1
+#define CMPQ_ACT_GELU 2
+#define CMPQ_ACT_GELU_TANH 3
+#define CMPQ_ACT_RELU 4
+
+/* Rows of values: element (row, i) lies at ptr + (row * ld + i) elements of `dtype`.  Vectors have no use for ld. */
+typedef struct cmpq_rows {
+    void *ptr; /* device; null: none */
+    int64_t ld;
+    int dtype;
+} cmpq_rows;
+
+/*
+ * Two weights gate, up [d_out, d_in] (ld_gate, ld_up >= d_in) of one type as a gated product takes them: groups of 16 rows, as
+ * in cmpq_int8_prepare, of the one and the other in turn.
+ *   codes  cmpq_int8_weight_bytes(cmpq_int8_gated_rows(d_out), d_in) bytes out, 16-byte aligned.
+ *   scale  [cmpq_int8_gated_rows(d_out)] fp32 out, in the rows' order; 0 for rows that fill up a group.
+ * No workspace.  Limits: d_in <= 131072, d_out < 2^23 (cmpq_int8_gated_rows is 0 beyond).
+ */
+int64_t cmpq_int8_gated_rows(int64_t d_out); /* 32 * ceil(d_out / 16) */
+int cmpq_int8_prepare_gated(const void *gate, const void *up, int dtype, int64_t d_out, int64_t d_in, int64_t ld_gate,
+                            int64_t ld_up, int8_t *codes, float *scale, int32_t *status, void *stream);
+
+/*
+ * cmpq_int8_product with what may follow it, of inputs [m, d_in] as values or already in 8 bits, by one weight:
+ *   Y = act(P + bias) + residual,  P[t,o] the scaled sum of cmpq_int8_product;
+ * or `gated`, by two (codes and scale of cmpq_int8_prepare_gated, d_out outputs each), in one pass over the inputs:
+ *   Y = act(P_gate + bias) * (P_up + up_bias) + residual.
+ * Inputs in 8 bits (X null) are what cmpq_int8_prepare gives for [m, d_in], or cmpq_rms_norm; one set of them serves all
+ * products that share the input.  With nothing behind the sums the outputs are those of cmpq_int8_product, bit for bit.
+ * `residual` may be Y itself (place, type and stride); else Y overlaps nothing that is read.
+ * Workspace: CMPQ_OP_INT8_PRODUCT with n = m; none where X is null.  Limits: those of cmpq_int8_product, gated those of
+ * cmpq_int8_prepare_gated.  Status: CMPQ_STATUS_NONFINITE for X alone.
+ */
+typedef struct cmpq_int8_job {
+    const void *X; /* device, [m, d_in]; null: x_codes, x_scale */
+    int x_dtype;
+    int64_t m, d_in, ldx;
+    const int8_t *x_codes; /* device, 16-byte aligned */
+    const float *x_scale;  /* device, [m] */
+    const int8_t *codes;   /* device, 16-byte aligned */
+    const float *scale;    /* device */
+    int64_t d_out;
+    int gated;
+    const void *bias, *up_bias; /* device, [d_out], nullable; up_bias if gated */
+    int bias_dtype, activation;
+    const void *residual; /* device, [m, d_out], nullable */
+    int r_dtype;
+    int64_t ldr;
+    void *Y; /* device, [m, d_out] */
+    int y_dtype;
+    int64_t ldy;
+    int32_t *status; /* device, nullable */
+} cmpq_int8_job;
+int cmpq_int8_product_job(const cmpq_int8_job *job, void *ws, size_t ws_bytes, void *stream);
+
+/*
+ * The same steps for values Y [m, d] of a product that gave them to memory (cmpq_lut_matvec: fp32):
+ *   out = act(Y + bias) * (times + times_bias) + residual.
+ * Y, times, residual and out are [m, d], bias and times_bias [d], each of its own type; all but Y and out may be null.
+ * `out` may be Y, times or residual (place, type and stride); else it overlaps nothing that is read.
+ * No workspace.  Limits: m and d below 2^24.
+ */
+typedef struct cmpq_epilogue_job {
+    cmpq_rows Y, bias, times, times_bias, residual, out;
+    int64_t m, d;
+    int activation;
+} cmpq_epilogue_job;
+int cmpq_epilogue(const cmpq_epilogue_job *job, void *stream);
+
+/*
+ * Root-mean-square norm of a stream X [m, d], or of the sum of two, X + add:
+ *   s = x + add in fp32, rounded to the type of S if S is given;
+ *   r = 1 / sqrt(mean_i s_i^2 + eps), worked out in fp64 and rounded to fp32;
+ *   y = (s * r) * gain, both products rounded to fp32 (gain null: the first alone).
+ *   S      [m, d] out, nullable: the sum, for the next part of the layer.
+ *   Y      [m, d] out, y rounded once to its type; or, where it is null,
+ *   codes, scale  the rows in 8 bits, as cmpq_int8_prepare makes them of y in fp32: cmpq_int8_weight_bytes(m, d) bytes,
+ *          16-byte aligned, and [m] fp32.  Exactly one of the two forms is asked for.
+ * Each tensor has its own type.  S or Y may be X or add (place, type and stride) but not each other; else they overlap
+ * nothing.  A row with a NaN or an infinity raises CMPQ_STATUS_NONFINITE and gives NaN where s is either and, if an
+ * infinity is the cause, 0 elsewhere; if a NaN, NaN.  eps is finite and at least 2^-126.  No workspace.  Limits: m < 2^24, d <= 131072.
+ */
+typedef struct cmpq_norm_job {
+    cmpq_rows X, add, gain, S, Y;
+    int8_t *codes;
+    float *scale;
+    int64_t m, d;
+    double eps;
+    int32_t *status; /* device, nullable */
+} cmpq_norm_job;
+int cmpq_rms_norm(const cmpq_norm_job *job, void *stream);
 
 /*
  * A cache of keys and values in pages of `page` tokens, 8 bits a value, one scale per page and head for the keys

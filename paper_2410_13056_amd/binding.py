@@ -45,7 +45,8 @@ EXPORTS = ("cmpq_workspace_bytes", "cmpq_strerror", "cmpq_count_ppm", "cmpq_act_
            "cmpq_pack_with_error", "cmpq_time_kernel", "cmpq_act_stats_static", "cmpq_kmeans_launch_shape",
            "cmpq_shader_clock_probe", "cmpq_lut_matvec_group_fp16acc", "cmpq_kmeans_build_shape", "cmpq_rank_channels",
            "cmpq_lut_matvec_shape", "cmpq_int8_weight_bytes", "cmpq_kv_page_bytes", "cmpq_kv_attention_workspace",
-           "cmpq_int8_prepare", "cmpq_int8_product", "cmpq_kv_append", "cmpq_kv_read", "cmpq_kv_attention")
+           "cmpq_int8_prepare", "cmpq_int8_product", "cmpq_kv_append", "cmpq_kv_read", "cmpq_kv_attention",
+           "cmpq_int8_gated_rows", "cmpq_int8_prepare_gated", "cmpq_int8_product_job", "cmpq_epilogue", "cmpq_rms_norm")
 
 _i64, _i32, _int, _vp, _dbl, _sz = (ctypes.c_int64, ctypes.c_int32, ctypes.c_int, ctypes.c_void_p,
                                     ctypes.c_double, ctypes.c_size_t)
@@ -101,6 +102,30 @@ class KvAttentionJob(ctypes.Structure):
                 ("n_seq", _i64), ("n_rows", _i64), ("max_rows", _i64), ("max_length", _i64), ("Q", Heads), ("O", Heads),
                 ("q_dtype", _int), ("o_dtype", _int), ("q_heads", _int), ("softmax_scale", ctypes.c_float),
                 ("causal", _int), ("window", _i64), ("rotation", RotationView), ("status", _vp)]
+
+
+class Int8Job(ctypes.Structure):
+    """`cmpq_int8_job` of the header, field for field."""
+    _fields_ = [("X", _vp), ("x_dtype", _int), ("m", _i64), ("d_in", _i64), ("ldx", _i64), ("x_codes", _vp), ("x_scale", _vp),
+                ("codes", _vp), ("scale", _vp), ("d_out", _i64), ("gated", _int), ("bias", _vp), ("up_bias", _vp),
+                ("bias_dtype", _int), ("activation", _int), ("residual", _vp), ("r_dtype", _int), ("ldr", _i64), ("Y", _vp),
+                ("y_dtype", _int), ("ldy", _i64), ("status", _vp)]
+
+
+def _rows_fields(*names):
+    """A `cmpq_rows` for each name, its three fields in a row: the layout is the same."""
+    return [f for n in names for f in ((n, _vp), ("ld_" + n, _i64), (n + "_dtype", _int))]
+
+
+class EpilogueJob(ctypes.Structure):
+    """`cmpq_epilogue_job` of the header."""
+    _fields_ = _rows_fields("Y", "bias", "times", "times_bias", "residual", "out") + [("m", _i64), ("d", _i64), ("activation", _int)]
+
+
+class NormJob(ctypes.Structure):
+    """`cmpq_norm_job` of the header."""
+    _fields_ = _rows_fields("X", "add", "gain", "S", "Y") + [("codes", _vp), ("scale", _vp), ("m", _i64), ("d", _i64),
+                                                             ("eps", _dbl), ("status", _vp)]
 
 
 class CmpqError(RuntimeError):
@@ -162,10 +187,16 @@ def lib() -> ctypes.CDLL:
         L.cmpq_kv_append.argtypes = rows + [ctypes.POINTER(RotationView), _vp, _vp]
         L.cmpq_kv_read.argtypes = rows + [_vp, _vp]
         L.cmpq_kv_attention.argtypes = [ctypes.POINTER(KvAttentionJob), _vp, _sz, _vp]
+        L.cmpq_int8_gated_rows.argtypes = [_i64]
+        L.cmpq_int8_prepare_gated.argtypes = [_vp, _vp, _int, _i64, _i64, _i64, _i64, _vp, _vp, _vp, _vp]
+        L.cmpq_int8_product_job.argtypes = [ctypes.POINTER(Int8Job), _vp, _sz, _vp]
+        L.cmpq_epilogue.argtypes = [ctypes.POINTER(EpilogueJob), _vp]
+        L.cmpq_rms_norm.argtypes = [ctypes.POINTER(NormJob), _vp]
         for name in EXPORTS[3:]:
             getattr(L, name).restype = _int
         for name in ("cmpq_int8_weight_bytes", "cmpq_kv_page_bytes", "cmpq_kv_attention_workspace"):
             getattr(L, name).restype = _sz
+        L.cmpq_int8_gated_rows.restype = _i64
         _lib = L
     return _lib
 
@@ -667,6 +698,51 @@ def lut4_quantize(centroids: torch.Tensor, bits: torch.Tensor, codes4: torch.Ten
 
 # ---- serving in 8 bits -----------------------------------------------------------------------
 
+ACTIVATIONS = {None: 0, "silu": 1, "gelu": 2, "gelu_tanh": 3, "relu": 4}
+
+
+def activation(name: Optional[str]) -> int:
+    try:
+        return ACTIVATIONS[name]
+    except (KeyError, TypeError):
+        raise ValueError(f"activation is one of {[n for n in ACTIVATIONS if n]} or None, got {name!r}") from None
+
+
+def _here(t: torch.Tensor) -> int:
+    """The address of a tensor on the current device, whose stream the call goes to."""
+    if not t.is_cuda:
+        raise ValueError("cmpq entry points take device tensors")
+    if t.get_device() != (torch.cuda.current_device() if _current_device is None else _current_device()):
+        raise ValueError("tensors must be on the current device")
+    return t.data_ptr()
+
+
+def _matrix(t: torch.Tensor, m: int, d: int, what: str):
+    """(address, leading dimension, type) of a [m, d] tensor whose rows are contiguous: a `cmpq_rows`."""
+    if t.dim() == 2:
+        shape, (ld, unit) = t.shape, t.stride()
+        if shape[0] == m and shape[1] == d and (unit == 1 or d <= 1):
+            return _here(t), ld if m > 1 else d, serving_dtype(t.dtype)
+    raise ValueError(f"{what} must be [{m}, {d}] with unit stride along its rows")
+
+
+def _vector(t: torch.Tensor, d: int, what: str):
+    if t.dim() != 1 or t.shape[0] != d or not t.is_contiguous():
+        raise ValueError(f"{what} must be contiguous [{d}]")
+    return _here(t), 0, serving_dtype(t.dtype)
+
+
+_NONE = (None, 0, 0)
+
+
+def _flags(status: Optional[torch.Tensor]) -> Optional[int]:
+    if status is None:
+        return None
+    if status.dtype != torch.int32 or status.numel() < 1:
+        raise ValueError("status must be int32 [1]")
+    return _here(status)
+
+
 _SERVING = {torch.float16: F16, torch.float32: F32, torch.bfloat16: BF16}
 
 
@@ -698,18 +774,86 @@ def int8_prepare(W: torch.Tensor, codes: torch.Tensor, scale: torch.Tensor,
                                    _ptr(status), _stream()), "cmpq_int8_prepare")
 
 
-class Int8ProductCall:
-    """``cmpq_int8_product`` for one prepared weight: what stays the same from call to call is kept.  Holds the tensors
-    it points into."""
+def int8_gated_rows(d_out: int) -> int:
+    """Rows of the two weights of a gated product of `d_out` outputs, filled up to whole groups; 0: not supported."""
+    return int(lib().cmpq_int8_gated_rows(int(d_out)))
 
-    def __init__(self, d_in: int, d_out: int, codes: torch.Tensor, scale: torch.Tensor):
-        if codes.dtype != torch.int8 or not codes.is_contiguous() or codes.numel() != int8_weight_bytes(d_out, d_in):
+
+def int8_prepare_gated(gate: torch.Tensor, up: torch.Tensor, codes: torch.Tensor, scale: torch.Tensor,
+                       status: Optional[torch.Tensor] = None) -> None:
+    """Two weights [d_out, d_in] in 8 bits, groups of their rows in turn (`cmpq_int8_prepare_gated`)."""
+    d_out, d_in = gate.shape
+    if gate.dtype != up.dtype:
+        raise ValueError("gate and up must have the same dtype")
+    (g, ldg, dtype), (u, ldu, _) = _matrix(gate, d_out, d_in, "gate"), _matrix(up, d_out, d_in, "up")
+    rows = int8_gated_rows(d_out)
+    _int8_operand(codes, scale, rows, d_in)
+    _check(lib().cmpq_int8_prepare_gated(g, u, dtype, d_out, d_in, ldg, ldu, _here(codes), _here(scale), _flags(status),
+                                         _stream()), "cmpq_int8_prepare_gated")
+
+
+def _int8_operand(codes: torch.Tensor, scale: torch.Tensor, rows: int, dim: int) -> None:
+    """Refuses what is no operand of `rows` rows of `dim` inputs in 8 bits."""
+    if codes.dtype != torch.int8 or not codes.is_contiguous() or codes.numel() != int8_weight_bytes(rows, dim):
+        raise ValueError("codes must be contiguous int8 of int8_weight_bytes(rows, dim)")
+    if scale.dtype != torch.float32 or not scale.is_contiguous() or scale.numel() != rows:
+        raise ValueError("scale must be contiguous float32 [rows]")
+
+
+class Int8RowsView:
+    """Inputs of a product in 8 bits, as the library takes them.  Holds the tensors it points into."""
+
+    def __init__(self, rows: int, dim: int, codes: torch.Tensor, scale: torch.Tensor):
+        _int8_operand(codes, scale, rows, dim)
+        self.rows, self.dim, self.codes, self.scale = int(rows), int(dim), _ptr(codes), _ptr(scale)
+        self.keep = (codes, scale)
+
+
+class Int8ProductCall:
+    """``cmpq_int8_product`` and ``cmpq_int8_product_job`` for one prepared weight (`gated`: for two): what stays the same
+    from call to call is kept.  Holds the tensors it points into."""
+
+    def __init__(self, d_in: int, d_out: int, codes: torch.Tensor, scale: torch.Tensor, gated: bool = False):
+        rows = int8_gated_rows(d_out) if gated else d_out
+        if codes.dtype != torch.int8 or not codes.is_contiguous() or codes.numel() != int8_weight_bytes(rows, d_in):
             raise ValueError("codes must be contiguous int8 of int8_weight_bytes(d_out, d_in)")
-        if scale.dtype != torch.float32 or not scale.is_contiguous() or scale.numel() != d_out:
+        if scale.dtype != torch.float32 or not scale.is_contiguous() or scale.numel() != rows:
             raise ValueError("scale must be contiguous float32 [d_out]")
         self._keep = (codes, scale)
         self.d_in, self.d_out, self._codes, self._scale = int(d_in), int(d_out), _ptr(codes), _ptr(scale)
-        self._fn = lib().cmpq_int8_product
+        self._gated, self._fn = int(bool(gated)), lib().cmpq_int8_product
+
+    def job(self, X, Y: torch.Tensor, ws: Workspace, status: Optional[torch.Tensor] = None, bias: Optional[torch.Tensor] = None,
+            up_bias: Optional[torch.Tensor] = None, act: Optional[str] = None, residual: Optional[torch.Tensor] = None) -> None:
+        """The product with what follows it; X a tensor [m, d_in] or an `Int8RowsView`."""
+        d, o = self.d_in, self.d_out
+        if isinstance(X, Int8RowsView):
+            if X.dim != d:
+                raise ValueError(f"rows of {X.dim} inputs for a layer of {d}")
+            m, x, ldx, xt, xc, xs = X.rows, None, 0, 0, X.codes, X.scale
+            if X.keep[0].device != Y.device:
+                raise ValueError("tensors must be on the current device")
+        else:
+            m, xc, xs = X.shape[0], None, None
+            x, ldx, xt = _matrix(X, m, d, "X")
+        if self._keep[0].device != Y.device:
+            raise ValueError("tensors must be on the current device")
+        y, ldy, yt = _matrix(Y, m, o, "Y")
+        b, _, bt = _NONE if bias is None else _vector(bias, o, "bias")
+        u, _, ut = _NONE if up_bias is None else _vector(up_bias, o, "up_bias")
+        if b and u and bt != ut:
+            raise ValueError("both biases must have the same dtype")
+        r, ldr, rt = _NONE if residual is None else _matrix(residual, m, o, "residual")
+        j = Int8Job(x, xt, m, d, ldx, xc, xs, self._codes, self._scale, o, self._gated, b, u, bt if b else ut,
+                    activation(act), r, rt, ldr, y, yt, ldy, _flags(status))
+        for _ in range(2):          # asks for the workspace's size only where what is there does not do
+            buf = ws.buf
+            rc = _lib.cmpq_int8_product_job(j, buf.data_ptr(), buf.numel(), _stream())
+            if rc != EWORKSPACE:
+                break
+            ws.get(workspace_bytes(OP_INT8_PRODUCT, d, o, m))
+        if rc:
+            _check(rc, "cmpq_int8_product_job")
 
     def __call__(self, X: torch.Tensor, Y: torch.Tensor, ws: Workspace, status: Optional[torch.Tensor] = None) -> None:
         m, d_in, ldx = _rows(X)
@@ -732,6 +876,39 @@ def int8_product(X: torch.Tensor, codes: torch.Tensor, scale: torch.Tensor, Y: t
                  status: Optional[torch.Tensor] = None) -> None:
     """Y [m, d_out] = X [m, d_in] times a weight of `int8_prepare`, X in 8 bits with a scale per token on the way."""
     Int8ProductCall(_rows(X)[1], scale.numel(), codes, scale)(X, Y, ws, status)
+
+
+def epilogue(Y: torch.Tensor, out: torch.Tensor, bias: Optional[torch.Tensor] = None, act: Optional[str] = None,
+             times: Optional[torch.Tensor] = None, times_bias: Optional[torch.Tensor] = None,
+             residual: Optional[torch.Tensor] = None) -> None:
+    """`cmpq_epilogue`: out [m, d] = act(Y + bias) * (times + times_bias) + residual."""
+    m, d = Y.shape
+    j = EpilogueJob(*_matrix(Y, m, d, "Y"), *(_NONE if bias is None else _vector(bias, d, "bias")),
+                    *(_NONE if times is None else _matrix(times, m, d, "times")),
+                    *(_NONE if times_bias is None else _vector(times_bias, d, "times_bias")),
+                    *(_NONE if residual is None else _matrix(residual, m, d, "residual")), *_matrix(out, m, d, "out"),
+                    m, d, activation(act))
+    rc = lib().cmpq_epilogue(j, _stream())
+    if rc:
+        _check(rc, "cmpq_epilogue")
+
+
+def rms_norm(X: torch.Tensor, gain: Optional[torch.Tensor], eps: float, Y, add: Optional[torch.Tensor] = None,
+             S: Optional[torch.Tensor] = None, status: Optional[torch.Tensor] = None) -> None:
+    """`cmpq_rms_norm`: the norm of X (+ add) [m, d] into Y, a tensor or an `Int8RowsView`; the sum into S."""
+    m, d = X.shape
+    if isinstance(Y, Int8RowsView):
+        if (Y.rows, Y.dim) != (m, d) or Y.keep[0].device != X.device:
+            raise ValueError(f"the rows in 8 bits must be [{m}, {d}], on the device of X")
+        y, codes, scale = _NONE, Y.codes, Y.scale
+    else:
+        y, codes, scale = _matrix(Y, m, d, "Y"), None, None
+    j = NormJob(*_matrix(X, m, d, "X"), *(_NONE if add is None else _matrix(add, m, d, "add")),
+                *(_NONE if gain is None else _vector(gain, d, "weight")), *(_NONE if S is None else _matrix(S, m, d, "the sum")),
+                *y, codes, scale, m, d, eps, _flags(status))
+    rc = lib().cmpq_rms_norm(j, _stream())
+    if rc:
+        _check(rc, "cmpq_rms_norm")
 
 
 def kv_cache_view(k: torch.Tensor, v: torch.Tensor, k_scale: torch.Tensor, v_scale: torch.Tensor, page: int,

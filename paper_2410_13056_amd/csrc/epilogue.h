@@ -1,0 +1,114 @@
+// What follows a product: bias, activation, second factor and residual, in fp32.  One form for the integer products,
+// which have it behind their sums, and for the call that runs it by itself.
+#pragma once
+
+#include "serving.h"
+
+// N elements from p + i on, of which `n` are there (the others read 0).
+template <int N>
+__device__ __forceinline__ void load_some(const void *p, int dtype, int64_t i, int n, float (&x)[N]) {
+    with_dtype(dtype, [&](auto like) {
+        typedef decltype(like) T;
+        const T *at = static_cast<const T *>(p) + i;
+        if (n >= N) {
+            load_f32<T, N>(at, x);
+        } else {
+#pragma unroll
+            for (int k = 0; k < N; ++k) x[k] = k < n ? (float)at[k] : 0.f;
+        }
+    });
+}
+
+// The first `n` of N values, each rounded once, to p + i on.
+template <int N>
+__device__ __forceinline__ void store_some(void *p, int dtype, int64_t i, int n, const float (&x)[N]) {
+    with_dtype(dtype, [&](auto like) {
+        typedef decltype(like) T;
+        typedef T V __attribute__((ext_vector_type(N)));
+        typedef V Any __attribute__((aligned(sizeof(T))));
+        T *at = static_cast<T *>(p) + i;
+        V v;
+#pragma unroll
+        for (int k = 0; k < N; ++k) v[k] = (T)x[k];
+        if (n >= N) {
+            *reinterpret_cast<Any *>(at) = v;
+        } else {
+#pragma unroll
+            for (int k = 0; k < N; ++k)
+                if (k < n) at[k] = v[k];
+        }
+    });
+}
+
+// Eight values as they lie in memory, on their way before anything is done with them.
+struct Raw8 {
+    typedef uint32_t U4 __attribute__((ext_vector_type(4)));
+    U4 w[2];
+    __device__ __forceinline__ void load(const cmpq_rows &a, int64_t i, int n) {
+        typedef U4 Any __attribute__((aligned(2)));
+        const int size = a.dtype == CMPQ_F32 ? 4 : 2;
+        const char *p = static_cast<const char *>(a.ptr) + i * size;
+        if (n >= 8) {
+            w[0] = *reinterpret_cast<const Any *>(p);
+            if (size == 4) w[1] = *reinterpret_cast<const Any *>(p + 16);
+        } else {
+            float x[8];
+            load_some<8>(a.ptr, a.dtype, i, n, x);
+            with_dtype(a.dtype, [&](auto like) {
+                typedef decltype(like) T;
+                typedef T V __attribute__((ext_vector_type(8)));
+                V v;
+#pragma unroll
+                for (int k = 0; k < 8; ++k) v[k] = (T)x[k];
+                __builtin_memcpy(w, &v, sizeof(V));
+            });
+        }
+    }
+    __device__ __forceinline__ void values(int dtype, float (&x)[8]) const {
+        with_dtype(dtype, [&](auto like) {
+            typedef decltype(like) T;
+            typedef T V __attribute__((ext_vector_type(8)));
+            V v;
+            __builtin_memcpy(&v, w, sizeof(V));
+#pragma unroll
+            for (int k = 0; k < 8; ++k) x[k] = (float)v[k];
+        });
+    }
+};
+
+// e^x to about 2 steps of fp32: 2^(x log2 e), with what the product's rounding and the constant's left out put back
+// as a factor 1 + d ln 2.  Beyond +-1000 (0 and infinity) x counts as that, so an infinite x is right too.
+__device__ __forceinline__ float exp_near(float x) {
+#pragma clang fp contract(off)
+    constexpr float kLog2e = 0x1.715476p+0f, kRest = 0x1.4ae0cp-26f, kLn2 = 0x1.62e43p-1f;  // log2 e = the first two's sum
+    const float c = __builtin_amdgcn_fmed3f(x, -1000.f, 1000.f), t = c * kLog2e;
+    const float d = fmaf(c, kLog2e, -t) + c * kRest;
+    return __builtin_amdgcn_exp2f(t) * fmaf(d, kLn2, 1.f);
+}
+
+// v / (1 + e^z)
+__device__ __forceinline__ float over_one_plus_exp(float v, float z) {
+#pragma clang fp contract(off)
+    return v * __builtin_amdgcn_rcpf(1.f + exp_near(z));
+}
+
+// `act` is the same in all lanes.  A NaN stays one; the limits at minus infinity are not taken (0 times infinity: NaN).
+template <int N>
+__device__ __forceinline__ void activate(int act, float (&v)[N]) {
+#pragma clang fp contract(off)
+    if (act == CMPQ_ACT_SILU) {
+#pragma unroll
+        for (int i = 0; i < N; ++i) v[i] = over_one_plus_exp(v[i], -v[i]);
+    } else if (act == CMPQ_ACT_GELU) {  // v Phi(v), Phi(v) = erfc(-v / sqrt 2) / 2: no difference of near numbers
+#pragma unroll
+        for (int i = 0; i < N; ++i) v[i] = v[i] * (0.5f * erfcf(v[i] * -0.707106781f));
+    } else if (act == CMPQ_ACT_GELU_TANH) {  // v (1 + tanh u) / 2 = v / (1 + e^-2u), u = sqrt(2 / pi) (v + 0.044715 v^3)
+#pragma unroll
+        for (int i = 0; i < N; ++i) v[i] = over_one_plus_exp(v[i], -1.59576912f * (v[i] + 0.044715f * v[i] * v[i] * v[i]));
+    } else if (act == CMPQ_ACT_RELU) {
+#pragma unroll
+        for (int i = 0; i < N; ++i) v[i] = v[i] < 0.f ? 0.f : v[i];
+    }
+}
+
+static inline bool known_activation(int act) { return act >= CMPQ_ACT_NONE && act <= CMPQ_ACT_RELU; }

@@ -1,23 +1,11 @@
 // Products in 8-bit integers: codes with a scale per row of either operand, exact sums, one multiplication by each
-// scale at the end.  Both operands lie in pieces of 16 rows by 64 inputs (1 KB), byte [g][r][j] of a piece being row r,
-// input 16 g + j: what lane 16 g + r of a wavefront hands the 16x16x64 matrix instruction is 16 bytes in order, and
-// a wavefront's load is 1 KB in order, from memory and from LDS alike.
-#include "serving.h"
+// scale at the end, and what may follow it (epilogue.h).
+#include "epilogue.h"
+#include "int8_rows.h"
 
 namespace {
 
 typedef int32_t Int4 __attribute__((ext_vector_type(4)));
-
-constexpr int kRows = 16, kDepth = 64, kPiece = kRows * kDepth;  // a piece
-constexpr int64_t kMostDepth = 131072;                            // 127 * 127 * d_in < 2^31
-
-__host__ __device__ inline int64_t pieces_deep(int64_t d) { return (d + 127) / 128 * 2; }
-
-// Workgroups in the order in which they are handed to the eight dies, so that each die gets a run of them.
-__device__ __forceinline__ int64_t die_order(int64_t x, int64_t n) {
-    const int64_t each = n / 8, more = n % 8, die = x % 8;
-    return die * each + min(die, more) + x / 8;
-}
 
 // Sixteen inputs of a row as they lie in memory; `valid` of them are there, the others read 0.
 template <typename T>
@@ -58,6 +46,11 @@ struct Sixteen {
     }
 };
 
+// Rows come in groups of 16; this operand's is every `of`-th of them, from `at` on.
+struct Turn {
+    int of, at;
+};
+
 // One workgroup a row: its largest magnitude, then its codes, 16 inputs a lane and step.  Rows of up to KEPT * 4096
 // inputs stay in registers between the two, longer ones are read again.  The rows of a piece write 16 bytes each
 // of the same lines, so consecutive rows go to one die, whose cache puts the lines together.  Bound by bytes where rows are
@@ -65,13 +58,15 @@ struct Sixteen {
 // where they are few: 333 rows 4 us.
 template <typename T, int KEPT>
 __global__ __launch_bounds__(256) void code_rows_kernel(const T *__restrict__ X, int64_t n, int64_t d, int64_t ld,
-                                                        int8_t *__restrict__ codes, float *__restrict__ scale,
+                                                        int8_t *__restrict__ codes, float *__restrict__ scale, Turn turn,
                                                         int32_t *__restrict__ status) {
     __shared__ float scratch[4];
-    const int64_t row = die_order(blockIdx.x, gridDim.x), deep = pieces_deep(d);
-    uint8_t *out = reinterpret_cast<uint8_t *>(codes) + row / kRows * deep * kPiece + row % kRows * 16;
+    const int64_t row = die_order(blockIdx.x, gridDim.x), deep = pieces_deep(d), group = row / kRows * turn.of + turn.at;
+    uint8_t *out = reinterpret_cast<uint8_t *>(codes) + group * deep * kPiece + row % kRows * 16;
     const int groups = (int)deep * 4;
+    scale += group * kRows + row % kRows;
     if (row >= n) {  // rows that fill up the last piece
+        if (turn.of > 1 && threadIdx.x == 0) *scale = 0.f;
         for (int c = threadIdx.x; c < groups; c += 256)
             *reinterpret_cast<uint4 *>(out + c / 4 * kPiece + c % 4 * 256) = make_uint4(0, 0, 0, 0);
         return;
@@ -106,7 +101,7 @@ __global__ __launch_bounds__(256) void code_rows_kernel(const T *__restrict__ X,
         if (status) atomicOr(status, CMPQ_STATUS_NONFINITE);
     }
     const float s = code_scale(block_max(largest.most(), scratch)), inv = 1.f / s;
-    if (threadIdx.x == 0) scale[row] = s;
+    if (threadIdx.x == 0) *scale = s;
     auto put = [&](const Sixteen<T> &s, int c, bool clean) {
         *reinterpret_cast<uint4 *>(out + c / 4 * kPiece + c % 4 * 256) = s.codes(inv, clean);
     };
@@ -116,21 +111,21 @@ __global__ __launch_bounds__(256) void code_rows_kernel(const T *__restrict__ X,
 
 template <typename T>
 void launch_code_rows(const void *X, int64_t n, int64_t d, int64_t ld, int64_t rows, int8_t *codes, float *scale,
-                      int32_t *status, hipStream_t st) {
+                      Turn turn, int32_t *status, hipStream_t st) {
     const dim3 grid((unsigned)rows);
     const T *x = static_cast<const T *>(X);
-    if (d <= 4096) code_rows_kernel<T, 1><<<grid, 256, 0, st>>>(x, n, d, ld, codes, scale, status);
-    else if (d <= 8192) code_rows_kernel<T, 2><<<grid, 256, 0, st>>>(x, n, d, ld, codes, scale, status);
-    else if (d <= 16384) code_rows_kernel<T, 4><<<grid, 256, 0, st>>>(x, n, d, ld, codes, scale, status);
-    else code_rows_kernel<T, 0><<<grid, 256, 0, st>>>(x, n, d, ld, codes, scale, status);
+    if (d <= 4096) code_rows_kernel<T, 1><<<grid, 256, 0, st>>>(x, n, d, ld, codes, scale, turn, status);
+    else if (d <= 8192) code_rows_kernel<T, 2><<<grid, 256, 0, st>>>(x, n, d, ld, codes, scale, turn, status);
+    else if (d <= 16384) code_rows_kernel<T, 4><<<grid, 256, 0, st>>>(x, n, d, ld, codes, scale, turn, status);
+    else code_rows_kernel<T, 0><<<grid, 256, 0, st>>>(x, n, d, ld, codes, scale, turn, status);
 }
 
 // `rows` of them, those from n on zeros.
 int launch_code_rows_of(const void *X, int dtype, int64_t n, int64_t d, int64_t ld, int64_t rows, int8_t *codes,
-                     float *scale, int32_t *status, hipStream_t st) {
-    if (dtype == CMPQ_F16) launch_code_rows<_Float16>(X, n, d, ld, rows, codes, scale, status, st);
-    else if (dtype == CMPQ_BF16) launch_code_rows<__bf16>(X, n, d, ld, rows, codes, scale, status, st);
-    else launch_code_rows<float>(X, n, d, ld, rows, codes, scale, status, st);
+                     float *scale, Turn turn, int32_t *status, hipStream_t st) {
+    if (dtype == CMPQ_F16) launch_code_rows<_Float16>(X, n, d, ld, rows, codes, scale, turn, status, st);
+    else if (dtype == CMPQ_BF16) launch_code_rows<__bf16>(X, n, d, ld, rows, codes, scale, turn, status, st);
+    else launch_code_rows<float>(X, n, d, ld, rows, codes, scale, turn, status, st);
     CMPQ_LAUNCH_CHECK();
     return CMPQ_OK;
 }
@@ -173,6 +168,79 @@ __device__ __forceinline__ void put4(const Scaled &y, int64_t t, int64_t o, cons
     }
 }
 
+// What follows the scaled sums.  The kernels come without anything behind them, with an epilogue, and gated: pieces of 16
+// outputs of the gate and of the second factor in turn, so that the wavefront that has the one has the other.
+struct Plain {
+    static constexpr bool kPlain = true, kGated = false;
+};
+struct Epilogue {
+    static constexpr bool kPlain = false, kGated = false;
+    const void *bias, *up_bias, *residual;
+    int64_t ldr;
+    int bias_dtype, r_dtype, y_dtype, act;
+};
+struct GatedEpilogue : Epilogue {
+    static constexpr bool kGated = true;
+};
+template <typename E>
+constexpr int kPerOutput = E::kGated ? 2 : 1;  // rows of the weight that make an output
+
+// N outputs o, o + 1, ... of token t, `n` of them there, from their scaled sums v (and u, the second factor's); b: biases
+template <typename E, int N>
+__device__ __forceinline__ void finish(const Scaled &y, const E &e, int64_t t, int64_t o, int n, float (&v)[N],
+                                       const float (&u)[N], const float (&b)[N], const float (&bu)[N]) {
+#pragma clang fp contract(off)
+    float r[N];
+    if (e.residual) load_some<N>(e.residual, e.r_dtype, t * e.ldr + o, n, r);
+    if (e.bias) {
+#pragma unroll
+        for (int i = 0; i < N; ++i) v[i] += b[i];
+    }
+    activate(e.act, v);
+    if (E::kGated) {
+#pragma unroll
+        for (int i = 0; i < N; ++i) v[i] *= e.up_bias ? u[i] + bu[i] : u[i];
+    }
+    if (e.residual) {
+#pragma unroll
+        for (int i = 0; i < N; ++i) v[i] += r[i];
+    }
+    store_some<N>(y.Y, e.y_dtype, t * y.ldy + o, n, v);
+}
+
+// Scales of a weight's rows and biases of N outputs from o on, `n` of them there.
+template <typename E, int N>
+struct Columns {
+    float sw[N], su[N], b[N], bu[N];
+    __device__ __forceinline__ void load(const Scaled &y, const E &e, int64_t o, int n) {
+        if (E::kGated) {  // whole pieces of either
+            const float *s = y.sw + o / kRows * (2 * kRows) + o % kRows;
+            load_f32<float, N>(s, sw);
+            load_f32<float, N>(s + kRows, su);
+        } else {
+            load_some<N>(y.sw, CMPQ_F32, o, n, sw);
+        }
+        if (e.bias) load_some<N>(e.bias, e.bias_dtype, o, n, b);
+        if (E::kGated && e.up_bias) load_some<N>(e.up_bias, e.bias_dtype, o, n, bu);
+    }
+};
+
+// Outputs o .. o + 3 of token t with everything that follows the sums.
+template <typename T, typename E>
+__device__ __forceinline__ void put_finished(const Scaled &y, const E &e, int64_t t, int64_t o, const Int4 &acc, const Int4 &up, float sx) {
+    const int n = (int)min(y.d_out - o, (int64_t)4);
+    if (t >= y.m || n <= 0) return;
+    Columns<E, 4> c;
+    c.load(y, e, o, n);
+    float v[4], u[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        v[i] = scaled(acc[i], sx, c.sw[i]);
+        if (E::kGated) u[i] = scaled(up[i], sx, c.su[i]);
+    }
+    finish<E, 4>(y, e, t, o, n, v, u, c.b, c.bu);
+}
+
 __device__ __forceinline__ Int4 multiply(const Int4 &w, const Int4 &x, const Int4 &acc) {
     return __builtin_amdgcn_mfma_i32_16x16x64_i8(w, x, acc, 0, 0, 0);
 }
@@ -181,32 +249,33 @@ __device__ __forceinline__ Int4 multiply(const Int4 &w, const Int4 &x, const Int
 // add up through LDS.  Operands come straight from memory, kAhead steps of 64 inputs at once, overlapped with the
 // products only where a workgroup has many of them (registers).  Bound by the weights' bytes: 16 tokens 5120 -> 13824
 // 12.2 us (71 MB, 5.8 TB/s: of this size the cache behind the dies holds them between calls), and 3 for the codes.
-template <typename T, int OP, int TP, int WAVES>
+template <typename T, typename E, int OP, int TP, int WAVES>
 __global__ __launch_bounds__(WAVES * 64) void shared_depth_kernel(const uint8_t *__restrict__ W,
                                                                   const uint8_t *__restrict__ X, int deep, int t_tiles,
-                                                                  Scaled y) {
+                                                                  Scaled y, E e) {
     constexpr int kAhead = OP + TP <= 3 ? 4 : 2;
     constexpr bool kOverlap = OP * TP >= 8;
     __shared__ Int4 red[WAVES][OP * TP][64];
     const int lane = threadIdx.x & 63, wave = wave_index();
     const int n = (int)die_order(blockIdx.x, gridDim.x);  // the token tiles of an output tile on one die
     const int64_t o0 = (int64_t)(n / t_tiles) * OP, t0 = (int64_t)(n % t_tiles) * TP;
-    const int64_t last_o = (y.d_out - 1) / kRows, last_t = (y.m - 1) / kRows;
+    const int64_t last_o = ((y.d_out - 1) / kRows + 1) * kPerOutput<E> - 1, last_t = (y.m - 1) / kRows;
     const uint8_t *w[OP], *x[TP];
 #pragma unroll
     for (int i = 0; i < OP; ++i) w[i] = W + min(o0 + i, last_o) * deep * kPiece + lane * 16;
 #pragma unroll
     for (int i = 0; i < TP; ++i) x[i] = X + min(t0 + i, last_t) * deep * kPiece + lane * 16;
     // the scales that the results will take, on their way meanwhile
-    constexpr int kMine = (OP * TP + WAVES - 1) / WAVES;
-    const int64_t t = t0 * kRows + (lane & 15), o = o0 * kRows + (lane >> 4) * 4;
+    static_assert(OP % kPerOutput<E> == 0, "pieces of an output in one workgroup");
+    constexpr int kResults = OP / kPerOutput<E> * TP, kMine = (kResults + WAVES - 1) / WAVES;
+    const int64_t t = t0 * kRows + (lane & 15), o = o0 / kPerOutput<E> * kRows + (lane >> 4) * 4;
     float sx[kMine];
     float4 sw[kMine];
 #pragma unroll
     for (int i = 0; i < kMine; ++i) {
         const int q = wave + i * WAVES;
         sx[i] = token_scale(y, t + q % TP * kRows);
-        sw[i] = output_scales(y, o + q / TP * kRows);
+        if (E::kPlain) sw[i] = output_scales(y, o + q / TP * kRows);
     }
     Int4 acc[OP][TP] = {};
     const int k0 = (int)((int64_t)deep * wave / WAVES), k1 = (int)((int64_t)deep * (wave + 1) / WAVES);
@@ -253,11 +322,20 @@ __global__ __launch_bounds__(WAVES * 64) void shared_depth_kernel(const uint8_t 
 #pragma unroll
     for (int i = 0; i < kMine; ++i) {
         const int q = wave + i * WAVES;
-        if (q >= OP * TP) break;
-        Int4 sum = red[0][q][lane];
-#pragma unroll
-        for (int v = 1; v < WAVES; ++v) sum += red[v][q][lane];
-        put4<T>(y, t + q % TP * kRows, o + q / TP * kRows, sum, sx[i], sw[i]);
+        if (q >= kResults) break;
+        auto total = [&](int p) {
+            Int4 sum = red[0][p][lane];
+#pragma unroll(E::kPlain ? WAVES : 4)
+            for (int v = 1; v < WAVES; ++v) sum += red[v][p][lane];
+            return sum;
+        };
+        const int64_t tq = t + q % TP * kRows, oq = o + q / TP * kRows;
+        if constexpr (E::kPlain) {
+            put4<T>(y, tq, oq, total(q), sx[i], sw[i]);
+        } else {
+            const int p = q / TP * kPerOutput<E> * TP + q % TP;  // the gate's result; the second factor's is TP further on
+            put_finished<T, E>(y, e, tq, oq, total(p), E::kGated ? total(p + TP) : Int4{}, sx[i]);
+        }
     }
 }
 
@@ -268,21 +346,24 @@ __global__ __launch_bounds__(WAVES * 64) void shared_depth_kernel(const uint8_t 
 // its largest, two barriers, the products, the join), large ones by the weights' bytes.
 constexpr int kFewWaves = 16, kFewDepth = kFewWaves * 64 * 16;
 
-template <typename TX, int M>
+template <typename TX, typename E, int M>
 __global__ __launch_bounds__(kFewWaves * 64) void few_tokens_kernel(const uint8_t *__restrict__ W, const TX *__restrict__ X,
-                                                                    int64_t d, int64_t ldx, int deep, Scaled y, int dtype,
+                                                                    int64_t d, int64_t ldx, int deep, Scaled y, E e, int dtype,
                                                                     int32_t *__restrict__ status) {
-    constexpr int kAhead = 4;
+    constexpr int kAhead = 4, P = kPerOutput<E>;
     __shared__ __align__(16) uint8_t codes[M * kFewDepth];
-    __shared__ Int4 red[kFewWaves][64];
+    __shared__ Int4 red[P][kFewWaves][64];
     __shared__ float most[M][kFewWaves], scales[M];
     const int lane = threadIdx.x & 63, wave = wave_index(), m = (int)y.m;
-    const uint8_t *w = W + (int64_t)blockIdx.x * deep * kPiece + lane * 16;
+    const uint8_t *w = W + (int64_t)blockIdx.x * P * deep * kPiece + lane * 16;
     const int k0 = deep * wave / kFewWaves, k1 = deep * (wave + 1) / kFewWaves;
-    Int4 a[kAhead];
+    Int4 a[kAhead][P];
     auto load = [&](int k) {
 #pragma unroll
-        for (int u = 0; u < kAhead; ++u) a[u] = *reinterpret_cast<const Int4 *>(w + (int64_t)min(k + u, deep - 1) * kPiece);
+        for (int u = 0; u < kAhead; ++u)
+#pragma unroll
+            for (int p = 0; p < P; ++p)
+                a[u][p] = *reinterpret_cast<const Int4 *>(w + ((int64_t)p * deep + min(k + u, deep - 1)) * kPiece);
     };
     const int c = threadIdx.x, chunks = deep * 4;
     Sixteen<TX> x[M];
@@ -316,30 +397,84 @@ __global__ __launch_bounds__(kFewWaves * 64) void few_tokens_kernel(const uint8_
         if (c < chunks) *reinterpret_cast<uint4 *>(codes + t * kFewDepth + c * 16) = x[t].codes(inv, !bad);
     }
     __syncthreads();
-    Int4 acc = {};
+    Int4 acc[P] = {};
     const uint8_t *mine = codes + min(lane & 15, m - 1) * kFewDepth + (lane >> 4) * 16;
     for (int k = k0; k < k1; k += kAhead) {
 #pragma unroll
         for (int u = 0; u < kAhead; ++u) {
             if (k + u >= k1) break;
-            acc = multiply(a[u], *reinterpret_cast<const Int4 *>(mine + (k + u) * kDepth), acc);
+            const Int4 b = *reinterpret_cast<const Int4 *>(mine + (k + u) * kDepth);
+#pragma unroll
+            for (int p = 0; p < P; ++p) acc[p] = multiply(a[u][p], b, acc[p]);
         }
         if (k + kAhead < k1) load(k + kAhead);
     }
-    red[wave][lane] = acc;
+#pragma unroll
+    for (int p = 0; p < P; ++p) red[p][wave][lane] = acc[p];
     __syncthreads();
     if (wave != 0) return;
 #pragma unroll 5  // more at once would take the registers of a second workgroup a unit
-    for (int v = 1; v < kFewWaves; ++v) acc += red[v][lane];
+    for (int v = 1; v < kFewWaves; ++v)
+#pragma unroll
+        for (int p = 0; p < P; ++p) acc[p] += red[p][v][lane];
     const int64_t o = (int64_t)blockIdx.x * kRows + (lane >> 4) * 4;
     const float sx = scales[min(lane & 15, m - 1)];
-    const float4 sw = output_scales(y, o);
-    with_dtype(dtype, [&](auto like) { put4<decltype(like)>(y, lane & 15, o, acc, sx, sw); });
+    if constexpr (E::kPlain) {
+        const float4 sw = output_scales(y, o);
+        with_dtype(dtype, [&](auto like) { put4<decltype(like)>(y, lane & 15, o, acc[0], sx, sw); });
+    } else {
+        put_finished<float, E>(y, e, lane & 15, o, acc[0], acc[P - 1], sx);
+    }
 }
 
 __device__ __forceinline__ void load_lds16(const uint8_t *src, uint8_t *dst) {
     __builtin_amdgcn_global_load_lds(reinterpret_cast<const __attribute__((address_space(1))) uint32_t *>(reinterpret_cast<uintptr_t>(src)),
                                      reinterpret_cast<__attribute__((address_space(3))) uint32_t *>((uint32_t)reinterpret_cast<uintptr_t>(dst)), 16, 0, 0);
+}
+
+// Sums of a wavefront on their way through LDS, a token's 16 A next to each other: where four of them (`four` < 4 A) of a row
+// lie.  The rows of one store, and the fours of one load, go to different banks.
+template <int A>
+__device__ __forceinline__ int staged_sum(int row, int four) {
+    return row * (A * 4) + (four ^ (row & (A * 4 - 1)));
+}
+// Pieces of 16 tokens that the wavefronts stage at once.
+constexpr int tokens_at_once(int a, int b, int waves, int bytes) {
+    while (b * a * 1024 * waves > bytes) b /= 2;
+    return b;
+}
+
+// Finishes staged sums: ROWS tokens from t0 on, outputs from o0 on, eight outputs a lane, so that residuals and
+// outputs pass in runs of whole lines and the code behind the sums is there once.
+template <typename E, int A, int ROWS>
+__device__ __forceinline__ void finish_rows(const Int4 *sums, const Scaled &y, const E &e, int64_t t0, int64_t o0) {
+    constexpr int kLanes = A * 2 / kPerOutput<E>, kRowsAtOnce = 64 / kLanes;  // lanes that share a token
+    const int lane = threadIdx.x & 63, j = lane % kLanes;
+    const int64_t o = o0 + j * 8;
+    const int n = (int)min(y.d_out - o, (int64_t)8);
+    if (n <= 0) return;
+    Columns<E, 8> c;
+    c.load(y, e, o, n);
+    const int first = E::kGated ? j / 2 * 8 + j % 2 * 2 : j * 2;
+#pragma unroll 2
+    for (int row = lane / kLanes; row < ROWS; row += kRowsAtOnce) {
+        const int64_t t = t0 + row;
+        if (t >= y.m) break;
+        const float sx = y.sx[t];
+        float v[8], u[8];
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            const Int4 a = sums[staged_sum<A>(row, first + h)];
+#pragma unroll
+            for (int i = 0; i < 4; ++i) v[4 * h + i] = scaled(a[i], sx, c.sw[4 * h + i]);
+            if (E::kGated) {
+                const Int4 b = sums[staged_sum<A>(row, first + 4 + h)];
+#pragma unroll
+                for (int i = 0; i < 4; ++i) u[4 * h + i] = scaled(b[i], sx, c.su[4 * h + i]);
+            }
+        }
+        finish<E, 8>(y, e, t, o, n, v, u, c.b, c.bu);
+    }
 }
 
 // Tiles of OT x TT pieces a workgroup, WO x WT wavefronts.  Pieces reach LDS by direct loads in the order in which they
@@ -351,9 +486,9 @@ __device__ __forceinline__ void load_lds16(const uint8_t *src, uint8_t *dst) {
 // cache while the weights pass once a band.
 constexpr int kBand = 4;
 
-template <typename T, int OT, int TT, int WO, int WT, int BUFS>
+template <typename T, typename E, int OT, int TT, int WO, int WT, int BUFS>
 __global__ __launch_bounds__(WO * WT * 64, 2) void tile_kernel(const uint8_t *__restrict__ W, const uint8_t *__restrict__ X,
-                                                               int deep, int o_tiles, int t_tiles, Scaled y) {
+                                                               int deep, int o_tiles, int t_tiles, Scaled y, E e) {
     constexpr int kWaves = WO * WT, kLoads = (OT + TT) / kWaves, kStepBytes = (OT + TT) * kPiece, A = OT / WO, B = TT / WT;
     static_assert(kLoads * kWaves == OT + TT && A * WO == OT && B * WT == TT, "shares of the wavefronts");
     __shared__ __align__(16) uint8_t smem[BUFS * kStepBytes];
@@ -363,7 +498,7 @@ __global__ __launch_bounds__(WO * WT * 64, 2) void tile_kernel(const uint8_t *__
     const int band = (int)(n / ((int64_t)kBand * o_tiles)), in_band = (int)(n - (int64_t)band * kBand * o_tiles);
     const int wide = min(kBand, t_tiles - band * kBand);
     const int64_t o0 = (int64_t)(in_band / wide) * OT, t0 = (int64_t)(band * kBand + in_band % wide) * TT;
-    const int64_t last_o = (y.d_out - 1) / kRows, last_t = (y.m - 1) / kRows;
+    const int64_t last_o = ((y.d_out - 1) / kRows + 1) * kPerOutput<E> - 1, last_t = (y.m - 1) / kRows;
     const uint8_t *src[kLoads];
 #pragma unroll
     for (int q = 0; q < kLoads; ++q) {
@@ -421,6 +556,22 @@ __global__ __launch_bounds__(WO * WT * 64, 2) void tile_kernel(const uint8_t *__
         turn(step + 1, 1);
     }
     asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");  // what nothing reads ends before the LDS does
+    if constexpr (!E::kPlain) {
+        __syncthreads();  // nobody's loads are under way to the LDS that the sums pass through now
+        constexpr int kAtOnce = tokens_at_once(A, B, kWaves, BUFS * kStepBytes);
+        Int4 *mine = reinterpret_cast<Int4 *>(smem) + wave * (kAtOnce * A * 64);
+#pragma unroll
+        for (int q0 = 0; q0 < B; q0 += kAtOnce) {
+#pragma unroll
+            for (int q = 0; q < kAtOnce; ++q)
+#pragma unroll
+                for (int p = 0; p < A; ++p) mine[staged_sum<A>(q * kRows + (lane & 15), p * 4 + (lane >> 4))] = acc[p][q0 + q];
+            __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+            finish_rows<E, A, kAtOnce * kRows>(mine, y, e, (t0 + wt + q0) * kRows, (o0 + wo) / kPerOutput<E> * kRows);
+            __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+        }
+        return;
+    }
     const int64_t t = (t0 + wt) * kRows + (lane & 15), o = (o0 + wo) * kRows + (lane >> 4) * 4;
     float sx[B];
     float4 sw[A];
@@ -434,19 +585,28 @@ __global__ __launch_bounds__(WO * WT * 64, 2) void tile_kernel(const uint8_t *__
         for (int p = 0; p < A; ++p) put4<T>(y, t + q * kRows, o + p * kRows, acc[p][q], sx[q], sw[p]);
 }
 
-template <typename T, int OT, int TT, int WO, int WT, int BUFS>
-void launch_tiles(const uint8_t *W, const uint8_t *X, int deep, const Scaled &y, hipStream_t st) {
-    const int o_tiles = (int)cdiv(y.d_out, OT * kRows), t_tiles = (int)cdiv(y.m, TT * kRows);
-    tile_kernel<T, OT, TT, WO, WT, BUFS><<<dim3((unsigned)(o_tiles * t_tiles)), WO * WT * 64, 0, st>>>(W, X, deep, o_tiles, t_tiles, y);
+// Groups of 16 rows of the weight.
+template <typename E>
+int64_t pieces_of(const Scaled &y) {
+    return cdiv(y.d_out, kRows) * kPerOutput<E>;
 }
 
-template <typename T, int OP, int TP, int WAVES>
-void launch_shared(const uint8_t *W, const uint8_t *X, int deep, const Scaled &y, hipStream_t st) {
-    const int64_t t_tiles = cdiv(y.m, TP * kRows), tiles = cdiv(y.d_out, OP * kRows) * t_tiles;
-    shared_depth_kernel<T, OP, TP, WAVES><<<dim3((unsigned)tiles), WAVES * 64, 0, st>>>(W, X, deep, (int)t_tiles, y);
+template <typename E>
+int64_t tiles_of(const Scaled &y, int ot, int tt) {
+    return cdiv(pieces_of<E>(y), ot) * cdiv(y.m, tt * kRows);
 }
 
-int64_t tiles_of(const Scaled &y, int ot, int tt) { return cdiv(y.d_out, ot * kRows) * cdiv(y.m, tt * kRows); }
+template <typename T, typename E, int OT, int TT, int WO, int WT, int BUFS>
+void launch_tiles(const uint8_t *W, const uint8_t *X, int deep, const Scaled &y, const E &e, hipStream_t st) {
+    const int o_tiles = (int)cdiv(pieces_of<E>(y), OT), t_tiles = (int)cdiv(y.m, TT * kRows);
+    tile_kernel<T, E, OT, TT, WO, WT, BUFS><<<dim3((unsigned)(o_tiles * t_tiles)), WO * WT * 64, 0, st>>>(W, X, deep, o_tiles, t_tiles, y, e);
+}
+
+template <typename T, typename E, int OP, int TP, int WAVES>
+void launch_shared(const uint8_t *W, const uint8_t *X, int deep, const Scaled &y, const E &e, hipStream_t st) {
+    const int64_t t_tiles = cdiv(y.m, TP * kRows), tiles = tiles_of<E>(y, OP, TP);
+    shared_depth_kernel<T, E, OP, TP, WAVES><<<dim3((unsigned)tiles), WAVES * 64, 0, st>>>(W, X, deep, (int)t_tiles, y, e);
+}
 
 // Which kernel: the largest tile that fills the chip.  A tile of 256 x 256 or 256 x 128 takes a compute unit for itself, so
 // its last round has to be two thirds full, or one of many.  us (4096 tokens 8192 -> 28672; 2048 tokens 4096 -> 4096; 1024
@@ -456,33 +616,34 @@ int64_t tiles_of(const Scaled &y, int ot, int tt) { return cdiv(y.d_out, ot * kR
 // 4096 -> 4096 9.4, 12.3).  Up to 16 tokens: two pieces of outputs a workgroup where there are many (16 tokens 5120 -> 13824
 // 16.0, one piece 17.9), 8 wavefronts for some (8192 -> 8192 15.8, 16 wavefronts 16.4), 16 for few (8 tokens 8192 -> 1024
 // 8.6, 8 wavefronts 9.8).
-template <typename T>
-int launch_product(const uint8_t *W, const uint8_t *X, int deep, const Scaled &y, hipStream_t st) {
+template <typename T, typename E>
+int launch_product(const uint8_t *W, const uint8_t *X, int deep, const Scaled &y, const E &e, hipStream_t st) {
     constexpr int64_t kUnits = 256;  // compute units
     auto fills = [](int64_t n) { return n >= 4 * kUnits || (n + kUnits / 3) / kUnits * kUnits >= n; };  // 171 .. 256, 427 .. 512, ...
-    const int64_t pieces = cdiv(y.d_out, kRows);
-    if (tiles_of(y, 1, 1) > INT32_MAX) return CMPQ_ESHAPE;
-    if (y.m <= 16 && pieces >= 768) launch_shared<T, 2, 1, 8>(W, X, deep, y, st);
-    else if (y.m <= 16 && pieces >= 320) launch_shared<T, 1, 1, 8>(W, X, deep, y, st);
-    else if (y.m <= 16) launch_shared<T, 1, 1, 16>(W, X, deep, y, st);
-    else if (y.m <= 32) launch_shared<T, 4, 2, 4>(W, X, deep, y, st);
-    else if (fills(tiles_of(y, 16, 16))) launch_tiles<T, 16, 16, 4, 2, 4>(W, X, deep, y, st);
-    else if (fills(tiles_of(y, 16, 8))) launch_tiles<T, 16, 8, 4, 2, 4>(W, X, deep, y, st);
-    else if (tiles_of(y, 8, 8) >= 192) launch_tiles<T, 8, 8, 2, 2, 4>(W, X, deep, y, st);
-    else if (tiles_of(y, 4, 4) >= 150) launch_tiles<T, 4, 4, 2, 2, 8>(W, X, deep, y, st);
-    else launch_shared<T, 4, 2, 4>(W, X, deep, y, st);
+    const int64_t pieces = pieces_of<E>(y);
+    constexpr int kLeast = kPerOutput<E>;  // pieces of a workgroup at least
+    if (tiles_of<E>(y, kLeast, 1) > INT32_MAX) return CMPQ_ESHAPE;
+    if (y.m <= 16 && pieces >= 768) launch_shared<T, E, 2, 1, 8>(W, X, deep, y, e, st);
+    else if (y.m <= 16 && pieces >= 320) launch_shared<T, E, kLeast, 1, 8>(W, X, deep, y, e, st);
+    else if (y.m <= 16) launch_shared<T, E, kLeast, 1, 16>(W, X, deep, y, e, st);
+    else if (y.m <= 32) launch_shared<T, E, 4, 2, 4>(W, X, deep, y, e, st);
+    else if (fills(tiles_of<E>(y, 16, 16))) launch_tiles<T, E, 16, 16, 4, 2, 4>(W, X, deep, y, e, st);
+    else if (fills(tiles_of<E>(y, 16, 8))) launch_tiles<T, E, 16, 8, 4, 2, 4>(W, X, deep, y, e, st);
+    else if (tiles_of<E>(y, 8, 8) >= 192) launch_tiles<T, E, 8, 8, 2, 2, 4>(W, X, deep, y, e, st);
+    else if (tiles_of<E>(y, 4, 4) >= 150) launch_tiles<T, E, 4, 4, 2, 2, 8>(W, X, deep, y, e, st);
+    else launch_shared<T, E, 4, 2, 4>(W, X, deep, y, e, st);
     CMPQ_LAUNCH_CHECK();
     return CMPQ_OK;
 }
 
-template <typename TX>
-void launch_few(const uint8_t *W, const void *X, int64_t d, int64_t ldx, const Scaled &y, int y_dtype, int32_t *status,
+template <typename TX, typename E>
+void launch_few(const uint8_t *W, const void *X, int64_t d, int64_t ldx, const Scaled &y, const E &e, int y_dtype, int32_t *status,
                 hipStream_t st) {
     const dim3 grid((unsigned)cdiv(y.d_out, kRows));
     const TX *x = static_cast<const TX *>(X);
     const int deep = (int)pieces_deep(d);
-    if (y.m == 1) few_tokens_kernel<TX, 1><<<grid, kFewWaves * 64, 0, st>>>(W, x, d, ldx, deep, y, y_dtype, status);
-    else few_tokens_kernel<TX, 2><<<grid, kFewWaves * 64, 0, st>>>(W, x, d, ldx, deep, y, y_dtype, status);
+    if (y.m == 1) few_tokens_kernel<TX, E, 1><<<grid, kFewWaves * 64, 0, st>>>(W, x, d, ldx, deep, y, e, y_dtype, status);
+    else few_tokens_kernel<TX, E, 2><<<grid, kFewWaves * 64, 0, st>>>(W, x, d, ldx, deep, y, e, y_dtype, status);
 }
 
 struct Work {
@@ -501,6 +662,48 @@ Work carve(void *ws, int64_t m, int64_t d_in) {
 
 bool sizes_fit(int64_t d_in, int64_t d_out) { return d_in <= kMostDepth && d_out < (1 << 24); }
 
+// What every form of the product is asked for.
+struct Asked {
+    const void *X;  // null: rows in 8 bits
+    int dtype;
+    int64_t d_in, ldx;
+    const int8_t *x_codes, *codes;
+    int y_dtype;
+    int32_t *status;
+};
+
+// Codes the rows if they are not coded yet, then multiplies.  `y.sx` is filled in here.
+template <typename E>
+int run_product(const Asked &a, Scaled y, const E &e, const Work &w, hipStream_t st) {
+    const uint8_t *cw = reinterpret_cast<const uint8_t *>(a.codes);
+    if (a.X && y.m <= 2 && a.d_in <= kFewDepth) {
+        if (a.dtype == CMPQ_F16) launch_few<_Float16>(cw, a.X, a.d_in, a.ldx, y, e, a.y_dtype, a.status, st);
+        else if (a.dtype == CMPQ_BF16) launch_few<__bf16>(cw, a.X, a.d_in, a.ldx, y, e, a.y_dtype, a.status, st);
+        else launch_few<float>(cw, a.X, a.d_in, a.ldx, y, e, a.y_dtype, a.status, st);
+        CMPQ_LAUNCH_CHECK();
+        return CMPQ_OK;
+    }
+    const uint8_t *cx = reinterpret_cast<const uint8_t *>(a.x_codes);
+    if (a.X) {
+        if (int rc = launch_code_rows_of(a.X, a.dtype, y.m, a.d_in, a.ldx, y.m, w.codes, w.scale, {1, 0}, a.status, st)) return rc;
+        cx = reinterpret_cast<const uint8_t *>(w.codes);
+        y.sx = w.scale;
+    }
+    const int deep = (int)pieces_deep(a.d_in);
+    if constexpr (E::kPlain) {
+        if (a.y_dtype == CMPQ_F16) return launch_product<_Float16>(cw, cx, deep, y, e, st);
+        if (a.y_dtype == CMPQ_BF16) return launch_product<__bf16>(cw, cx, deep, y, e, st);
+    }
+    return launch_product<float>(cw, cx, deep, y, e, st);
+}
+
+bool aligned16(const void *p) { return reinterpret_cast<uintptr_t>(p) % 16 == 0; }
+
+// Whether four outputs next to each other may be written, and their scales read, at once.
+bool fours(const void *Y, int y_dtype, int64_t ldy, const float *scale) {
+    return ldy % 4 == 0 && reinterpret_cast<uintptr_t>(Y) % (4 * dtype_bytes(y_dtype)) == 0 && aligned16(scale);
+}
+
 }  // namespace
 
 size_t cmpq_ws_int8_product(int64_t d_in, int64_t m) { return carve(nullptr, m > 0 ? m : 1, d_in).bytes; }
@@ -514,10 +717,25 @@ extern "C" int cmpq_int8_prepare(const void *W, int dtype, int64_t d_out, int64_
                                  float *scale, int32_t *status, void *stream) {
     if (d_out < 0 || d_in < 0 || !serving_dtype(dtype)) return CMPQ_EINVAL;
     if (d_out == 0 || d_in == 0) return CMPQ_OK;
-    if (!W || !codes || !scale || reinterpret_cast<uintptr_t>(codes) % 16) return CMPQ_EINVAL;
+    if (!W || !codes || !scale || !aligned16(codes)) return CMPQ_EINVAL;
     if (ldw < d_in || !sizes_fit(d_in, d_out)) return CMPQ_ESHAPE;
-    return launch_code_rows_of(W, dtype, d_out, d_in, ldw, cdiv(d_out, kRows) * kRows, codes, scale, status,
+    return launch_code_rows_of(W, dtype, d_out, d_in, ldw, cdiv(d_out, kRows) * kRows, codes, scale, {1, 0}, status,
                             static_cast<hipStream_t>(stream));
+}
+
+extern "C" int64_t cmpq_int8_gated_rows(int64_t d_out) { return d_out < 0 || d_out >= (1 << 23) ? 0 : cdiv(d_out, kRows) * 2 * kRows; }
+
+extern "C" int cmpq_int8_prepare_gated(const void *gate, const void *up, int dtype, int64_t d_out, int64_t d_in,
+                                       int64_t ld_gate, int64_t ld_up, int8_t *codes, float *scale, int32_t *status,
+                                       void *stream) {
+    if (d_out < 0 || d_in < 0 || !serving_dtype(dtype)) return CMPQ_EINVAL;
+    if (d_out == 0 || d_in == 0) return CMPQ_OK;
+    if (!gate || !up || !codes || !scale || !aligned16(codes)) return CMPQ_EINVAL;
+    if (ld_gate < d_in || ld_up < d_in || !sizes_fit(d_in, 2 * d_out)) return CMPQ_ESHAPE;
+    const int64_t rows = cdiv(d_out, kRows) * kRows;
+    hipStream_t st = static_cast<hipStream_t>(stream);
+    if (int rc = launch_code_rows_of(gate, dtype, d_out, d_in, ld_gate, rows, codes, scale, {2, 0}, status, st)) return rc;
+    return launch_code_rows_of(up, dtype, d_out, d_in, ld_up, rows, codes, scale, {2, 1}, status, st);
 }
 
 extern "C" int cmpq_int8_product(const void *X, int dtype, int64_t m, int64_t d_in, int64_t ldx, const int8_t *codes,
@@ -525,25 +743,40 @@ extern "C" int cmpq_int8_product(const void *X, int dtype, int64_t m, int64_t d_
                                  size_t ws_bytes, int32_t *status, void *stream) {
     if (m < 0 || d_in < 1 || d_out < 0 || !serving_dtype(dtype) || !serving_dtype(y_dtype)) return CMPQ_EINVAL;
     if (m == 0 || d_out == 0) return CMPQ_OK;
-    if (!X || !codes || !scale || !Y || reinterpret_cast<uintptr_t>(codes) % 16) return CMPQ_EINVAL;
+    if (!X || !codes || !scale || !Y || !aligned16(codes)) return CMPQ_EINVAL;
     if (ldx < d_in || ldy < d_out || m >= (1 << 24) || !sizes_fit(d_in, d_out)) return CMPQ_ESHAPE;
     const Work w = carve(ws, m, d_in);
     if (!ws || reinterpret_cast<uintptr_t>(ws) % 256 || ws_bytes < w.bytes) return CMPQ_EWORKSPACE;
-    hipStream_t st = static_cast<hipStream_t>(stream);
-    const size_t four = 4 * dtype_bytes(y_dtype);
-    const Scaled y = {w.scale, scale, Y, m, d_out, ldy,
-                      ldy % 4 == 0 && reinterpret_cast<uintptr_t>(Y) % four == 0 && reinterpret_cast<uintptr_t>(scale) % 16 == 0};
-    const uint8_t *cw = reinterpret_cast<const uint8_t *>(codes), *cx = reinterpret_cast<const uint8_t *>(w.codes);
-    if (m <= 2 && d_in <= kFewDepth) {
-        if (dtype == CMPQ_F16) launch_few<_Float16>(cw, X, d_in, ldx, y, y_dtype, status, st);
-        else if (dtype == CMPQ_BF16) launch_few<__bf16>(cw, X, d_in, ldx, y, y_dtype, status, st);
-        else launch_few<float>(cw, X, d_in, ldx, y, y_dtype, status, st);
-        CMPQ_LAUNCH_CHECK();
-        return CMPQ_OK;
+    const Scaled y = {nullptr, scale, Y, m, d_out, ldy, fours(Y, y_dtype, ldy, scale)};
+    return run_product(Asked{X, dtype, d_in, ldx, nullptr, codes, y_dtype, status}, y, Plain(), w, static_cast<hipStream_t>(stream));
+}
+
+extern "C" int cmpq_int8_product_job(const cmpq_int8_job *j, void *ws, size_t ws_bytes, void *stream) {
+    if (!j || j->m < 0 || j->d_in < 1 || j->d_out < 0 || !serving_dtype(j->y_dtype) || !known_activation(j->activation)) return CMPQ_EINVAL;
+    if (j->X ? !serving_dtype(j->x_dtype) : false) return CMPQ_EINVAL;
+    if ((j->bias || j->up_bias) && !serving_dtype(j->bias_dtype)) return CMPQ_EINVAL;
+    if ((j->residual && !serving_dtype(j->r_dtype)) || (j->up_bias && !j->gated)) return CMPQ_EINVAL;
+    if (j->m == 0 || j->d_out == 0) return CMPQ_OK;
+    if (!j->codes || !j->scale || !j->Y || !aligned16(j->codes)) return CMPQ_EINVAL;
+    if (!j->X && (!j->x_codes || !j->x_scale || !aligned16(j->x_codes))) return CMPQ_EINVAL;
+    if ((j->X && j->ldx < j->d_in) || j->ldy < j->d_out || (j->residual && j->ldr < j->d_out)) return CMPQ_ESHAPE;
+    if (j->m >= (1 << 24) || !sizes_fit(j->d_in, j->gated ? 2 * j->d_out : j->d_out)) return CMPQ_ESHAPE;
+    Work w = {};
+    if (j->X) {
+        w = carve(ws, j->m, j->d_in);
+        if (!ws || reinterpret_cast<uintptr_t>(ws) % 256 || ws_bytes < w.bytes) return CMPQ_EWORKSPACE;
     }
-    if (int rc = launch_code_rows_of(X, dtype, m, d_in, ldx, m, w.codes, w.scale, status, st)) return rc;
-    const int deep = (int)pieces_deep(d_in);
-    if (y_dtype == CMPQ_F16) return launch_product<_Float16>(cw, cx, deep, y, st);
-    if (y_dtype == CMPQ_BF16) return launch_product<__bf16>(cw, cx, deep, y, st);
-    return launch_product<float>(cw, cx, deep, y, st);
+    const Scaled y = {j->X ? nullptr : j->x_scale, j->scale, j->Y, j->m, j->d_out, j->ldy, fours(j->Y, j->y_dtype, j->ldy, j->scale)};
+    const Asked a = {j->X, j->x_dtype, j->d_in, j->ldx, j->x_codes, j->codes, j->y_dtype, j->status};
+    hipStream_t st = static_cast<hipStream_t>(stream);
+    Epilogue e;
+    e.bias = j->bias, e.up_bias = j->up_bias, e.residual = j->residual, e.ldr = j->ldr;
+    e.bias_dtype = j->bias_dtype, e.r_dtype = j->r_dtype, e.y_dtype = j->y_dtype, e.act = j->activation;
+    if (j->gated) {
+        GatedEpilogue g;
+        static_cast<Epilogue &>(g) = e;
+        return run_product(a, y, g, w, st);
+    }
+    if (!e.bias && !e.residual && e.act == CMPQ_ACT_NONE) return run_product(a, y, Plain(), w, st);
+    return run_product(a, y, e, w, st);
 }

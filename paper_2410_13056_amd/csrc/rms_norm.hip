@@ -1,0 +1,174 @@
+// Root-mean-square norm of a stream, or of two streams' sum, given as values or as rows in 8 bits.
+// A workgroup a row, which stays in registers between its sum of squares and its outputs.  The squares are summed in 64
+// bits, where the order of additions decides nothing that is left after the one rounding to fp32, so a row's codes are those of
+// the definition, whatever the number of lanes.
+#include "epilogue.h"
+#include "int8_rows.h"
+
+namespace {
+
+template <int N>
+__device__ __forceinline__ void round_to(int dtype, float (&x)[N]) {
+    if (dtype == CMPQ_F32) return;
+    with_dtype(dtype, [&](auto like) {
+#pragma unroll
+        for (int i = 0; i < N; ++i) x[i] = (float)(decltype(like))x[i];
+    });
+}
+
+// KEPT steps of THREADS * 8 values hold the row; 0: it is read again for each pass.
+template <int THREADS, int KEPT, bool CODED>
+__global__ __launch_bounds__(THREADS) void rms_norm_kernel(cmpq_norm_job a) {
+#pragma clang fp contract(off)
+    constexpr int kWaves = THREADS / 64, kStep = THREADS * 8, kHeld = KEPT > 0 ? KEPT : 1;
+    __shared__ double sums[kWaves];
+    __shared__ float most[kWaves];
+    const int64_t row = CODED ? die_order(blockIdx.x, gridDim.x) : (int64_t)blockIdx.x;
+    const int d = (int)a.d, first = threadIdx.x * 8;
+    const int whole = CODED ? (int)pieces_deep(d) * kDepth : d;  // what is written of a row
+    uint8_t *codes = nullptr;
+    if (CODED) {
+        codes = reinterpret_cast<uint8_t *>(a.codes) + row / kRows * pieces_deep(d) * kPiece + row % kRows * 16;
+        if (row >= a.m) {  // rows that fill up the last piece
+            for (int i = first; i < whole; i += kStep)
+                *reinterpret_cast<uint2 *>(codes + i / kDepth * kPiece + i % kDepth / 16 * 256 + i % 16) = make_uint2(0, 0);
+            return;
+        }
+    }
+    float x[kHeld][8];
+    Raw8 gain[kHeld];
+    // s = x + a, rounded to its type.  `sum_is_there`: it has been written.
+    auto load = [&](int i, float (&s)[8], bool sum_is_there) {
+        const int n = min(max(d - i, 0), 8);
+        Raw8 p, q;
+        if (sum_is_there) {
+            p.load(a.S, row * a.S.ld + i, n);
+            p.values(a.S.dtype, s);
+            return;
+        }
+        p.load(a.X, row * a.X.ld + i, n);
+        if (a.add.ptr) q.load(a.add, row * a.add.ld + i, n);
+        p.values(a.X.dtype, s);
+        if (a.add.ptr) {
+            float t[8];
+            q.values(a.add.dtype, t);
+#pragma unroll
+            for (int k = 0; k < 8; ++k) s[k] += t[k];
+        }
+        if (a.S.ptr) round_to(a.S.dtype, s);
+    };
+    auto each = [&](auto fn, bool again) {  // fn(values, their first, gain), from registers where they were kept
+        if (KEPT > 0) {
+#pragma unroll
+            for (int k = 0; k < kHeld; ++k)
+                if (first + k * kStep < whole) fn(x[k], first + k * kStep, gain[k]);
+        } else {
+            for (int i = first; i < whole; i += kStep) {
+                load(i, x[0], again && a.S.ptr);
+                if (a.gain.ptr) gain[0].load(a.gain, i, min(max(d - i, 0), 8));
+                fn(x[0], i, gain[0]);
+            }
+        }
+    };
+    if (KEPT > 0) {
+#pragma unroll
+        for (int k = 0; k < kHeld; ++k) load(first + k * kStep, x[k], false);
+        if (a.gain.ptr) {
+#pragma unroll
+            for (int k = 0; k < kHeld; ++k) gain[k].load(a.gain, first + k * kStep, min(max(d - first - k * kStep, 0), 8));
+        }
+    }
+    double sum = 0;
+    each([&](float (&s)[8], int i, const Raw8 &) {
+#pragma unroll
+        for (int k = 0; k < 8; ++k) sum = fma((double)s[k], (double)s[k], sum);
+        if (a.S.ptr && i < d) store_some<8>(a.S.ptr, a.S.dtype, row * a.S.ld + i, min(d - i, 8), s);
+    }, false);
+    sum = wave_sum_f64(sum);
+    if ((threadIdx.x & 63) == 0) sums[threadIdx.x >> 6] = sum;
+    __syncthreads();
+    double q = sums[0];
+#pragma unroll
+    for (int w = 1; w < kWaves; ++w) q += sums[w];
+    const float r = (float)(1.0 / sqrt(q / (double)d + a.eps));
+    bool bad = !(q < __builtin_huge_val());
+    auto normed = [&](float (&s)[8], const Raw8 &g) {
+#pragma unroll
+        for (int k = 0; k < 8; ++k) s[k] *= r;
+        if (a.gain.ptr) {
+            float t[8];
+            g.values(a.gain.dtype, t);
+#pragma unroll
+            for (int k = 0; k < 8; ++k) s[k] *= t[k];
+        }
+    };
+    if (!CODED) {
+        if (bad && a.status && threadIdx.x == 0) atomicOr(a.status, CMPQ_STATUS_NONFINITE);
+        each([&](float (&s)[8], int i, const Raw8 &g) {
+            normed(s, g);
+            if (i < d) store_some<8>(a.Y.ptr, a.Y.dtype, row * a.Y.ld + i, min(d - i, 8), s);
+        }, true);
+        return;
+    }
+    Largest largest;
+    each([&](float (&s)[8], int, const Raw8 &g) {
+        normed(s, g);
+#pragma unroll
+        for (int k = 0; k < 8; ++k) largest.add(s[k]);
+    }, true);
+    if (__ballot(largest.bad())) {
+        bad = true;
+        largest.bits = 0;
+        each([&](float (&s)[8], int, const Raw8 &g) {
+            if (KEPT == 0) normed(s, g);
+#pragma unroll
+            for (int k = 0; k < 8; ++k) largest.add_finite(s[k]);
+        }, true);
+    }
+    if (bad && a.status) atomicOr(a.status, CMPQ_STATUS_NONFINITE);
+    const float scale = code_scale(block_max(largest.most(), most)), inv = 1.f / scale;
+    if (threadIdx.x == 0) a.scale[row] = scale;
+    each([&](float (&s)[8], int i, const Raw8 &g) {
+        if (KEPT == 0) normed(s, g);
+        uint32_t w[2];
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            float v[4];
+#pragma unroll
+            for (int k = 0; k < 4; ++k) v[k] = bad ? no_nan(s[4 * h + k]) : s[4 * h + k];
+            w[h] = low_bytes(code_byte<0>(v[0], inv), code_byte<0>(v[1], inv), code_byte<0>(v[2], inv), code_byte<0>(v[3], inv));
+        }
+        *reinterpret_cast<uint2 *>(codes + i / kDepth * kPiece + i % kDepth / 16 * 256 + i % 16) = make_uint2(w[0], w[1]);
+    }, true);
+}
+
+template <int THREADS, int KEPT>
+void launch_norm(const cmpq_norm_job &a, hipStream_t st) {
+    if (a.codes) rms_norm_kernel<THREADS, KEPT, true><<<dim3((unsigned)(cdiv(a.m, kRows) * kRows)), THREADS, 0, st>>>(a);
+    else rms_norm_kernel<THREADS, KEPT, false><<<dim3((unsigned)a.m), THREADS, 0, st>>>(a);
+}
+
+}  // namespace
+
+extern "C" int cmpq_rms_norm(const cmpq_norm_job *j, void *stream) {
+    if (!j || j->m < 0 || j->d < 1 || !(j->eps >= 0x1p-126 && j->eps < __builtin_huge_val())) return CMPQ_EINVAL;
+    const cmpq_rows all[] = {j->X, j->add, j->gain, j->S, j->Y};
+    for (const cmpq_rows &a : all)
+        if (a.ptr && !serving_dtype(a.dtype)) return CMPQ_EINVAL;
+    if (j->m == 0) return CMPQ_OK;
+    if (!j->Y.ptr == !j->codes || (j->codes && (!j->scale || reinterpret_cast<uintptr_t>(j->codes) % 16))) return CMPQ_EINVAL;
+    if (!j->X.ptr) return CMPQ_EINVAL;
+    if (j->m >= (1 << 24) || j->d > kMostDepth) return CMPQ_ESHAPE;
+    const cmpq_rows rows[] = {j->X, j->add, j->S, j->Y};
+    for (const cmpq_rows &a : rows)
+        if (a.ptr && a.ld < j->d) return CMPQ_ESHAPE;
+    hipStream_t st = static_cast<hipStream_t>(stream);
+    if (j->d <= 2048) launch_norm<256, 1>(*j, st);
+    else if (j->d <= 4096) launch_norm<256, 2>(*j, st);
+    else if (j->d <= 8192) launch_norm<1024, 1>(*j, st);
+    else if (j->d <= 16384) launch_norm<1024, 2>(*j, st);
+    else if (j->d <= 32768) launch_norm<1024, 4>(*j, st);
+    else launch_norm<1024, 0>(*j, st);
+    CMPQ_LAUNCH_CHECK();
+    return CMPQ_OK;
+}

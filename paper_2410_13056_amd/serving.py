@@ -1,11 +1,16 @@
-"""Serving in 8 bits: what a decoder's attention needs beside the products with the mixed-precision
+"""Serving in 8 bits: what a decoder layer needs beside the products with the mixed-precision
 weights (`pipeline.lut_matvec`, `pipeline.group_products`).
 
 * `prepare_int8`, `int8_product`: a linear layer in 8-bit integers, for layers that are not to go below
-  8 bits and for prompts, where multiplications bound the product;
+  8 bits and for prompts, where multiplications bound the product; bias, activation and residual on the way out;
+* `prepare_int8_gated`, `int8_gated_product`: the two projections of a gated feed-forward part in one pass;
+* `rms_norm`: the norm before a part of the layer, with the sum of the residual stream, as values or as rows in 8
+  bits (`Int8Rows`, `int8_rows`), which one coding hands to all products that share the input;
+* `epilogue`: what may follow a product, for products in mixed precision;
+* `feed_forward_block`: norm, gated projections, output projection and residual, as a decoder layer runs them;
 * `KvCache`, `kv_append`, `kv_read`: keys and values in pages of 8-bit codes, keys turned by position on the way in;
 * `kv_attention`: attention over the cache, for single tokens, drafts and chunks of prompts;
-* `attention_block`: the three together, as a decoder layer's attention runs them.
+* `attention_block`: products, cache and attention together, as a decoder layer's attention runs them.
 
 Everything is enqueued on the current stream and nothing synchronises; there is no gradient, since
 codes have none.  `status` ([1] int32, cleared by the caller) collects the flags of `binding.STATUS_*`: codes have no NaN
@@ -65,15 +70,129 @@ def prepare_int8(W: torch.Tensor, status: Optional[torch.Tensor] = None) -> Int8
     return Int8Weight(d_in, d_out, codes, scale)
 
 
-def int8_product(w: Int8Weight, X: torch.Tensor, ws: Optional[B.Workspace] = None,
-                 out_dtype: Optional[torch.dtype] = None, out: Optional[torch.Tensor] = None,
-                 status: Optional[torch.Tensor] = None) -> torch.Tensor:
-    """Y [m, d_out] = X [m, d_in] times the weight, X in 8 bits with a scale per token on the way.  `out_dtype`
-    defaults to X's."""
+@dataclasses.dataclass
+class Int8Rows(_Kept):
+    """Inputs [rows, dim] in 8 bits with a scale each, as the products read them (device tensors)."""
+    rows: int
+    dim: int
+    codes: torch.Tensor     # int8, in the order of the matrix instruction's operands
+    scale: torch.Tensor     # [rows] fp32
+
+    def _make(self) -> B.Int8RowsView:
+        return B.Int8RowsView(self.rows, self.dim, self.codes, self.scale)
+
+
+def _empty_rows(rows: int, dim: int, device) -> Int8Rows:
+    return Int8Rows(rows, dim, torch.empty(B.int8_weight_bytes(rows, dim), dtype=torch.int8, device=device),
+                    torch.empty(rows, dtype=torch.float32, device=device))
+
+
+def int8_rows(X: torch.Tensor, out: Optional[Int8Rows] = None, status: Optional[torch.Tensor] = None) -> Int8Rows:
+    """Inputs X [m, d_in] in 8 bits, coded once for all products that share them: these give what they give for X."""
     if out is None:
-        out = torch.empty((X.shape[0], w.d_out), dtype=out_dtype or X.dtype, device=X.device)
-    w._args(X, out, ws or B.Workspace(X.device), status)
+        out = _empty_rows(X.shape[0], X.shape[1], X.device)
+    elif (out.rows, out.dim) != tuple(X.shape):
+        raise ValueError("the rows in 8 bits must be of X's shape")
+    B.int8_prepare(X, out.codes, out.scale, status)
     return out
+
+
+Inputs = Union[torch.Tensor, Int8Rows]
+
+
+def _output(X: Inputs, d_out: int, out_dtype: Optional[torch.dtype]) -> torch.Tensor:
+    if isinstance(X, Int8Rows):
+        return torch.empty((X.rows, d_out), dtype=out_dtype or torch.float16, device=X.codes.device)
+    return torch.empty((X.shape[0], d_out), dtype=out_dtype or X.dtype, device=X.device)
+
+
+def int8_product(w: Int8Weight, X: Inputs, ws: Optional[B.Workspace] = None,
+                 out_dtype: Optional[torch.dtype] = None, out: Optional[torch.Tensor] = None,
+                 status: Optional[torch.Tensor] = None, bias: Optional[torch.Tensor] = None,
+                 activation: Optional[str] = None, residual: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """Y [m, d_out] = act(X [m, d_in] times the weight + bias) + residual, X in 8 bits with a scale per token on the way, or
+    already (`Int8Rows`).  `out_dtype` defaults to X's (float16 for rows in 8 bits).  `bias` [d_out]; `activation`
+    "silu", "gelu", "gelu_tanh" or "relu"; `residual` [m, d_out], which may be `out` itself; each of its own type.  All of it
+    is worked out in fp32 and rounded once."""
+    if out is None:
+        out = _output(X, w.d_out, out_dtype)
+    coded = isinstance(X, Int8Rows)
+    if not coded and bias is None and activation is None and residual is None:
+        w._args(X, out, ws or B.Workspace(X.device), status)
+    else:
+        w._args.job(X._args if coded else X, out, ws or B.Workspace(out.device), status, bias, None, activation, residual)
+    return out
+
+
+@dataclasses.dataclass
+class Int8GatedWeight(_Kept):
+    """The two projections of a gated feed-forward part as `int8_gated_product` reads them (device tensors)."""
+    d_in: int
+    d_out: int              # of each
+    codes: torch.Tensor     # int8, groups of 16 outputs of the gate and of the second factor in turn
+    scale: torch.Tensor     # fp32, in that order
+
+    def _make(self) -> B.Int8ProductCall:
+        return B.Int8ProductCall(self.d_in, self.d_out, self.codes, self.scale, gated=True)
+
+
+def prepare_int8_gated(W_gate: torch.Tensor, W_up: torch.Tensor, status: Optional[torch.Tensor] = None) -> Int8GatedWeight:
+    """Two weights [d_out, d_in] of one type in 8 bits with a scale per output channel."""
+    d_out, d_in = W_gate.shape
+    rows = B.int8_gated_rows(d_out)
+    codes = torch.empty(B.int8_weight_bytes(rows, d_in), dtype=torch.int8, device=W_gate.device)
+    scale = torch.empty(rows, dtype=torch.float32, device=W_gate.device)
+    B.int8_prepare_gated(W_gate, W_up, codes, scale, status)
+    return Int8GatedWeight(d_in, d_out, codes, scale)
+
+
+def int8_gated_product(w: Int8GatedWeight, X: Inputs, ws: Optional[B.Workspace] = None, activation: Optional[str] = "silu",
+                       gate_bias: Optional[torch.Tensor] = None, up_bias: Optional[torch.Tensor] = None,
+                       out_dtype: Optional[torch.dtype] = None, out: Optional[torch.Tensor] = None,
+                       status: Optional[torch.Tensor] = None, residual: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """H [m, d_out] = act(X Wg' + gate_bias) * (X Wu' + up_bias) (+ residual): one pass over the inputs, neither projection in
+    memory.  Otherwise as `int8_product`; the biases are of one type."""
+    if out is None:
+        out = _output(X, w.d_out, out_dtype)
+    w._args.job(X._args if isinstance(X, Int8Rows) else X, out, ws or B.Workspace(out.device), status, gate_bias, up_bias,
+                activation, residual)
+    return out
+
+
+# ---- what stands between products --------------------------------------------------------------
+
+def epilogue(Y: torch.Tensor, bias: Optional[torch.Tensor] = None, activation: Optional[str] = None,
+             times: Optional[torch.Tensor] = None, times_bias: Optional[torch.Tensor] = None,
+             residual: Optional[torch.Tensor] = None, out_dtype: Optional[torch.dtype] = None,
+             out: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """act(Y + bias) * (times + times_bias) + residual for the outputs Y [m, d] of a product in mixed precision; times and
+    residual are [m, d], the biases [d], each of its own type.  `out_dtype` defaults to Y's; `out` may be Y, times or residual."""
+    if out is None:
+        out = torch.empty(Y.shape, dtype=out_dtype or Y.dtype, device=Y.device)
+    B.epilogue(Y, out, bias, activation, times, times_bias, residual)
+    return out
+
+
+def rms_norm(X: torch.Tensor, weight: Optional[torch.Tensor] = None, eps: float = 1e-6, add: Optional[torch.Tensor] = None,
+             coded: bool = False, out: Optional[Inputs] = None, out_dtype: Optional[torch.dtype] = None,
+             sum_out: Optional[torch.Tensor] = None, status: Optional[torch.Tensor] = None):
+    """s / sqrt(mean(s^2) + eps) * weight along the rows of s = X [m, d], or of s = X + add; the weight [d] may be None.
+    `coded`: as `Int8Rows` for the products that follow, else of `out_dtype`, by default X's.  With `add` the answer is (norm, s),
+    s of X's type unless `sum_out` says otherwise, which may be X or `add` itself; the norm is that of s as rounded."""
+    if out is None:
+        out = _empty_rows(X.shape[0], X.shape[1], X.device) if coded else \
+            torch.empty(X.shape, dtype=out_dtype or X.dtype, device=X.device)
+    if add is not None and sum_out is None:
+        sum_out = torch.empty(X.shape, dtype=X.dtype, device=X.device)
+    B.rms_norm(X, weight, eps, out._args if isinstance(out, Int8Rows) else out, add, sum_out, status)
+    return out if add is None else (out, sum_out)
+
+
+@dataclasses.dataclass
+class RmsNorm:
+    """A norm's weight [d] (None: ones) and epsilon, as `rms_norm` takes them."""
+    weight: Optional[torch.Tensor] = None
+    eps: float = 1e-6
 
 
 # ---- the cache -------------------------------------------------------------------------------
@@ -181,7 +300,7 @@ Layer = Union[Int8Weight, P.Deployed, Callable[[torch.Tensor], torch.Tensor]]
 def apply_layer(layer: Layer, X: torch.Tensor, ws: B.Workspace, status: Optional[torch.Tensor] = None) -> torch.Tensor:
     """X [m, d_in] times a layer in whichever form it was prepared: 8-bit integers, the mixed-precision tables
     (fp32 out of FP16 in), or any function.  The last two carry a NaN or an infinity on into their outputs; 8-bit
-    integers raise it in `status`."""
+    integers raise it in `status`, and take rows in 8 bits too."""
     if isinstance(layer, Int8Weight):
         return int8_product(layer, X, ws, out_dtype=torch.float32, status=status)
     if isinstance(layer, P.Deployed):
@@ -195,22 +314,84 @@ def _as_heads(Y: torch.Tensor, head_dim: int) -> torch.Tensor:
     return Y.reshape(Y.shape[0], Y.shape[1] // head_dim, head_dim)
 
 
+def _normed(X: torch.Tensor, norm: Optional[RmsNorm], layers, status: Optional[torch.Tensor]) -> Inputs:
+    """What layers take that share the input X: its norm if there is one, in 8 bits if all of them are."""
+    if norm is None:
+        return X
+    if all(isinstance(l, Int8Weight) for l in layers):
+        return rms_norm(X, norm.weight, norm.eps, coded=True, status=status)
+    wide = not any(isinstance(l, P.Deployed) for l in layers)            # those read float16
+    return rms_norm(X, norm.weight, norm.eps, out_dtype=X.dtype if wide else torch.float16, status=status)
+
+
 def attention_block(cache: KvCache, X: torch.Tensor, q: Layer, k: Layer, v: Layer, o: Layer, page_table: torch.Tensor,
                     held: torch.Tensor, lengths: torch.Tensor, cu_rows: torch.Tensor, max_rows: int,
                     max_length: int, ws: B.Workspace, rotation: Optional[Rotation] = None, causal: bool = True,
                     window: int = 0, status: Optional[torch.Tensor] = None,
-                    attention_dtype: Optional[torch.dtype] = None) -> torch.Tensor:
+                    attention_dtype: Optional[torch.dtype] = None, norm: Optional[RmsNorm] = None) -> torch.Tensor:
     """A decoder layer's attention for new tokens X [rows, hidden] of several sequences (see `kv_append`; lengths[i] =
     held[i] + the sequence's rows): the three projections, keys and values into the cache, attention over it, the
     output projection [rows, hidden].  The projections may be of different kinds, for instance queries and outputs in
     mixed precision and the short key and value layers in 8 bits.  `status` collects the flags of all of them.
     `attention_dtype`, float16 or bfloat16: what the attention hands to `o`.  By default bfloat16 for a bfloat16 X, whose
-    values may pass float16's range, unless `o` is in mixed precision, which reads float16; else float16."""
+    values may pass float16's range, unless `o` is in mixed precision, which reads float16; else float16.
+    `norm`: X is the residual stream, and the projections take its norm."""
     if attention_dtype is None:
         wide = X.dtype == torch.bfloat16 and not isinstance(o, P.Deployed)
         attention_dtype = torch.bfloat16 if wide else torch.float16
+    X = _normed(X, norm, (q, k, v), status)
     Q, K, V = (_as_heads(apply_layer(layer, X, ws, status), cache.head_dim) for layer in (q, k, v))
     kv_append(cache, K, V, page_table, held, cu_rows, rotation, status)
     O = kv_attention(cache, Q, page_table, lengths, cu_rows, max_rows, max_length, ws, causal=causal, window=window,
                      rotation=rotation, out_dtype=attention_dtype, status=status)
     return apply_layer(o, O.flatten(1), ws, status)
+
+
+# ---- a decoder layer's feed-forward part ---------------------------------------------------------
+
+@dataclasses.dataclass
+class GatedLayers(_Kept):
+    """The two projections of a gated feed-forward part as layers of any kind; two in mixed precision are launched together."""
+    gate: Layer
+    up: Layer
+
+    def _make(self) -> Optional[B.LutMatvecGroupCall]:
+        both = isinstance(self.gate, P.Deployed) and isinstance(self.up, P.Deployed)
+        return P.group_products([self.gate, self.up]) if both else None
+
+    def apply(self, X: torch.Tensor, ws: B.Workspace, status: Optional[torch.Tensor] = None):
+        """Both projections of X [m, d_in]."""
+        if self._args is None:
+            return tuple(_as_matrix(apply_layer(l, X, ws, status)) for l in (self.gate, self.up))
+        X = X.to(torch.float16)
+        Y = [torch.empty((X.shape[0], l.d_out), dtype=torch.float32, device=X.device) for l in (self.gate, self.up)]
+        if X.shape[0]:
+            self._args([X, X], Y, ws)
+        return tuple(Y)
+
+
+def _as_matrix(Y: torch.Tensor) -> torch.Tensor:
+    return Y if Y.stride(1) == 1 or Y.shape[1] == 1 else Y.contiguous()
+
+
+def feed_forward_block(X: torch.Tensor, norm: RmsNorm, gate_up: Union[Int8GatedWeight, GatedLayers], down: Layer,
+                       ws: B.Workspace, add: Optional[torch.Tensor] = None, activation: Optional[str] = "silu",
+                       status: Optional[torch.Tensor] = None, hidden_dtype: Optional[torch.dtype] = None) -> torch.Tensor:
+    """A decoder layer's gated feed-forward part on the residual stream: s + down(act(gate n) * (up n)), n the norm of s = X
+    [rows, hidden] (+ `add`, what the layer's attention gave, in any type).  The projections may be of different kinds, as in
+    `attention_block`; the answer has X's type.  `hidden_dtype`: what `down` is handed, by default X's type, or
+    float16 where `down` is in mixed precision, which reads that."""
+    if hidden_dtype is None:
+        hidden_dtype = torch.float16 if isinstance(down, P.Deployed) else X.dtype
+    gated = isinstance(gate_up, Int8GatedWeight)
+    mixed = not gated and any(isinstance(l, P.Deployed) for l in (gate_up.gate, gate_up.up))
+    N = rms_norm(X, norm.weight, norm.eps, add=add, coded=gated, out_dtype=torch.float16 if mixed else X.dtype, status=status)
+    N, stream = N if add is not None else (N, X)
+    if gated:
+        H = int8_gated_product(gate_up, N, ws, activation, out_dtype=hidden_dtype, status=status)
+    else:
+        G, U = gate_up.apply(N, ws, status)
+        H = epilogue(G, activation=activation, times=U, out_dtype=hidden_dtype)
+    if isinstance(down, Int8Weight):
+        return int8_product(down, H, ws, out_dtype=X.dtype, status=status, residual=stream)
+    return epilogue(_as_matrix(apply_layer(down, H, ws, status)), residual=stream, out_dtype=X.dtype)
