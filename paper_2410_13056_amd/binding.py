@@ -708,39 +708,46 @@ def activation(name: Optional[str]) -> int:
         raise ValueError(f"activation is one of {[n for n in ACTIVATIONS if n]} or None, got {name!r}") from None
 
 
-def _here(t: torch.Tensor) -> int:
-    """The address of a tensor on the current device, whose stream the call goes to."""
-    if not t.is_cuda:
-        raise ValueError("cmpq entry points take device tensors")
-    if t.get_device() != (torch.cuda.current_device() if _current_device is None else _current_device()):
-        raise ValueError("tensors must be on the current device")
-    return t.data_ptr()
+def _device() -> int:
+    """The current device, whose stream a call goes to."""
+    return torch.cuda.current_device() if _current_device is None else _current_device()
 
 
-def _matrix(t: torch.Tensor, m: int, d: int, what: str):
+def _not_here(t: torch.Tensor):
+    return ValueError("tensors must be on the current device" if t.is_cuda else "cmpq entry points take device tensors")
+
+
+def _matrix(t: torch.Tensor, m: int, d: int, dev: int, what: str):
     """(address, leading dimension, type) of a [m, d] tensor whose rows are contiguous: a `cmpq_rows`."""
-    if t.dim() == 2:
-        shape, (ld, unit) = t.shape, t.stride()
-        if shape[0] == m and shape[1] == d and (unit == 1 or d <= 1):
-            return _here(t), ld if m > 1 else d, serving_dtype(t.dtype)
-    raise ValueError(f"{what} must be [{m}, {d}] with unit stride along its rows")
+    if t.shape != (m, d):
+        raise ValueError(f"{what} must be [{m}, {d}], got {list(t.shape)}")
+    ld, unit = t.stride()
+    if unit != 1 and d > 1:
+        raise ValueError(f"{what} must have unit stride along its rows")
+    if t.get_device() != dev:
+        raise _not_here(t)
+    return t.data_ptr(), ld if m > 1 else d, serving_dtype(t.dtype)
 
 
-def _vector(t: torch.Tensor, d: int, what: str):
-    if t.dim() != 1 or t.shape[0] != d or not t.is_contiguous():
+def _vector(t: torch.Tensor, d: int, dev: int, what: str):
+    if t.shape != (d,) or not t.is_contiguous():
         raise ValueError(f"{what} must be contiguous [{d}]")
-    return _here(t), 0, serving_dtype(t.dtype)
+    if t.get_device() != dev:
+        raise _not_here(t)
+    return t.data_ptr(), 0, serving_dtype(t.dtype)
 
 
 _NONE = (None, 0, 0)
 
 
-def _flags(status: Optional[torch.Tensor]) -> Optional[int]:
+def _flags(status: Optional[torch.Tensor], dev: int) -> Optional[int]:
     if status is None:
         return None
     if status.dtype != torch.int32 or status.numel() < 1:
         raise ValueError("status must be int32 [1]")
-    return _here(status)
+    if status.get_device() != dev:
+        raise _not_here(status)
+    return status.data_ptr()
 
 
 _SERVING = {torch.float16: F16, torch.float32: F32, torch.bfloat16: BF16}
@@ -785,10 +792,12 @@ def int8_prepare_gated(gate: torch.Tensor, up: torch.Tensor, codes: torch.Tensor
     d_out, d_in = gate.shape
     if gate.dtype != up.dtype:
         raise ValueError("gate and up must have the same dtype")
-    (g, ldg, dtype), (u, ldu, _) = _matrix(gate, d_out, d_in, "gate"), _matrix(up, d_out, d_in, "up")
-    rows = int8_gated_rows(d_out)
-    _int8_operand(codes, scale, rows, d_in)
-    _check(lib().cmpq_int8_prepare_gated(g, u, dtype, d_out, d_in, ldg, ldu, _here(codes), _here(scale), _flags(status),
+    dev = _device()
+    (g, ldg, dtype), (u, ldu, _) = _matrix(gate, d_out, d_in, dev, "gate"), _matrix(up, d_out, d_in, dev, "up")
+    _int8_operand(codes, scale, int8_gated_rows(d_out), d_in)
+    if codes.get_device() != dev or scale.get_device() != dev:
+        raise _not_here(codes)
+    _check(lib().cmpq_int8_prepare_gated(g, u, dtype, d_out, d_in, ldg, ldu, codes.data_ptr(), scale.data_ptr(), _flags(status, dev),
                                          _stream()), "cmpq_int8_prepare_gated")
 
 
@@ -802,10 +811,13 @@ def _int8_operand(codes: torch.Tensor, scale: torch.Tensor, rows: int, dim: int)
 
 class Int8RowsView:
     """Inputs of a product in 8 bits, as the library takes them.  Holds the tensors it points into."""
+    __slots__ = ("rows", "dim", "codes", "scale", "device", "keep")
 
-    def __init__(self, rows: int, dim: int, codes: torch.Tensor, scale: torch.Tensor):
-        _int8_operand(codes, scale, rows, dim)
-        self.rows, self.dim, self.codes, self.scale = int(rows), int(dim), _ptr(codes), _ptr(scale)
+    def __init__(self, rows: int, dim: int, codes: torch.Tensor, scale: torch.Tensor, fits: bool = False):
+        """`fits`: the tensors were made for these sizes."""
+        if not fits:
+            _int8_operand(codes, scale, rows, dim)
+        self.rows, self.dim, self.codes, self.scale, self.device = rows, dim, _ptr(codes), _ptr(scale), codes.get_device()
         self.keep = (codes, scale)
 
 
@@ -821,31 +833,29 @@ class Int8ProductCall:
             raise ValueError("scale must be contiguous float32 [d_out]")
         self._keep = (codes, scale)
         self.d_in, self.d_out, self._codes, self._scale = int(d_in), int(d_out), _ptr(codes), _ptr(scale)
-        self._gated, self._fn = int(bool(gated)), lib().cmpq_int8_product
+        self._gated, self._fn, self._device = int(bool(gated)), lib().cmpq_int8_product, codes.get_device()
 
     def job(self, X, Y: torch.Tensor, ws: Workspace, status: Optional[torch.Tensor] = None, bias: Optional[torch.Tensor] = None,
             up_bias: Optional[torch.Tensor] = None, act: Optional[str] = None, residual: Optional[torch.Tensor] = None) -> None:
         """The product with what follows it; X a tensor [m, d_in] or an `Int8RowsView`."""
-        d, o = self.d_in, self.d_out
+        d, o, dev = self.d_in, self.d_out, _device()
         if isinstance(X, Int8RowsView):
             if X.dim != d:
                 raise ValueError(f"rows of {X.dim} inputs for a layer of {d}")
-            m, x, ldx, xt, xc, xs = X.rows, None, 0, 0, X.codes, X.scale
-            if X.keep[0].device != Y.device:
-                raise ValueError("tensors must be on the current device")
+            m, x, ldx, xt, xc, xs, at = X.rows, None, 0, 0, X.codes, X.scale, X.device
         else:
-            m, xc, xs = X.shape[0], None, None
-            x, ldx, xt = _matrix(X, m, d, "X")
-        if self._keep[0].device != Y.device:
-            raise ValueError("tensors must be on the current device")
-        y, ldy, yt = _matrix(Y, m, o, "Y")
-        b, _, bt = _NONE if bias is None else _vector(bias, o, "bias")
-        u, _, ut = _NONE if up_bias is None else _vector(up_bias, o, "up_bias")
+            m, xc, xs, at = X.shape[0], None, None, dev
+            x, ldx, xt = _matrix(X, m, d, dev, "X")
+        if self._device != dev or at != dev:
+            raise ValueError("layers and rows in 8 bits must be on the current device")
+        y, ldy, yt = _matrix(Y, m, o, dev, "Y")
+        b, _, bt = _NONE if bias is None else _vector(bias, o, dev, "bias")
+        u, _, ut = _NONE if up_bias is None else _vector(up_bias, o, dev, "up_bias")
         if b and u and bt != ut:
             raise ValueError("both biases must have the same dtype")
-        r, ldr, rt = _NONE if residual is None else _matrix(residual, m, o, "residual")
+        r, ldr, rt = _NONE if residual is None else _matrix(residual, m, o, dev, "residual")
         j = Int8Job(x, xt, m, d, ldx, xc, xs, self._codes, self._scale, o, self._gated, b, u, bt if b else ut,
-                    activation(act), r, rt, ldr, y, yt, ldy, _flags(status))
+                    activation(act), r, rt, ldr, y, yt, ldy, _flags(status, dev))
         for _ in range(2):          # asks for the workspace's size only where what is there does not do
             buf = ws.buf
             rc = _lib.cmpq_int8_product_job(j, buf.data_ptr(), buf.numel(), _stream())
@@ -883,10 +893,11 @@ def epilogue(Y: torch.Tensor, out: torch.Tensor, bias: Optional[torch.Tensor] = 
              residual: Optional[torch.Tensor] = None) -> None:
     """`cmpq_epilogue`: out [m, d] = act(Y + bias) * (times + times_bias) + residual."""
     m, d = Y.shape
-    j = EpilogueJob(*_matrix(Y, m, d, "Y"), *(_NONE if bias is None else _vector(bias, d, "bias")),
-                    *(_NONE if times is None else _matrix(times, m, d, "times")),
-                    *(_NONE if times_bias is None else _vector(times_bias, d, "times_bias")),
-                    *(_NONE if residual is None else _matrix(residual, m, d, "residual")), *_matrix(out, m, d, "out"),
+    dev = _device()
+    j = EpilogueJob(*_matrix(Y, m, d, dev, "Y"), *(_NONE if bias is None else _vector(bias, d, dev, "bias")),
+                    *(_NONE if times is None else _matrix(times, m, d, dev, "times")),
+                    *(_NONE if times_bias is None else _vector(times_bias, d, dev, "times_bias")),
+                    *(_NONE if residual is None else _matrix(residual, m, d, dev, "residual")), *_matrix(out, m, d, dev, "out"),
                     m, d, activation(act))
     rc = lib().cmpq_epilogue(j, _stream())
     if rc:
@@ -897,15 +908,18 @@ def rms_norm(X: torch.Tensor, gain: Optional[torch.Tensor], eps: float, Y, add: 
              S: Optional[torch.Tensor] = None, status: Optional[torch.Tensor] = None) -> None:
     """`cmpq_rms_norm`: the norm of X (+ add) [m, d] into Y, a tensor or an `Int8RowsView`; the sum into S."""
     m, d = X.shape
+    dev = _device()
     if isinstance(Y, Int8RowsView):
-        if (Y.rows, Y.dim) != (m, d) or Y.keep[0].device != X.device:
-            raise ValueError(f"the rows in 8 bits must be [{m}, {d}], on the device of X")
+        if (Y.rows, Y.dim) != (m, d):
+            raise ValueError(f"the rows in 8 bits must be [{m}, {d}]")
+        if Y.device != dev:
+            raise ValueError("layers and rows in 8 bits must be on the current device")
         y, codes, scale = _NONE, Y.codes, Y.scale
     else:
-        y, codes, scale = _matrix(Y, m, d, "Y"), None, None
-    j = NormJob(*_matrix(X, m, d, "X"), *(_NONE if add is None else _matrix(add, m, d, "add")),
-                *(_NONE if gain is None else _vector(gain, d, "weight")), *(_NONE if S is None else _matrix(S, m, d, "the sum")),
-                *y, codes, scale, m, d, eps, _flags(status))
+        y, codes, scale = _matrix(Y, m, d, dev, "Y"), None, None
+    j = NormJob(*_matrix(X, m, d, dev, "X"), *(_NONE if add is None else _matrix(add, m, d, dev, "add")),
+                *(_NONE if gain is None else _vector(gain, d, dev, "weight")), *(_NONE if S is None else _matrix(S, m, d, dev, "the sum")),
+                *y, codes, scale, m, d, eps, _flags(status, dev))
     rc = lib().cmpq_rms_norm(j, _stream())
     if rc:
         _check(rc, "cmpq_rms_norm")

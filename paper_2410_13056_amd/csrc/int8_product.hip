@@ -51,23 +51,24 @@ struct Turn {
     int of, at;
 };
 
-// One workgroup a row: its largest magnitude, then its codes, 16 inputs a lane and step.  Rows of up to KEPT * 4096
+// One workgroup a row: its largest magnitude, then its codes, 16 inputs a lane and step.  Rows of up to KEPT * THREADS * 16
 // inputs stay in registers between the two, longer ones are read again.  The rows of a piece write 16 bytes each
 // of the same lines, so consecutive rows go to one die, whose cache puts the lines together.  Bound by bytes where rows are
 // many: 4096 rows of 8192 in FP16 29 us, 3.5 TB/s (three quarters of a copy's rate; vector instructions 38 %); by a row's latency
-// where they are few: 333 rows 4 us.
-template <typename T, int KEPT>
-__global__ __launch_bounds__(256) void code_rows_kernel(const T *__restrict__ X, int64_t n, int64_t d, int64_t ld,
+// where they are few: 333 rows 4 us.  Long rows where there are few of them take 16 wavefronts in place of 4: 1 row of 28672 5.1
+// us and 6.3, 16 of 13824 4.7 and 5.2, but 1 of 8192 4.1 and 3.6, 700 of 13824 9.9 and 8.4; 2048 of 28672 33 us kept, 45 read twice.
+template <typename T, int THREADS, int KEPT>
+__global__ __launch_bounds__(THREADS) void code_rows_kernel(const T *__restrict__ X, int64_t n, int64_t d, int64_t ld,
                                                         int8_t *__restrict__ codes, float *__restrict__ scale, Turn turn,
                                                         int32_t *__restrict__ status) {
-    __shared__ float scratch[4];
+    __shared__ float scratch[THREADS / 64];
     const int64_t row = die_order(blockIdx.x, gridDim.x), deep = pieces_deep(d), group = row / kRows * turn.of + turn.at;
     uint8_t *out = reinterpret_cast<uint8_t *>(codes) + group * deep * kPiece + row % kRows * 16;
     const int groups = (int)deep * 4;
     scale += group * kRows + row % kRows;
     if (row >= n) {  // rows that fill up the last piece
         if (turn.of > 1 && threadIdx.x == 0) *scale = 0.f;
-        for (int c = threadIdx.x; c < groups; c += 256)
+        for (int c = threadIdx.x; c < groups; c += THREADS)
             *reinterpret_cast<uint4 *>(out + c / 4 * kPiece + c % 4 * 256) = make_uint4(0, 0, 0, 0);
         return;
     }
@@ -78,9 +79,9 @@ __global__ __launch_bounds__(256) void code_rows_kernel(const T *__restrict__ X,
         if (KEPT > 0) {
 #pragma unroll
             for (int k = 0; k < KEPT; ++k)
-                if ((int)threadIdx.x + k * 256 < groups) fn(kept[k], (int)threadIdx.x + k * 256);
+                if ((int)threadIdx.x + k * THREADS < groups) fn(kept[k], (int)threadIdx.x + k * THREADS);
         } else {
-            for (int c = threadIdx.x; c < groups; c += 256) {
+            for (int c = threadIdx.x; c < groups; c += THREADS) {
                 kept[0].load(x + c * 16, d - c * 16);
                 fn(kept[0], c);
             }
@@ -89,7 +90,7 @@ __global__ __launch_bounds__(256) void code_rows_kernel(const T *__restrict__ X,
     if (KEPT > 0) {
 #pragma unroll
         for (int k = 0; k < KEPT; ++k) {
-            const int c = threadIdx.x + k * 256;
+            const int c = threadIdx.x + k * THREADS;
             kept[k].load(x + c * 16, c < groups ? d - c * 16 : 0);
         }
     }
@@ -109,15 +110,27 @@ __global__ __launch_bounds__(256) void code_rows_kernel(const T *__restrict__ X,
     else each([&](const Sixteen<T> &s, int c) { put(s, c, true); });
 }
 
+template <int N>
+using Kept = std::integral_constant<int, N>;
+
 template <typename T>
 void launch_code_rows(const void *X, int64_t n, int64_t d, int64_t ld, int64_t rows, int8_t *codes, float *scale,
                       Turn turn, int32_t *status, hipStream_t st) {
     const dim3 grid((unsigned)rows);
     const T *x = static_cast<const T *>(X);
-    if (d <= 4096) code_rows_kernel<T, 1><<<grid, 256, 0, st>>>(x, n, d, ld, codes, scale, turn, status);
-    else if (d <= 8192) code_rows_kernel<T, 2><<<grid, 256, 0, st>>>(x, n, d, ld, codes, scale, turn, status);
-    else if (d <= 16384) code_rows_kernel<T, 4><<<grid, 256, 0, st>>>(x, n, d, ld, codes, scale, turn, status);
-    else code_rows_kernel<T, 0><<<grid, 256, 0, st>>>(x, n, d, ld, codes, scale, turn, status);
+    const auto run = [&](auto threads, auto kept) {
+        code_rows_kernel<T, threads(), kept()><<<grid, threads(), 0, st>>>(x, n, d, ld, codes, scale, turn, status);
+    };
+    typedef std::integral_constant<int, 256> Four;  // wavefronts
+    typedef std::integral_constant<int, 1024> Many;
+    const bool few = rows <= 256;
+    if (d <= 4096) run(Four(), Kept<1>());
+    else if (d <= 8192) run(Four(), Kept<2>());
+    else if (d <= 16384 && few) run(Many(), Kept<1>());
+    else if (d <= 32768 && few) run(Many(), Kept<2>());
+    else if (d <= 16384) run(Four(), Kept<4>());
+    else if (d <= 32768) run(Four(), Kept<8>());
+    else run(Four(), Kept<0>());
 }
 
 // `rows` of them, those from n on zeros.
@@ -341,44 +354,58 @@ __global__ __launch_bounds__(WAVES * 64) void shared_depth_kernel(const uint8_t 
 
 // One or two tokens in one launch: every workgroup codes the tokens for itself, 16 inputs a lane, while the first pieces
 // of its 16 outputs' weights are on their way; the wavefronts share the depth.  Against coding them in a launch of
-// its own, us: 1 token 8192 -> 1024 5.2 and 8.2, -> 28672 34.6 and 38.5; 2 tokens 8192 -> 8192 11.8 and 15.4; 4
-// tokens 20.5 and 15.4, which is why it ends there.  Small ones are bound by what comes one after the other (the token,
-// its largest, two barriers, the products, the join), large ones by the weights' bytes.
-constexpr int kFewWaves = 16, kFewDepth = kFewWaves * 64 * 16;
+// its own, us: 1 token 8192 -> 1024 5.2 and 8.2, -> 28672 34.6 and 38.5, 28672 -> 8192 37.7 and 41.6, -> 512 9.1 and 18.6; 2 tokens
+// 8192 -> 8192 11.8 and 15.4, 28672 -> 1000 12.0 and 19.4, -> 4000 23.6 and 27.0 (a gated product's second token of more
+// than 16384 inputs has no room in registers); 4 tokens 20.5 and 15.4, which is why it ends there.  Small ones are bound by what comes one after the other (the
+// token, its largest, two barriers, the products, the join), large ones by the weights' bytes.
+// Wavefronts, us with 8 and 16: 1 token 5120 -> 13824 13.0 and 15.7, 4096 -> 11008 7.8 and 8.9, but 8192 -> 28672 36.3 and
+// 34.8; gated 5120 -> 2 x 13824 23.9 and 30.5, 8192 -> 2 x 28672 87.7 (8 steps ahead; 93 with 4) and 95, at 5.4 TB/s.
+constexpr int kFewDepth = 16384;
 
-template <typename TX, typename E, int M>
-__global__ __launch_bounds__(kFewWaves * 64) void few_tokens_kernel(const uint8_t *__restrict__ W, const TX *__restrict__ X,
+template <typename TX, typename E, int M, int C, int WAVES>  // up to C * 1024 * WAVES inputs
+__global__ __launch_bounds__(WAVES * 64) void few_tokens_kernel(const uint8_t *__restrict__ W, const TX *__restrict__ X,
                                                                     int64_t d, int64_t ldx, int deep, Scaled y, E e, int dtype,
                                                                     int32_t *__restrict__ status) {
-    constexpr int kAhead = 4, P = kPerOutput<E>;
-    __shared__ __align__(16) uint8_t codes[M * kFewDepth];
-    __shared__ Int4 red[P][kFewWaves][64];
-    __shared__ float most[M][kFewWaves], scales[M];
+    constexpr int kAhead = E::kGated && WAVES == 8 ? 8 : 4, P = kPerOutput<E>, kMost = C * WAVES * 1024;
+    __shared__ __align__(16) uint8_t codes[M * kMost];
+    __shared__ Int4 red[P][WAVES][64];
+    __shared__ float most[M][WAVES], scales[M];
     const int lane = threadIdx.x & 63, wave = wave_index(), m = (int)y.m;
     const uint8_t *w = W + (int64_t)blockIdx.x * P * deep * kPiece + lane * 16;
-    const int k0 = deep * wave / kFewWaves, k1 = deep * (wave + 1) / kFewWaves;
+    const int k0 = deep * wave / WAVES, k1 = deep * (wave + 1) / WAVES;
     Int4 a[kAhead][P];
+    // Past the wavefront's share: with 8 wavefronts nothing, where that would be much of its steps; else bytes that nothing
+    // multiplies, which costs less there than to ask.
+    constexpr bool kAsk = WAVES == 8;
     auto load = [&](int k) {
+        const bool all = k + kAhead <= k1;
 #pragma unroll
-        for (int u = 0; u < kAhead; ++u)
+        for (int u = 0; u < kAhead; ++u) {
+            if (kAsk && !all && k + u >= k1) break;
+            const int at = kAsk ? k + u : min(k + u, deep - 1);
 #pragma unroll
-            for (int p = 0; p < P; ++p)
-                a[u][p] = *reinterpret_cast<const Int4 *>(w + ((int64_t)p * deep + min(k + u, deep - 1)) * kPiece);
+            for (int p = 0; p < P; ++p) a[u][p] = *reinterpret_cast<const Int4 *>(w + ((int64_t)p * deep + at) * kPiece);
+        }
     };
-    const int c = threadIdx.x, chunks = deep * 4;
-    Sixteen<TX> x[M];
+    const int chunks = deep * 4;
+    const auto chunk = [&](int i) { return (int)threadIdx.x + i * (WAVES * 64); };
+    Sixteen<TX> x[M][C];
 #pragma unroll
-    for (int t = 0; t < M; ++t) x[t].load(X + min(t, m - 1) * ldx + c * 16, c < chunks ? d - c * 16 : 0);
+    for (int t = 0; t < M; ++t)
+#pragma unroll
+        for (int i = 0; i < C; ++i) x[t][i].load(X + min(t, m - 1) * ldx + chunk(i) * 16, chunk(i) < chunks ? d - chunk(i) * 16 : 0);
     load(k0);
     bool bad = false;
 #pragma unroll
     for (int t = 0; t < M; ++t) {
         Largest largest;
-        x[t].look(largest);
+#pragma unroll
+        for (int i = 0; i < C; ++i) x[t][i].look(largest);
         if (__ballot(largest.bad())) {
             bad = true;
             largest.bits = 0;
-            x[t].look_again(largest);
+#pragma unroll
+            for (int i = 0; i < C; ++i) x[t][i].look_again(largest);
         }
         float v = largest.most();
 #pragma unroll
@@ -391,14 +418,16 @@ __global__ __launch_bounds__(kFewWaves * 64) void few_tokens_kernel(const uint8_
     for (int t = 0; t < M; ++t) {
         float v = most[t][0];
 #pragma unroll
-        for (int q = 1; q < kFewWaves; ++q) v = fmaxf(v, most[t][q]);
+        for (int q = 1; q < WAVES; ++q) v = fmaxf(v, most[t][q]);
         const float s = code_scale(v), inv = 1.f / s;
         if (threadIdx.x == 0) scales[t] = s;
-        if (c < chunks) *reinterpret_cast<uint4 *>(codes + t * kFewDepth + c * 16) = x[t].codes(inv, !bad);
+#pragma unroll
+        for (int i = 0; i < C; ++i)
+            if (chunk(i) < chunks) *reinterpret_cast<uint4 *>(codes + t * (kMost) + chunk(i) * 16) = x[t][i].codes(inv, !bad);
     }
     __syncthreads();
     Int4 acc[P] = {};
-    const uint8_t *mine = codes + min(lane & 15, m - 1) * kFewDepth + (lane >> 4) * 16;
+    const uint8_t *mine = codes + min(lane & 15, m - 1) * (kMost) + (lane >> 4) * 16;
     for (int k = k0; k < k1; k += kAhead) {
 #pragma unroll
         for (int u = 0; u < kAhead; ++u) {
@@ -414,7 +443,7 @@ __global__ __launch_bounds__(kFewWaves * 64) void few_tokens_kernel(const uint8_
     __syncthreads();
     if (wave != 0) return;
 #pragma unroll 5  // more at once would take the registers of a second workgroup a unit
-    for (int v = 1; v < kFewWaves; ++v)
+    for (int v = 1; v < WAVES; ++v)
 #pragma unroll
         for (int p = 0; p < P; ++p) acc[p] += red[p][v][lane];
     const int64_t o = (int64_t)blockIdx.x * kRows + (lane >> 4) * 4;
@@ -486,13 +515,16 @@ __device__ __forceinline__ void finish_rows(const Int4 *sums, const Scaled &y, c
 // cache while the weights pass once a band.
 constexpr int kBand = 4;
 
-template <typename T, typename E, int OT, int TT, int WO, int WT, int BUFS>
-__global__ __launch_bounds__(WO * WT * 64, 2) void tile_kernel(const uint8_t *__restrict__ W, const uint8_t *__restrict__ X,
+template <typename T, typename E, int OT, int TT, int WO, int WT, int G, int BUFS>
+__global__ __launch_bounds__(WO * WT * G * 64, 2) void tile_kernel(const uint8_t *__restrict__ W, const uint8_t *__restrict__ X,
                                                                int deep, int o_tiles, int t_tiles, Scaled y, E e) {
     constexpr int kWaves = WO * WT, kLoads = (OT + TT) / kWaves, kStepBytes = (OT + TT) * kPiece, A = OT / WO, B = TT / WT;
     static_assert(kLoads * kWaves == OT + TT && A * WO == OT && B * WT == TT, "shares of the wavefronts");
-    __shared__ __align__(16) uint8_t smem[BUFS * kStepBytes];
-    const int lane = threadIdx.x & 63, wave = wave_index();
+    static_assert((G - 1) * OT * TT <= G * BUFS * (OT + TT), "room for the sums that are joined");
+    __shared__ __align__(16) uint8_t smem[G * BUFS * kStepBytes];
+    const int lane = threadIdx.x & 63, wave = G > 1 ? wave_index() % kWaves : wave_index(), group = G > 1 ? wave_index() / kWaves : 0;
+    const int each = G > 1 ? (deep / 2 + G - 1) / G * 2 : deep;  // steps of a group, the last one's perhaps fewer
+    const int from = group * each, mine = G > 1 ? min(each, deep - from) : deep;
     // bands of kBand token tiles, all output tiles of a band one after the other
     const int64_t n = die_order(blockIdx.x, (int64_t)o_tiles * t_tiles);
     const int band = (int)(n / ((int64_t)kBand * o_tiles)), in_band = (int)(n - (int64_t)band * kBand * o_tiles);
@@ -505,16 +537,16 @@ __global__ __launch_bounds__(WO * WT * 64, 2) void tile_kernel(const uint8_t *__
         const int k = wave * kLoads + q;
         src[q] = (k < OT ? W + min(o0 + k, last_o) * deep * kPiece : X + min(t0 + k - OT, last_t) * deep * kPiece) + lane * 16;
     }
-    uint8_t *dst = smem + wave * kLoads * kPiece;
+    uint8_t *ring = smem + group * (BUFS * kStepBytes), *dst = ring + wave * kLoads * kPiece;
     auto load = [&](int step, int q) {  // past the last step: that one again, which nothing reads
-        load_lds16(src[q] + min(step, deep - 1) * kPiece, dst + (step % BUFS) * kStepBytes + q * kPiece);
+        load_lds16(src[q] + min(from + step, deep - 1) * kPiece, dst + (step % BUFS) * kStepBytes + q * kPiece);
     };
     const int wo = wave % WO * A, wt = wave / WO * B;
     Int4 acc[A][B] = {}, a[2][A], b[2][B];
     auto fetch = [&](int step, int buf, int q) {  // operand q of those of W, then of X
-        const uint8_t *from = smem + (step % BUFS) * kStepBytes + lane * 16;
-        if (q < A) a[buf][q] = *reinterpret_cast<const Int4 *>(from + (wo + q) * kPiece);
-        else b[buf][q - A] = *reinterpret_cast<const Int4 *>(from + (OT + wt + q - A) * kPiece);
+        const uint8_t *at = ring + (step % BUFS) * kStepBytes + lane * 16;
+        if (q < A) a[buf][q] = *reinterpret_cast<const Int4 *>(at + (wo + q) * kPiece);
+        else b[buf][q - A] = *reinterpret_cast<const Int4 *>(at + (OT + wt + q - A) * kPiece);
     };
     // This wavefront's loads of `step` have landed (those of BUFS - 2 later steps are under way) and its LDS reads have
     // returned.  After the barrier both hold for every wavefront: the step may be read, and the buffer of the one
@@ -536,7 +568,7 @@ __global__ __launch_bounds__(WO * WT * 64, 2) void tile_kernel(const uint8_t *__
             for (int q = (A + B) * s / kLoads; q < (A + B) * (s + 1) / kLoads; ++q) fetch(step + 1, buf ^ 1, q);
 #pragma unroll
             for (int i = A * B * s / kLoads; i < A * B * (s + 1) / kLoads; ++i) {
-                acc[i / B][i % B] = multiply(a[buf][i / B], b[buf][i % B], acc[i / B][i % B]);
+                if (G == 1 || step < mine) acc[i / B][i % B] = multiply(a[buf][i / B], b[buf][i % B], acc[i / B][i % B]);
                 if (i == A * B * (2 * s + 1) / (2 * kLoads)) load(step + BUFS, s);
             }
             __builtin_amdgcn_sched_barrier(0);
@@ -551,23 +583,40 @@ __global__ __launch_bounds__(WO * WT * 64, 2) void tile_kernel(const uint8_t *__
     for (int q = 0; q < A + B; ++q) fetch(0, 0, q);
 #pragma unroll
     for (int q = 0; q < kLoads; ++q) load(BUFS - 1, q);
-    for (int step = 0; step < deep; step += 2) {  // the depth is a multiple of two steps
+    for (int step = 0; step < each; step += 2) {  // the depth is a multiple of two steps
         turn(step, 0);
         turn(step + 1, 1);
     }
     asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");  // what nothing reads ends before the LDS does
+    if constexpr (G > 1) {  // the groups' sums, in order, with the first
+        __syncthreads();
+        Int4 *sums = reinterpret_cast<Int4 *>(smem);
+        if (group > 0) {
+#pragma unroll
+            for (int i = 0; i < A * B; ++i) sums[(((group - 1) * kWaves + wave) * A * B + i) * 64 + lane] = acc[i / B][i % B];
+        }
+        __syncthreads();
+        if (group == 0) {
+#pragma unroll
+            for (int g = 0; g < G - 1; ++g)
+#pragma unroll
+                for (int i = 0; i < A * B; ++i) acc[i / B][i % B] += sums[((g * kWaves + wave) * A * B + i) * 64 + lane];
+        }
+        if (!E::kPlain) __syncthreads();
+        if (group > 0) return;
+    }
     if constexpr (!E::kPlain) {
-        __syncthreads();  // nobody's loads are under way to the LDS that the sums pass through now
+        if (G == 1) __syncthreads();  // nobody's loads are under way to the LDS that the sums pass through now
         constexpr int kAtOnce = tokens_at_once(A, B, kWaves, BUFS * kStepBytes);
-        Int4 *mine = reinterpret_cast<Int4 *>(smem) + wave * (kAtOnce * A * 64);
+        Int4 *through = reinterpret_cast<Int4 *>(smem) + wave * (kAtOnce * A * 64);
 #pragma unroll
         for (int q0 = 0; q0 < B; q0 += kAtOnce) {
 #pragma unroll
             for (int q = 0; q < kAtOnce; ++q)
 #pragma unroll
-                for (int p = 0; p < A; ++p) mine[staged_sum<A>(q * kRows + (lane & 15), p * 4 + (lane >> 4))] = acc[p][q0 + q];
+                for (int p = 0; p < A; ++p) through[staged_sum<A>(q * kRows + (lane & 15), p * 4 + (lane >> 4))] = acc[p][q0 + q];
             __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-            finish_rows<E, A, kAtOnce * kRows>(mine, y, e, (t0 + wt + q0) * kRows, (o0 + wo) / kPerOutput<E> * kRows);
+            finish_rows<E, A, kAtOnce * kRows>(through, y, e, (t0 + wt + q0) * kRows, (o0 + wo) / kPerOutput<E> * kRows);
             __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
         }
         return;
@@ -596,10 +645,10 @@ int64_t tiles_of(const Scaled &y, int ot, int tt) {
     return cdiv(pieces_of<E>(y), ot) * cdiv(y.m, tt * kRows);
 }
 
-template <typename T, typename E, int OT, int TT, int WO, int WT, int BUFS>
+template <typename T, typename E, int OT, int TT, int WO, int WT, int G, int BUFS>
 void launch_tiles(const uint8_t *W, const uint8_t *X, int deep, const Scaled &y, const E &e, hipStream_t st) {
     const int o_tiles = (int)cdiv(pieces_of<E>(y), OT), t_tiles = (int)cdiv(y.m, TT * kRows);
-    tile_kernel<T, E, OT, TT, WO, WT, BUFS><<<dim3((unsigned)(o_tiles * t_tiles)), WO * WT * 64, 0, st>>>(W, X, deep, o_tiles, t_tiles, y, e);
+    tile_kernel<T, E, OT, TT, WO, WT, G, BUFS><<<dim3((unsigned)(o_tiles * t_tiles)), WO * WT * G * 64, 0, st>>>(W, X, deep, o_tiles, t_tiles, y, e);
 }
 
 template <typename T, typename E, int OP, int TP, int WAVES>
@@ -627,13 +676,20 @@ int launch_product(const uint8_t *W, const uint8_t *X, int deep, const Scaled &y
     else if (y.m <= 16 && pieces >= 320) launch_shared<T, E, kLeast, 1, 8>(W, X, deep, y, e, st);
     else if (y.m <= 16) launch_shared<T, E, kLeast, 1, 16>(W, X, deep, y, e, st);
     else if (y.m <= 32) launch_shared<T, E, 4, 2, 4>(W, X, deep, y, e, st);
-    else if (fills(tiles_of<E>(y, 16, 16))) launch_tiles<T, E, 16, 16, 4, 2, 4>(W, X, deep, y, e, st);
-    else if (fills(tiles_of<E>(y, 16, 8))) launch_tiles<T, E, 16, 8, 4, 2, 4>(W, X, deep, y, e, st);
-    else if (tiles_of<E>(y, 8, 8) >= 192) launch_tiles<T, E, 8, 8, 2, 2, 4>(W, X, deep, y, e, st);
-    else if (tiles_of<E>(y, 4, 4) >= 150) launch_tiles<T, E, 4, 4, 2, 2, 8>(W, X, deep, y, e, st);
+    else if (fills(tiles_of<E>(y, 16, 16))) launch_tiles<T, E, 16, 16, 4, 2, 1, 4>(W, X, deep, y, e, st);
+    else if (fills(tiles_of<E>(y, 16, 8))) launch_tiles<T, E, 16, 8, 4, 2, 1, 4>(W, X, deep, y, e, st);
+    else if (tiles_of<E>(y, 8, 8) >= 192) launch_tiles<T, E, 8, 8, 2, 2, 1, 4>(W, X, deep, y, e, st);
+    else if (tiles_of<E>(y, 4, 4) >= 150) launch_tiles<T, E, 4, 4, 2, 2, 1, 8>(W, X, deep, y, e, st);
     else launch_shared<T, E, 4, 2, 4>(W, X, deep, y, e, st);
     CMPQ_LAUNCH_CHECK();
     return CMPQ_OK;
+}
+
+// Whether the tokens go in one launch.
+template <typename E>
+bool few_fit(const Scaled &y, int64_t d) {
+    if (y.m == 1) return d <= 2 * kFewDepth;
+    return y.m == 2 && (d <= kFewDepth || (!E::kGated && d <= 2 * kFewDepth && pieces_of<E>(y) <= 256));
 }
 
 template <typename TX, typename E>
@@ -642,8 +698,26 @@ void launch_few(const uint8_t *W, const void *X, int64_t d, int64_t ldx, const S
     const dim3 grid((unsigned)cdiv(y.d_out, kRows));
     const TX *x = static_cast<const TX *>(X);
     const int deep = (int)pieces_deep(d);
-    if (y.m == 1) few_tokens_kernel<TX, E, 1><<<grid, kFewWaves * 64, 0, st>>>(W, x, d, ldx, deep, y, e, y_dtype, status);
-    else few_tokens_kernel<TX, E, 2><<<grid, kFewWaves * 64, 0, st>>>(W, x, d, ldx, deep, y, e, y_dtype, status);
+    const auto run = [&](auto tokens, auto chunks, auto waves) {
+        few_tokens_kernel<TX, E, tokens(), chunks(), waves()><<<grid, waves() * 64, 0, st>>>(W, x, d, ldx, deep, y, e, y_dtype, status);
+    };
+    typedef std::integral_constant<int, 1> One;
+    typedef std::integral_constant<int, 2> Two;
+    typedef std::integral_constant<int, 4> Four;
+    typedef std::integral_constant<int, 8> Eight;
+    typedef std::integral_constant<int, 16> Sixteen;
+    if (y.m == 2) {
+        if (d <= kFewDepth) run(Two(), One(), Sixteen());
+        else if constexpr (!E::kGated) run(Two(), Two(), Sixteen());
+    } else if constexpr (E::kGated) {
+        if (d <= 8192) run(One(), One(), Eight());
+        else if (d <= 16384) run(One(), Two(), Eight());
+        else run(One(), Four(), Eight());
+    } else {
+        if (d <= 6144) run(One(), One(), Eight());
+        else if (d <= kFewDepth) run(One(), One(), Sixteen());
+        else run(One(), Two(), Sixteen());
+    }
 }
 
 struct Work {
@@ -676,7 +750,7 @@ struct Asked {
 template <typename E>
 int run_product(const Asked &a, Scaled y, const E &e, const Work &w, hipStream_t st) {
     const uint8_t *cw = reinterpret_cast<const uint8_t *>(a.codes);
-    if (a.X && y.m <= 2 && a.d_in <= kFewDepth) {
+    if (a.X && few_fit<E>(y, a.d_in)) {
         if (a.dtype == CMPQ_F16) launch_few<_Float16>(cw, a.X, a.d_in, a.ldx, y, e, a.y_dtype, a.status, st);
         else if (a.dtype == CMPQ_BF16) launch_few<__bf16>(cw, a.X, a.d_in, a.ldx, y, e, a.y_dtype, a.status, st);
         else launch_few<float>(cw, a.X, a.d_in, a.ldx, y, e, a.y_dtype, a.status, st);

@@ -82,15 +82,20 @@ class Int8Rows(_Kept):
         return B.Int8RowsView(self.rows, self.dim, self.codes, self.scale)
 
 
-def _empty_rows(rows: int, dim: int, device) -> Int8Rows:
-    return Int8Rows(rows, dim, torch.empty(B.int8_weight_bytes(rows, dim), dtype=torch.int8, device=device),
-                    torch.empty(rows, dtype=torch.float32, device=device))
+def _empty_rows(like: torch.Tensor) -> Int8Rows:
+    """Room for the rows of `like` in 8 bits."""
+    rows, dim = like.shape
+    codes = like.new_empty(B.int8_weight_bytes(rows, dim), dtype=torch.int8)
+    scale = like.new_empty(rows, dtype=torch.float32)
+    made = Int8Rows.__new__(Int8Rows)           # without the checks of tensors that come from elsewhere
+    made.__dict__.update(rows=rows, dim=dim, codes=codes, scale=scale, _args=B.Int8RowsView(rows, dim, codes, scale, fits=True))
+    return made
 
 
 def int8_rows(X: torch.Tensor, out: Optional[Int8Rows] = None, status: Optional[torch.Tensor] = None) -> Int8Rows:
     """Inputs X [m, d_in] in 8 bits, coded once for all products that share them: these give what they give for X."""
     if out is None:
-        out = _empty_rows(X.shape[0], X.shape[1], X.device)
+        out = _empty_rows(X)
     elif (out.rows, out.dim) != tuple(X.shape):
         raise ValueError("the rows in 8 bits must be of X's shape")
     B.int8_prepare(X, out.codes, out.scale, status)
@@ -102,8 +107,8 @@ Inputs = Union[torch.Tensor, Int8Rows]
 
 def _output(X: Inputs, d_out: int, out_dtype: Optional[torch.dtype]) -> torch.Tensor:
     if isinstance(X, Int8Rows):
-        return torch.empty((X.rows, d_out), dtype=out_dtype or torch.float16, device=X.codes.device)
-    return torch.empty((X.shape[0], d_out), dtype=out_dtype or X.dtype, device=X.device)
+        return X.codes.new_empty((X.rows, d_out), dtype=out_dtype or torch.float16)
+    return X.new_empty((X.shape[0], d_out), dtype=out_dtype or X.dtype)
 
 
 def int8_product(w: Int8Weight, X: Inputs, ws: Optional[B.Workspace] = None,
@@ -168,7 +173,7 @@ def epilogue(Y: torch.Tensor, bias: Optional[torch.Tensor] = None, activation: O
     """act(Y + bias) * (times + times_bias) + residual for the outputs Y [m, d] of a product in mixed precision; times and
     residual are [m, d], the biases [d], each of its own type.  `out_dtype` defaults to Y's; `out` may be Y, times or residual."""
     if out is None:
-        out = torch.empty(Y.shape, dtype=out_dtype or Y.dtype, device=Y.device)
+        out = torch.empty_like(Y, dtype=out_dtype)
     B.epilogue(Y, out, bias, activation, times, times_bias, residual)
     return out
 
@@ -180,10 +185,9 @@ def rms_norm(X: torch.Tensor, weight: Optional[torch.Tensor] = None, eps: float 
     `coded`: as `Int8Rows` for the products that follow, else of `out_dtype`, by default X's.  With `add` the answer is (norm, s),
     s of X's type unless `sum_out` says otherwise, which may be X or `add` itself; the norm is that of s as rounded."""
     if out is None:
-        out = _empty_rows(X.shape[0], X.shape[1], X.device) if coded else \
-            torch.empty(X.shape, dtype=out_dtype or X.dtype, device=X.device)
+        out = _empty_rows(X) if coded else torch.empty_like(X, dtype=out_dtype)
     if add is not None and sum_out is None:
-        sum_out = torch.empty(X.shape, dtype=X.dtype, device=X.device)
+        sum_out = torch.empty_like(X)
     B.rms_norm(X, weight, eps, out._args if isinstance(out, Int8Rows) else out, add, sum_out, status)
     return out if add is None else (out, sum_out)
 

@@ -113,7 +113,7 @@ def test_norm_jobs(B):
 def S(B, monkeypatch):
     from paper_2410_13056_amd import serving
     monkeypatch.setattr(B, "_ptr", lambda t: None if t is None else t.data_ptr())
-    monkeypatch.setattr(B, "_here", lambda t: t.data_ptr())
+    monkeypatch.setattr(B, "_device", lambda: -1)                       # where host tensors say that they are
     monkeypatch.setattr(B, "_stream", lambda: 0)
 
     class Library:
@@ -170,28 +170,31 @@ def test_tensors_that_do_not_fit_are_refused(S, B):
     with pytest.raises(TypeError):
         S.rms_norm(X, add=X.double())
     with pytest.raises(ValueError):
-        S.rms_norm(X, out=S._empty_rows(2, 64, "cpu"))
+        S.rms_norm(X, out=S._empty_rows(z((2, 64))))
     with pytest.raises(ValueError):
-        S.int8_rows(X, out=S._empty_rows(2, 64, "cpu"))
+        S.int8_rows(X, out=S._empty_rows(z((2, 64))))
 
 
-def test_host_tensors_and_other_devices_are_refused(B, monkeypatch):
-    with pytest.raises(ValueError):
-        B._here(torch.zeros(3))
-
+def test_host_tensors_and_other_devices_are_refused(B):
     class Elsewhere:
-        is_cuda = True
+        is_cuda, shape, dtype = True, (3,), torch.float16
+
+        def is_contiguous(self):
+            return True
 
         def get_device(self):
             return 1
 
         def data_ptr(self):
             return FAKE
-    monkeypatch.setattr(B, "_current_device", lambda: 0)
+    for t, why in ((torch.zeros(3), "device tensors"), (Elsewhere(), "current device")):
+        with pytest.raises(ValueError, match=why):
+            B._vector(t, 3, 0, "bias")
+    with pytest.raises(ValueError, match="device tensors"):
+        B._matrix(torch.zeros((3, 4)), 3, 4, 0, "X")
     with pytest.raises(ValueError):
-        B._here(Elsewhere())
-    monkeypatch.setattr(B, "_current_device", lambda: 1)
-    assert B._here(Elsewhere()) == FAKE
+        B._flags(torch.zeros(1, dtype=torch.int32), 0)
+    assert B._vector(Elsewhere(), 3, 1, "bias") == (FAKE, 0, B.F16)
 
 
 def test_outputs_have_the_types_asked_for(S, B):
@@ -208,7 +211,7 @@ def test_outputs_have_the_types_asked_for(S, B):
 
 
 def test_objects_are_copied_and_give_their_memory_back(S, B):
-    for make in (lambda: S._empty_rows(5, 64, "cpu"), lambda: _weight(S, B, gated=True)):
+    for make in (lambda: S._empty_rows(torch.zeros((5, 64))), lambda: _weight(S, B, gated=True)):
         thing = make()
         thing.codes.zero_()
         for other in (copy.deepcopy(thing), pickle.loads(pickle.dumps(thing))):
