@@ -44,17 +44,17 @@ __device__ __forceinline__ void store_some(void *p, int dtype, int64_t i, int n,
 struct Raw8 {
     typedef uint32_t U4 __attribute__((ext_vector_type(4)));
     U4 w[2];
-    __device__ __forceinline__ void load(const cmpq_rows &a, int64_t i, int n) {
+    __device__ __forceinline__ void load(const void *from, int dtype, int64_t i, int n) {
         typedef U4 Any __attribute__((aligned(2)));
-        const int size = a.dtype == CMPQ_F32 ? 4 : 2;
-        const char *p = static_cast<const char *>(a.ptr) + i * size;
+        const int size = dtype == CMPQ_F32 ? 4 : 2;
+        const char *p = static_cast<const char *>(from) + i * size;
         if (n >= 8) {
             w[0] = *reinterpret_cast<const Any *>(p);
             if (size == 4) w[1] = *reinterpret_cast<const Any *>(p + 16);
         } else {
             float x[8];
-            load_some<8>(a.ptr, a.dtype, i, n, x);
-            with_dtype(a.dtype, [&](auto like) {
+            load_some<8>(from, dtype, i, n, x);
+            with_dtype(dtype, [&](auto like) {
                 typedef decltype(like) T;
                 typedef T V __attribute__((ext_vector_type(8)));
                 V v;

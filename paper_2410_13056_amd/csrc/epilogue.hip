@@ -13,11 +13,11 @@ __global__ __launch_bounds__(kThreads) void epilogue_kernel(cmpq_epilogue_job a,
         const int64_t t = at / columns, o = (at - t * columns) * 8;
         const int n = (int)min(a.d - o, (int64_t)8);
         Raw8 y, u, r, b, c;
-        y.load(a.Y, t * a.Y.ld + o, n);
-        if (a.times.ptr) u.load(a.times, t * a.times.ld + o, n);
-        if (a.residual.ptr) r.load(a.residual, t * a.residual.ld + o, n);
-        if (a.bias.ptr) b.load(a.bias, o, n);
-        if (a.times_bias.ptr) c.load(a.times_bias, o, n);
+        y.load(a.Y.ptr, a.Y.dtype, t * a.Y.ld + o, n);
+        if (a.times.ptr) u.load(a.times.ptr, a.times.dtype, t * a.times.ld + o, n);
+        if (a.residual.ptr) r.load(a.residual.ptr, a.residual.dtype, t * a.residual.ld + o, n);
+        if (a.bias.ptr) b.load(a.bias.ptr, a.bias.dtype, o, n);
+        if (a.times_bias.ptr) c.load(a.times_bias.ptr, a.times_bias.dtype, o, n);
         float v[8], x[8];
         y.values(a.Y.dtype, v);
         if (a.bias.ptr) {

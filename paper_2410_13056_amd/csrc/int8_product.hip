@@ -663,8 +663,9 @@ void launch_shared(const uint8_t *W, const uint8_t *X, int deep, const Scaled &y
 // 44.0, 28, 35.4; 64 x 64 (333 tokens 4099 -> 3001 20.4, 128 x 128 25.5; 48 tokens 4096 -> 11008 14.0, 21.3).  Fewer than 150
 // tiles of 64 x 64, and up to 32 tokens: wavefronts share the depth (512 tokens 8192 -> 1024 18.6, 64 x 64 23.0; 64 tokens
 // 4096 -> 4096 9.4, 12.3).  Up to 16 tokens: two pieces of outputs a workgroup where there are many (16 tokens 5120 -> 13824
-// 16.0, one piece 17.9), 8 wavefronts for some (8192 -> 8192 15.8, 16 wavefronts 16.4), 16 for few (8 tokens 8192 -> 1024
-// 8.6, 8 wavefronts 9.8).
+// 16.0, one piece 17.9), one by 8 wavefronts for some (8192 -> 10240, weights from memory, 19.6, two by 16 23.2), two by 16 where
+// they are a round of the units (13824 -> 5120 18.0, one by 8 20.1: its units read the tokens twice as often), one by 16 for few (8
+// tokens 8192 -> 1024 8.6, 8 wavefronts 9.8).
 template <typename T, typename E>
 int launch_product(const uint8_t *W, const uint8_t *X, int deep, const Scaled &y, const E &e, hipStream_t st) {
     constexpr int64_t kUnits = 256;  // compute units
@@ -673,7 +674,8 @@ int launch_product(const uint8_t *W, const uint8_t *X, int deep, const Scaled &y
     constexpr int kLeast = kPerOutput<E>;  // pieces of a workgroup at least
     if (tiles_of<E>(y, kLeast, 1) > INT32_MAX) return CMPQ_ESHAPE;
     if (y.m <= 16 && pieces >= 768) launch_shared<T, E, 2, 1, 8>(W, X, deep, y, e, st);
-    else if (y.m <= 16 && pieces >= 320) launch_shared<T, E, kLeast, 1, 8>(W, X, deep, y, e, st);
+    else if (y.m <= 16 && pieces > 512) launch_shared<T, E, kLeast, 1, 8>(W, X, deep, y, e, st);
+    else if (y.m <= 16 && pieces >= 320) launch_shared<T, E, 2, 1, 16>(W, X, deep, y, e, st);
     else if (y.m <= 16) launch_shared<T, E, kLeast, 1, 16>(W, X, deep, y, e, st);
     else if (y.m <= 32) launch_shared<T, E, 4, 2, 4>(W, X, deep, y, e, st);
     else if (fills(tiles_of<E>(y, 16, 16))) launch_tiles<T, E, 16, 16, 4, 2, 1, 4>(W, X, deep, y, e, st);

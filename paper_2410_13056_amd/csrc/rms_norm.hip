@@ -2,10 +2,17 @@
 // A workgroup a row, which stays in registers between its sum of squares and its outputs.  The squares are summed in 64
 // bits, where the order of additions decides nothing that is left after the one rounding to fp32, so a row's codes are those of
 // the definition, whatever the number of lanes.
+//
+// Bound.  Many rows: by bytes.  4096 rows of 8192 in bfloat16 with their sum, 268 MB, 40.5 us (6.6 TB/s, what caches keep between
+// calls included), as rows in 8 bits 40.  One row: by what comes one after the other (the loads, the sum over the lanes, the root, the
+// largest magnitude), 3.3 us, of rows in 8 bits 4.4.  Kernels for one type of all tensors are 10 to 20 % faster than the one
+// that looks at each tensor's: 64 coded rows of 4096 4.2 us and 5.2.
 #include "epilogue.h"
 #include "int8_rows.h"
 
 namespace {
+
+constexpr int kAny = -1;
 
 template <int N>
 __device__ __forceinline__ void round_to(int dtype, float (&x)[N]) {
@@ -16,14 +23,39 @@ __device__ __forceinline__ void round_to(int dtype, float (&x)[N]) {
     });
 }
 
-// KEPT steps of THREADS * 8 values hold the row; 0: it is read again for each pass.
-template <int THREADS, int KEPT, bool CODED>
-__global__ __launch_bounds__(THREADS) void rms_norm_kernel(cmpq_norm_job a) {
+// Sum of the wavefronts' parts, the same in every lane: a tree whose two sides only change places from lane to lane.
+template <int N>
+__device__ __forceinline__ double total(const double *parts) {
+    static_assert(N == 4 || N == 16, "wavefronts");
+    if (N == 4) return (parts[0] + parts[1]) + (parts[2] + parts[3]);
+    double v = parts[threadIdx.x & 15];
+    const auto turn = [](double x, auto by) {
+        const uint64_t u = (uint64_t)__double_as_longlong(x);
+        return join_f64(row_turn<by()>((uint32_t)u), row_turn<by()>((uint32_t)(u >> 32)));
+    };
+    v += turn(v, std::integral_constant<int, 8>());
+    v += turn(v, std::integral_constant<int, 4>());
+    v += turn(v, std::integral_constant<int, 2>());
+    return v + turn(v, std::integral_constant<int, 1>());
+}
+
+// 1 / sqrt(x) to about a step of fp64, rounded to fp32: the instruction's 26 bits, doubled twice by Newton's method.
+__device__ __forceinline__ float one_over_root(double x) {
+    double r = __builtin_amdgcn_rsq(x);
+#pragma unroll
+    for (int i = 0; i < 2; ++i) r = fma(r * 0.5, fma(-x * r, r, 1.0), r);
+    return (float)r;
+}
+
+// KEPT steps of THREADS * 8 values hold the row; 0: it is read again for each pass.  TYPE: that of all tensors, or kAny.
+template <int THREADS, int KEPT, bool CODED, int TYPE>
+__global__ __launch_bounds__(THREADS) void rms_norm_kernel(cmpq_norm_job a, double per_value) {
 #pragma clang fp contract(off)
     constexpr int kWaves = THREADS / 64, kStep = THREADS * 8, kHeld = KEPT > 0 ? KEPT : 1;
     __shared__ double sums[kWaves];
     __shared__ float most[kWaves];
     const int64_t row = CODED ? die_order(blockIdx.x, gridDim.x) : (int64_t)blockIdx.x;
+    const auto type = [](int dtype) { return TYPE == kAny ? dtype : TYPE; };
     const int d = (int)a.d, first = threadIdx.x * 8;
     const int whole = CODED ? (int)pieces_deep(d) * kDepth : d;  // what is written of a row
     uint8_t *codes = nullptr;
@@ -42,20 +74,20 @@ __global__ __launch_bounds__(THREADS) void rms_norm_kernel(cmpq_norm_job a) {
         const int n = min(max(d - i, 0), 8);
         Raw8 p, q;
         if (sum_is_there) {
-            p.load(a.S, row * a.S.ld + i, n);
-            p.values(a.S.dtype, s);
+            p.load(a.S.ptr, type(a.S.dtype), row * a.S.ld + i, n);
+            p.values(type(a.S.dtype), s);
             return;
         }
-        p.load(a.X, row * a.X.ld + i, n);
-        if (a.add.ptr) q.load(a.add, row * a.add.ld + i, n);
-        p.values(a.X.dtype, s);
+        p.load(a.X.ptr, type(a.X.dtype), row * a.X.ld + i, n);
+        if (a.add.ptr) q.load(a.add.ptr, type(a.add.dtype), row * a.add.ld + i, n);
+        p.values(type(a.X.dtype), s);
         if (a.add.ptr) {
             float t[8];
-            q.values(a.add.dtype, t);
+            q.values(type(a.add.dtype), t);
 #pragma unroll
             for (int k = 0; k < 8; ++k) s[k] += t[k];
         }
-        if (a.S.ptr) round_to(a.S.dtype, s);
+        if (a.S.ptr) round_to(type(a.S.dtype), s);
     };
     auto each = [&](auto fn, bool again) {  // fn(values, their first, gain), from registers where they were kept
         if (KEPT > 0) {
@@ -65,7 +97,7 @@ __global__ __launch_bounds__(THREADS) void rms_norm_kernel(cmpq_norm_job a) {
         } else {
             for (int i = first; i < whole; i += kStep) {
                 load(i, x[0], again && a.S.ptr);
-                if (a.gain.ptr) gain[0].load(a.gain, i, min(max(d - i, 0), 8));
+                if (a.gain.ptr) gain[0].load(a.gain.ptr, type(a.gain.dtype), i, min(max(d - i, 0), 8));
                 fn(x[0], i, gain[0]);
             }
         }
@@ -75,29 +107,27 @@ __global__ __launch_bounds__(THREADS) void rms_norm_kernel(cmpq_norm_job a) {
         for (int k = 0; k < kHeld; ++k) load(first + k * kStep, x[k], false);
         if (a.gain.ptr) {
 #pragma unroll
-            for (int k = 0; k < kHeld; ++k) gain[k].load(a.gain, first + k * kStep, min(max(d - first - k * kStep, 0), 8));
+            for (int k = 0; k < kHeld; ++k) gain[k].load(a.gain.ptr, type(a.gain.dtype), first + k * kStep, min(max(d - first - k * kStep, 0), 8));
         }
     }
     double sum = 0;
     each([&](float (&s)[8], int i, const Raw8 &) {
 #pragma unroll
         for (int k = 0; k < 8; ++k) sum = fma((double)s[k], (double)s[k], sum);
-        if (a.S.ptr && i < d) store_some<8>(a.S.ptr, a.S.dtype, row * a.S.ld + i, min(d - i, 8), s);
+        if (a.S.ptr && i < d) store_some<8>(a.S.ptr, type(a.S.dtype), row * a.S.ld + i, min(d - i, 8), s);
     }, false);
     sum = wave_sum_f64(sum);
     if ((threadIdx.x & 63) == 0) sums[threadIdx.x >> 6] = sum;
     __syncthreads();
-    double q = sums[0];
-#pragma unroll
-    for (int w = 1; w < kWaves; ++w) q += sums[w];
-    const float r = (float)(1.0 / sqrt(q / (double)d + a.eps));
+    const double q = total<kWaves>(sums);
     bool bad = !(q < __builtin_huge_val());
+    const float r = bad ? (q != q ? __builtin_nanf("") : 0.f) : one_over_root(q * per_value + a.eps);
     auto normed = [&](float (&s)[8], const Raw8 &g) {
 #pragma unroll
         for (int k = 0; k < 8; ++k) s[k] *= r;
         if (a.gain.ptr) {
             float t[8];
-            g.values(a.gain.dtype, t);
+            g.values(type(a.gain.dtype), t);
 #pragma unroll
             for (int k = 0; k < 8; ++k) s[k] *= t[k];
         }
@@ -106,7 +136,7 @@ __global__ __launch_bounds__(THREADS) void rms_norm_kernel(cmpq_norm_job a) {
         if (bad && a.status && threadIdx.x == 0) atomicOr(a.status, CMPQ_STATUS_NONFINITE);
         each([&](float (&s)[8], int i, const Raw8 &g) {
             normed(s, g);
-            if (i < d) store_some<8>(a.Y.ptr, a.Y.dtype, row * a.Y.ld + i, min(d - i, 8), s);
+            if (i < d) store_some<8>(a.Y.ptr, type(a.Y.dtype), row * a.Y.ld + i, min(d - i, 8), s);
         }, true);
         return;
     }
@@ -142,10 +172,27 @@ __global__ __launch_bounds__(THREADS) void rms_norm_kernel(cmpq_norm_job a) {
     }, true);
 }
 
-template <int THREADS, int KEPT>
+template <int THREADS, int KEPT, bool CODED, int TYPE>
+void run(const cmpq_norm_job &a, hipStream_t st) {
+    const int64_t rows = CODED ? cdiv(a.m, kRows) * kRows : a.m;
+    rms_norm_kernel<THREADS, KEPT, CODED, TYPE><<<dim3((unsigned)rows), THREADS, 0, st>>>(a, 1.0 / (double)a.d);
+}
+
+// Sixteen wavefronts a row where it is longer than four of them hold in two steps: us with 16 and 4, 1 row of 8192 with its sum
+// 3.3 and 4.7, 4096 rows 40.5 and 41.5.  Rows in 8 bits, where there are many, are better off with four, three or four
+// steps each, since more of a unit's rows are then at different stages: 4096 of 5120 27.5 us and 32.3, 1000 9.7 and 11.3, but 64 of 8192
+// 5.7 and 4.8.
+template <bool CODED, int TYPE>
 void launch_norm(const cmpq_norm_job &a, hipStream_t st) {
-    if (a.codes) rms_norm_kernel<THREADS, KEPT, true><<<dim3((unsigned)(cdiv(a.m, kRows) * kRows)), THREADS, 0, st>>>(a);
-    else rms_norm_kernel<THREADS, KEPT, false><<<dim3((unsigned)a.m), THREADS, 0, st>>>(a);
+    constexpr int64_t kMany = 512;
+    if (a.d <= 2048) run<256, 1, CODED, TYPE>(a, st);
+    else if (a.d <= 4096) run<256, 2, CODED, TYPE>(a, st);
+    else if (CODED && a.m >= kMany && a.d <= 6144) run<256, CODED ? 3 : 1, CODED, TYPE>(a, st);
+    else if (CODED && a.m >= kMany && a.d <= 8192) run<256, CODED ? 4 : 1, CODED, TYPE>(a, st);
+    else if (a.d <= 8192) run<1024, 1, CODED, TYPE>(a, st);
+    else if (a.d <= 16384) run<1024, 2, CODED, TYPE>(a, st);
+    else if (a.d <= 32768) run<1024, 4, CODED, TYPE>(a, st);
+    else run<1024, 0, CODED, TYPE>(a, st);
 }
 
 }  // namespace
@@ -163,12 +210,18 @@ extern "C" int cmpq_rms_norm(const cmpq_norm_job *j, void *stream) {
     for (const cmpq_rows &a : rows)
         if (a.ptr && a.ld < j->d) return CMPQ_ESHAPE;
     hipStream_t st = static_cast<hipStream_t>(stream);
-    if (j->d <= 2048) launch_norm<256, 1>(*j, st);
-    else if (j->d <= 4096) launch_norm<256, 2>(*j, st);
-    else if (j->d <= 8192) launch_norm<1024, 1>(*j, st);
-    else if (j->d <= 16384) launch_norm<1024, 2>(*j, st);
-    else if (j->d <= 32768) launch_norm<1024, 4>(*j, st);
-    else launch_norm<1024, 0>(*j, st);
+    int type = j->X.dtype;
+    for (const cmpq_rows &a : all)
+        if (a.ptr && a.dtype != j->X.dtype) type = kAny;
+    if (j->codes) {
+        if (type == CMPQ_F16) launch_norm<true, CMPQ_F16>(*j, st);
+        else if (type == CMPQ_BF16) launch_norm<true, CMPQ_BF16>(*j, st);
+        else launch_norm<true, kAny>(*j, st);
+    } else {
+        if (type == CMPQ_F16) launch_norm<false, CMPQ_F16>(*j, st);
+        else if (type == CMPQ_BF16) launch_norm<false, CMPQ_BF16>(*j, st);
+        else launch_norm<false, kAny>(*j, st);
+    }
     CMPQ_LAUNCH_CHECK();
     return CMPQ_OK;
 }

@@ -60,16 +60,32 @@ __device__ __forceinline__ uint32_t low_bytes(uint32_t a, uint32_t b, uint32_t c
 }
 __device__ __forceinline__ float no_nan(float x) { return x == x ? x : 0.f; }
 
-// Largest of non-negative values over the workgroup, in every lane.  `scratch`: one float a wavefront.  Has barriers.
-__device__ __forceinline__ float block_max(float v, float *scratch) {
-#pragma unroll
-    for (int s = 32; s > 0; s >>= 1) v = fmaxf(v, __shfl_xor(v, s, CMPQ_WAVE));
-    if ((threadIdx.x & 63) == 0) scratch[threadIdx.x >> 6] = v;
+// The value of the lane N further on in a row of 16, around its end.
+template <int N>
+__device__ __forceinline__ uint32_t row_turn(uint32_t v) {
+    return (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, 0x120 + N, 0xF, 0xF, true);
+}
+// Largest of a row of 16 lanes, in all of them.
+__device__ __forceinline__ uint32_t row_max(uint32_t v) {
+    v = max(v, row_turn<8>(v));
+    v = max(v, row_turn<4>(v));
+    v = max(v, row_turn<2>(v));
+    return max(v, row_turn<1>(v));
+}
+
+// Largest of non-negative values over the workgroup of up to 16 wavefronts, in every lane.  `scratch`: one float a wavefront.
+// Has a barrier.  Values are ordered as their bits are.  Row swaps and the DPP path: exchanges through LDS and a loop over the
+// wavefronts took 16 of them a microsecond longer.
+__device__ __forceinline__ float block_max(float value, float *scratch) {
+    uint32_t v = __float_as_uint(value);
+    const auto halves = __builtin_amdgcn_permlane32_swap(v, v, false, false);
+    v = max(halves[0], halves[1]);
+    const auto rows = __builtin_amdgcn_permlane16_swap(v, v, false, false);
+    v = row_max(max(rows[0], rows[1]));
+    if ((threadIdx.x & 63) == 0) scratch[threadIdx.x >> 6] = __uint_as_float(v);
     __syncthreads();
-    const int waves = (int)(blockDim.x >> 6);
-    float m = scratch[0];
-    for (int w = 1; w < waves; ++w) m = fmaxf(m, scratch[w]);
-    return m;
+    const int w = threadIdx.x & 15;
+    return __uint_as_float(row_max(w < (int)(blockDim.x >> 6) ? __float_as_uint(scratch[w]) : 0));
 }
 
 // The two results of the turn by position.  Products and sums are rounded one by one, as the header says.
