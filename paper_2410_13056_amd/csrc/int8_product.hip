@@ -510,8 +510,10 @@ __device__ __forceinline__ void finish_rows(const Int4 *sums, const Scaled &y, c
 // are read (no conflicts), BUFS steps of 64 inputs in a ring; while a step is multiplied its operands are in
 // registers, those of the next are on their way from LDS and the steps after it from memory.  Bound by the matrix
 // instructions at 256 x 256: 4096 tokens 8192 -> 28672 in 741 us with the codes (29), 2.6 POP/s, the instructions busy for 69 %
-// of the clocks, the rest at the barrier of a step.  64 x 64 (333 tokens 4099 -> 3001, 16 us): by what the caches deliver, 282 tiles
-// of 66 steps of 8 KB, 9.4 TB/s; matrix instructions 14 %.  Bands keep the inputs of a die's tiles in its
+// of the clocks, the rest at the barrier of a step.  64 x 64: by what a unit's caches deliver, 25 to 35 bytes a clock: 282 tiles
+// of 66 steps of 8 KB (333 tokens 4099 -> 3001) 15.4 us, 9.9 TB/s, 64 x 128 reads three quarters of that in 14.8; more buffers, or
+// steps in another order a workgroup, change nothing.  G groups of wavefronts share the depth, each with a ring of its own; their sums
+// are joined through LDS, in order.  Bands keep the inputs of a die's tiles in its
 // cache while the weights pass once a band.
 constexpr int kBand = 4;
 
@@ -657,18 +659,35 @@ void launch_shared(const uint8_t *W, const uint8_t *X, int deep, const Scaled &y
     shared_depth_kernel<T, E, OP, TP, WAVES><<<dim3((unsigned)tiles), WAVES * 64, 0, st>>>(W, X, deep, (int)t_tiles, y, e);
 }
 
+constexpr int64_t kUnits = 256;  // compute units
+
+// Two pieces of outputs by two of tokens a workgroup, its wavefronts sharing the depth, where those are a round of the units: a long
+// depth by 16 wavefronts, else by 8; twice the outputs by 4 wavefronts where there are more.  us (64 tokens 8192 -> 1024; 100 tokens
+// 5120 -> 2048; 64 tokens 28672 -> 2048; 40 tokens 8192 -> 8192): by 16 7.0, 6.2, 21.2, 15.0, by 8 7.0, 6.2, 31.0, 14.0, twice the
+// outputs 8.8, 7.1, 29.8, 13.8.
+template <typename T, typename E>
+void launch_pairs(const uint8_t *W, const uint8_t *X, int deep, const Scaled &y, const E &e, hipStream_t st) {
+    const bool round = tiles_of<E>(y, 2, 2) <= kUnits;
+    if (round && deep >= 96) launch_shared<T, E, 2, 2, 16>(W, X, deep, y, e, st);
+    else if (round) launch_shared<T, E, 2, 2, 8>(W, X, deep, y, e, st);
+    else launch_shared<T, E, 4, 2, 4>(W, X, deep, y, e, st);
+}
+
 // Which kernel: the largest tile that fills the chip.  A tile of 256 x 256 or 256 x 128 takes a compute unit for itself, so
 // its last round has to be two thirds full, or one of many.  us (4096 tokens 8192 -> 28672; 2048 tokens 4096 -> 4096; 1024
 // tokens 4096 -> 4096; 512 tokens 4096 -> 11008): 256 x 256 737, 60, 53, 53; 256 x 128 860, 43.1, 36, 34.8; 128 x 128 901,
-// 44.0, 28, 35.4; 64 x 64 (333 tokens 4099 -> 3001 20.4, 128 x 128 25.5; 48 tokens 4096 -> 11008 14.0, 21.3).  Fewer than 150
-// tiles of 64 x 64, and up to 32 tokens: wavefronts share the depth (512 tokens 8192 -> 1024 18.6, 64 x 64 23.0; 64 tokens
-// 4096 -> 4096 9.4, 12.3).  Up to 16 tokens: two pieces of outputs a workgroup where there are many (16 tokens 5120 -> 13824
-// 16.0, one piece 17.9), one by 8 wavefronts for some (8192 -> 10240, weights from memory, 19.6, two by 16 23.2), two by 16 where
-// they are a round of the units (13824 -> 5120 18.0, one by 8 20.1: its units read the tokens twice as often), one by 16 for few (8
-// tokens 8192 -> 1024 8.6, 8 wavefronts 9.8).
+// 44.0, 28, 35.4; 64 x 64 (48 tokens 4096 -> 11008 14.0, 128 x 128 21.3).
+// Up to a tile of 64 x 64 a unit, two groups of wavefronts halve the depth (100 tokens 5120 -> 5120 10.0, one group 11.8; 200
+// tokens 2048 -> 4096 6.6 and 7.2; but 333 tokens 4099 -> 3001, 282 tiles, 17.4 and 15.4: a unit with two tiles is what all wait
+// for).  Beyond, 64 outputs by 128 tokens in two groups, up to a tile a unit (512 tokens 4096 -> 4096 14.2, 64 x 64 15.5; 333 tokens
+// 8192 -> 4096 22 and 25; 400 tokens 6000 -> 3000 17.0 and 19.1; 333 tokens 4099 -> 3001 14.8 and 15.4), else 64 x 64 (150 tokens
+// 4096 -> 11008 20.2, 64 x 128 23.5).  Fewer than 150 tiles of 64 x 64, and up to 32 tokens: wavefronts share the depth (512 tokens
+// 8192 -> 1024 18.6, 64 x 64 23.0; 64 tokens 4096 -> 4096 9.4, 12.3).  Up to 16 tokens: two pieces of outputs a workgroup where there
+// are many (16 tokens 5120 -> 13824 16.0, one piece 17.9), one by 8 wavefronts for some (8192 -> 10240, weights from memory, 19.6, two
+// by 16 23.2), two by 16 where they are a round of the units (13824 -> 5120 18.0, one by 8 20.1: its units read the tokens twice as
+// often), one by 16 for few (8 tokens 8192 -> 1024 8.6, 8 wavefronts 9.8).
 template <typename T, typename E>
 int launch_product(const uint8_t *W, const uint8_t *X, int deep, const Scaled &y, const E &e, hipStream_t st) {
-    constexpr int64_t kUnits = 256;  // compute units
     auto fills = [](int64_t n) { return n >= 4 * kUnits || (n + kUnits / 3) / kUnits * kUnits >= n; };  // 171 .. 256, 427 .. 512, ...
     const int64_t pieces = pieces_of<E>(y);
     constexpr int kLeast = kPerOutput<E>;  // pieces of a workgroup at least
@@ -677,12 +696,14 @@ int launch_product(const uint8_t *W, const uint8_t *X, int deep, const Scaled &y
     else if (y.m <= 16 && pieces > 512) launch_shared<T, E, kLeast, 1, 8>(W, X, deep, y, e, st);
     else if (y.m <= 16 && pieces >= 320) launch_shared<T, E, 2, 1, 16>(W, X, deep, y, e, st);
     else if (y.m <= 16) launch_shared<T, E, kLeast, 1, 16>(W, X, deep, y, e, st);
-    else if (y.m <= 32) launch_shared<T, E, 4, 2, 4>(W, X, deep, y, e, st);
+    else if (y.m <= 32) launch_pairs<T, E>(W, X, deep, y, e, st);
     else if (fills(tiles_of<E>(y, 16, 16))) launch_tiles<T, E, 16, 16, 4, 2, 1, 4>(W, X, deep, y, e, st);
     else if (fills(tiles_of<E>(y, 16, 8))) launch_tiles<T, E, 16, 8, 4, 2, 1, 4>(W, X, deep, y, e, st);
     else if (tiles_of<E>(y, 8, 8) >= 192) launch_tiles<T, E, 8, 8, 2, 2, 1, 4>(W, X, deep, y, e, st);
-    else if (tiles_of<E>(y, 4, 4) >= 150) launch_tiles<T, E, 4, 4, 2, 2, 1, 8>(W, X, deep, y, e, st);
-    else launch_shared<T, E, 4, 2, 4>(W, X, deep, y, e, st);
+    else if (tiles_of<E>(y, 4, 4) < 150) launch_pairs<T, E>(W, X, deep, y, e, st);
+    else if (tiles_of<E>(y, 4, 4) <= kUnits) launch_tiles<T, E, 4, 4, 2, 2, 2, 4>(W, X, deep, y, e, st);
+    else if (tiles_of<E>(y, 4, 8) <= kUnits) launch_tiles<T, E, 4, 8, 2, 2, 2, 4>(W, X, deep, y, e, st);
+    else launch_tiles<T, E, 4, 4, 2, 2, 1, 4>(W, X, deep, y, e, st);
     CMPQ_LAUNCH_CHECK();
     return CMPQ_OK;
 }

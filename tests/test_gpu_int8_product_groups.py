@@ -1,0 +1,43 @@
+"""Sizes that launch the products in which groups of wavefronts share the depth - 64 x 64 and 64 x 128 tiles, two pieces by two - with
+depths that leave a group little or nothing, plain, with an epilogue and gated; and tokens that are coded within the one launch.  Exact sums:
+the plain outputs are bit for bit those of the codes."""
+import pytest
+import torch
+
+import test_gpu_int8_finish as T
+import test_gpu_int8_product as P
+from test_gpu_int8_finish import S  # noqa: F401
+
+pytestmark = pytest.mark.gpu
+
+DEV = "cuda"
+SIZES = [(700, d, 1000) for d in (1, 128, 129, 256, 300, 1000)] + [(100, 5120, 5120), (160, 130, 5333)] + \
+        [(333, d, 3001) for d in (64, 256, 390, 1025)] + [(290, 700, 4099)] + \
+        [(150, d, 11008) for d in (100, 200, 1030)] + \
+        [(64, 8192, 1024), (40, 6200, 300), (17, 7000, 130), (64, 300, 1024), (250, 1, 900), (40, 300, 8192), (24, 6150, 5000)] + \
+        [(1, 6144, 40), (1, 6145, 40), (1, 16000, 300), (1, 20000, 33), (1, 32768, 17), (1, 32769, 17), (2, 20000, 4000), (2, 32768, 30),
+         (2, 30000, 4200), (16, 700, 5130), (13, 1000, 8192), (16, 200, 8200)]
+
+
+@pytest.mark.parametrize("m,d_in,d_out", SIZES)
+def test_products(S, m, d_in, d_out):  # noqa: F811
+    k = m + d_in + d_out
+    X = T._randn(k, m, d_in, dtype=T.TYPES[k % 3], scale=3)
+    Ws = [T._randn(k + i, d_out, d_in, dtype=T.TYPES[k // 3 % 3], scale=d_in ** -0.5) for i in (1, 2)]
+    b, r, out = T._randn(k + 3, d_out), T._randn(k + 4, m, d_out), T.TYPES[k // 2 % 3]
+    w = S.prepare_int8(Ws[0])
+    P._check(S, X, Ws[0], torch.float32, w)
+    T._product(S, X, Ws[0], w, bias=b, activation="gelu_tanh", residual=r, out_dtype=out)
+    T._gated(S, X, *Ws, residual=r, out_dtype=out)
+    if d_out > 1000:
+        half = [W[:(d_out + 1) // 2] for W in Ws]
+        T._gated(S, X, *half, gate_bias=b[:(d_out + 1) // 2], out_dtype=torch.float32)
+
+
+def test_groups_add_up_to_the_same_sums(S):  # noqa: F811
+    """A row's outputs do not depend on which kernel the number of rows asks for."""
+    X, W = T._randn(1, 700, 1000, dtype=torch.float16), T._randn(2, 3001, 1000, dtype=torch.float16)
+    w = S.prepare_int8(W)
+    whole = S.int8_product(w, X, T._ws(), out_dtype=torch.float32)
+    for n in (1, 2, 10, 30, 64, 200, 300, 333, 500):
+        assert torch.equal(S.int8_product(w, X[:n], T._ws(), out_dtype=torch.float32), whole[:n]), n
