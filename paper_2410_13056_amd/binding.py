@@ -813,12 +813,18 @@ class Int8RowsView:
     """Inputs of a product in 8 bits, as the library takes them.  Holds the tensors it points into."""
     __slots__ = ("rows", "dim", "codes", "scale", "device", "keep")
 
-    def __init__(self, rows: int, dim: int, codes: torch.Tensor, scale: torch.Tensor, fits: bool = False):
-        """`fits`: the tensors were made for these sizes."""
-        if not fits:
-            _int8_operand(codes, scale, rows, dim)
+    def __init__(self, rows: int, dim: int, codes: torch.Tensor, scale: torch.Tensor):
+        _int8_operand(codes, scale, rows, dim)
         self.rows, self.dim, self.codes, self.scale, self.device = rows, dim, _ptr(codes), _ptr(scale), codes.get_device()
         self.keep = (codes, scale)
+
+    @classmethod
+    def of_whole(cls, rows: int, dim: int, whole: torch.Tensor, codes_bytes: int) -> "Int8RowsView":
+        """Codes and behind them the scales in one int8 tensor that was made for them."""
+        view = cls.__new__(cls)
+        view.rows, view.dim, view.codes, view.device, view.keep = rows, dim, whole.data_ptr(), whole.get_device(), (whole,)
+        view.scale = view.codes + codes_bytes
+        return view
 
 
 class Int8ProductCall:

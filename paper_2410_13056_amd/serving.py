@@ -81,14 +81,22 @@ class Int8Rows(_Kept):
     def _make(self) -> B.Int8RowsView:
         return B.Int8RowsView(self.rows, self.dim, self.codes, self.scale)
 
+    def __getattr__(self, name):
+        """Codes and scales of rows that were made in one piece, when something asks for them: most only pass through."""
+        if name in ("codes", "scale") and "_whole" in self.__dict__:
+            whole, n = self.__dict__["_whole"], B.int8_weight_bytes(self.rows, self.dim)
+            t = self.__dict__[name] = whole[:n] if name == "codes" else whole[n:].view(torch.float32)
+            return t
+        raise AttributeError(name)
+
 
 def _empty_rows(like: torch.Tensor) -> Int8Rows:
     """Room for the rows of `like` in 8 bits."""
     rows, dim = like.shape
-    codes = like.new_empty(B.int8_weight_bytes(rows, dim), dtype=torch.int8)
-    scale = like.new_empty(rows, dtype=torch.float32)
+    nbytes = B.int8_weight_bytes(rows, dim)     # a multiple of 1 KB: the scales behind it are aligned
+    whole = like.new_empty(nbytes + 4 * rows, dtype=torch.int8)
     made = Int8Rows.__new__(Int8Rows)           # without the checks of tensors that come from elsewhere
-    made.__dict__.update(rows=rows, dim=dim, codes=codes, scale=scale, _args=B.Int8RowsView(rows, dim, codes, scale, fits=True))
+    made.__dict__.update(rows=rows, dim=dim, _whole=whole, _args=B.Int8RowsView.of_whole(rows, dim, whole, nbytes))
     return made
 
 
@@ -107,7 +115,7 @@ Inputs = Union[torch.Tensor, Int8Rows]
 
 def _output(X: Inputs, d_out: int, out_dtype: Optional[torch.dtype]) -> torch.Tensor:
     if isinstance(X, Int8Rows):
-        return X.codes.new_empty((X.rows, d_out), dtype=out_dtype or torch.float16)
+        return X._args.keep[0].new_empty((X.rows, d_out), dtype=out_dtype or torch.float16)
     return X.new_empty((X.shape[0], d_out), dtype=out_dtype or X.dtype)
 
 
@@ -318,11 +326,13 @@ def _as_heads(Y: torch.Tensor, head_dim: int) -> torch.Tensor:
     return Y.reshape(Y.shape[0], Y.shape[1] // head_dim, head_dim)
 
 
-def _normed(X: torch.Tensor, norm: Optional[RmsNorm], layers, status: Optional[torch.Tensor]) -> Inputs:
-    """What layers take that share the input X: its norm if there is one, in 8 bits if all of them are."""
+def _shared(X: torch.Tensor, norm: Optional[RmsNorm], layers, status: Optional[torch.Tensor]) -> Inputs:
+    """What layers take that share the input X: its norm if there is one, in 8 bits if all of them are, coded once for
+    all (one or two tokens code themselves within the products' launches)."""
+    coded = all(isinstance(l, Int8Weight) for l in layers)
     if norm is None:
-        return X
-    if all(isinstance(l, Int8Weight) for l in layers):
+        return int8_rows(X, status=status) if coded and X.shape[0] > 2 else X
+    if coded:
         return rms_norm(X, norm.weight, norm.eps, coded=True, status=status)
     wide = not any(isinstance(l, P.Deployed) for l in layers)            # those read float16
     return rms_norm(X, norm.weight, norm.eps, out_dtype=X.dtype if wide else torch.float16, status=status)
@@ -343,7 +353,7 @@ def attention_block(cache: KvCache, X: torch.Tensor, q: Layer, k: Layer, v: Laye
     if attention_dtype is None:
         wide = X.dtype == torch.bfloat16 and not isinstance(o, P.Deployed)
         attention_dtype = torch.bfloat16 if wide else torch.float16
-    X = _normed(X, norm, (q, k, v), status)
+    X = _shared(X, norm, (q, k, v), status)
     Q, K, V = (_as_heads(apply_layer(layer, X, ws, status), cache.head_dim) for layer in (q, k, v))
     kv_append(cache, K, V, page_table, held, cu_rows, rotation, status)
     O = kv_attention(cache, Q, page_table, lengths, cu_rows, max_rows, max_length, ws, causal=causal, window=window,

@@ -187,3 +187,24 @@ def test_attention_of_a_normed_stream_with_layers_of_different_kinds(S):
     got = S.attention_block(S.make_cache(1, kv, dim, 32, DEV), X, *layers, *where, norm=norm)
     N = S.rms_norm(X, None, EPS)
     assert torch.equal(got, S.attention_block(S.make_cache(1, kv, dim, 32, DEV), N, *layers, *where))
+
+
+@pytest.mark.parametrize("n", [1, 2, 3, 40])
+def test_attention_codes_its_input_once(S, n):
+    """Three layers in 8 bits read rows coded once: what each would make of the values by itself, bit for bit."""
+    heads, kv, dim = 8, 2, 32
+    i32 = lambda v: torch.tensor(v, dtype=torch.int32, device=DEV)
+    from paper_2410_13056_amd import binding as B
+    ws, status = B.Workspace(DEV), torch.zeros(1, dtype=torch.int32, device=DEV)
+    W = [_randn(20 + i, o, d, dtype=torch.float16, scale=d ** -0.5) for i, (o, d) in
+         enumerate(((heads * dim, HIDDEN), (kv * dim, HIDDEN), (kv * dim, HIDDEN), (HIDDEN, heads * dim)))]
+    layers = [S.prepare_int8(w) for w in W]
+    X = _randn(1, n, HIDDEN + 3, dtype=torch.bfloat16)[:, 1:1 + HIDDEN]
+    where = (i32([[0, 1]]), i32([0]), i32([n]), i32([0, n]), n, n, ws)
+    got = S.attention_block(S.make_cache(2, kv, dim, 32, DEV), X, *layers, *where, status=status)
+    each = [lambda x, l=l: S.int8_product(l, x, ws, out_dtype=torch.float32) for l in layers[:3]]
+    assert torch.equal(got, S.attention_block(S.make_cache(2, kv, dim, 32, DEV), X, *each, layers[3], *where))
+    assert status.item() == 0
+    X[n - 1, 5] = float("inf")
+    S.attention_block(S.make_cache(2, kv, dim, 32, DEV), X, *layers, *where, status=status)
+    assert status.item() == B.STATUS_NONFINITE
