@@ -760,6 +760,30 @@ typedef struct cmpq_norm_job {
 int cmpq_rms_norm(const cmpq_norm_job *job, void *stream);
 
 /*
+ * A decoder layer's gated feed-forward part in 8 bits, in one call what three do:
+ *   s = X (+ add), n its norm (cmpq_rms_norm: S of X's type if there is `add`, the rows in 8 bits);
+ *   h = act(n Wg') * (n Wu'), rounded to hidden_dtype (cmpq_int8_product_job, gated);
+ *   Y = s + h Wd' (cmpq_int8_product_job with the residual s).
+ * gate_up: of cmpq_int8_prepare_gated for two weights [d_ff, d]; down: of cmpq_int8_prepare for [d, d_ff].  X, add and Y are [m, d],
+ * each of its own type; Y may be X or add (place, type and stride).  Results are those of the three calls, bit for bit.
+ * Workspace: cmpq_int8_feed_forward_workspace(job), a function of the sizes and types and of whether there is `add`; 0 where they
+ * are refused.  Limits and errors: those of the three; nothing is launched when one is rejected.  Status: CMPQ_STATUS_NONFINITE.
+ */
+typedef struct cmpq_int8_feed_forward_job {
+    cmpq_rows X, add, gain, Y;
+    double eps;
+    int64_t m, d, d_ff;
+    const int8_t *gate_up_codes;
+    const float *gate_up_scale;
+    const int8_t *down_codes;
+    const float *down_scale;
+    int activation, hidden_dtype;
+    int32_t *status; /* device, nullable */
+} cmpq_int8_feed_forward_job;
+size_t cmpq_int8_feed_forward_workspace(const cmpq_int8_feed_forward_job *job);
+int cmpq_int8_feed_forward(const cmpq_int8_feed_forward_job *job, void *ws, size_t ws_bytes, void *stream);
+
+/*
  * A cache of keys and values in pages of `page` tokens, 8 bits a value, one scale per page and head for the keys
  * and one for the values.  A byte is code + 128.  Codes of a page and head lie together, in pieces of 32 tokens by
  * 32 dims (1 KB, in the order in which the matrix instruction takes them), [page / 32][ceil(head_dim / 32)];

@@ -46,7 +46,8 @@ EXPORTS = ("cmpq_workspace_bytes", "cmpq_strerror", "cmpq_count_ppm", "cmpq_act_
            "cmpq_shader_clock_probe", "cmpq_lut_matvec_group_fp16acc", "cmpq_kmeans_build_shape", "cmpq_rank_channels",
            "cmpq_lut_matvec_shape", "cmpq_int8_weight_bytes", "cmpq_kv_page_bytes", "cmpq_kv_attention_workspace",
            "cmpq_int8_prepare", "cmpq_int8_product", "cmpq_kv_append", "cmpq_kv_read", "cmpq_kv_attention",
-           "cmpq_int8_gated_rows", "cmpq_int8_prepare_gated", "cmpq_int8_product_job", "cmpq_epilogue", "cmpq_rms_norm")
+           "cmpq_int8_gated_rows", "cmpq_int8_prepare_gated", "cmpq_int8_product_job", "cmpq_epilogue", "cmpq_rms_norm",
+           "cmpq_int8_feed_forward_workspace", "cmpq_int8_feed_forward")
 
 _i64, _i32, _int, _vp, _dbl, _sz = (ctypes.c_int64, ctypes.c_int32, ctypes.c_int, ctypes.c_void_p,
                                     ctypes.c_double, ctypes.c_size_t)
@@ -128,6 +129,13 @@ class NormJob(ctypes.Structure):
                                                              ("eps", _dbl), ("status", _vp)]
 
 
+class Int8FeedForwardJob(ctypes.Structure):
+    """`cmpq_int8_feed_forward_job` of the header."""
+    _fields_ = _rows_fields("X", "add", "gain", "Y") + [("eps", _dbl), ("m", _i64), ("d", _i64), ("d_ff", _i64), ("gate_up_codes", _vp),
+                                                        ("gate_up_scale", _vp), ("down_codes", _vp), ("down_scale", _vp),
+                                                        ("activation", _int), ("hidden_dtype", _int), ("status", _vp)]
+
+
 class CmpqError(RuntimeError):
     def __init__(self, code: int, where: str):
         self.code = code
@@ -192,9 +200,12 @@ def lib() -> ctypes.CDLL:
         L.cmpq_int8_product_job.argtypes = [ctypes.POINTER(Int8Job), _vp, _sz, _vp]
         L.cmpq_epilogue.argtypes = [ctypes.POINTER(EpilogueJob), _vp]
         L.cmpq_rms_norm.argtypes = [ctypes.POINTER(NormJob), _vp]
+        L.cmpq_int8_feed_forward_workspace.argtypes = [ctypes.POINTER(Int8FeedForwardJob)]
+        L.cmpq_int8_feed_forward.argtypes = [ctypes.POINTER(Int8FeedForwardJob), _vp, _sz, _vp]
         for name in EXPORTS[3:]:
             getattr(L, name).restype = _int
-        for name in ("cmpq_int8_weight_bytes", "cmpq_kv_page_bytes", "cmpq_kv_attention_workspace"):
+        for name in ("cmpq_int8_weight_bytes", "cmpq_kv_page_bytes", "cmpq_kv_attention_workspace",
+                     "cmpq_int8_feed_forward_workspace"):
             getattr(L, name).restype = _sz
         L.cmpq_int8_gated_rows.restype = _i64
         _lib = L
@@ -729,6 +740,11 @@ def _matrix(t: torch.Tensor, m: int, d: int, dev: int, what: str):
     return t.data_ptr(), ld if m > 1 else d, serving_dtype(t.dtype)
 
 
+def _output(t: torch.Tensor, m: int, d: int, dev: int, what: str, made: bool):
+    """`_matrix` of an output; `made`: the caller has just made it, [m, d] without gaps beside inputs that are looked at."""
+    return (t.data_ptr(), d, serving_dtype(t.dtype)) if made else _matrix(t, m, d, dev, what)
+
+
 def _vector(t: torch.Tensor, d: int, dev: int, what: str):
     if t.shape != (d,) or not t.is_contiguous():
         raise ValueError(f"{what} must be contiguous [{d}]")
@@ -842,8 +858,9 @@ class Int8ProductCall:
         self._gated, self._fn, self._device = int(bool(gated)), lib().cmpq_int8_product, codes.get_device()
 
     def job(self, X, Y: torch.Tensor, ws: Workspace, status: Optional[torch.Tensor] = None, bias: Optional[torch.Tensor] = None,
-            up_bias: Optional[torch.Tensor] = None, act: Optional[str] = None, residual: Optional[torch.Tensor] = None) -> None:
-        """The product with what follows it; X a tensor [m, d_in] or an `Int8RowsView`."""
+            up_bias: Optional[torch.Tensor] = None, act: Optional[str] = None, residual: Optional[torch.Tensor] = None,
+            made: bool = False) -> None:
+        """The product with what follows it; X a tensor [m, d_in] or an `Int8RowsView`.  `made`: see `_output`."""
         d, o, dev = self.d_in, self.d_out, _device()
         if isinstance(X, Int8RowsView):
             if X.dim != d:
@@ -854,7 +871,7 @@ class Int8ProductCall:
             x, ldx, xt = _matrix(X, m, d, dev, "X")
         if self._device != dev or at != dev:
             raise ValueError("layers and rows in 8 bits must be on the current device")
-        y, ldy, yt = _matrix(Y, m, o, dev, "Y")
+        y, ldy, yt = _output(Y, m, o, dev, "Y", made)
         b, _, bt = _NONE if bias is None else _vector(bias, o, dev, "bias")
         u, _, ut = _NONE if up_bias is None else _vector(up_bias, o, dev, "up_bias")
         if b and u and bt != ut:
@@ -896,14 +913,14 @@ def int8_product(X: torch.Tensor, codes: torch.Tensor, scale: torch.Tensor, Y: t
 
 def epilogue(Y: torch.Tensor, out: torch.Tensor, bias: Optional[torch.Tensor] = None, act: Optional[str] = None,
              times: Optional[torch.Tensor] = None, times_bias: Optional[torch.Tensor] = None,
-             residual: Optional[torch.Tensor] = None) -> None:
-    """`cmpq_epilogue`: out [m, d] = act(Y + bias) * (times + times_bias) + residual."""
+             residual: Optional[torch.Tensor] = None, made: bool = False) -> None:
+    """`cmpq_epilogue`: out [m, d] = act(Y + bias) * (times + times_bias) + residual.  `made`: see `_output`."""
     m, d = Y.shape
     dev = _device()
     j = EpilogueJob(*_matrix(Y, m, d, dev, "Y"), *(_NONE if bias is None else _vector(bias, d, dev, "bias")),
                     *(_NONE if times is None else _matrix(times, m, d, dev, "times")),
                     *(_NONE if times_bias is None else _vector(times_bias, d, dev, "times_bias")),
-                    *(_NONE if residual is None else _matrix(residual, m, d, dev, "residual")), *_matrix(out, m, d, dev, "out"),
+                    *(_NONE if residual is None else _matrix(residual, m, d, dev, "residual")), *_output(out, m, d, dev, "out", made),
                     m, d, activation(act))
     rc = lib().cmpq_epilogue(j, _stream())
     if rc:
@@ -911,8 +928,10 @@ def epilogue(Y: torch.Tensor, out: torch.Tensor, bias: Optional[torch.Tensor] = 
 
 
 def rms_norm(X: torch.Tensor, gain: Optional[torch.Tensor], eps: float, Y, add: Optional[torch.Tensor] = None,
-             S: Optional[torch.Tensor] = None, status: Optional[torch.Tensor] = None) -> None:
-    """`cmpq_rms_norm`: the norm of X (+ add) [m, d] into Y, a tensor or an `Int8RowsView`; the sum into S."""
+             S: Optional[torch.Tensor] = None, status: Optional[torch.Tensor] = None, made: bool = False,
+             sum_made: bool = False) -> None:
+    """`cmpq_rms_norm`: the norm of X (+ add) [m, d] into Y, a tensor or an `Int8RowsView`; the sum into S.  `made`: see
+    `_output`."""
     m, d = X.shape
     dev = _device()
     if isinstance(Y, Int8RowsView):
@@ -922,13 +941,38 @@ def rms_norm(X: torch.Tensor, gain: Optional[torch.Tensor], eps: float, Y, add: 
             raise ValueError("layers and rows in 8 bits must be on the current device")
         y, codes, scale = _NONE, Y.codes, Y.scale
     else:
-        y, codes, scale = _matrix(Y, m, d, dev, "Y"), None, None
+        y, codes, scale = _output(Y, m, d, dev, "Y", made), None, None
     j = NormJob(*_matrix(X, m, d, dev, "X"), *(_NONE if add is None else _matrix(add, m, d, dev, "add")),
-                *(_NONE if gain is None else _vector(gain, d, dev, "weight")), *(_NONE if S is None else _matrix(S, m, d, dev, "the sum")),
+                *(_NONE if gain is None else _vector(gain, d, dev, "weight")), *(_NONE if S is None else _output(S, m, d, dev, "the sum", sum_made)),
                 *y, codes, scale, m, d, eps, _flags(status, dev))
     rc = lib().cmpq_rms_norm(j, _stream())
     if rc:
         _check(rc, "cmpq_rms_norm")
+
+
+def int8_feed_forward(X: torch.Tensor, gain: Optional[torch.Tensor], eps: float, gate_up: Int8ProductCall, down: Int8ProductCall,
+                      Y: torch.Tensor, ws: Workspace, add: Optional[torch.Tensor] = None, act: Optional[str] = None,
+                      hidden_dtype: Optional[torch.dtype] = None, status: Optional[torch.Tensor] = None, made: bool = False) -> None:
+    """`cmpq_int8_feed_forward`: norm, gated product and output product of X (+ add) [m, d] into Y.  `made`: see `_output`."""
+    m, d = X.shape
+    dev, d_ff = _device(), gate_up.d_out
+    if not gate_up._gated or down._gated or gate_up.d_in != d or (down.d_in, down.d_out) != (d_ff, d):
+        raise ValueError(f"layers must be gated {d} -> 2 x {d_ff} and {d_ff} -> {d}")
+    if gate_up._device != dev or down._device != dev:
+        raise ValueError("layers and rows in 8 bits must be on the current device")
+    x = _matrix(X, m, d, dev, "X")
+    j = Int8FeedForwardJob(*x, *(_NONE if add is None else _matrix(add, m, d, dev, "add")),
+                           *(_NONE if gain is None else _vector(gain, d, dev, "weight")), *_output(Y, m, d, dev, "Y", made), eps, m, d,
+                           d_ff, gate_up._codes, gate_up._scale, down._codes, down._scale, activation(act),
+                           x[2] if hidden_dtype is None else serving_dtype(hidden_dtype), _flags(status, dev))
+    for _ in range(2):              # asks for the workspace's size only where what is there does not do
+        buf = ws.buf
+        rc = _lib.cmpq_int8_feed_forward(j, buf.data_ptr(), buf.numel(), _stream())
+        if rc != EWORKSPACE:
+            break
+        ws.get(_lib.cmpq_int8_feed_forward_workspace(j))
+    if rc:
+        _check(rc, "cmpq_int8_feed_forward")
 
 
 def kv_cache_view(k: torch.Tensor, v: torch.Tensor, k_scale: torch.Tensor, v_scale: torch.Tensor, page: int,

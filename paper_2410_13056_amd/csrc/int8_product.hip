@@ -848,9 +848,9 @@ extern "C" int cmpq_int8_product(const void *X, int dtype, int64_t m, int64_t d_
     return run_product(Asked{X, dtype, d_in, ldx, nullptr, codes, y_dtype, status}, y, Plain(), w, static_cast<hipStream_t>(stream));
 }
 
-extern "C" int cmpq_int8_product_job(const cmpq_int8_job *j, void *ws, size_t ws_bytes, void *stream) {
+int cmpq_check_int8_product(const cmpq_int8_job *j) {
     if (!j || j->m < 0 || j->d_in < 1 || j->d_out < 0 || !serving_dtype(j->y_dtype) || !known_activation(j->activation)) return CMPQ_EINVAL;
-    if (j->X ? !serving_dtype(j->x_dtype) : false) return CMPQ_EINVAL;
+    if (j->X && !serving_dtype(j->x_dtype)) return CMPQ_EINVAL;
     if ((j->bias || j->up_bias) && !serving_dtype(j->bias_dtype)) return CMPQ_EINVAL;
     if ((j->residual && !serving_dtype(j->r_dtype)) || (j->up_bias && !j->gated)) return CMPQ_EINVAL;
     if (j->m == 0 || j->d_out == 0) return CMPQ_OK;
@@ -858,6 +858,12 @@ extern "C" int cmpq_int8_product_job(const cmpq_int8_job *j, void *ws, size_t ws
     if (!j->X && (!j->x_codes || !j->x_scale || !aligned16(j->x_codes))) return CMPQ_EINVAL;
     if ((j->X && j->ldx < j->d_in) || j->ldy < j->d_out || (j->residual && j->ldr < j->d_out)) return CMPQ_ESHAPE;
     if (j->m >= (1 << 24) || !sizes_fit(j->d_in, j->gated ? 2 * j->d_out : j->d_out)) return CMPQ_ESHAPE;
+    return CMPQ_OK;
+}
+
+extern "C" int cmpq_int8_product_job(const cmpq_int8_job *j, void *ws, size_t ws_bytes, void *stream) {
+    if (int rc = cmpq_check_int8_product(j)) return rc;
+    if (j->m == 0 || j->d_out == 0) return CMPQ_OK;
     Work w = {};
     if (j->X) {
         w = carve(ws, j->m, j->d_in);

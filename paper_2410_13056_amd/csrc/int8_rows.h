@@ -8,6 +8,11 @@
 constexpr int kRows = 16, kDepth = 64, kPiece = kRows * kDepth;  // a piece
 constexpr int64_t kMostDepth = 131072;                            // 127 * 127 * d_in < 2^31
 
+// The host's checks of cmpq_rms_norm and cmpq_int8_product_job (but for its workspace), for calls that make several of these.
+int cmpq_check_rms_norm(const cmpq_norm_job *job);
+int cmpq_check_int8_product(const cmpq_int8_job *job);
+size_t cmpq_ws_int8_product(int64_t d_in, int64_t m);
+
 __host__ __device__ inline int64_t pieces_deep(int64_t d) { return (d + 127) / 128 * 2; }
 
 // Workgroups in the order in which they are handed to the eight dies, so that each die gets a run of them.

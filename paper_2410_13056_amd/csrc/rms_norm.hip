@@ -197,7 +197,7 @@ void launch_norm(const cmpq_norm_job &a, hipStream_t st) {
 
 }  // namespace
 
-extern "C" int cmpq_rms_norm(const cmpq_norm_job *j, void *stream) {
+int cmpq_check_rms_norm(const cmpq_norm_job *j) {
     if (!j || j->m < 0 || j->d < 1 || !(j->eps >= 0x1p-126 && j->eps < __builtin_huge_val())) return CMPQ_EINVAL;
     const cmpq_rows all[] = {j->X, j->add, j->gain, j->S, j->Y};
     for (const cmpq_rows &a : all)
@@ -209,7 +209,14 @@ extern "C" int cmpq_rms_norm(const cmpq_norm_job *j, void *stream) {
     const cmpq_rows rows[] = {j->X, j->add, j->S, j->Y};
     for (const cmpq_rows &a : rows)
         if (a.ptr && a.ld < j->d) return CMPQ_ESHAPE;
+    return CMPQ_OK;
+}
+
+extern "C" int cmpq_rms_norm(const cmpq_norm_job *j, void *stream) {
+    if (int rc = cmpq_check_rms_norm(j)) return rc;
+    if (j->m == 0) return CMPQ_OK;
     hipStream_t st = static_cast<hipStream_t>(stream);
+    const cmpq_rows all[] = {j->X, j->add, j->gain, j->S, j->Y};
     int type = j->X.dtype;
     for (const cmpq_rows &a : all)
         if (a.ptr && a.dtype != j->X.dtype) type = kAny;

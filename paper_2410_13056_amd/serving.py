@@ -116,7 +116,7 @@ Inputs = Union[torch.Tensor, Int8Rows]
 def _output(X: Inputs, d_out: int, out_dtype: Optional[torch.dtype]) -> torch.Tensor:
     if isinstance(X, Int8Rows):
         return X._args.keep[0].new_empty((X.rows, d_out), dtype=out_dtype or torch.float16)
-    return X.new_empty((X.shape[0], d_out), dtype=out_dtype or X.dtype)
+    return X.new_empty((X.shape[0], d_out)) if out_dtype is None else X.new_empty((X.shape[0], d_out), dtype=out_dtype)
 
 
 def int8_product(w: Int8Weight, X: Inputs, ws: Optional[B.Workspace] = None,
@@ -127,13 +127,15 @@ def int8_product(w: Int8Weight, X: Inputs, ws: Optional[B.Workspace] = None,
     already (`Int8Rows`).  `out_dtype` defaults to X's (float16 for rows in 8 bits).  `bias` [d_out]; `activation`
     "silu", "gelu", "gelu_tanh" or "relu"; `residual` [m, d_out], which may be `out` itself; each of its own type.  All of it
     is worked out in fp32 and rounded once."""
-    if out is None:
+    made = out is None
+    if made:
         out = _output(X, w.d_out, out_dtype)
     coded = isinstance(X, Int8Rows)
     if not coded and bias is None and activation is None and residual is None:
         w._args(X, out, ws or B.Workspace(X.device), status)
     else:
-        w._args.job(X._args if coded else X, out, ws or B.Workspace(out.device), status, bias, None, activation, residual)
+        w._args.job(X._args if coded else X, out, ws or B.Workspace(out.device), status, bias, None, activation, residual,
+                    made)
     return out
 
 
@@ -165,10 +167,11 @@ def int8_gated_product(w: Int8GatedWeight, X: Inputs, ws: Optional[B.Workspace] 
                        status: Optional[torch.Tensor] = None, residual: Optional[torch.Tensor] = None) -> torch.Tensor:
     """H [m, d_out] = act(X Wg' + gate_bias) * (X Wu' + up_bias) (+ residual): one pass over the inputs, neither projection in
     memory.  Otherwise as `int8_product`; the biases are of one type."""
-    if out is None:
+    made = out is None
+    if made:
         out = _output(X, w.d_out, out_dtype)
     w._args.job(X._args if isinstance(X, Int8Rows) else X, out, ws or B.Workspace(out.device), status, gate_bias, up_bias,
-                activation, residual)
+                activation, residual, made)
     return out
 
 
@@ -180,9 +183,10 @@ def epilogue(Y: torch.Tensor, bias: Optional[torch.Tensor] = None, activation: O
              out: Optional[torch.Tensor] = None) -> torch.Tensor:
     """act(Y + bias) * (times + times_bias) + residual for the outputs Y [m, d] of a product in mixed precision; times and
     residual are [m, d], the biases [d], each of its own type.  `out_dtype` defaults to Y's; `out` may be Y, times or residual."""
-    if out is None:
+    made = out is None
+    if made:
         out = torch.empty_like(Y, dtype=out_dtype)
-    B.epilogue(Y, out, bias, activation, times, times_bias, residual)
+    B.epilogue(Y, out, bias, activation, times, times_bias, residual, made)
     return out
 
 
@@ -192,11 +196,12 @@ def rms_norm(X: torch.Tensor, weight: Optional[torch.Tensor] = None, eps: float 
     """s / sqrt(mean(s^2) + eps) * weight along the rows of s = X [m, d], or of s = X + add; the weight [d] may be None.
     `coded`: as `Int8Rows` for the products that follow, else of `out_dtype`, by default X's.  With `add` the answer is (norm, s),
     s of X's type unless `sum_out` says otherwise, which may be X or `add` itself; the norm is that of s as rounded."""
-    if out is None:
+    made, sum_made = out is None, add is not None and sum_out is None
+    if made:
         out = _empty_rows(X) if coded else torch.empty_like(X, dtype=out_dtype)
-    if add is not None and sum_out is None:
+    if sum_made:
         sum_out = torch.empty_like(X)
-    B.rms_norm(X, weight, eps, out._args if isinstance(out, Int8Rows) else out, add, sum_out, status)
+    B.rms_norm(X, weight, eps, out._args if isinstance(out, Int8Rows) else out, add, sum_out, status, made, sum_made)
     return out if add is None else (out, sum_out)
 
 
@@ -393,11 +398,15 @@ def feed_forward_block(X: torch.Tensor, norm: RmsNorm, gate_up: Union[Int8GatedW
                        status: Optional[torch.Tensor] = None, hidden_dtype: Optional[torch.dtype] = None) -> torch.Tensor:
     """A decoder layer's gated feed-forward part on the residual stream: s + down(act(gate n) * (up n)), n the norm of s = X
     [rows, hidden] (+ `add`, what the layer's attention gave, in any type).  The projections may be of different kinds, as in
-    `attention_block`; the answer has X's type.  `hidden_dtype`: what `down` is handed, by default X's type, or
+    `attention_block` (all in 8 bits, it is one call); the answer has X's type.  `hidden_dtype`: what `down` is handed, by default X's type, or
     float16 where `down` is in mixed precision, which reads that."""
+    gated = isinstance(gate_up, Int8GatedWeight)
+    if gated and isinstance(down, Int8Weight):
+        Y = torch.empty_like(X)
+        B.int8_feed_forward(X, norm.weight, norm.eps, gate_up._args, down._args, Y, ws, add, activation, hidden_dtype, status, True)
+        return Y
     if hidden_dtype is None:
         hidden_dtype = torch.float16 if isinstance(down, P.Deployed) else X.dtype
-    gated = isinstance(gate_up, Int8GatedWeight)
     mixed = not gated and any(isinstance(l, P.Deployed) for l in (gate_up.gate, gate_up.up))
     N = rms_norm(X, norm.weight, norm.eps, add=add, coded=gated, out_dtype=torch.float16 if mixed else X.dtype, status=status)
     N, stream = N if add is not None else (N, X)

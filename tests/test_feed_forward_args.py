@@ -27,6 +27,8 @@ def B():
 def test_structures_have_the_headers_layout(B, tmp_path):
     fields = {"cmpq_int8_job": (B.Int8Job, ["x_codes", "gated", "bias", "activation", "residual", "ldr", "Y", "ldy", "status"]),
               "cmpq_epilogue_job": (B.EpilogueJob, ["bias", "times", "times_bias", "residual", "out", "m", "activation"]),
+              "cmpq_int8_feed_forward_job": (B.Int8FeedForwardJob, ["add", "gain", "Y", "eps", "m", "d_ff", "gate_up_codes", "down_scale",
+                                                                     "activation", "hidden_dtype", "status"]),
               "cmpq_norm_job": (B.NormJob, ["add", "gain", "S", "Y", "codes", "scale", "m", "eps", "status"])}
     lines = ['#include <stdio.h>', '#include "cmpq.h"', "int main(void) {"]
     for name, (_, names) in fields.items():
@@ -107,6 +109,28 @@ def test_norm_jobs(B):
     assert run(m=0) == run(m=0, codes=FAKE, scale=FAKE) == 0 and B.lib().cmpq_rms_norm(None, None) == -1
 
 
+def test_feed_forward_jobs(B):
+    def job(m=4, d=64, d_ff=96, eps=1e-6, gc=FAKE, gs=FAKE, dc=FAKE, ds=FAKE, act=1, hidden=0, **k):
+        f = {n: NONE for n in ("X", "add", "gain", "Y")}
+        f.update(X=_rows(), Y=_rows())
+        f.update(k)
+        return B.Int8FeedForwardJob(*f["X"], *f["add"], *f["gain"], *f["Y"], eps, m, d, d_ff, gc, gs, dc, ds, act, hidden, None)
+    run = lambda ws=FAKE, n=1 << 40, **k: B.lib().cmpq_int8_feed_forward(ctypes.byref(job(**k)), ws, n, None)
+    for bad in (dict(m=-1), dict(d=0), dict(d_ff=0), dict(eps=0.0), dict(gc=None), dict(gs=None), dict(dc=None), dict(ds=None), dict(act=9),
+                dict(hidden=3), dict(X=NONE), dict(Y=NONE), dict(X=_rows(dtype=3)), dict(Y=_rows(dtype=3)), dict(add=_rows(dtype=5)),
+                dict(gain=_rows(dtype=-1)), dict(gc=FAKE + 8), dict(dc=FAKE + 8)):
+        assert run(**bad) == -1, bad
+    for bad in (dict(m=1 << 24), dict(d=131073, X=_rows(ld=131073), Y=_rows(ld=131073)), dict(d_ff=131073), dict(X=_rows(ld=63)),
+                dict(Y=_rows(ld=63)), dict(add=_rows(ld=63))):
+        assert run(**bad) == -2, bad
+    size = lambda **k: B.lib().cmpq_int8_feed_forward_workspace(ctypes.byref(job(**k)))
+    need = size()
+    assert need % 256 == 0 and size(add=_rows()) >= need + 4 * 64 * 2 and size(hidden=1) > need and size(m=0) >= 256
+    assert run(ws=None) == run(ws=FAKE + 16) == run(n=need - 1) == -5 and run(m=0) == run(m=0, X=NONE[:2] + (0,), Y=NONE) == 0
+    assert size(m=-1) == size(d_ff=131073) == size(hidden=7) == 0
+    assert B.lib().cmpq_int8_feed_forward(None, FAKE, 1 << 40, None) == -1 and B.lib().cmpq_int8_feed_forward_workspace(None) == 0
+
+
 # ---- the Python side, on host tensors with the library's part left out ---------------------------------
 
 @pytest.fixture
@@ -121,7 +145,7 @@ def S(B, monkeypatch):
             self.real = real
 
         def __getattr__(self, name):
-            if name in ("cmpq_int8_weight_bytes", "cmpq_int8_gated_rows", "cmpq_workspace_bytes", "cmpq_strerror"):
+            if name in ("cmpq_int8_weight_bytes", "cmpq_int8_feed_forward_workspace", "cmpq_int8_gated_rows", "cmpq_workspace_bytes", "cmpq_strerror"):
                 return getattr(self.real, name)
             return lambda *args: 0
     monkeypatch.setattr(B, "_lib", Library(B.lib()))
@@ -160,6 +184,14 @@ def test_tensors_that_do_not_fit_are_refused(S, B):
         S.prepare_int8_gated(z((24, 64)), z((24, 64)).half())
     with pytest.raises(ValueError):
         S.prepare_int8_gated(z((24, 64)), z((23, 64)))
+    gate_up, down, norm = _weight(S, B, 64, 24, True), _weight(S, B, 24, 64), S.RmsNorm(z(64))
+    assert S.feed_forward_block(X, norm, gate_up, down, ws, add=X.half()).shape == (3, 64)
+    for bad in (dict(norm=S.RmsNorm(z(63))), dict(add=z((3, 63))), dict(down=_weight(S, B, 24, 63)), dict(down=_weight(S, B, 23, 64)),
+                dict(gate_up=_weight(S, B, 63, 24, True)), dict(activation="tanh")):
+        with pytest.raises(ValueError):
+            S.feed_forward_block(**{**dict(X=X, norm=norm, gate_up=gate_up, down=down, ws=ws), **bad})
+    with pytest.raises(TypeError):
+        S.feed_forward_block(X, norm, gate_up, down, ws, hidden_dtype=torch.float64)
     for bad in (dict(bias=z(63)), dict(times=z((3, 63))), dict(times_bias=z(64), times=z((2, 64))), dict(residual=z(64)), dict(out=z((3, 65))),
                 dict(activation="swish")):
         with pytest.raises(ValueError):

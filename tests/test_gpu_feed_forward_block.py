@@ -208,3 +208,30 @@ def test_attention_codes_its_input_once(S, n):
     X[n - 1, 5] = float("inf")
     S.attention_block(S.make_cache(2, kv, dim, 32, DEV), X, *layers, *where, status=status)
     assert status.item() == B.STATUS_NONFINITE
+
+
+@pytest.mark.parametrize("m", [1, 2, 3, 16, 50, 300, 2100])
+@pytest.mark.parametrize("dtype", TYPES)
+def test_one_call_is_its_three_bit_for_bit(S, m, dtype):
+    """Whatever the types of what is added, the weight and the hidden values; rows that lie apart; the answer in the place of the
+    stream or of what is added."""
+    from paper_2410_13056_amd import binding as B
+    part = Part(S, "g8", 1500)
+    X, A = (_randn(i, m, HIDDEN + 8, dtype=t)[:, 3:3 + HIDDEN] for i, t in ((1, dtype), (2, torch.float32)))
+    for add, act, hidden in ((None, "silu", None), (A, "gelu", torch.bfloat16), (X, None, torch.float32), (A.half(), "relu", torch.float16)):
+        got = part(X, add=add, activation=act, hidden_dtype=hidden)
+        rows = S.rms_norm(X, part.norm.weight, EPS, add=add, coded=True)
+        rows, stream = (rows, X) if add is None else rows
+        H = S.int8_gated_product(part.gate_up, rows, part.ws, act, out_dtype=hidden or dtype)
+        assert torch.equal(got, S.int8_product(part.down, H, part.ws, out_dtype=dtype, residual=stream))
+        args = (part.norm.weight, EPS, part.gate_up._args, part.down._args)
+        for place in [X] if add is None else [X, add]:
+            if place.dtype != dtype:
+                continue
+            whole = {id(t): (t if t._base is None else t._base).clone() for t in (X, add) if t is not None}
+            mine = {k: w if w.shape[1] == HIDDEN else w[:, 3:3 + HIDDEN] for k, w in whole.items()}
+            Y = mine[id(place)]
+            B.int8_feed_forward(mine[id(X)], *args, Y, part.ws, None if add is None else mine[id(add)], act, hidden)
+            assert torch.equal(Y, got)
+            if place._base is not None:
+                assert torch.equal(whole[id(place)][:, -5:], place._base[:, -5:]) and torch.equal(whole[id(place)][:, :3], place._base[:, :3])
