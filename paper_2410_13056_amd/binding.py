@@ -740,6 +740,12 @@ def _matrix(t: torch.Tensor, m: int, d: int, dev: int, what: str):
     return t.data_ptr(), ld if m > 1 else d, serving_dtype(t.dtype)
 
 
+def check_matrix(t: torch.Tensor) -> None:
+    """Refuses what no call would take as a matrix."""
+    m, d = t.shape
+    _matrix(t, m, d, _device(), "Y")
+
+
 def _output(t: torch.Tensor, m: int, d: int, dev: int, what: str, made: bool):
     """`_matrix` of an output; `made`: the caller has just made it, [m, d] without gaps beside inputs that are looked at."""
     return (t.data_ptr(), d, serving_dtype(t.dtype)) if made else _matrix(t, m, d, dev, what)

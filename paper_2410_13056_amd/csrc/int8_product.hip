@@ -594,50 +594,62 @@ __global__ __launch_bounds__(WO * WT * G * 64, 2) void tile_kernel(const uint8_t
         turn(step + 1, 1);
     }
     asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");  // what nothing reads ends before the LDS does
-    if constexpr (G > 1) {  // the groups' sums, in order, with the first
-        __syncthreads();
-        Int4 *sums = reinterpret_cast<Int4 *>(smem);
-        if (group > 0) {
+    // The groups' sums are joined through LDS, in order; each group finishes its share of the tokens.
+    constexpr int kOwn = B / G;
+    static_assert(kOwn * G == B, "tokens of a group");
+    Int4 own[A][kOwn];
+    if constexpr (G == 1) {
 #pragma unroll
-            for (int i = 0; i < A * B; ++i) sums[(((group - 1) * kWaves + wave) * A * B + i) * 64 + lane] = acc[i / B][i % B];
+        for (int i = 0; i < A * B; ++i) own[i / B][i % B] = acc[i / B][i % B];
+    } else {
+        constexpr int kPart = A * kOwn * 64;
+        __syncthreads();
+        Int4 *sums = reinterpret_cast<Int4 *>(smem);  // [finishing group][wavefront][other group]
+#pragma unroll
+        for (int g = 0; g < G; ++g) {
+            Int4 *to = sums + ((g * kWaves + wave) * (G - 1) + (group < g ? group : group - 1)) * kPart + lane;
+#pragma unroll
+            for (int i = 0; i < A * kOwn; ++i) {
+                if (group == g) own[i / kOwn][i % kOwn] = acc[i / kOwn][g * kOwn + i % kOwn];
+                else to[i * 64] = acc[i / kOwn][g * kOwn + i % kOwn];
+            }
         }
         __syncthreads();
-        if (group == 0) {
 #pragma unroll
-            for (int g = 0; g < G - 1; ++g)
+        for (int g = 0; g < G - 1; ++g) {
+            const Int4 *from = sums + ((group * kWaves + wave) * (G - 1) + g) * kPart + lane;
 #pragma unroll
-                for (int i = 0; i < A * B; ++i) acc[i / B][i % B] += sums[((g * kWaves + wave) * A * B + i) * 64 + lane];
+            for (int i = 0; i < A * kOwn; ++i) own[i / kOwn][i % kOwn] += from[i * 64];
         }
-        if (!E::kPlain) __syncthreads();
-        if (group > 0) return;
     }
+    const int64_t t_own = t0 + wt + group * kOwn;
     if constexpr (!E::kPlain) {
-        if (G == 1) __syncthreads();  // nobody's loads are under way to the LDS that the sums pass through now
-        constexpr int kAtOnce = tokens_at_once(A, B, kWaves, BUFS * kStepBytes);
-        Int4 *through = reinterpret_cast<Int4 *>(smem) + wave * (kAtOnce * A * 64);
+        __syncthreads();  // nobody's loads or sums are under way in the LDS that the results pass through now
+        constexpr int kAtOnce = tokens_at_once(A, kOwn, kWaves * G, G * BUFS * kStepBytes);
+        Int4 *through = reinterpret_cast<Int4 *>(smem) + (group * kWaves + wave) * (kAtOnce * A * 64);
 #pragma unroll
-        for (int q0 = 0; q0 < B; q0 += kAtOnce) {
+        for (int q0 = 0; q0 < kOwn; q0 += kAtOnce) {
 #pragma unroll
             for (int q = 0; q < kAtOnce; ++q)
 #pragma unroll
-                for (int p = 0; p < A; ++p) through[staged_sum<A>(q * kRows + (lane & 15), p * 4 + (lane >> 4))] = acc[p][q0 + q];
+                for (int p = 0; p < A; ++p) through[staged_sum<A>(q * kRows + (lane & 15), p * 4 + (lane >> 4))] = own[p][q0 + q];
             __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-            finish_rows<E, A, kAtOnce * kRows>(through, y, e, (t0 + wt + q0) * kRows, (o0 + wo) / kPerOutput<E> * kRows);
+            finish_rows<E, A, kAtOnce * kRows>(through, y, e, (t_own + q0) * kRows, (o0 + wo) / kPerOutput<E> * kRows);
             __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
         }
         return;
     }
-    const int64_t t = (t0 + wt) * kRows + (lane & 15), o = (o0 + wo) * kRows + (lane >> 4) * 4;
-    float sx[B];
+    const int64_t t = t_own * kRows + (lane & 15), o = (o0 + wo) * kRows + (lane >> 4) * 4;
+    float sx[kOwn];
     float4 sw[A];
 #pragma unroll
-    for (int q = 0; q < B; ++q) sx[q] = token_scale(y, t + q * kRows);
+    for (int q = 0; q < kOwn; ++q) sx[q] = token_scale(y, t + q * kRows);
 #pragma unroll
     for (int p = 0; p < A; ++p) sw[p] = output_scales(y, o + p * kRows);
 #pragma unroll
-    for (int q = 0; q < B; ++q)
+    for (int q = 0; q < kOwn; ++q)
 #pragma unroll
-        for (int p = 0; p < A; ++p) put4<T>(y, t + q * kRows, o + p * kRows, acc[p][q], sx[q], sw[p]);
+        for (int p = 0; p < A; ++p) put4<T>(y, t + q * kRows, o + p * kRows, own[p][q], sx[q], sw[p]);
 }
 
 // Groups of 16 rows of the weight.

@@ -182,8 +182,12 @@ def epilogue(Y: torch.Tensor, bias: Optional[torch.Tensor] = None, activation: O
              residual: Optional[torch.Tensor] = None, out_dtype: Optional[torch.dtype] = None,
              out: Optional[torch.Tensor] = None) -> torch.Tensor:
     """act(Y + bias) * (times + times_bias) + residual for the outputs Y [m, d] of a product in mixed precision; times and
-    residual are [m, d], the biases [d], each of its own type.  `out_dtype` defaults to Y's; `out` may be Y, times or residual."""
+    residual are [m, d], the biases [d], each of its own type.  `out_dtype` defaults to Y's; `out` may be Y, times or residual.
+    Asked for nothing, the answer is Y itself, as with `Tensor.to`."""
     made = out is None
+    if made and bias is activation is times is times_bias is residual is None and out_dtype in (None, Y.dtype):
+        B.check_matrix(Y)
+        return Y
     if made:
         out = torch.empty_like(Y, dtype=out_dtype)
     B.epilogue(Y, out, bias, activation, times, times_bias, residual, made)

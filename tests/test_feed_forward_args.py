@@ -240,6 +240,10 @@ def test_outputs_have_the_types_asked_for(S, B):
     assert norm.dtype == torch.float16 and total.dtype == torch.bfloat16
     assert S.rms_norm(X, add=A, sum_out=A)[1] is A
     assert S.epilogue(A, out_dtype=torch.float16).dtype == torch.float16 and S.epilogue(A, out=A) is A
+    assert S.epilogue(A) is A and S.epilogue(A, out_dtype=A.dtype) is A and S.epilogue(A, activation="relu") is not A
+    for bad in (A.t(), A.double(), A[0]):
+        with pytest.raises((ValueError, TypeError)):
+            S.epilogue(bad)
 
 
 def test_objects_are_copied_and_give_their_memory_back(S, B):
