@@ -1,6 +1,6 @@
 // A gated feed-forward part in 8 bits: the norm, the gated projections and the output projection one after the other, what passes
-// between them in the caller's workspace.  Four launches (three for one or two tokens) for one call: 16 us of the host's time where
-// the three calls from Python took 28.
+// between them in the caller's workspace.  Four launches (three for one or two tokens) for one call, since the host bounds a small
+// part: 13 tokens of 102, 2 x 2491 take 17.7 us, as three calls from Python 29.6.
 #include "int8_rows.h"
 
 namespace {
