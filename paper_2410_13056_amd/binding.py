@@ -875,8 +875,8 @@ class Int8ProductCall:
         else:
             m, xc, xs, at = X.shape[0], None, None, dev
             x, ldx, xt = _matrix(X, m, d, dev, "X")
-        if self._device != dev or at != dev:
-            raise ValueError("layers and rows in 8 bits must be on the current device")
+        if self._device != dev or at != dev or ws.buf.get_device() != dev:
+            raise ValueError("layers, rows in 8 bits and workspaces must be on the current device")
         y, ldy, yt = _output(Y, m, o, dev, "Y", made)
         b, _, bt = _NONE if bias is None else _vector(bias, o, dev, "bias")
         u, _, ut = _NONE if up_bias is None else _vector(up_bias, o, dev, "up_bias")
@@ -964,8 +964,8 @@ def int8_feed_forward(X: torch.Tensor, gain: Optional[torch.Tensor], eps: float,
     dev, d_ff = _device(), gate_up.d_out
     if not gate_up._gated or down._gated or gate_up.d_in != d or (down.d_in, down.d_out) != (d_ff, d):
         raise ValueError(f"layers must be gated {d} -> 2 x {d_ff} and {d_ff} -> {d}")
-    if gate_up._device != dev or down._device != dev:
-        raise ValueError("layers and rows in 8 bits must be on the current device")
+    if gate_up._device != dev or down._device != dev or ws.buf.get_device() != dev:
+        raise ValueError("layers, rows in 8 bits and workspaces must be on the current device")
     x = _matrix(X, m, d, dev, "X")
     j = Int8FeedForwardJob(*x, *(_NONE if add is None else _matrix(add, m, d, dev, "add")),
                            *(_NONE if gain is None else _vector(gain, d, dev, "weight")), *_output(Y, m, d, dev, "Y", made), eps, m, d,

@@ -229,6 +229,25 @@ def test_host_tensors_and_other_devices_are_refused(B):
     assert B._vector(Elsewhere(), 3, 1, "bias") == (FAKE, 0, B.F16)
 
 
+def test_layers_and_workspaces_of_another_device_are_refused(S, B, monkeypatch):
+    class Elsewhere:
+        class buf:
+            get_device = staticmethod(lambda: 1)
+    X, layers = torch.zeros((3, 64)), (_weight(S, B, 64, 24, True), _weight(S, B, 24, 64))
+    rows = S.rms_norm(X, coded=True)
+    calls = [lambda ws, x: S.int8_gated_product(layers[0], x, ws), lambda ws, x: S.int8_product(_weight(S, B), x, ws, activation="relu")]
+    for call in calls:
+        for x in (X, rows):
+            with pytest.raises(ValueError, match="current device"):
+                call(Elsewhere(), x)
+    with pytest.raises(ValueError, match="current device"):
+        S.feed_forward_block(X, S.RmsNorm(), *layers, Elsewhere())
+    monkeypatch.setattr(B, "_device", lambda: 0)
+    for call in calls + [lambda ws, x: S.rms_norm(X, out=rows), lambda ws, x: S.epilogue(X)]:
+        with pytest.raises(ValueError):
+            call(_Workspace(), rows)
+
+
 def test_outputs_have_the_types_asked_for(S, B):
     ws, X, A = _Workspace(), torch.zeros((3, 64), dtype=torch.bfloat16), torch.zeros((3, 64))
     rows = S.rms_norm(X, coded=True)
