@@ -260,7 +260,8 @@ __device__ __forceinline__ Int4 multiply(const Int4 &w, const Int4 &x, const Int
 
 // Few outputs or tokens: a workgroup has OP x TP pieces of 16 outputs by 16 tokens, its wavefronts share the depth and
 // add up through LDS.  Operands come straight from memory, kAhead steps of 64 inputs at once, overlapped with the
-// products only where a workgroup has many of them (registers).  Bound by the weights' bytes: 16 tokens 5120 -> 13824
+// products only where a workgroup has many of them (registers).  A step in turn for each wavefront and not a run of steps: 4 tokens
+// 28672 -> 8192, weights from memory, 44 us and 49, 16 tokens 13824 -> 5120 19.9 and 20.8.  Bound by the weights' bytes: 16 tokens 5120 -> 13824
 // 12.2 us (71 MB, 5.8 TB/s: of this size the cache behind the dies holds them between calls), and 3 for the codes.
 template <typename T, typename E, int OP, int TP, int WAVES>
 __global__ __launch_bounds__(WAVES * 64) void shared_depth_kernel(const uint8_t *__restrict__ W,
@@ -291,12 +292,12 @@ __global__ __launch_bounds__(WAVES * 64) void shared_depth_kernel(const uint8_t 
         if (E::kPlain) sw[i] = output_scales(y, o + q / TP * kRows);
     }
     Int4 acc[OP][TP] = {};
-    const int k0 = (int)((int64_t)deep * wave / WAVES), k1 = (int)((int64_t)deep * (wave + 1) / WAVES);
+    const int steps = (deep - wave + WAVES - 1) / WAVES;  // of the wavefront: every WAVES-th, so that they read next to each other
     Int4 a[2][kAhead][OP], b[2][kAhead][TP];
     auto load = [&](int k, int buf) {  // past the last step: that one again, which nothing multiplies
 #pragma unroll
         for (int u = 0; u < kAhead; ++u) {
-            const int at = min(k + u, k1 - 1) * kPiece;
+            const int at = (min(k + u, steps - 1) * WAVES + wave) * kPiece;
 #pragma unroll
             for (int i = 0; i < OP; ++i) a[buf][u][i] = *reinterpret_cast<const Int4 *>(w[i] + at);
 #pragma unroll
@@ -306,7 +307,7 @@ __global__ __launch_bounds__(WAVES * 64) void shared_depth_kernel(const uint8_t 
     auto compute = [&](int k, int buf) {
 #pragma unroll
         for (int u = 0; u < kAhead; ++u) {
-            if (k + u >= k1) break;
+            if (k + u >= steps) break;
 #pragma unroll
             for (int i = 0; i < OP; ++i)
 #pragma unroll
@@ -314,13 +315,13 @@ __global__ __launch_bounds__(WAVES * 64) void shared_depth_kernel(const uint8_t 
         }
     };
     if (!kOverlap) {
-        for (int k = k0; k < k1; k += kAhead) {
+        for (int k = 0; k < steps; k += kAhead) {
             load(k, 0);
             compute(k, 0);
         }
-    } else if (k0 < k1) {
-        load(k0, 0);
-        for (int k = k0; k < k1; k += 2 * kAhead) {
+    } else if (steps > 0) {
+        load(0, 0);
+        for (int k = 0; k < steps; k += 2 * kAhead) {
             load(k + kAhead, 1);
             compute(k, 0);
             load(k + 2 * kAhead, 0);
@@ -359,30 +360,34 @@ __global__ __launch_bounds__(WAVES * 64) void shared_depth_kernel(const uint8_t 
 // than 16384 inputs has no room in registers); 4 tokens 20.5 and 15.4, which is why it ends there.  Small ones are bound by what comes one after the other (the
 // token, its largest, two barriers, the products, the join), large ones by the weights' bytes.
 // Wavefronts, us with 8 and 16: 1 token 5120 -> 13824 13.0 and 15.7, 4096 -> 11008 7.8 and 8.9, but 8192 -> 28672 36.3 and
-// 34.8; gated 5120 -> 2 x 13824 23.9 and 30.5, 8192 -> 2 x 28672 87.7 (8 steps ahead; 93 with 4) and 95, at 5.4 TB/s.
+// 34.8; gated, weights from memory, 5120 -> 2 x 13824 29.8 and 29.6, 8192 -> 2 x 28672 86.6 and 85.0 (5.5 TB/s; loads alone in
+// runs of 128 KB reach 6.2).  A step in turn for each wavefront in place of a run of steps: gated 85.0 and 90, but 8192 -> 28672 42.8
+// and 41.7.
 constexpr int kFewDepth = 16384;
 
 template <typename TX, typename E, int M, int C, int WAVES>  // up to C * 1024 * WAVES inputs
 __global__ __launch_bounds__(WAVES * 64) void few_tokens_kernel(const uint8_t *__restrict__ W, const TX *__restrict__ X,
                                                                     int64_t d, int64_t ldx, int deep, Scaled y, E e, int dtype,
                                                                     int32_t *__restrict__ status) {
-    constexpr int kAhead = E::kGated && WAVES == 8 ? 8 : 4, P = kPerOutput<E>, kMost = C * WAVES * 1024;
+    constexpr int kAhead = 4, P = kPerOutput<E>, kMost = C * WAVES * 1024;
     __shared__ __align__(16) uint8_t codes[M * kMost];
     __shared__ Int4 red[P][WAVES][64];
     __shared__ float most[M][WAVES], scales[M];
     const int lane = threadIdx.x & 63, wave = wave_index(), m = (int)y.m;
     const uint8_t *w = W + (int64_t)blockIdx.x * P * deep * kPiece + lane * 16;
-    const int k0 = deep * wave / WAVES, k1 = deep * (wave + 1) / WAVES;
+    // Steps of the wavefront: gated, every WAVES-th, else a run of them.
+    const int first = E::kGated ? wave : deep * wave / WAVES, apart = E::kGated ? WAVES : 1;
+    const int steps = E::kGated ? (deep - wave + WAVES - 1) / WAVES : deep * (wave + 1) / WAVES - first;
     Int4 a[kAhead][P];
-    // Past the wavefront's share: with 8 wavefronts nothing, where that would be much of its steps; else bytes that nothing
-    // multiplies, which costs less there than to ask.
+    // Past the wavefront's steps: with 8 wavefronts nothing, where that would be much of its loads; else the last bytes again, which
+    // nothing multiplies: that costs less there than to ask.
     constexpr bool kAsk = WAVES == 8;
     auto load = [&](int k) {
-        const bool all = k + kAhead <= k1;
+        const bool all = k + kAhead <= steps;
 #pragma unroll
         for (int u = 0; u < kAhead; ++u) {
-            if (kAsk && !all && k + u >= k1) break;
-            const int at = kAsk ? k + u : min(k + u, deep - 1);
+            if (kAsk && !all && k + u >= steps) break;
+            const int at = min(first + (k + u) * apart, deep - 1);
 #pragma unroll
             for (int p = 0; p < P; ++p) a[u][p] = *reinterpret_cast<const Int4 *>(w + ((int64_t)p * deep + at) * kPiece);
         }
@@ -394,7 +399,7 @@ __global__ __launch_bounds__(WAVES * 64) void few_tokens_kernel(const uint8_t *_
     for (int t = 0; t < M; ++t)
 #pragma unroll
         for (int i = 0; i < C; ++i) x[t][i].load(X + min(t, m - 1) * ldx + chunk(i) * 16, chunk(i) < chunks ? d - chunk(i) * 16 : 0);
-    load(k0);
+    load(0);
     bool bad = false;
 #pragma unroll
     for (int t = 0; t < M; ++t) {
@@ -428,15 +433,15 @@ __global__ __launch_bounds__(WAVES * 64) void few_tokens_kernel(const uint8_t *_
     __syncthreads();
     Int4 acc[P] = {};
     const uint8_t *mine = codes + min(lane & 15, m - 1) * (kMost) + (lane >> 4) * 16;
-    for (int k = k0; k < k1; k += kAhead) {
+    for (int k = 0; k < steps; k += kAhead) {
 #pragma unroll
         for (int u = 0; u < kAhead; ++u) {
-            if (k + u >= k1) break;
-            const Int4 b = *reinterpret_cast<const Int4 *>(mine + (k + u) * kDepth);
+            if (k + u >= steps) break;
+            const Int4 b = *reinterpret_cast<const Int4 *>(mine + (first + (k + u) * apart) * kDepth);
 #pragma unroll
             for (int p = 0; p < P; ++p) acc[p] = multiply(a[u][p], b, acc[p]);
         }
-        if (k + kAhead < k1) load(k + kAhead);
+        if (k + kAhead < steps) load(k + kAhead);
     }
 #pragma unroll
     for (int p = 0; p < P; ++p) red[p][wave][lane] = acc[p];
@@ -742,19 +747,15 @@ void launch_few(const uint8_t *W, const void *X, int64_t d, int64_t ldx, const S
     };
     typedef std::integral_constant<int, 1> One;
     typedef std::integral_constant<int, 2> Two;
-    typedef std::integral_constant<int, 4> Four;
     typedef std::integral_constant<int, 8> Eight;
     typedef std::integral_constant<int, 16> Sixteen;
     if (y.m == 2) {
         if (d <= kFewDepth) run(Two(), One(), Sixteen());
         else if constexpr (!E::kGated) run(Two(), Two(), Sixteen());
-    } else if constexpr (E::kGated) {
-        if (d <= 8192) run(One(), One(), Eight());
-        else if (d <= 16384) run(One(), Two(), Eight());
-        else run(One(), Four(), Eight());
+    } else if (!E::kGated && d <= 6144) {
+        if constexpr (!E::kGated) run(One(), One(), Eight());
     } else {
-        if (d <= 6144) run(One(), One(), Eight());
-        else if (d <= kFewDepth) run(One(), One(), Sixteen());
+        if (d <= kFewDepth) run(One(), One(), Sixteen());
         else run(One(), Two(), Sixteen());
     }
 }
