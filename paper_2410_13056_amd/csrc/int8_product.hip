@@ -515,10 +515,11 @@ __device__ __forceinline__ void finish_rows(const Int4 *sums, const Scaled &y, c
 // are read (no conflicts), BUFS steps of 64 inputs in a ring; while a step is multiplied its operands are in
 // registers, those of the next are on their way from LDS and the steps after it from memory.  Bound by the matrix
 // instructions at 256 x 256: 4096 tokens 8192 -> 28672 in 741 us with the codes (29), 2.6 POP/s, the instructions busy for 69 %
-// of the clocks, the rest at the barrier of a step.  64 x 64: by what a unit's caches deliver, 25 to 35 bytes a clock: 282 tiles
-// of 66 steps of 8 KB (333 tokens 4099 -> 3001) 15.4 us, 9.9 TB/s, 64 x 128 reads three quarters of that in 14.8; more buffers, or
-// steps in another order a workgroup, change nothing.  G groups of wavefronts share the depth, each with a ring of its own; their sums
-// are joined through LDS, in order.  Bands keep the inputs of a die's tiles in its
+// of the clocks; without the barriers 690 in place of 718 us, without the loads 626, without the LDS reads 677.  G groups of
+// wavefronts share the depth, each with a ring of its own; their sums are joined through LDS, in order.  One round of small tiles: 3 us
+// of a launch, 2 to 5 before the first step and behind the last, then 80 to 120 ns a step of 64 x 64 (of 118 bytes a ns that a unit's
+// loads reach 70 to 100), 160 of 64 x 128, 230 of 128 x 128; without loads, without LDS reads or without barriers 0 to 15 % less.
+// More buffers, or steps in another order a workgroup, change nothing.  Bands keep the inputs of a die's tiles in its
 // cache while the weights pass once a band.
 constexpr int kBand = 4;
 
@@ -697,12 +698,15 @@ void launch_pairs(const uint8_t *W, const uint8_t *X, int deep, const Scaled &y,
 // Which kernel: the largest tile that fills the chip.  A tile of 256 x 256 or 256 x 128 takes a compute unit for itself, so
 // its last round has to be two thirds full, or one of many.  us (4096 tokens 8192 -> 28672; 2048 tokens 4096 -> 4096; 1024
 // tokens 4096 -> 4096; 512 tokens 4096 -> 11008): 256 x 256 737, 60, 53, 53; 256 x 128 860, 43.1, 36, 34.8; 128 x 128 901,
-// 44.0, 28, 35.4; 64 x 64 (48 tokens 4096 -> 11008 14.0, 128 x 128 21.3).
-// Up to a tile of 64 x 64 a unit, two groups of wavefronts halve the depth (100 tokens 5120 -> 5120 10.0, one group 11.8; 200
-// tokens 2048 -> 4096 6.6 and 7.2; but 333 tokens 4099 -> 3001, 282 tiles, 17.4 and 15.4: a unit with two tiles is what all wait
-// for).  Beyond, 64 outputs by 128 tokens in two groups, up to a tile a unit (512 tokens 4096 -> 4096 14.2, 64 x 64 15.5; 333 tokens
-// 8192 -> 4096 22 and 25; 400 tokens 6000 -> 3000 17.0 and 19.1; 333 tokens 4099 -> 3001 14.8 and 15.4), else 64 x 64 (150 tokens
-// 4096 -> 11008 20.2, 64 x 128 23.5).  Fewer than 150 tiles of 64 x 64, and up to 32 tokens: wavefronts share the depth (512 tokens
+// 44.0, 28, 35.4.
+// Where 128 x 128 would be no more than one a unit: the smallest tile that is still at most one a unit, since the unit with most
+// tiles is what all wait for, its depth shared by two or three groups of wavefronts, since one group alone keeps neither the
+// matrix instructions nor the loads busy.  us of a round of each at a depth of 4096: 64 x 64 9, 96 x 48 10.9, 64 x 128 and 128 x 64
+// 13.5, 96 x 96 14.8, 128 x 128 18 to 20, two rounds 17, 21, ...  Groups against one: 100 tokens 5120 -> 5120 10.0 and 11.8, 128 x 128:
+// 700 tokens 4096 -> 4096 19.0 and 20.4, 200 tokens 2048 -> 13824 14.2 and 15.6.  One round against two of a smaller: 333 tokens 4099 -> 3001
+// 96 x 48 12.9, 64 x 128 14.8, 64 x 64 15.4; 150 tokens 4096 -> 11008 96 x 96 14.7, 64 x 64 19.4; 64 tokens 5120 -> 28672 128 x 64 25.7,
+// 128 x 128 28.2; 400 tokens 8192 -> 5120 128 x 128 28.4, 64 x 64 34.8 (but 1000 tokens 2048 -> 2560 12.6 and 12.1).
+// Fewer than 150 tiles of 64 x 64, and up to 32 tokens: wavefronts share the depth (512 tokens
 // 8192 -> 1024 18.6, 64 x 64 23.0; 64 tokens 4096 -> 4096 9.4, 12.3).  Up to 16 tokens: two pieces of outputs a workgroup where there
 // are many (16 tokens 5120 -> 13824 16.0, one piece 17.9), one by 8 wavefronts for some (8192 -> 10240, weights from memory, 19.6, two
 // by 16 23.2), two by 16 where they are a round of the units (13824 -> 5120 18.0, one by 8 20.1: its units read the tokens twice as
@@ -720,11 +724,14 @@ int launch_product(const uint8_t *W, const uint8_t *X, int deep, const Scaled &y
     else if (y.m <= 32) launch_pairs<T, E>(W, X, deep, y, e, st);
     else if (fills(tiles_of<E>(y, 16, 16))) launch_tiles<T, E, 16, 16, 4, 2, 1, 4>(W, X, deep, y, e, st);
     else if (fills(tiles_of<E>(y, 16, 8))) launch_tiles<T, E, 16, 8, 4, 2, 1, 4>(W, X, deep, y, e, st);
-    else if (tiles_of<E>(y, 8, 8) >= 192) launch_tiles<T, E, 8, 8, 2, 2, 1, 4>(W, X, deep, y, e, st);
+    else if (tiles_of<E>(y, 8, 8) > kUnits) launch_tiles<T, E, 8, 8, 2, 2, 1, 4>(W, X, deep, y, e, st);
     else if (tiles_of<E>(y, 4, 4) < 150) launch_pairs<T, E>(W, X, deep, y, e, st);
     else if (tiles_of<E>(y, 4, 4) <= kUnits) launch_tiles<T, E, 4, 4, 2, 2, 2, 4>(W, X, deep, y, e, st);
+    else if (tiles_of<E>(y, 6, 3) <= kUnits) launch_tiles<T, E, 6, 3, 3, 1, 3, 4>(W, X, deep, y, e, st);
     else if (tiles_of<E>(y, 4, 8) <= kUnits) launch_tiles<T, E, 4, 8, 2, 2, 2, 4>(W, X, deep, y, e, st);
-    else launch_tiles<T, E, 4, 4, 2, 2, 1, 4>(W, X, deep, y, e, st);
+    else if (tiles_of<E>(y, 8, 4) <= kUnits) launch_tiles<T, E, 8, 4, 2, 2, 2, 4>(W, X, deep, y, e, st);
+    else if (tiles_of<E>(y, 6, 6) <= kUnits) launch_tiles<T, E, 6, 6, 3, 1, 3, 4>(W, X, deep, y, e, st);
+    else launch_tiles<T, E, 8, 8, 2, 2, 2, 4>(W, X, deep, y, e, st);
     CMPQ_LAUNCH_CHECK();
     return CMPQ_OK;
 }

@@ -1,5 +1,5 @@
-"""Sizes that launch the products in which groups of wavefronts share the depth - 64 x 64 and 64 x 128 tiles, two pieces by two - with
-depths that leave a group little or nothing, plain, with an epilogue and gated; and tokens that are coded within the one launch.  Exact sums:
+"""Sizes that launch the products in which groups of wavefronts share the depth - tiles of 64 x 64 to 128 x 128 in two and three
+groups, two pieces by two - with depths that leave a group little or nothing, plain, with an epilogue and gated; and tokens that are coded within the one launch.  Exact sums:
 the plain outputs are bit for bit those of the codes."""
 import pytest
 import torch
@@ -19,7 +19,11 @@ SIZES = [(700, d, 1000) for d in (1, 128, 129, 256, 300, 1000)] + [(100, 5120, 5
          (2, 30000, 4200), (16, 700, 5130), (13, 1000, 8192), (16, 200, 8200)]
 
 
-@pytest.mark.parametrize("m,d_in,d_out", SIZES)
+ROUNDS = [(m, d, n) for m, n in [(330, 3000), (50, 16500), (145, 11001), (700, 4000), (690, 4003)] for d in (1, 129, 300, 515, 1100)] + \
+         [(333, 4099, 3001), (96, 2000, 8200), (64, 1000, 28600), (400, 1000, 5003)]
+
+
+@pytest.mark.parametrize("m,d_in,d_out", SIZES + ROUNDS)
 def test_products(S, m, d_in, d_out):  # noqa: F811
     k = m + d_in + d_out
     X = T._randn(k, m, d_in, dtype=T.TYPES[k % 3], scale=3)
@@ -32,6 +36,15 @@ def test_products(S, m, d_in, d_out):  # noqa: F811
     if d_out > 1000:
         half = [W[:(d_out + 1) // 2] for W in Ws]
         T._gated(S, X, *half, gate_bias=b[:(d_out + 1) // 2], out_dtype=torch.float32)
+
+
+def test_one_row_in_every_tile(S):  # noqa: F811
+    """As below, by the tiles that take a round of the units."""
+    X, W = T._randn(1, 1000, 1000, dtype=torch.float16), T._randn(2, 11008, 1000, dtype=torch.float16)
+    w = S.prepare_int8(W)
+    whole = S.int8_product(w, X, T._ws(), out_dtype=torch.float32)
+    for n in (40, 64, 96, 144, 150, 200, 256):
+        assert torch.equal(S.int8_product(w, X[:n], T._ws(), out_dtype=torch.float32), whole[:n]), n
 
 
 def test_groups_add_up_to_the_same_sums(S):  # noqa: F811
