@@ -651,7 +651,8 @@ int cmpq_int8_prepare(const void *W, int dtype, int64_t d_out, int64_t d_in, int
 /*
  * Y[t,o] = (sum_i cx[t,i] * cw[o,i]) * sx[t] * sw[o]: X [m, d_in] (ldx) is coded with a scale per token on the
  * way, the sum is exact, its fp32 value is multiplied by the smaller scale, then by the larger (so that nothing
- * on the way leaves the range that the result is in), and rounded once more to y_dtype.  Y [m, d_out] (ldy).
+ * on the way leaves the range that the result is in), and rounded once more to y_dtype (FP16: the last multiplication and
+ * this rounding are one).  Y [m, d_out] (ldy).
  * codes, scale: from cmpq_int8_prepare.
  * Workspace: CMPQ_OP_INT8_PRODUCT with n = m.  Limits: m < 2^24 and those of cmpq_int8_prepare.
  */

@@ -54,3 +54,23 @@ def test_groups_add_up_to_the_same_sums(S):  # noqa: F811
     whole = S.int8_product(w, X, T._ws(), out_dtype=torch.float32)
     for n in (1, 2, 10, 30, 64, 200, 300, 333, 500):
         assert torch.equal(S.int8_product(w, X[:n], T._ws(), out_dtype=torch.float32), whole[:n]), n
+
+
+@pytest.mark.parametrize("out", T.TYPES)
+@pytest.mark.parametrize("m,d_out", [(700, 3000), (330, 3001), (2100, 4100), (100, 300)])
+def test_outputs_at_any_address(S, m, d_out, out):  # noqa: F811
+    """Outputs that cannot be written four at once are the bits of those that can, and nothing beside them is written.  (Those of
+    FP16 are not the ones in 32 bits rounded: their last multiplication and its rounding to FP16 are one.)"""
+    X, W = T._randn(m, m, 300, dtype=torch.float16), T._randn(d_out, d_out, 300, dtype=torch.float16)
+    w = S.prepare_int8(W)
+    want = torch.empty((m, (d_out + 3) // 4 * 4), dtype=out, device=DEV)[:, :d_out]
+    S.int8_product(w, X, T._ws(), out=want)
+    exact = S.int8_product(w, X, T._ws(), out_dtype=torch.float32)
+    assert ((want.double() - exact.double()).abs() <= exact.abs().double() * torch.finfo(out).eps / 2 * (1 + 2.0 ** -9) + 2.0 ** -24).all()
+    for columns, first in [(d_out + 1, 0), (d_out + 1, 1), (d_out + 6, 3), (d_out + 8 - d_out % 4, 4)]:
+        room = torch.full((m, columns), -7.0, dtype=out, device=DEV)
+        place = room[:, first:first + d_out]
+        S.int8_product(w, X, T._ws(), out=place)
+        assert torch.equal(place, want)
+        place.fill_(-7.0)
+        assert torch.equal(room, torch.full_like(room, -7.0))
