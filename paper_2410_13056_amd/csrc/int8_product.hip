@@ -51,27 +51,29 @@ struct Turn {
     int of, at;
 };
 
-// One workgroup a row: its largest magnitude, then its codes, 16 inputs a lane and step.  Rows of up to KEPT * THREADS * 16
-// inputs stay in registers between the two, longer ones are read again.  The rows of a piece write 16 bytes each
-// of the same lines, so consecutive rows go to one die, whose cache puts the lines together.  Bound by bytes where rows are
-// many: 4096 rows of 8192 in FP16 29 us, 3.5 TB/s (three quarters of a copy's rate; vector instructions 38 %); by a row's latency
-// where they are few: 333 rows 4 us.  Long rows where there are few of them take 16 wavefronts in place of 4: 1 row of 28672 5.1
-// us and 6.3, 16 of 13824 4.7 and 5.2, but 1 of 8192 4.1 and 3.6, 700 of 13824 9.9 and 8.4; 2048 of 28672 33 us kept, 45 read twice.
-template <typename T, int THREADS, int KEPT>
-__global__ __launch_bounds__(THREADS) void code_rows_kernel(const T *__restrict__ X, int64_t n, int64_t d, int64_t ld,
+// One row a workgroup, or four in turn from lane to lane: the row's largest magnitude, then its codes, 16 inputs a lane and step.
+// Rows of up to KEPT * THREADS / ROWS * 16 inputs stay in registers between the two, longer ones are read again.  Rows from n to
+// `all` are zeros.
+//
+// The rows of a piece write 16 bytes each of the same lines, so consecutive rows go to one die, whose cache puts the lines together.
+// Bound by bytes where rows are many, and then by the number of runs that the stores come in (one of 1 KB each in place of 64 of 16
+// bytes: 38 us where it is 47 for 2048 rows of 28672): four rows together write 64 bytes in order.  4096 rows of 8192 from memory 26 us, 3.9
+// TB/s, one by one 29.8, 2048 of 13824 22.1 and 26.8; from the cache behind the dies the same, and fewer rows are better off one by one, 1280
+// of 8192 7.2 and 8.9.  Bound by a row's latency where they are few: 333 rows 4 us.  Long rows take 16 wavefronts in place of 4: 2048 of
+// 28672 from memory 47 us and 55 (34 and 32 from the cache), 300 of 28672 8.0 and 8.5, 1 of 28672 5.1 and 6.3, 16 of 13824 4.7 and 5.2,
+// but 1 of 8192 4.1 and 3.6, 700 of 13824 9.9 and 8.4.
+template <typename T, int THREADS, int KEPT, int ROWS>
+__global__ __launch_bounds__(THREADS) void code_rows_kernel(const T *__restrict__ X, int64_t n, int64_t all, int64_t d, int64_t ld,
                                                         int8_t *__restrict__ codes, float *__restrict__ scale, Turn turn,
                                                         int32_t *__restrict__ status) {
-    __shared__ float scratch[THREADS / 64];
-    const int64_t row = die_order(blockIdx.x, gridDim.x), deep = pieces_deep(d), group = row / kRows * turn.of + turn.at;
+    constexpr int kLanes = THREADS / ROWS;  // of a row
+    static_assert(ROWS == 1 || (ROWS == 4 && THREADS == 1024), "what four_rows_max joins");
+    __shared__ float scratch[THREADS / 64 * ROWS];
+    const int64_t row = die_order(blockIdx.x, gridDim.x) * ROWS + threadIdx.x % ROWS, deep = pieces_deep(d);
+    const int64_t group = row / kRows * turn.of + turn.at;
+    const int first = threadIdx.x / ROWS, groups = row < all ? (int)deep * 4 : 0;
+    const int64_t valid = row < n ? d : 0;
     uint8_t *out = reinterpret_cast<uint8_t *>(codes) + group * deep * kPiece + row % kRows * 16;
-    const int groups = (int)deep * 4;
-    scale += group * kRows + row % kRows;
-    if (row >= n) {  // rows that fill up the last piece
-        if (turn.of > 1 && threadIdx.x == 0) *scale = 0.f;
-        for (int c = threadIdx.x; c < groups; c += THREADS)
-            *reinterpret_cast<uint4 *>(out + c / 4 * kPiece + c % 4 * 256) = make_uint4(0, 0, 0, 0);
-        return;
-    }
     const T *x = X + row * ld;
     Largest largest;
     Sixteen<T> kept[KEPT > 0 ? KEPT : 1];
@@ -79,10 +81,10 @@ __global__ __launch_bounds__(THREADS) void code_rows_kernel(const T *__restrict_
         if (KEPT > 0) {
 #pragma unroll
             for (int k = 0; k < KEPT; ++k)
-                if ((int)threadIdx.x + k * THREADS < groups) fn(kept[k], (int)threadIdx.x + k * THREADS);
+                if (first + k * kLanes < groups) fn(kept[k], first + k * kLanes);
         } else {
-            for (int c = threadIdx.x; c < groups; c += THREADS) {
-                kept[0].load(x + c * 16, d - c * 16);
+            for (int c = first; c < groups; c += kLanes) {
+                kept[0].load(x + c * 16, valid - c * 16);
                 fn(kept[0], c);
             }
         }
@@ -90,8 +92,8 @@ __global__ __launch_bounds__(THREADS) void code_rows_kernel(const T *__restrict_
     if (KEPT > 0) {
 #pragma unroll
         for (int k = 0; k < KEPT; ++k) {
-            const int c = threadIdx.x + k * THREADS;
-            kept[k].load(x + c * 16, c < groups ? d - c * 16 : 0);
+            const int c = first + k * kLanes;
+            kept[k].load(x + c * 16, c < groups ? valid - c * 16 : 0);
         }
     }
     each([&](const Sixteen<T> &s, int) { s.look(largest); });
@@ -101,8 +103,14 @@ __global__ __launch_bounds__(THREADS) void code_rows_kernel(const T *__restrict_
         each([&](const Sixteen<T> &s, int) { s.look_again(largest); });
         if (status) atomicOr(status, CMPQ_STATUS_NONFINITE);
     }
-    const float s = code_scale(block_max(largest.most(), scratch)), inv = 1.f / s;
-    if (threadIdx.x == 0) *scale = s;
+    float most;
+    if constexpr (ROWS == 1) most = block_max(largest.most(), scratch);
+    else most = four_rows_max(largest.most(), scratch);
+    const float s = code_scale(most), inv = 1.f / s;
+    if (first == 0 && row < all) {
+        if (row < n) scale[group * kRows + row % kRows] = s;
+        else if (turn.of > 1) scale[group * kRows + row % kRows] = 0.f;
+    }
     auto put = [&](const Sixteen<T> &s, int c, bool clean) {
         *reinterpret_cast<uint4 *>(out + c / 4 * kPiece + c % 4 * 256) = s.codes(inv, clean);
     };
@@ -116,21 +124,25 @@ using Kept = std::integral_constant<int, N>;
 template <typename T>
 void launch_code_rows(const void *X, int64_t n, int64_t d, int64_t ld, int64_t rows, int8_t *codes, float *scale,
                       Turn turn, int32_t *status, hipStream_t st) {
-    const dim3 grid((unsigned)rows);
     const T *x = static_cast<const T *>(X);
-    const auto run = [&](auto threads, auto kept) {
-        code_rows_kernel<T, threads(), kept()><<<grid, threads(), 0, st>>>(x, n, d, ld, codes, scale, turn, status);
+    const auto run = [&](auto threads, auto kept, auto together) {
+        const dim3 grid((unsigned)cdiv(rows, together()));
+        code_rows_kernel<T, threads(), kept(), together()><<<grid, threads(), 0, st>>>(x, n, rows, d, ld, codes, scale, turn, status);
     };
     typedef std::integral_constant<int, 256> Four;  // wavefronts
     typedef std::integral_constant<int, 1024> Many;
-    const bool few = rows <= 256;
-    if (d <= 4096) run(Four(), Kept<1>());
-    else if (d <= 8192) run(Four(), Kept<2>());
-    else if (d <= 16384 && few) run(Many(), Kept<1>());
-    else if (d <= 32768 && few) run(Many(), Kept<2>());
-    else if (d <= 16384) run(Four(), Kept<4>());
-    else if (d <= 32768) run(Four(), Kept<8>());
-    else run(Four(), Kept<0>());
+    typedef std::integral_constant<int, 1> One;  // row
+    typedef std::integral_constant<int, 4> Rows;
+    const bool few = rows <= 256, many = rows >= 2048;
+    if (d <= 4096 && many) run(Many(), Kept<1>(), Rows());
+    else if (d <= 4096) run(Four(), Kept<1>(), One());
+    else if (d <= 8192 && many) run(Many(), Kept<2>(), Rows());
+    else if (d <= 8192) run(Four(), Kept<2>(), One());
+    else if (d <= 16384 && many) run(Many(), Kept<4>(), Rows());
+    else if (d <= 16384 && few) run(Many(), Kept<1>(), One());
+    else if (d <= 16384) run(Four(), Kept<4>(), One());
+    else if (d <= 32768) run(Many(), Kept<2>(), One());
+    else run(Four(), Kept<0>(), One());
 }
 
 // `rows` of them, those from n on zeros.

@@ -88,6 +88,23 @@ __device__ __forceinline__ float block_max(float value, float *scratch) {
     return __uint_as_float(row_max(w < (int)(blockDim.x >> 6) ? __float_as_uint(scratch[w]) : 0));
 }
 
+// The same of four rows that lie in turn from lane to lane of 16 wavefronts.  `scratch`: 64 floats.
+__device__ __forceinline__ float four_rows_max(float value, float *scratch) {
+    const auto join = [](uint32_t v) {
+        v = max(v, row_turn<8>(v));
+        v = max(v, row_turn<4>(v));
+        const auto halves = __builtin_amdgcn_permlane32_swap(v, v, false, false);
+        v = max(halves[0], halves[1]);
+        const auto rows = __builtin_amdgcn_permlane16_swap(v, v, false, false);
+        return max(rows[0], rows[1]);
+    };
+    const uint32_t v = join(__float_as_uint(value));
+    const int lane = threadIdx.x & 63;
+    if (lane < 4) scratch[(threadIdx.x >> 6) * 4 + lane] = __uint_as_float(v);
+    __syncthreads();
+    return __uint_as_float(join(__float_as_uint(scratch[lane])));  // a wavefront's four, then the next one's
+}
+
 // The two results of the turn by position.  Products and sums are rounded one by one, as the header says.
 __device__ __forceinline__ float turned_first(float a, float b, float c, float s) {
 #pragma clang fp contract(off)

@@ -74,3 +74,22 @@ def test_outputs_at_any_address(S, m, d_out, out):  # noqa: F811
         assert torch.equal(place, want)
         place.fill_(-7.0)
         assert torch.equal(room, torch.full_like(room, -7.0))
+
+
+@pytest.mark.parametrize("kind", T.TYPES)
+@pytest.mark.parametrize("m,d", [(2048, 4096), (2051, 130), (2050, 4097), (2100, 8190), (2065, 16384), (2049, 9001), (2047, 700), (300, 16385), (2048, 20000)])
+def test_many_rows_are_coded_as_few(S, m, d, kind):  # noqa: F811
+    """Codes, scales and flags of a row do not depend on the number of rows, and a row that is not finite is none of its neighbours' matter."""
+    X = T._randn(m + d, m, d, dtype=kind, scale=5)
+    X[5, d // 2], X[6, 0], X[m - 1, d - 1], X[9] = float("inf"), float("nan"), -float("inf"), 0
+    X = torch.cat([X, X], 1)[:, 1:d + 1] if d % 2 else X
+    status = torch.zeros(1, dtype=torch.int32, device=DEV)
+    rows = S.int8_rows(X, status=status)
+    pieces = rows.codes.view(-1, rows.codes.numel() // ((m + 15) // 16))
+    assert status.item()
+    for i in [0, 16 * (m // 32), (m - 1) // 16 * 16]:
+        some = S.int8_rows(X[i:i + 16])
+        assert torch.equal(some.codes, pieces[i // 16]) and torch.equal(some.scale, rows.scale[i:i + 16])
+    status.zero_()
+    S.int8_rows(X[16:m - 16], status=status)
+    assert not status.item()
