@@ -579,7 +579,8 @@ class LutMatvecCall:
 class LutMatvecGroupCall:
     """``cmpq_lut_matvec_group`` (``cmpq_lut_matvec_group_fp16acc`` with `fp16acc`) for a fixed set
     of deployed layers (`LutMatvecCall` objects): the array of layer descriptions is built once; a
-    call fills in inputs and outputs."""
+    call fills in inputs and outputs in a copy of its own, since other threads may be in calls of the
+    same group."""
 
     def __init__(self, calls: Sequence[LutMatvecCall], fp16acc: bool = False):
         if not 1 <= len(calls) <= MAX_GROUP:
@@ -592,6 +593,7 @@ class LutMatvecGroupCall:
             L.bit_set, L.counts_host = ctypes.addressof(bs), ctypes.addressof(cn)
             L.packed, L.chan_idx, L.lut = ctypes.addressof(pk), ctypes.addressof(ci), ctypes.addressof(lt)
             L.act_idx, L.W_act, L.colptr, L.row_idx, L.delta = act_idx, W_act, colptr, row_idx, delta
+        self._free = []                 # copies of the array that no call has at the moment
         self._ws_bytes = {}
         self._fn = lib().cmpq_lut_matvec_group_fp16acc if fp16acc else lib().cmpq_lut_matvec_group
 
@@ -599,7 +601,11 @@ class LutMatvecGroupCall:
         if len(Xs) != len(self._calls) or len(Ys) != len(self._calls):
             raise ValueError("one input and one output per layer")
         m = Xs[0].shape[0]
-        for L, c, X, Y in zip(self._arr, self._calls, Xs, Ys):
+        try:                            # a list's pop and append are one step each
+            arr = self._free.pop()
+        except IndexError:
+            arr = type(self._arr).from_buffer_copy(self._arr)
+        for L, c, X, Y in zip(arr, self._calls, Xs, Ys):
             if X.dtype != torch.float16 or Y.dtype != torch.float32:
                 raise ValueError("X must be fp16 and Y fp32")
             mx, d_in, ldx = _rows(X)
@@ -611,7 +617,8 @@ class LutMatvecGroupCall:
         if need is None:
             need = self._ws_bytes[m] = sum(workspace_bytes(OP_LUT_MATVEC, c.d_in, c.d_out, m) for c in self._calls)
         buf = ws.get(need)
-        rc = self._fn(self._arr, len(self._calls), m, buf.data_ptr(), buf.numel(), _stream())
+        rc = self._fn(arr, len(self._calls), m, buf.data_ptr(), buf.numel(), _stream())
+        self._free.append(arr)
         if rc:
             _check(rc, "cmpq_lut_matvec_group")
 
