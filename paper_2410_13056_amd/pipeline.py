@@ -440,6 +440,10 @@ class Deployed:
     delta: torch.Tensor               # [k_q] fp32: outlier value minus the table level it overrides
     _call: Optional[B.LutMatvecCall] = None
 
+    def __getstate__(self):
+        """Copies marshal their own arguments: these are addresses of this layer's tensors."""
+        return {**self.__dict__, "_call": None}
+
     def call(self) -> B.LutMatvecCall:
         """The layer's fixed call arguments, marshalled at the first use."""
         if self._call is None:

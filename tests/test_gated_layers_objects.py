@@ -76,3 +76,19 @@ def test_calls_one_after_the_other_and_refused_ones(S, monkeypatch):  # noqa: F8
             group([X, X[:, :60]], Y, _Workspace())
         group([X, X], Y, _Workspace())
         assert seen.pop() == ([(X.data_ptr(), 70 if rows > 1 else 64, y.data_ptr(), y.shape[1]) for y in Y], [24, 16]) and not seen
+
+
+def test_copies_are_copies(S):  # noqa: F811
+    import copy
+    import pickle
+    layers = S.GatedLayers(_deployed(), _deployed())
+    for other in (copy.deepcopy(layers), pickle.loads(pickle.dumps(layers))):
+        for a, b in ((layers.gate, other.gate), (layers.up, other.up)):
+            assert torch.equal(a.act_idx, b.act_idx) and a.act_idx.data_ptr() != b.act_idx.data_ptr()
+            assert b.call() is not a.call() and b.call()._head[7] == b.act_idx.data_ptr()
+        assert other._args is not layers._args and other._args._arr[1].act_idx == other.up.act_idx.data_ptr()
+    shallow = copy.copy(layers)
+    assert shallow.gate is layers.gate and shallow._args is not layers._args
+    one = copy.copy(layers.gate)
+    one.act_idx = one.act_idx.clone()                        # a copy's calls read what its fields say
+    assert one.call()._head[7] == one.act_idx.data_ptr() != layers.gate.call()._head[7]
