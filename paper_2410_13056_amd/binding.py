@@ -735,6 +735,12 @@ def _not_here(t: torch.Tensor):
     return ValueError("tensors must be on the current device" if t.is_cuda else "cmpq entry points take device tensors")
 
 
+def _all_here(dev: int, *tensors: Optional[torch.Tensor]) -> None:
+    for t in tensors:
+        if t is not None and t.get_device() != dev:
+            raise _not_here(t)
+
+
 def _matrix(t: torch.Tensor, m: int, d: int, dev: int, what: str):
     """(address, leading dimension, type) of a [m, d] tensor whose rows are contiguous: a `cmpq_rows`."""
     if t.shape != (m, d):
@@ -806,8 +812,9 @@ def int8_prepare(W: torch.Tensor, codes: torch.Tensor, scale: torch.Tensor,
         raise ValueError("codes must be contiguous int8 of int8_weight_bytes(d_out, d_in)")
     if scale.dtype != torch.float32 or not scale.is_contiguous() or scale.numel() != d_out:
         raise ValueError("scale must be contiguous float32 [d_out]")
-    _check(lib().cmpq_int8_prepare(_ptr(W), serving_dtype(W.dtype), d_out, d_in, ldw, _ptr(codes), _ptr(scale),
-                                   _ptr(status), _stream()), "cmpq_int8_prepare")
+    w, c, s = _ptr(W), _ptr(codes), _ptr(scale)
+    _all_here(_device(), W, codes, scale, status)
+    _check(lib().cmpq_int8_prepare(w, serving_dtype(W.dtype), d_out, d_in, ldw, c, s, _ptr(status), _stream()), "cmpq_int8_prepare")
 
 
 def int8_gated_rows(d_out: int) -> int:
@@ -844,6 +851,7 @@ class Int8RowsView:
 
     def __init__(self, rows: int, dim: int, codes: torch.Tensor, scale: torch.Tensor):
         _int8_operand(codes, scale, rows, dim)
+        _all_here(codes.get_device(), scale)
         self.rows, self.dim, self.codes, self.scale, self.device = rows, dim, _ptr(codes), _ptr(scale), codes.get_device()
         self.keep = (codes, scale)
 
@@ -866,6 +874,7 @@ class Int8ProductCall:
             raise ValueError("codes must be contiguous int8 of int8_weight_bytes(d_out, d_in)")
         if scale.dtype != torch.float32 or not scale.is_contiguous() or scale.numel() != rows:
             raise ValueError("scale must be contiguous float32 [d_out]")
+        _all_here(codes.get_device(), scale)
         self._keep = (codes, scale)
         self.d_in, self.d_out, self._codes, self._scale = int(d_in), int(d_out), _ptr(codes), _ptr(scale)
         self._gated, self._fn, self._device = int(bool(gated)), lib().cmpq_int8_product, codes.get_device()
@@ -907,6 +916,10 @@ class Int8ProductCall:
         if my != m or d_in != self.d_in or d_out != self.d_out:
             raise ValueError("X must be [m, d_in] and Y [m, d_out] of the prepared weight")
         x, xt, y, yt = _ptr(X), serving_dtype(X.dtype), _ptr(Y), serving_dtype(Y.dtype)
+        dev = _device()
+        _all_here(dev, X, Y, status)
+        if self._device != dev or ws.buf.get_device() != dev:
+            raise ValueError("layers, rows in 8 bits and workspaces must be on the current device")
         for _ in range(2):          # asks for the workspace's size only where what is there does not do
             buf = ws.buf
             rc = self._fn(x, xt, m, d_in, ldx, self._codes, self._scale, d_out, y, yt, ldy, buf.data_ptr(), buf.numel(),
