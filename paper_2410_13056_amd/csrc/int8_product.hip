@@ -832,6 +832,7 @@ Work carve(void *ws, int64_t m, int64_t d_in) {
 }
 
 bool sizes_fit(int64_t d_in, int64_t d_out) { return d_in <= kMostDepth && d_out < (1 << 24); }
+bool gated_sizes_fit(int64_t d_in, int64_t d_out) { return d_in <= kMostDepth && d_out < (1 << 23); }
 
 // What every form of the product is asked for.
 struct Asked {
@@ -902,7 +903,7 @@ extern "C" int cmpq_int8_prepare_gated(const void *gate, const void *up, int dty
     if (d_out < 0 || d_in < 0 || !serving_dtype(dtype)) return CMPQ_EINVAL;
     if (d_out == 0 || d_in == 0) return CMPQ_OK;
     if (!gate || !up || !codes || !scale || !aligned16(codes)) return CMPQ_EINVAL;
-    if (ld_gate < d_in || ld_up < d_in || !sizes_fit(d_in, 2 * d_out)) return CMPQ_ESHAPE;
+    if (ld_gate < d_in || ld_up < d_in || !gated_sizes_fit(d_in, d_out)) return CMPQ_ESHAPE;
     const int64_t rows = cdiv(d_out, kRows) * kRows;
     hipStream_t st = static_cast<hipStream_t>(stream);
     if (int rc = launch_code_rows_of(gate, dtype, d_out, d_in, ld_gate, rows, codes, scale, {2, 0}, status, st)) return rc;
@@ -931,7 +932,7 @@ int cmpq_check_int8_product(const cmpq_int8_job *j) {
     if (!j->codes || !j->scale || !j->Y || !aligned16(j->codes)) return CMPQ_EINVAL;
     if (!j->X && (!j->x_codes || !j->x_scale || !aligned16(j->x_codes))) return CMPQ_EINVAL;
     if ((j->X && j->ldx < j->d_in) || j->ldy < j->d_out || (j->residual && j->ldr < j->d_out)) return CMPQ_ESHAPE;
-    if (j->m >= (1 << 24) || !sizes_fit(j->d_in, j->gated ? 2 * j->d_out : j->d_out)) return CMPQ_ESHAPE;
+    if (j->m >= (1 << 24) || !(j->gated ? gated_sizes_fit : sizes_fit)(j->d_in, j->d_out)) return CMPQ_ESHAPE;
     return CMPQ_OK;
 }
 
