@@ -126,8 +126,11 @@ void launch_code_rows(const void *X, int64_t n, int64_t d, int64_t ld, int64_t r
                       Turn turn, int32_t *status, hipStream_t st) {
     const T *x = static_cast<const T *>(X);
     const auto run = [&](auto threads, auto kept, auto together) {
-        const dim3 grid((unsigned)cdiv(rows, together()));
-        code_rows_kernel<T, threads(), kept(), together()><<<grid, threads(), 0, st>>>(x, n, rows, d, ld, codes, scale, turn, status);
+        for (int64_t at = 0; at < rows; at += kRowsOfLaunch) {
+            const int64_t here = rows - at < kRowsOfLaunch ? rows - at : kRowsOfLaunch;
+            code_rows_kernel<T, threads(), kept(), together()><<<dim3((unsigned)cdiv(here, together())), threads(), 0, st>>>(
+                x + at * ld, n - at, here, d, ld, codes + at / kRows * turn.of * pieces_deep(d) * kPiece, scale + at * turn.of, turn, status);
+        }
     };
     typedef std::integral_constant<int, 256> Four;  // wavefronts
     typedef std::integral_constant<int, 1024> Many;

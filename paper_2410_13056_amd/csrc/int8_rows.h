@@ -7,6 +7,9 @@
 
 constexpr int kRows = 16, kDepth = 64, kPiece = kRows * kDepth;  // a piece
 constexpr int64_t kMostDepth = 131072;                            // 127 * 127 * d_in < 2^31
+// Rows that one launch takes, up to 1024 lanes each: of 2^32 lanes or more HIP launches what 32 bits hold of the number, as a rule
+// without an error.
+constexpr int64_t kRowsOfLaunch = 1 << 21;
 
 // The host's checks of cmpq_rms_norm and cmpq_int8_product_job (but for its workspace), for calls that make several of these.
 int cmpq_check_rms_norm(const cmpq_norm_job *job);

@@ -174,8 +174,15 @@ __global__ __launch_bounds__(THREADS) void rms_norm_kernel(cmpq_norm_job a, doub
 
 template <int THREADS, int KEPT, bool CODED, int TYPE>
 void run(const cmpq_norm_job &a, hipStream_t st) {
-    const int64_t rows = CODED ? cdiv(a.m, kRows) * kRows : a.m;
-    rms_norm_kernel<THREADS, KEPT, CODED, TYPE><<<dim3((unsigned)rows), THREADS, 0, st>>>(a, 1.0 / (double)a.d);
+    for (int64_t at = 0; at < a.m; at += kRowsOfLaunch) {
+        cmpq_norm_job part = a;
+        part.m = a.m - at < kRowsOfLaunch ? a.m - at : kRowsOfLaunch;
+        for (cmpq_rows *r : {&part.X, &part.add, &part.S, &part.Y})
+            if (r->ptr) r->ptr = static_cast<char *>(r->ptr) + at * r->ld * (int64_t)dtype_bytes(r->dtype);
+        if (CODED) part.codes += at / kRows * pieces_deep(a.d) * kPiece, part.scale += at;
+        const int64_t rows = CODED ? cdiv(part.m, kRows) * kRows : part.m;
+        rms_norm_kernel<THREADS, KEPT, CODED, TYPE><<<dim3((unsigned)rows), THREADS, 0, st>>>(part, 1.0 / (double)a.d);
+    }
 }
 
 // Sixteen wavefronts a row where it is longer than four of them hold in two steps: us with 16 and 4, 1 row of 8192 with its sum
