@@ -843,14 +843,15 @@ typedef struct cmpq_heads {
  *   codes of the tokens before these in the page become rint(code * (scale * (1 / scale')));
  *   the new ones are coded with scale'.
  * A page is given to one sequence alone while tokens are appended to it.  K and V may be views of one tensor.
- * No workspace.  Status: CMPQ_STATUS_NONFINITE, CMPQ_STATUS_RANGE.
+ * No workspace.  Limits: min(n_rows, n_rows / page + 2 n_seq) below 2^24.  Status: CMPQ_STATUS_NONFINITE, CMPQ_STATUS_RANGE.
  */
 int cmpq_kv_append(const cmpq_kv_cache *cache, const cmpq_kv_rows *rows, const cmpq_heads *K, const cmpq_heads *V,
                    int dtype, const cmpq_rotation *rotation, int32_t *status, void *stream);
 
 /*
  * The values that tokens of the cache stand for, code * scale rounded once to `dtype`, into K and V
- * [n_rows, kv_heads, head_dim].  Rows that are left out (see cmpq_kv_rows) are not written.  No workspace.
+ * [n_rows, kv_heads, head_dim].  Rows that are left out (see cmpq_kv_rows) are not written.  No workspace.  Limits: those of
+ * cmpq_kv_append.
  */
 int cmpq_kv_read(const cmpq_kv_cache *cache, const cmpq_kv_rows *rows, const cmpq_heads *K, const cmpq_heads *V,
                  int dtype, int32_t *status, void *stream);
@@ -873,7 +874,9 @@ int cmpq_kv_read(const cmpq_kv_cache *cache, const cmpq_kv_rows *rows, const cmp
  * the host bounds alone: results are reproducible bit for bit, and a row's do not depend on the other rows' queries.
  * Workspace: cmpq_kv_attention_workspace(job) (a function of the sizes, not of the pointers; 0 where they are refused).
  * Limits: max_rows, ld_table and n_seq below 2^31, max_length below 2^31 - 32, q_heads <= 65535, n_rows * q_heads <= 2^32,
- * min(n_rows, max_rows) * q_heads / kv_heads below 2^31 - 1024, 48 * n_seq * q_heads below 2^31.
+ * min(n_rows, max_rows) * q_heads / kv_heads below 2^31 - 1024, 48 * n_seq * q_heads below 2^31; and, with a workspace of the size
+ * that is asked for, launches that HIP has lanes for: fewer than some 2^24 tiles of a sequence's 16 to 192 rows times heads, and, where long
+ * lengths are cut into parts, fewer than some 2^26 rows times heads.
  */
 typedef struct cmpq_kv_attention_job {
     cmpq_kv_cache cache;

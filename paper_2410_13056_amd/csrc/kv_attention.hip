@@ -1035,6 +1035,25 @@ int check_job(const cmpq_kv_attention_job *a) {
     return check_rotation(&a->rotation, a->cache.head_dim);
 }
 
+// Rows of a sequence that the kernel for few rows has at most, and the items of its join; the heads that a wavefront of the other
+// join has one after the other (only where there are wavefronts enough all the same), and that join's wavefronts.
+int64_t few_rows(const Kernel &h, int64_t group, int64_t max_rows) { return h.most_cols / group < max_rows ? h.most_cols / group : max_rows; }
+int64_t few_items(const Kernel &h, int64_t n_seq, int64_t q_heads, int64_t group, int64_t max_rows) {
+    return n_seq * few_rows(h, group, max_rows) * q_heads;
+}
+int64_t heads_each(int64_t n_rows, int64_t q_heads, int64_t group) {
+    const int64_t all = cdiv(n_rows * q_heads, 4096);
+    return all < group ? all : group;
+}
+int64_t rows_waves(int64_t n_rows, int64_t q_heads, int64_t group) { return n_rows * (q_heads / group) * cdiv(group, heads_each(n_rows, q_heads, group)); }
+
+bool launches_fit(const cmpq_kv_attention_job *a, const Launches &l) {
+    const int64_t group = a->q_heads / a->cache.kv_heads;
+    if (!one_launch(l.few.grid, l.few.wide ? 512 : 256) || !one_launch(l.rows.grid, 256)) return false;
+    if (l.few.kept && !one_launch(cdiv(few_items(l.few, a->n_seq, a->q_heads, group, a->max_rows), 4), 256)) return false;
+    return !l.rows.kept || one_launch(cdiv(rows_waves(a->n_rows, a->q_heads, group), 4), 256);
+}
+
 template <int C, int NT>
 void launch_few(const Job &j, const Kernel &h, hipStream_t st) {
     if constexpr (C * NT <= 8) {
@@ -1044,8 +1063,7 @@ void launch_few(const Job &j, const Kernel &h, hipStream_t st) {
         attend_kernel<C, NT, 4><<<dim3((unsigned)h.grid), 256, 0, st>>>(j);
     }
     if (!h.kept) return;
-    const int64_t each = h.most_cols / j.group < j.max_rows ? h.most_cols / j.group : j.max_rows;
-    const int64_t items = j.n_seq * each * j.q_heads;
+    const int64_t each = few_rows(h, j.group, j.max_rows), items = few_items(h, j.n_seq, j.q_heads, j.group, j.max_rows);
     // us, 4 wavefronts and 1: 2 sequences of 64 heads (up to 80 parts) 9.0 and 12.4, 64 of them (3 parts) 12.5 and 6.6
     if (items < 2048) join_kernel<C, NT * 16, 4><<<dim3((unsigned)items), 256, 0, st>>>(j, (int)each);
     else join_kernel<C, NT * 16, 1><<<dim3((unsigned)cdiv(items, 4)), 256, 0, st>>>(j, (int)each);
@@ -1055,9 +1073,7 @@ template <int C, int NT>
 void launch_rows(const Job &j, const Kernel &h, hipStream_t st) {
     attend_rows_kernel<C, NT><<<dim3((unsigned)h.grid), kWaves * 64, 0, st>>>(j);
     if (!h.kept) return;
-    // heads one after the other only where there are wavefronts enough all the same
-    const int64_t all = cdiv(j.n_rows * j.q_heads, 4096), each = all < j.group ? all : j.group;
-    const int64_t waves = j.n_rows * j.c.kv_heads * cdiv(j.group, each);
+    const int64_t each = heads_each(j.n_rows, j.q_heads, j.group), waves = rows_waves(j.n_rows, j.q_heads, j.group);
     join_rows_kernel<C, NT * 16 * kWaves><<<dim3((unsigned)cdiv(waves, 4)), 256, 0, st>>>(j, (int)each);
 }
 
@@ -1106,6 +1122,7 @@ extern "C" int cmpq_kv_attention(const cmpq_kv_attention_job *a, void *ws, size_
     const Launches l = plan_launches(a);
     if (l.few.grid > INT32_MAX || l.rows.grid > INT32_MAX) return CMPQ_ESHAPE;
     if (!ws || reinterpret_cast<uintptr_t>(ws) % 256 || ws_bytes < workspace_of(l)) return CMPQ_EWORKSPACE;
+    if (!launches_fit(a, l)) return CMPQ_ESHAPE;
     WsCarver w(ws);
     Job j = {};
     j.c = a->cache;

@@ -404,12 +404,13 @@ extern "C" int cmpq_kv_append(const cmpq_kv_cache *cache, const cmpq_kv_rows *ro
         return cmpq_flag_named_rows(rows->cu_rows, rows->n_seq, status, static_cast<hipStream_t>(stream));
     const cmpq_rotation rot = rotation ? *rotation : cmpq_rotation{};
     const dim3 grid = page_grid(*cache, *rows);
+    const bool whole = cache->head_dim % 8 == 0 && turns_by_eight(rot), wavefronts = whole && rows->n_rows <= 4 * rows->n_seq;
+    if (!one_launch(grid.x, wavefronts ? 64 : 256)) return CMPQ_ESHAPE;
     hipStream_t st = static_cast<hipStream_t>(stream);
     auto launch = [&](auto like) {
         using T = decltype(like);
-        const bool whole = cache->head_dim % 8 == 0 && turns_by_eight(rot);
         if (!whole) append_kernel<T, false, 256><<<grid, 256, 0, st>>>(*cache, *rows, *K, *V, rot, status);
-        else if (rows->n_rows > 4 * rows->n_seq) append_kernel<T, true, 256><<<grid, 256, 0, st>>>(*cache, *rows, *K, *V, rot, status);
+        else if (!wavefronts) append_kernel<T, true, 256><<<grid, 256, 0, st>>>(*cache, *rows, *K, *V, rot, status);
         else append_kernel<T, true, 64><<<grid, 64, 0, st>>>(*cache, *rows, *K, *V, rot, status);
     };
     if (dtype == CMPQ_F16) launch(_Float16());
@@ -425,6 +426,7 @@ extern "C" int cmpq_kv_read(const cmpq_kv_cache *cache, const cmpq_kv_rows *rows
     if (rows->n_seq == 0 || rows->n_rows == 0 || rows->ld_table == 0)
         return cmpq_flag_named_rows(rows->cu_rows, rows->n_seq, status, static_cast<hipStream_t>(stream));
     const dim3 grid = page_grid(*cache, *rows);
+    if (!one_launch(grid.x, 256)) return CMPQ_ESHAPE;
     hipStream_t st = static_cast<hipStream_t>(stream);
     if (dtype == CMPQ_F16) read_kernel<_Float16, 256><<<grid, 256, 0, st>>>(*cache, *rows, *K, *V, status);
     else if (dtype == CMPQ_BF16) read_kernel<__bf16, 256><<<grid, 256, 0, st>>>(*cache, *rows, *K, *V, status);

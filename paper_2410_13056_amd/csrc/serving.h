@@ -178,5 +178,8 @@ static inline int check_cache(const cmpq_kv_cache &c) {
     return CMPQ_OK;
 }
 
+// Of 2^32 lanes or more HIP launches what 32 bits hold of the number, as a rule without an error.
+static inline bool one_launch(int64_t workgroups, int lanes) { return workgroups <= (int64_t)UINT32_MAX / lanes; }
+
 // For calls that do no row: CMPQ_STATUS_RANGE where a sequence names one all the same.
 int cmpq_flag_named_rows(const int32_t *cu, int64_t n_seq, int32_t *status, hipStream_t stream);
