@@ -318,7 +318,7 @@ def kv_attention(cache: KvCache, Q: torch.Tensor, page_table: torch.Tensor, leng
 Layer = Union[Int8Weight, P.Deployed, Callable[[torch.Tensor], torch.Tensor]]
 
 
-def apply_layer(layer: Layer, X: torch.Tensor, ws: B.Workspace, status: Optional[torch.Tensor] = None) -> torch.Tensor:
+def apply_layer(layer: Layer, X: Inputs, ws: B.Workspace, status: Optional[torch.Tensor] = None) -> torch.Tensor:
     """X [m, d_in] times a layer in whichever form it was prepared: 8-bit integers, the mixed-precision tables
     (fp32 out of FP16 in), or any function.  The last two carry a NaN or an infinity on into their outputs; 8-bit
     integers raise it in `status`, and take rows in 8 bits too."""
@@ -335,16 +335,22 @@ def _as_heads(Y: torch.Tensor, head_dim: int) -> torch.Tensor:
     return Y.reshape(Y.shape[0], Y.shape[1] // head_dim, head_dim)
 
 
-def _shared(X: torch.Tensor, norm: Optional[RmsNorm], layers, status: Optional[torch.Tensor]) -> Inputs:
-    """What layers take that share the input X: its norm if there is one, in 8 bits if all of them are, coded once for
-    all (one or two tokens code themselves within the products' launches)."""
-    coded = all(isinstance(l, Int8Weight) for l in layers)
-    if norm is None:
-        return int8_rows(X, status=status) if coded and X.shape[0] > 2 else X
-    if coded:
-        return rms_norm(X, norm.weight, norm.eps, coded=True, status=status)
+def _in_8_bits(layers) -> bool:
+    return all(isinstance(l, (Int8Weight, Int8GatedWeight)) for l in layers)
+
+
+def _shared(X: torch.Tensor, layers, status: Optional[torch.Tensor]) -> Inputs:
+    """What layers take that share the input X: in 8 bits if all of them are, coded once for all (one or two tokens code
+    themselves within the products' launches)."""
+    return int8_rows(X, status=status) if _in_8_bits(layers) and X.shape[0] > 2 else X
+
+
+def _normed(X: torch.Tensor, norm: RmsNorm, layers, status: Optional[torch.Tensor],
+            add: Optional[torch.Tensor] = None) -> Tuple[Inputs, torch.Tensor]:
+    """What layers take that share the norm of X (+ `add`), and that sum: in 8 bits if all of them are, coded once for all."""
     wide = not any(isinstance(l, P.Deployed) for l in layers)            # those read float16
-    return rms_norm(X, norm.weight, norm.eps, out_dtype=X.dtype if wide else torch.float16, status=status)
+    N = rms_norm(X, norm.weight, norm.eps, add, _in_8_bits(layers), out_dtype=X.dtype if wide else torch.float16, status=status)
+    return (N, X) if add is None else N
 
 
 def attention_block(cache: KvCache, X: torch.Tensor, q: Layer, k: Layer, v: Layer, o: Layer, page_table: torch.Tensor,
@@ -362,7 +368,7 @@ def attention_block(cache: KvCache, X: torch.Tensor, q: Layer, k: Layer, v: Laye
     if attention_dtype is None:
         wide = X.dtype == torch.bfloat16 and not isinstance(o, P.Deployed)
         attention_dtype = torch.bfloat16 if wide else torch.float16
-    X = _shared(X, norm, (q, k, v), status)
+    X = _shared(X, (q, k, v), status) if norm is None else _normed(X, norm, (q, k, v), status)[0]
     Q, K, V = (_as_heads(apply_layer(layer, X, ws, status), cache.head_dim) for layer in (q, k, v))
     kv_append(cache, K, V, page_table, held, cu_rows, rotation, status)
     O = kv_attention(cache, Q, page_table, lengths, cu_rows, max_rows, max_length, ws, causal=causal, window=window,
@@ -382,7 +388,7 @@ class GatedLayers(_Kept):
         both = isinstance(self.gate, P.Deployed) and isinstance(self.up, P.Deployed)
         return P.group_products([self.gate, self.up]) if both else None
 
-    def apply(self, X: torch.Tensor, ws: B.Workspace, status: Optional[torch.Tensor] = None):
+    def apply(self, X: Inputs, ws: B.Workspace, status: Optional[torch.Tensor] = None):
         """Both projections of X [m, d_in]."""
         if self._args is None:
             return tuple(_as_matrix(apply_layer(l, X, ws, status)) for l in (self.gate, self.up))
@@ -411,9 +417,7 @@ def feed_forward_block(X: torch.Tensor, norm: RmsNorm, gate_up: Union[Int8GatedW
         return Y
     if hidden_dtype is None:
         hidden_dtype = torch.float16 if isinstance(down, P.Deployed) else X.dtype
-    mixed = not gated and any(isinstance(l, P.Deployed) for l in (gate_up.gate, gate_up.up))
-    N = rms_norm(X, norm.weight, norm.eps, add=add, coded=gated, out_dtype=torch.float16 if mixed else X.dtype, status=status)
-    N, stream = N if add is not None else (N, X)
+    N, stream = _normed(X, norm, (gate_up,) if gated else (gate_up.gate, gate_up.up), status, add)
     if gated:
         H = int8_gated_product(gate_up, N, ws, activation, out_dtype=hidden_dtype, status=status)
     else:
