@@ -20,7 +20,7 @@ from __future__ import annotations
 
 import dataclasses
 import functools
-from typing import Callable, Optional, Tuple, Union
+from typing import Callable, Optional, Sequence, Tuple, Union
 
 import torch
 
@@ -346,11 +346,22 @@ def _shared(X: torch.Tensor, layers, status: Optional[torch.Tensor]) -> Inputs:
 
 
 def _normed(X: torch.Tensor, norm: RmsNorm, layers, status: Optional[torch.Tensor],
-            add: Optional[torch.Tensor] = None) -> Tuple[Inputs, torch.Tensor]:
-    """What layers take that share the norm of X (+ `add`), and that sum: in 8 bits if all of them are, coded once for all."""
-    wide = not any(isinstance(l, P.Deployed) for l in layers)            # those read float16
-    N = rms_norm(X, norm.weight, norm.eps, add, _in_8_bits(layers), out_dtype=X.dtype if wide else torch.float16, status=status)
-    return (N, X) if add is None else N
+            add: Optional[torch.Tensor] = None) -> Tuple[Sequence[Inputs], torch.Tensor]:
+    """What each of the layers takes that share the norm of X (+ `add`), and that sum: in 8 bits if all of them are, coded once for
+    all.  Else values: functions take X's type, the others too, or float16 where one of them is in mixed precision, which
+    reads that."""
+    if _in_8_bits(layers):
+        kinds = [None] * len(layers)
+    else:
+        others = torch.float16 if any(isinstance(l, P.Deployed) for l in layers) else X.dtype
+        kinds = [others if isinstance(l, (Int8Weight, P.Deployed)) else X.dtype for l in layers]
+    norms = {}
+    for k in kinds:
+        if k not in norms:                       # a second type: of the sum that the first has left
+            N = rms_norm(X, norm.weight, norm.eps, add, k is None, out_dtype=k, status=status)
+            norms[k], X = (N, X) if add is None else N
+            add = None
+    return [norms[k] for k in kinds], X
 
 
 def attention_block(cache: KvCache, X: torch.Tensor, q: Layer, k: Layer, v: Layer, o: Layer, page_table: torch.Tensor,
@@ -368,8 +379,8 @@ def attention_block(cache: KvCache, X: torch.Tensor, q: Layer, k: Layer, v: Laye
     if attention_dtype is None:
         wide = X.dtype == torch.bfloat16 and not isinstance(o, P.Deployed)
         attention_dtype = torch.bfloat16 if wide else torch.float16
-    X = _shared(X, (q, k, v), status) if norm is None else _normed(X, norm, (q, k, v), status)[0]
-    Q, K, V = (_as_heads(apply_layer(layer, X, ws, status), cache.head_dim) for layer in (q, k, v))
+    Xs = [_shared(X, (q, k, v), status)] * 3 if norm is None else _normed(X, norm, (q, k, v), status)[0]
+    Q, K, V = (_as_heads(apply_layer(layer, x, ws, status), cache.head_dim) for layer, x in zip((q, k, v), Xs))
     kv_append(cache, K, V, page_table, held, cu_rows, rotation, status)
     O = kv_attention(cache, Q, page_table, lengths, cu_rows, max_rows, max_length, ws, causal=causal, window=window,
                      rotation=rotation, out_dtype=attention_dtype, status=status)
@@ -388,10 +399,11 @@ class GatedLayers(_Kept):
         both = isinstance(self.gate, P.Deployed) and isinstance(self.up, P.Deployed)
         return P.group_products([self.gate, self.up]) if both else None
 
-    def apply(self, X: Inputs, ws: B.Workspace, status: Optional[torch.Tensor] = None):
-        """Both projections of X [m, d_in]."""
+    def apply(self, X: Inputs, ws: B.Workspace, status: Optional[torch.Tensor] = None, X_up: Optional[Inputs] = None):
+        """Both projections of X [m, d_in].  `X_up`: what `up` takes, if that is of another type."""
         if self._args is None:
-            return tuple(_as_matrix(apply_layer(l, X, ws, status)) for l in (self.gate, self.up))
+            inputs = (X, X if X_up is None else X_up)
+            return tuple(_as_matrix(apply_layer(l, x, ws, status)) for l, x in zip((self.gate, self.up), inputs))
         X = X.to(torch.float16)
         Y = [torch.empty((X.shape[0], l.d_out), dtype=torch.float32, device=X.device) for l in (self.gate, self.up)]
         if X.shape[0]:
@@ -417,11 +429,11 @@ def feed_forward_block(X: torch.Tensor, norm: RmsNorm, gate_up: Union[Int8GatedW
         return Y
     if hidden_dtype is None:
         hidden_dtype = torch.float16 if isinstance(down, P.Deployed) else X.dtype
-    N, stream = _normed(X, norm, (gate_up,) if gated else (gate_up.gate, gate_up.up), status, add)
+    Ns, stream = _normed(X, norm, (gate_up,) if gated else (gate_up.gate, gate_up.up), status, add)
     if gated:
-        H = int8_gated_product(gate_up, N, ws, activation, out_dtype=hidden_dtype, status=status)
+        H = int8_gated_product(gate_up, Ns[0], ws, activation, out_dtype=hidden_dtype, status=status)
     else:
-        G, U = gate_up.apply(N, ws, status)
+        G, U = gate_up.apply(Ns[0], ws, status, Ns[1])
         H = epilogue(G, activation=activation, times=U, out_dtype=hidden_dtype)
     if isinstance(down, Int8Weight):
         return int8_product(down, H, ws, out_dtype=X.dtype, status=status, residual=stream)

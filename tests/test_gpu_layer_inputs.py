@@ -21,3 +21,27 @@ def test_two_gated_layers_in_8_bits_read_rows_coded_once(S, m, dtype):  # noqa: 
         H = S.epilogue(G, activation="silu", times=U, out_dtype=dtype)
         assert torch.equal(got, S.int8_product(part.down, H, part.ws, out_dtype=dtype, residual=stream))
         assert torch.equal(got, one(X, add=add)) and part.status.item() == 0
+
+
+@pytest.mark.parametrize("kinds", ["fd8", "df8", "8df", "f8d"])
+@pytest.mark.parametrize("dtype", TYPES)
+def test_layers_of_several_kinds_take_their_own_norms(S, kinds, dtype):  # noqa: F811
+    """Functions that of X's type, layers in mixed precision and those in 8 bits beside them that in float16, of one sum."""
+    part = Part(S, kinds)
+    W = {n: w.to(dtype) for n, w in part.W.items()}
+    function = lambda n: lambda x: torch.nn.functional.linear(x, W[n])             # of one type alone
+    gate, up = (function(n) if k == "f" else l for n, k, l in zip(("gate", "up"), kinds, (part.gate_up.gate, part.gate_up.up)))
+    part.gate_up = S.GatedLayers(gate, up)
+    half = torch.float16 if "d" in kinds[:2] else dtype
+    for m in (1, 5, 40):
+        X, A = _randn(m, m, HIDDEN, dtype=dtype, scale=2), _randn(m + 1, m, HIDDEN)
+        for add in (None, A):
+            got = part(X, add=add)
+            N, stream = (S.rms_norm(X, part.norm.weight, EPS), X) if add is None else S.rms_norm(X, part.norm.weight, EPS, add=add)
+            N16 = S.rms_norm(X, part.norm.weight, EPS, add=add, out_dtype=half)
+            N16 = N16 if add is None else N16[0]
+            G, U = (l(N) if k == "f" else S.apply_layer(l, N16, part.ws) for k, l in zip(kinds, (gate, up)))
+            H = S.epilogue(G, activation="silu", times=U, out_dtype=torch.float16 if kinds[2] == "d" else dtype)
+            want = S.int8_product(part.down, H, part.ws, out_dtype=dtype, residual=stream) if kinds[2] == "8" else \
+                S.epilogue(S.apply_layer(part.down, H, part.ws), residual=stream, out_dtype=dtype)
+            assert got.dtype == dtype and torch.equal(got, want) and part.status.item() == 0
