@@ -1,7 +1,8 @@
 // Root-mean-square norm of a stream, or of two streams' sum, given as values or as rows in 8 bits.
 // A workgroup a row, which stays in registers between its sum of squares and its outputs.  The squares are summed in 64
-// bits, where the order of additions decides nothing that is left after the one rounding to fp32, so a row's codes are those of
-// the definition, whatever the number of lanes.
+// bits, in an order that depends on the row's length alone, so a row's bits are the same in any batch and form.  Another
+// order (a definition's, summed one by one) gives the same root but for a row in a hundred million or so, whose root lies
+// within the sum's last bits of the middle between two numbers of fp32.
 //
 // Bound.  Many rows: by bytes.  4096 rows of 8192 in bfloat16 with their sum, 268 MB, 40.5 us (6.6 TB/s, what caches keep between
 // calls included), as rows in 8 bits 40.  One row: by what comes one after the other (the loads, the sum over the lanes, the root, the
@@ -39,6 +40,25 @@ __device__ __forceinline__ double total(const double *parts) {
     return v + turn(v, std::integral_constant<int, 1>());
 }
 
+// Four sums over the wavefront for little more than one: lanes 16 q have that of v[0], v[2], v[1], v[3] (q = 0 .. 3), added in the
+// order of wave_sum_f64.
+__device__ __forceinline__ double wave_sums_f64(const double (&v)[4]) {
+    const auto halves = [](double x, double y) {
+        const uint64_t a = (uint64_t)__double_as_longlong(x), b = (uint64_t)__double_as_longlong(y);
+        const auto lo = __builtin_amdgcn_permlane32_swap((uint32_t)a, (uint32_t)b, false, false);
+        const auto hi = __builtin_amdgcn_permlane32_swap((uint32_t)(a >> 32), (uint32_t)(b >> 32), false, false);
+        return join_f64(lo[0], hi[0]) + join_f64(lo[1], hi[1]);
+    };
+    const uint64_t a = (uint64_t)__double_as_longlong(halves(v[0], v[1])), b = (uint64_t)__double_as_longlong(halves(v[2], v[3]));
+    const auto lo = __builtin_amdgcn_permlane16_swap((uint32_t)a, (uint32_t)b, false, false);
+    const auto hi = __builtin_amdgcn_permlane16_swap((uint32_t)(a >> 32), (uint32_t)(b >> 32), false, false);
+    double x = join_f64(lo[0], hi[0]) + join_f64(lo[1], hi[1]);
+    x += row_up_f64<8>(x);
+    x += row_up_f64<4>(x);
+    x += row_up_f64<2>(x);
+    return x + row_up_f64<1>(x);
+}
+
 // 1 / sqrt(x) to about a step of fp64, rounded to fp32: the instruction's 26 bits, doubled twice by Newton's method.
 __device__ __forceinline__ float one_over_root(double x) {
     double r = __builtin_amdgcn_rsq(x);
@@ -52,7 +72,10 @@ template <int THREADS, int KEPT, bool CODED, int TYPE>
 __global__ __launch_bounds__(THREADS) void rms_norm_kernel(cmpq_norm_job a, double per_value) {
 #pragma clang fp contract(off)
     constexpr int kWaves = THREADS / 64, kStep = THREADS * 8, kHeld = KEPT > 0 ? KEPT : 1;
-    __shared__ double sums[kWaves];
+    // The sum's parts are those of 16 wavefronts with a step each, in their order, where rows in 8 bits may have either kernel.
+    constexpr bool kApart = kWaves == 4 && KEPT > 2;
+    static_assert(!kApart || KEPT <= 4, "steps");
+    __shared__ double sums[kApart ? 16 : kWaves];
     __shared__ float most[kWaves];
     const int64_t row = CODED ? die_order(blockIdx.x, gridDim.x) : (int64_t)blockIdx.x;
     const auto type = [](int dtype) { return TYPE == kAny ? dtype : TYPE; };
@@ -110,16 +133,23 @@ __global__ __launch_bounds__(THREADS) void rms_norm_kernel(cmpq_norm_job a, doub
             for (int k = 0; k < kHeld; ++k) gain[k].load(a.gain.ptr, type(a.gain.dtype), first + k * kStep, min(max(d - first - k * kStep, 0), 8));
         }
     }
-    double sum = 0;
+    double sum[kApart ? 4 : 1] = {};
     each([&](float (&s)[8], int i, const Raw8 &) {
+        double &part = sum[kApart ? (i - first) / kStep : 0];
 #pragma unroll
-        for (int k = 0; k < 8; ++k) sum = fma((double)s[k], (double)s[k], sum);
+        for (int k = 0; k < 8; ++k) part = fma((double)s[k], (double)s[k], part);
         if (a.S.ptr && i < d) store_some<8>(a.S.ptr, type(a.S.dtype), row * a.S.ld + i, min(d - i, 8), s);
     }, false);
-    sum = wave_sum_f64(sum);
-    if ((threadIdx.x & 63) == 0) sums[threadIdx.x >> 6] = sum;
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    if constexpr (kApart) {
+        const double part = wave_sums_f64(sum);
+        if (lane % 16 == 0) sums[(lane >> 5 | (lane >> 4 & 1) << 1) * 4 + wave] = part;
+    } else {
+        const double part = wave_sum_f64(sum[0]);
+        if (lane == 0) sums[wave] = part;
+    }
     __syncthreads();
-    const double q = total<kWaves>(sums);
+    const double q = total<kApart ? 16 : kWaves>(sums);
     bool bad = !(q < __builtin_huge_val());
     const float r = bad ? (q != q ? __builtin_nanf("") : 0.f) : one_over_root(q * per_value + a.eps);
     auto normed = [&](float (&s)[8], const Raw8 &g) {
