@@ -374,10 +374,9 @@ __global__ __launch_bounds__(WAVES * 64) void shared_depth_kernel(const uint8_t 
 // 8192 -> 8192 11.8 and 15.4, 28672 -> 1000 12.0 and 19.4, -> 4000 23.6 and 27.0 (a gated product's second token of more
 // than 16384 inputs has no room in registers); 4 tokens 20.5 and 15.4, which is why it ends there.  Small ones are bound by what comes one after the other (the
 // token, its largest, two barriers, the products, the join), large ones by the weights' bytes.
-// Wavefronts, us with 8 and 16: 1 token 5120 -> 13824 13.0 and 15.7, 4096 -> 11008 7.8 and 8.9, but 8192 -> 28672 36.3 and
-// 34.8; gated, weights from memory, 5120 -> 2 x 13824 29.8 and 29.6, 8192 -> 2 x 28672 86.6 and 85.0 (5.5 TB/s; loads alone in
-// runs of 128 KB reach 6.2).  A step in turn for each wavefront in place of a run of steps: gated 85.0 and 90, but 8192 -> 28672 42.8
-// and 41.7.
+// Wavefronts: eight_wavefronts; 1 token 8192 -> 28672 36.3 us with 8 and 34.8 with 16; gated, weights from memory, 5120 -> 2 x 13824
+// 29.8 and 29.6, 8192 -> 2 x 28672 86.6 and 85.0 (5.5 TB/s; loads alone in runs of 128 KB reach 6.2).  A step in turn for each
+// wavefront in place of a run of steps: gated 85.0 and 90, but 8192 -> 28672 42.8 and 41.7.
 constexpr int kFewDepth = 16384;
 
 template <typename TX, typename E, int M, int C, int WAVES>  // up to C * 1024 * WAVES inputs
@@ -789,6 +788,15 @@ int launch_product(const uint8_t *W, const uint8_t *X, int deep, const Scaled &y
     return CMPQ_OK;
 }
 
+// Whether one token's product is better off with 8 wavefronts a workgroup than with 16.  Weights from memory, us with 8 and 16: 2048 -> 28672
+// 13.2 and 16.0, 5120 -> 13824 15.9 and 18.0, 1000 -> 4096 4.7 and 4.5 (from the caches 4.1 and 4.5); but 2048 -> 4096 5.1 and 4.5, 4096 -> 4096 7.2
+// and 5.7, -> 28672 22.6 and 21.8, 5120 -> 4096 8.0 and 6.9, -> 8192 10.9 and 11.2 (9.2 and 7.9).  Where workgroups are few, those of 8 lie two in
+// a unit beside units without one; of up to 4096 inputs 16 bring all they need at once, and 8 half of more than 2048.
+bool eight_wavefronts(const Scaled &y, int64_t d) {
+    const int64_t pieces = cdiv(y.d_out, kRows);
+    return d <= 1024 || (d <= 2048 && pieces > kUnits) || (d > 4096 && d <= 6144 && pieces > 2 * kUnits);
+}
+
 // Whether the tokens go in one launch.
 template <typename E>
 bool few_fit(const Scaled &y, int64_t d) {
@@ -812,7 +820,7 @@ void launch_few(const uint8_t *W, const void *X, int64_t d, int64_t ldx, const S
     if (y.m == 2) {
         if (d <= kFewDepth) run(Two(), One(), Sixteen());
         else if constexpr (!E::kGated) run(Two(), Two(), Sixteen());
-    } else if (!E::kGated && d <= 6144) {
+    } else if (!E::kGated && eight_wavefronts(y, d)) {
         if constexpr (!E::kGated) run(One(), One(), Eight());
     } else {
         if (d <= kFewDepth) run(One(), One(), Sixteen());
