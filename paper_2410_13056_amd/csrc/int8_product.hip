@@ -758,6 +758,10 @@ void launch_pairs(const uint8_t *W, const uint8_t *X, int deep, const Scaled &y,
 // 700 tokens 4096 -> 4096 19.0 and 20.4, 200 tokens 2048 -> 13824 14.2 and 15.6.  One round against two of a smaller: 333 tokens 4099 -> 3001
 // 96 x 48 12.9, 64 x 128 14.8, 64 x 64 15.4; 150 tokens 4096 -> 11008 96 x 96 14.7, 64 x 64 19.4; 64 tokens 5120 -> 28672 128 x 64 25.7,
 // 128 x 128 28.2; 400 tokens 8192 -> 5120 128 x 128 28.4, 64 x 64 34.8 (but 1000 tokens 2048 -> 2560 12.6 and 12.1).
+// 64 x 64: a ring of 8 steps, since a unit's one workgroup has to have the weights' way from memory covered, and two groups for more than
+// 128 tokens of 4096 inputs or more.  us with the codes, weights from memory (from the caches): 333 tokens 28672 -> 2048 one group 60.0 (55.1),
+// two 59.7 (49.9), two with 4 steps 67.9 (50.5); 333 tokens 8192 -> 2560 23.7 (22.2), 23.4 (20.8), 25.6 (20.9); but 100 tokens 5120 -> 5120 18.1
+// (15.3), 19.0 (14.4), 19.0 (14.3); 333 tokens 2048 -> 2048 10.9 (10.5), 11.2 (10.4), 10.9 (10.2).
 // Fewer than 150 tiles of 64 x 64, and up to 32 tokens: wavefronts share the depth (512 tokens
 // 8192 -> 1024 18.6, 64 x 64 23.0; 64 tokens 4096 -> 4096 9.4, 12.3).  Up to 16 tokens: two pieces of outputs a workgroup where there
 // are many (16 tokens 5120 -> 13824 16.0, one piece 17.9), one by 8 wavefronts for some (8192 -> 10240, weights from memory, 19.6, two
@@ -778,7 +782,8 @@ int launch_product(const uint8_t *W, const uint8_t *X, int deep, const Scaled &y
     else if (fills(tiles_of<E>(y, 16, 8))) launch_tiles<T, E, 16, 8, 4, 2, 1, 4>(W, X, deep, y, e, st);
     else if (tiles_of<E>(y, 8, 8) > kUnits) launch_tiles<T, E, 8, 8, 2, 2, 1, 4>(W, X, deep, y, e, st);
     else if (tiles_of<E>(y, 4, 4) < 150) launch_pairs<T, E>(W, X, deep, y, e, st);
-    else if (tiles_of<E>(y, 4, 4) <= kUnits) launch_tiles<T, E, 4, 4, 2, 2, 2, 4>(W, X, deep, y, e, st);
+    else if (tiles_of<E>(y, 4, 4) <= kUnits && y.m > 128 && deep >= 64) launch_tiles<T, E, 4, 4, 2, 2, 2, 8>(W, X, deep, y, e, st);
+    else if (tiles_of<E>(y, 4, 4) <= kUnits) launch_tiles<T, E, 4, 4, 2, 2, 1, 8>(W, X, deep, y, e, st);
     else if (tiles_of<E>(y, 6, 3) <= kUnits) launch_tiles<T, E, 6, 3, 3, 1, 3, 4>(W, X, deep, y, e, st);
     else if (tiles_of<E>(y, 4, 8) <= kUnits) launch_tiles<T, E, 4, 8, 2, 2, 2, 4>(W, X, deep, y, e, st);
     else if (tiles_of<E>(y, 8, 4) <= kUnits) launch_tiles<T, E, 8, 4, 2, 2, 2, 4>(W, X, deep, y, e, st);

@@ -1,4 +1,5 @@
-"""Sizes on both sides of the lines that the choice of kernels is made by: one token by 8 or 16 wavefronts."""
+"""Sizes on both sides of the lines that the choice of kernels is made by: one token by 8 or 16 wavefronts; tiles of 64 x 64 by one
+or two groups of wavefronts."""
 import pytest
 import torch
 
@@ -9,9 +10,11 @@ from test_gpu_int8_finish import S  # noqa: F401
 pytestmark = pytest.mark.gpu
 
 ONE = [(1, d, n) for d in (1024, 1025, 2048, 2049, 4096, 4097, 6144) for n in (4096, 4097, 8200)] + [(1, 6145, 4100), (1, 70, 5000)]
+TILES = [(128, 130, 4700), (128, 4200, 5000), (129, 4030, 3401), (129, 4032, 3400), (333, 4096, 2050), (200, 4200, 3300), (140, 6000, 4000),
+         (100, 1, 5000), (600, 3000, 1000), (600, 5000, 999)]
 
 
-@pytest.mark.parametrize("m,d_in,d_out", ONE)
+@pytest.mark.parametrize("m,d_in,d_out", ONE + TILES)
 def test_products(S, m, d_in, d_out):  # noqa: F811
     k = m + d_in + d_out
     X = T._randn(k, m, d_in, dtype=T.TYPES[k % 3], scale=3)
@@ -25,7 +28,7 @@ def test_products(S, m, d_in, d_out):  # noqa: F811
 
 
 def test_a_graph_of_each(S):  # noqa: F811
-    for m, d_in, d_out in ((1, 4096, 4096), (1, 5120, 8200)):
+    for m, d_in, d_out in ((1, 4096, 4096), (1, 5120, 8200), (128, 300, 4700), (333, 4096, 2050)):
         X, W = T._randn(1, m, d_in, dtype=torch.float16), T._randn(2, d_out, d_in, dtype=torch.float16)
         w, ws = S.prepare_int8(W), T._ws()
         out = S.int8_product(w, X, ws)
