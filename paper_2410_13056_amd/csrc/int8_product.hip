@@ -571,7 +571,7 @@ __device__ __forceinline__ void put_rows(const Int4 *sums, const Scaled &y, int6
 // cache while the weights pass once a band.
 constexpr int kBand = 4;
 
-template <typename T, typename E, int OT, int TT, int WO, int WT, int G, int BUFS>
+template <typename T, typename E, int OT, int TT, int WO, int WT, int G, int BUFS, bool BEHIND_FIRST>
 __global__ __launch_bounds__(WO * WT * G * 64, 2) void tile_kernel(const uint8_t *__restrict__ W, const uint8_t *__restrict__ X,
                                                                int deep, int o_tiles, int t_tiles, Scaled y, E e) {
     constexpr int kWaves = WO * WT, kLoads = (OT + TT) / kWaves, kStepBytes = (OT + TT) * kPiece, A = OT / WO, B = TT / WT;
@@ -620,10 +620,12 @@ __global__ __launch_bounds__(WO * WT * G * 64, 2) void tile_kernel(const uint8_t
         arrive();
         // The two wavefronts of a SIMD are seldom as far as each other: the one that is behind goes first until its last share.  4096
         // tokens 8192 -> 28672 747 us and 757, gated 1452 and 1482; raised for half of a step 750, for all of it 757.
-        __builtin_amdgcn_s_setprio(1);
+        // Not for tiles of 128 x 128 that are more than two a unit: 700 tokens 13824 -> 13824 171 us without, 186 with; but 333 tokens
+        // 8192 -> 11008, 258 tiles, 54 and 49.
+        if (BEHIND_FIRST) __builtin_amdgcn_s_setprio(1);
 #pragma unroll
         for (int s = 0; s < kLoads; ++s) {
-            if (s == kLoads - 1) __builtin_amdgcn_s_setprio(0);
+            if (BEHIND_FIRST && s == kLoads - 1) __builtin_amdgcn_s_setprio(0);
 #pragma unroll
             for (int q = (A + B) * s / kLoads; q < (A + B) * (s + 1) / kLoads; ++q) fetch(step + 1, buf ^ 1, q);
 #pragma unroll
@@ -721,10 +723,10 @@ int64_t tiles_of(const Scaled &y, int ot, int tt) {
     return cdiv(pieces_of<E>(y), ot) * cdiv(y.m, tt * kRows);
 }
 
-template <typename T, typename E, int OT, int TT, int WO, int WT, int G, int BUFS>
+template <typename T, typename E, int OT, int TT, int WO, int WT, int G, int BUFS, bool BEHIND_FIRST = true>
 void launch_tiles(const uint8_t *W, const uint8_t *X, int deep, const Scaled &y, const E &e, hipStream_t st) {
     const int o_tiles = (int)cdiv(pieces_of<E>(y), OT), t_tiles = (int)cdiv(y.m, TT * kRows);
-    tile_kernel<T, E, OT, TT, WO, WT, G, BUFS><<<dim3((unsigned)(o_tiles * t_tiles)), WO * WT * G * 64, 0, st>>>(W, X, deep, o_tiles, t_tiles, y, e);
+    tile_kernel<T, E, OT, TT, WO, WT, G, BUFS, BEHIND_FIRST><<<dim3((unsigned)(o_tiles * t_tiles)), WO * WT * G * 64, 0, st>>>(W, X, deep, o_tiles, t_tiles, y, e);
 }
 
 template <typename T, typename E, int OP, int TP, int WAVES>
@@ -780,6 +782,7 @@ int launch_product(const uint8_t *W, const uint8_t *X, int deep, const Scaled &y
     else if (y.m <= 32) launch_pairs<T, E>(W, X, deep, y, e, st);
     else if (fills(tiles_of<E>(y, 16, 16))) launch_tiles<T, E, 16, 16, 4, 2, 1, 4>(W, X, deep, y, e, st);
     else if (fills(tiles_of<E>(y, 16, 8))) launch_tiles<T, E, 16, 8, 4, 2, 1, 4>(W, X, deep, y, e, st);
+    else if (tiles_of<E>(y, 8, 8) > 2 * kUnits) launch_tiles<T, E, 8, 8, 2, 2, 1, 4, false>(W, X, deep, y, e, st);
     else if (tiles_of<E>(y, 8, 8) > kUnits) launch_tiles<T, E, 8, 8, 2, 2, 1, 4>(W, X, deep, y, e, st);
     else if (tiles_of<E>(y, 4, 4) < 150) launch_pairs<T, E>(W, X, deep, y, e, st);
     else if (tiles_of<E>(y, 4, 4) <= kUnits && y.m > 128 && deep >= 64) launch_tiles<T, E, 4, 4, 2, 2, 2, 8>(W, X, deep, y, e, st);
