@@ -61,7 +61,9 @@ struct Turn {
 // TB/s, one by one 29.8, 2048 of 13824 22.1 and 26.8; from the cache behind the dies the same, and fewer rows are better off one by one, 1280
 // of 8192 7.2 and 8.9.  Bound by a row's latency where they are few: 333 rows 4 us.  Long rows take 16 wavefronts in place of 4: 2048 of
 // 28672 from memory 47 us and 55 (34 and 32 from the cache), 300 of 28672 8.0 and 8.5, 1 of 28672 5.1 and 6.3, 16 of 13824 4.7 and 5.2,
-// but 1 of 8192 4.1 and 3.6, 700 of 13824 9.9 and 8.4.
+// but 1 of 8192 4.1 and 3.6.  Lines: rows of 13824 by 16 and by 4, 192 rows 4.5 and 5.2, 256 4.9 and 5.3, 320 5.5 and 5.8, 512 6.5 and 6.6, 768 8.6 and
+// 8.1; rows of 8192 one by one and four together, from memory 1280 10.9 and 11.4, 1792 14.5 and 12.7, 2048 16.1 and 13.8, 4096 29.0 and 25.5 (from
+// the caches 7.2 and 8.8, 10.5 and 10.4, 12.1 and 11.0, 19.4 and 19.6).
 template <typename T, int THREADS, int KEPT, int ROWS>
 __global__ __launch_bounds__(THREADS) void code_rows_kernel(const T *__restrict__ X, int64_t n, int64_t all, int64_t d, int64_t ld,
                                                         int8_t *__restrict__ codes, float *__restrict__ scale, Turn turn,
@@ -562,8 +564,8 @@ __device__ __forceinline__ void put_rows(const Int4 *sums, const Scaled &y, int6
 // Tiles of OT x TT pieces a workgroup, WO x WT wavefronts.  Pieces reach LDS by direct loads in the order in which they
 // are read (no conflicts), BUFS steps of 64 inputs in a ring; while a step is multiplied its operands are in
 // registers, those of the next are on their way from LDS and the steps after it from memory.  Bound by the matrix
-// instructions at 256 x 256: 4096 tokens 8192 -> 28672 in 741 us with the codes (29), 2.6 POP/s, the instructions busy for 69 %
-// of the clocks; without the barriers 690 in place of 718 us, without the loads 626, without the LDS reads 677.  G groups of
+// instructions at 256 x 256: 4096 tokens 8192 -> 28672 in 690 us, and 24 for the codes (cards differ by 5 %), 2.8 POP/s, the
+// instructions busy for 70 % of the clocks; on another day without the barriers 690 in place of 718 us, without the loads 626, without the LDS reads 677.  G groups of
 // wavefronts share the depth, each with a ring of its own; their sums are joined through LDS, in order.  One round of small tiles: 3 us
 // of a launch, 2 to 5 before the first step and behind the last, then 80 to 120 ns a step of 64 x 64 (of 118 bytes a ns that a unit's
 // loads reach 70 to 100), 160 of 64 x 128, 230 of 128 x 128; without loads, without LDS reads or without barriers 0 to 15 % less.
@@ -756,19 +758,24 @@ void launch_pairs(const uint8_t *W, const uint8_t *X, int deep, const Scaled &y,
 // Where 128 x 128 would be no more than one a unit: the smallest tile that is still at most one a unit, since the unit with most
 // tiles is what all wait for, its depth shared by two or three groups of wavefronts, since one group alone keeps neither the
 // matrix instructions nor the loads busy.  us of a round of each at a depth of 4096: 64 x 64 9, 96 x 48 10.9, 64 x 128 and 128 x 64
-// 13.5, 96 x 96 14.8, 128 x 128 18 to 20, two rounds 17, 21, ...  Groups against one: 100 tokens 5120 -> 5120 10.0 and 11.8, 128 x 128:
-// 700 tokens 4096 -> 4096 19.0 and 20.4, 200 tokens 2048 -> 13824 14.2 and 15.6.  One round against two of a smaller: 333 tokens 4099 -> 3001
-// 96 x 48 12.9, 64 x 128 14.8, 64 x 64 15.4; 150 tokens 4096 -> 11008 96 x 96 14.7, 64 x 64 19.4; 64 tokens 5120 -> 28672 128 x 64 25.7,
+// 13.5, 96 x 96 14.8, 128 x 128 18 to 20, two rounds 17, 21, ...  Groups against one, 128 x 128: 700 tokens 4096 -> 4096 19.0 and
+// 20.4, 200 tokens 2048 -> 13824 14.2 and 15.6.  One round against two of a smaller: 333 tokens 4099 -> 3001 96 x 48 12.9 (11.7 since its outputs
+// pass through LDS), 64 x 128 14.8, 64 x 64 15.4; 150 tokens 4096 -> 11008 96 x 96 14.7, 64 x 64 19.4; 64 tokens 5120 -> 28672 128 x 64 25.7,
 // 128 x 128 28.2; 400 tokens 8192 -> 5120 128 x 128 28.4, 64 x 64 34.8 (but 1000 tokens 2048 -> 2560 12.6 and 12.1).
 // 64 x 64: a ring of 8 steps, since a unit's one workgroup has to have the weights' way from memory covered, and two groups for more than
 // 128 tokens of 4096 inputs or more.  us with the codes, weights from memory (from the caches): 333 tokens 28672 -> 2048 one group 60.0 (55.1),
 // two 59.7 (49.9), two with 4 steps 67.9 (50.5); 333 tokens 8192 -> 2560 23.7 (22.2), 23.4 (20.8), 25.6 (20.9); but 100 tokens 5120 -> 5120 18.1
 // (15.3), 19.0 (14.4), 19.0 (14.3); 333 tokens 2048 -> 2048 10.9 (10.5), 11.2 (10.4), 10.9 (10.2).
-// Fewer than 150 tiles of 64 x 64, and up to 32 tokens: wavefronts share the depth (512 tokens
-// 8192 -> 1024 18.6, 64 x 64 23.0; 64 tokens 4096 -> 4096 9.4, 12.3).  Up to 16 tokens: two pieces of outputs a workgroup where there
-// are many (16 tokens 5120 -> 13824 16.0, one piece 17.9), one by 8 wavefronts for some (8192 -> 10240, weights from memory, 19.6, two
-// by 16 23.2), two by 16 where they are a round of the units (13824 -> 5120 18.0, one by 8 20.1: its units read the tokens twice as
-// often), one by 16 for few (8 tokens 8192 -> 1024 8.6, 8 wavefronts 9.8).
+// Fewer than 150 tiles of 64 x 64, and up to 32 tokens: wavefronts share the depth.  us without the codes, weights from the caches, shared and
+// 64 x 64, 512 tokens of 4096: 128 tiles 7.6 and 9.3, 144 10.8 and 9.3, 152 10.8 and 9.4; of 1024: 4.8 and 6.0, 6.2 and 6.0, 6.2 and 6.0; 128
+// tokens of 8192, weights from memory: 16.9 and 21.8, 26.5 and 21.6, 26.7 and 21.8 (pieces of two by two end at 128).
+// Up to 16 tokens, us without the codes, weights from memory, 16 tokens of 4096 (of 13824):
+//   pieces            256          304          320          512          520          752          768          832
+//   two by 8       8.5 (22.4)   8.8 (22.7)   8.9 (22.8)   9.6 (25.4)  10.5 (29.7)  12.2 (33.2)  11.8 (33.5)  12.2 (34.9)
+//   one by 8       7.5 (18.0)   8.2 (19.3)   8.2 (19.7)   9.7 (22.2)  11.0 (28.4)  11.9 (31.3)  11.5 (31.7)  15.5 (44.7)
+//   two by 16      7.1 (17.0)   7.4 (17.5)   7.6 (17.7)   8.5 (21.5)  11.7 (32.9)  13.0 (37.2)  12.7 (37.1)  13.0 (38.1)
+//   one by 16      6.1 (13.0)   8.8 (22.6)   8.9 (22.9)  10.2 (25.3)  11.7 (28.7)  12.5 (32.3)  12.3 (32.6)  14.8 (40.1)
+// A round of the units is 256 workgroups, of small ones (8 wavefronts) three.
 template <typename T, typename E>
 int launch_product(const uint8_t *W, const uint8_t *X, int deep, const Scaled &y, const E &e, hipStream_t st) {
     auto fills = [](int64_t n) { return n >= 4 * kUnits || (n + kUnits / 3) / kUnits * kUnits >= n; };  // 171 .. 256, 427 .. 512, ...

@@ -4,10 +4,10 @@
 // order (a definition's, summed one by one) gives the same root but for a row in a hundred million or so, whose root lies
 // within the sum's last bits of the middle between two numbers of fp32.
 //
-// Bound.  Many rows: by bytes.  4096 rows of 8192 in bfloat16 with their sum, 268 MB, 40.5 us (6.6 TB/s, what caches keep between
-// calls included), as rows in 8 bits 40.  One row: by what comes one after the other (the loads, the sum over the lanes, the root, the
-// largest magnitude), 3.3 us, of rows in 8 bits 4.4.  Kernels for one type of all tensors are 10 to 20 % faster than the one
-// that looks at each tensor's: 64 coded rows of 4096 4.2 us and 5.2.
+// Bound.  Many rows: by bytes.  4096 rows of 8192 in bfloat16 with their sum, 268 MB, 42.6 us (6.3 TB/s, what caches keep between
+// calls included), as rows in 8 bits 42; where an fp32 stream is added 59 and 72.  One row: by what comes one after the other
+// (the loads, the sum over the lanes, the root, the largest magnitude), 3.3 us, of rows in 8 bits 4.4.  Kernels for one type of all
+// tensors are 10 to 20 % faster than the one that looks at each tensor's: 64 coded rows of 4096 4.2 us and 5.2.
 #include "epilogue.h"
 #include "int8_rows.h"
 
@@ -217,8 +217,9 @@ void run(const cmpq_norm_job &a, hipStream_t st) {
 
 // Sixteen wavefronts a row where it is longer than four of them hold in two steps: us with 16 and 4, 1 row of 8192 with its sum
 // 3.3 and 4.7, 4096 rows 40.5 and 41.5.  Rows in 8 bits, where there are many, are better off with four, three or four
-// steps each, since more of a unit's rows are then at different stages: 4096 of 5120 27.5 us and 32.3, 1000 9.7 and 11.3, but 64 of 8192
-// 5.7 and 4.8.
+// steps each, since more of a unit's rows are then at different stages: rows of 5120 (of 8192 with their sum) with 16 and 4, 256 rows 4.44
+// and 4.90 (5.51 and 6.45), 320 5.46 and 5.01 (7.26 and 7.10), 512 5.77 and 5.20 (7.72 and 7.83), 576 7.40 and 5.74 (10.1 and 9.3), 1024 9.1 and 6.8
+// (14.7 and 14.0), 4096 of 5120 32.3 and 29.
 template <bool CODED, int TYPE>
 void launch_norm(const cmpq_norm_job &a, hipStream_t st) {
     constexpr int64_t kMany = 512;
