@@ -45,3 +45,32 @@ def test_layers_of_several_kinds_take_their_own_norms(S, kinds, dtype):  # noqa:
             want = S.int8_product(part.down, H, part.ws, out_dtype=dtype, residual=stream) if kinds[2] == "8" else \
                 S.epilogue(S.apply_layer(part.down, H, part.ws), residual=stream, out_dtype=dtype)
             assert got.dtype == dtype and torch.equal(got, want) and part.status.item() == 0
+
+
+@pytest.mark.parametrize("kinds", ["ddd", "dd8", "g8"])
+def test_threads_share_layers(S, kinds):  # noqa: F811
+    """Two threads in blocks of the same layers, each with its stream and workspace: what each gets alone."""
+    import threading
+    from paper_2410_13056_amd import binding as B
+    part = Part(S, kinds)
+    X = [_randn(i, m, HIDDEN, dtype=torch.float16, scale=2) for i, m in ((1, 3), (2, 20))]
+    want = [part(x) for x in X]
+    got, errors = [[], []], []
+
+    def run(i):
+        try:
+            ws, stream = B.Workspace(DEV), torch.cuda.Stream()
+            with torch.cuda.stream(stream):
+                for _ in range(60):
+                    got[i].append(S.feed_forward_block(X[i], part.norm, part.gate_up, part.down, ws))
+            stream.synchronize()
+        except Exception as e:
+            errors.append(e)
+    torch.cuda.synchronize()
+    threads = [threading.Thread(target=run, args=(i,)) for i in (0, 1)]
+    [t.start() for t in threads]
+    [t.join(60) for t in threads]
+    torch.cuda.synchronize()
+    assert not errors
+    for i in (0, 1):
+        assert len(got[i]) == 60 and all(torch.equal(y, want[i]) for y in got[i])
