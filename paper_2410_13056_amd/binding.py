@@ -736,6 +736,7 @@ def _not_here(t: torch.Tensor):
 
 
 def _all_here(dev: int, *tensors: Optional[torch.Tensor]) -> None:
+    """Refuses tensors that are not on the device `dev`."""
     for t in tensors:
         if t is not None and t.get_device() != dev:
             raise _not_here(t)
@@ -812,9 +813,13 @@ def int8_prepare(W: torch.Tensor, codes: torch.Tensor, scale: torch.Tensor,
         raise ValueError("codes must be contiguous int8 of int8_weight_bytes(d_out, d_in)")
     if scale.dtype != torch.float32 or not scale.is_contiguous() or scale.numel() != d_out:
         raise ValueError("scale must be contiguous float32 [d_out]")
-    w, c, s = _ptr(W), _ptr(codes), _ptr(scale)
-    _all_here(_device(), W, codes, scale, status)
-    _check(lib().cmpq_int8_prepare(w, serving_dtype(W.dtype), d_out, d_in, ldw, c, s, _ptr(status), _stream()), "cmpq_int8_prepare")
+    dev = codes.get_device()
+    if W.get_device() != dev or scale.get_device() != dev or _device() != dev or status is not None:
+        _all_here(_device(), W, codes, scale, status)
+    rc = lib().cmpq_int8_prepare(W.data_ptr(), serving_dtype(W.dtype), d_out, d_in, ldw, codes.data_ptr(), scale.data_ptr(),
+                                 _ptr(status), _stream())
+    if rc:
+        _check(rc, "cmpq_int8_prepare")
 
 
 def int8_gated_rows(d_out: int) -> int:
@@ -915,11 +920,12 @@ class Int8ProductCall:
         my, d_out, ldy = _rows(Y)
         if my != m or d_in != self.d_in or d_out != self.d_out:
             raise ValueError("X must be [m, d_in] and Y [m, d_out] of the prepared weight")
-        x, xt, y, yt = _ptr(X), serving_dtype(X.dtype), _ptr(Y), serving_dtype(Y.dtype)
-        dev = _device()
-        _all_here(dev, X, Y, status)
-        if self._device != dev or ws.buf.get_device() != dev:
-            raise ValueError("layers, rows in 8 bits and workspaces must be on the current device")
+        dev = self._device
+        if X.get_device() != dev or Y.get_device() != dev or ws.buf.get_device() != dev or _device() != dev or status is not None:
+            _all_here(_device(), X, Y, status)
+            if _device() != dev or ws.buf.get_device() != dev:
+                raise ValueError("layers, rows in 8 bits and workspaces must be on the current device")
+        x, xt, y, yt = X.data_ptr(), serving_dtype(X.dtype), Y.data_ptr(), serving_dtype(Y.dtype)
         for _ in range(2):          # asks for the workspace's size only where what is there does not do
             buf = ws.buf
             rc = self._fn(x, xt, m, d_in, ldx, self._codes, self._scale, d_out, y, yt, ldy, buf.data_ptr(), buf.numel(),
