@@ -335,14 +335,11 @@ def _as_heads(Y: torch.Tensor, head_dim: int) -> torch.Tensor:
     return Y.reshape(Y.shape[0], Y.shape[1] // head_dim, head_dim)
 
 
-def _in_8_bits(layers) -> bool:
-    return all(isinstance(l, (Int8Weight, Int8GatedWeight)) for l in layers)
-
-
 def _shared(X: torch.Tensor, layers, status: Optional[torch.Tensor]) -> Inputs:
     """What layers take that share the input X: in 8 bits if all of them are, coded once for all (one or two tokens code
     themselves within the products' launches)."""
-    return int8_rows(X, status=status) if _in_8_bits(layers) and X.shape[0] > 2 else X
+    coded = X.shape[0] > 2 and all(isinstance(l, Int8Weight) for l in layers)
+    return int8_rows(X, status=status) if coded else X
 
 
 def _normed(X: torch.Tensor, norm: RmsNorm, layers, status: Optional[torch.Tensor],
@@ -350,18 +347,19 @@ def _normed(X: torch.Tensor, norm: RmsNorm, layers, status: Optional[torch.Tenso
     """What each of the layers takes that share the norm of X (+ `add`), and that sum: in 8 bits if all of them are, coded once for
     all.  Else values: functions take X's type, the others too, or float16 where one of them is in mixed precision, which
     reads that."""
-    if _in_8_bits(layers):
-        kinds = [None] * len(layers)
-    else:
-        others = torch.float16 if any(isinstance(l, P.Deployed) for l in layers) else X.dtype
-        kinds = [others if isinstance(l, (Int8Weight, P.Deployed)) else X.dtype for l in layers]
-    norms = {}
-    for k in kinds:
-        if k not in norms:                       # a second type: of the sum that the first has left
-            N = rms_norm(X, norm.weight, norm.eps, add, k is None, out_dtype=k, status=status)
-            norms[k], X = (N, X) if add is None else N
-            add = None
-    return [norms[k] for k in kinds], X
+    mixed = functions = False
+    for l in layers:
+        if isinstance(l, P.Deployed):
+            mixed = True
+        elif not isinstance(l, (Int8Weight, Int8GatedWeight)):
+            functions = True
+    N = rms_norm(X, norm.weight, norm.eps, add, not (mixed or functions), out_dtype=torch.float16 if mixed else X.dtype, status=status)
+    if add is not None:
+        N, X = N
+    if not (mixed and functions) or X.dtype == torch.float16:
+        return [N] * len(layers), X
+    own = rms_norm(X, norm.weight, norm.eps, status=status)
+    return [N if isinstance(l, (Int8Weight, P.Deployed)) else own for l in layers], X
 
 
 def attention_block(cache: KvCache, X: torch.Tensor, q: Layer, k: Layer, v: Layer, o: Layer, page_table: torch.Tensor,
